@@ -202,7 +202,8 @@ int kraken_kv_view(kraken_handle *h, int32_t layer, int32_t branch, int32_t whic
                    int64_t strides[4]);
 
 /* Synchronises the stream of the last call and reports the device status word:
- * bit 0 = a token id was out of range, bit 1 = a bounded wait inside a kernel gave up. */
+ * bit 0 = a token id was out of range, bit 1 = a bounded wait inside a kernel gave up (bit 2, a page or position
+ * that does not exist, is raised by the paged calls below only, in the status word given to them). */
 int kraken_device_status(kraken_handle *h, uint32_t *flags);
 
 /* Current sequence length held in the cache (0 before any prefill). */
@@ -419,6 +420,104 @@ int kraken_op_decode_attention_static(const void *q, int64_t q_gstride, const vo
                                       int32_t n_keys, int32_t n_head, int32_t head_dim, int32_t max_pos,
                                       int32_t splits, void *out, int64_t out_gstride, void *stream);
 size_t kraken_decode_attention_static_capacity(void);
+
+/* ------------------------------------------------------------------------------------------
+ * A key/value cache in pages, and the reading of a model's logits: the steps of a server that holds
+ * sequences of any length side by side (the KV cache whose size Sec. 4.2 discusses), next to the contiguous
+ * cache of a handle.  Every pointer is a device pointer of the current device; nothing is kept between calls.
+ *
+ * A page holds page_size consecutive positions of one sequence for every key/value head: position p of sequence s
+ * lies in slot p % page_size of page page_table[s * table_stride + p / page_size].  Element e of (page, head, slot)
+ * of k or v is at  page * page_stride + head * head_stride + slot * slot_stride + e  (elements), so both
+ * [page][head][slot][e] and [page][slot][head][e] are served.  The table's entries past a sequence's length are never
+ * read.  A sequence index, position or page number that does not exist raises bit 2 of *d_status
+ * (KRAKEN_STATUS_BAD_PAGE, device uint32, may be NULL) and is left out, as each call says; nothing is read or written
+ * outside the arrays.
+ * Requirements: head_dim in {64, 72, 96, 104, 128}; every 16-bit base pointer 16-byte aligned and every stride of a
+ * 16-bit tensor a multiple of 8 elements (EUNSUPPORTED otherwise).
+ * ------------------------------------------------------------------------------------------ */
+#define KRAKEN_STATUS_BAD_PAGE 4u
+
+typedef struct kraken_paged_cache {
+    void *k, *v;                                          /* 16-bit [n_pages], strides below              */
+    const int32_t *page_table;                            /* int32 [n_seqs][max_pages]                    */
+    int64_t page_stride, head_stride, slot_stride;        /* elements, the same for k and v               */
+    int64_t table_stride;                                 /* entries between the rows of the page table   */
+    int32_t n_pages, page_size, n_kv_head, head_dim, n_seqs, max_pages;
+} kraken_paged_cache;
+
+/* Appends the keys and values of new tokens, with the rotation by position applied to keys and queries on the way:
+ * row r goes to position row_pos[r] of sequence row_seq[r] (row_seq NULL: sequence r), whose page must already be in
+ * the table.  With theta_i = row_pos[r] * inv_freq[i], i < rot_dim / 2, the pair (x_i, x_{i + rot_dim/2}) of every head
+ * (interleaved: (x_2i, x_2i+1)) becomes (a cos - b sin, b cos + a sin); elements from rot_dim on are copied, and so
+ * are the values.  The angle is formed and reduced in 64 bits; the products are fp32, rounded once.  rot_dim = 0 (then
+ * inv_freq may be NULL) appends the rows as they are: the learned positions of this library's models.
+ * q (or NULL): the rows' queries, rotated into q_out, which may be q itself (same strides) but must not overlap k, v
+ * or the cache otherwise.  A row with row_seq[r] < 0 is padding, and one whose sequence, position or page does not
+ * exist raises the status bit: neither changes the cache nor q_out.  The rows of one call must go to distinct
+ * positions: of two rows with the same one, which of them the cache then holds is not defined, element by element.
+ * Errors: EINVAL, EUNSUPPORTED (alignment, head_dim, rot_dim no multiple of 8 or above head_dim), ECUDA. */
+typedef struct kraken_paged_append_args {
+    const void *k, *v;  int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;   /* [rows][n_kv_head] */
+    const void *q;      int64_t q_row_stride, q_head_stride;                                /* [rows][n_head]    */
+    void *q_out;        int64_t q_out_row_stride, q_out_head_stride;
+    const int32_t *row_seq, *row_pos;                     /* int32 [rows]                                 */
+    const float *inv_freq;                                /* fp32 [rot_dim / 2]                           */
+    int32_t rows, n_head, rot_dim, interleaved;
+} kraken_paged_append_args;
+int kraken_op_paged_append(const kraken_paged_cache *cache, const kraken_paged_append_args *args, uint32_t *d_status,
+                           void *stream);
+
+/* Decode-step attention over the pages: row r holds one query per head of sequence row_seq[r] (NULL: sequence r), which
+ * sees the n_keys[r] first positions of the sequence, with window > 0 only the last `window` of these.  For key j
+ *     x_j = scale * q . k_j;   score_cap > 0:  x_j = score_cap * tanh(x_j / score_cap);
+ *     slopes != NULL:  x_j += slopes[h] * (j - (n_keys[r] - 1));
+ * out = sum_j softmax(x)_j v_j, and lse (or NULL) = log sum_j exp(x_j), with which attention over other keys can be
+ * joined.  Query head h reads key/value head h / (n_head / n_kv_head).  n_keys[r] = 0 gives out = 0 and lse = -inf; so
+ * does a row all of whose scores are -inf.  Several rows may name the same sequence (draft tokens: n_keys grows from
+ * row to row).  A row with row_seq[r] < 0 is padding: its out and lse are left as they were.  So are those of a row
+ * whose sequence does not exist, or whose n_keys[r] is negative or more than max_pages * page_size; a key whose
+ * page does not exist is not visible; all of these raise the status bit.
+ * The keys are shared out evenly over the whole grid, whatever the lengths, and rows that several CTAs worked on are
+ * joined by a second kernel through `workspace` (kraken_paged_attention_workspace bytes, 16-byte aligned, contents of
+ * no importance; calls that may overlap on the device each need their own).  The result depends on the device's
+ * number of SMs and on all the lengths of the call in its last bits only, and is the same from run to run.
+ * Errors: EINVAL, EUNSUPPORTED, ECAPACITY (workspace_bytes too small), ECUDA. */
+typedef struct kraken_paged_attention_args {
+    const void *q;  int64_t q_row_stride, q_head_stride;                                    /* [rows][n_head]    */
+    void *out;      int64_t out_row_stride, out_head_stride;                                /* [rows][n_head]    */
+    float *lse;     int64_t lse_row_stride;                                                 /* [rows][n_head]    */
+    const int32_t *row_seq, *n_keys;                      /* int32 [rows]                                 */
+    const float *slopes;                                  /* fp32 [n_head] or NULL                        */
+    void *workspace;  size_t workspace_bytes;
+    float scale, score_cap;
+    int32_t rows, n_head, window;
+} kraken_paged_attention_args;
+int kraken_op_paged_attention(const kraken_paged_cache *cache, const kraken_paged_attention_args *args,
+                              uint32_t *d_status, void *stream);
+/* Workspace bytes that kraken_op_paged_attention needs on the current device, whatever the lengths (host arithmetic
+ * and a device query). */
+int kraken_paged_attention_workspace(int32_t n_head, int32_t n_kv_head, int32_t head_dim, size_t *bytes);
+
+/* Reads rows of logits: with x = scale * logits[r, :] and p = softmax(x),
+ *     lse[r] = log sum_j exp(x_j);       logprob[r] = x_target - lse[r]   (0 for a target < 0: not asked for);
+ *     entropy[r] = -sum_j p_j log p_j;   top_ids[r, 0..top-1], top_logprobs[r, 0..top-1]: the largest logits in
+ * descending order, equal ones by ascending index, and their log probabilities.
+ * logits: [rows, vocab], row stride in elements, any alignment of the element type; dtype 0 = fp32, 1 = the library's
+ * 16-bit type.  Any output may be NULL (top_* when top = 0); targets may be NULL when logprob is.
+ * -inf logits (forbidden tokens) have weight 0 and log probability -inf.  A row that holds a NaN or +inf, or nothing
+ * but -inf, has no distribution: its numbers are NaN, lse of the last kind -inf; its top_ids are still the order of
+ * its logits, a NaN counting as -inf.  A target >= vocab gives NaN and raises bit 0 of *d_status (device uint32 or NULL).
+ * 0 <= top <= 32, top <= vocab; scale > 0, finite.  Errors: EINVAL, EUNSUPPORTED (top > 32), ECUDA. */
+typedef struct kraken_logprobs_args {
+    const void *logits;  int64_t row_stride;
+    const int32_t *targets;                               /* int32 [rows] or NULL                         */
+    float *logprob, *entropy, *lse;                       /* fp32 [rows]                                  */
+    int32_t *top_ids;  float *top_logprobs;               /* [rows][top], contiguous                      */
+    int32_t rows, vocab, dtype, top;
+    float scale;
+} kraken_logprobs_args;
+int kraken_op_token_logprobs(const kraken_logprobs_args *args, uint32_t *d_status, void *stream);
 
 #ifdef __cplusplus
 }

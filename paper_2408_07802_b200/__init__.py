@@ -10,7 +10,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import os
-from typing import Dict, Optional
+from typing import Dict, NamedTuple, Optional
 
 import torch
 
@@ -42,10 +42,12 @@ EXPORTS = (
     "kraken_op_decode_attention", "kraken_decode_attention_sizes",
     "kraken_op_decode_attention_static", "kraken_decode_attention_static_capacity", "kraken_storage_dtype",
     "kraken_tuning_set", "kraken_test_wait_limit", "kraken_test_mma_issue_rate",
+    "kraken_op_paged_append", "kraken_op_paged_attention", "kraken_paged_attention_workspace",
+    "kraken_op_token_logprobs",
 )
 
 TUNE_LN_ROW_KERNEL, TUNE_ATTN_SCHEDULE, TUNE_LN_FUSION, TUNE_LAST_LAYER = 0, 1, 2, 3
-STATUS_BAD_TOKEN, STATUS_WAIT_LIMIT = 1, 2
+STATUS_BAD_TOKEN, STATUS_WAIT_LIMIT, STATUS_BAD_PAGE = 1, 2, 4
 
 
 class KrakenConfig(C.Structure):
@@ -84,6 +86,47 @@ class GemmLnArgs(C.Structure):
         ("y", C.c_void_p), ("ld_y", C.c_int32),
         ("eps", C.c_float),
         ("d_scratch", C.c_void_p), ("scratch_bytes", C.c_size_t),
+    ]
+
+
+class PagedCacheArgs(C.Structure):
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p), ("page_table", C.c_void_p),
+        ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("slot_stride", C.c_int64), ("table_stride", C.c_int64),
+        ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_head", C.c_int32), ("head_dim", C.c_int32),
+        ("n_seqs", C.c_int32), ("max_pages", C.c_int32),
+    ]
+
+
+class PagedAppendArgs(C.Structure):
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p), ("k_row_stride", C.c_int64), ("k_head_stride", C.c_int64),
+        ("v_row_stride", C.c_int64), ("v_head_stride", C.c_int64),
+        ("q", C.c_void_p), ("q_row_stride", C.c_int64), ("q_head_stride", C.c_int64),
+        ("q_out", C.c_void_p), ("q_out_row_stride", C.c_int64), ("q_out_head_stride", C.c_int64),
+        ("row_seq", C.c_void_p), ("row_pos", C.c_void_p), ("inv_freq", C.c_void_p),
+        ("rows", C.c_int32), ("n_head", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32),
+    ]
+
+
+class PagedAttentionArgs(C.Structure):
+    _fields_ = [
+        ("q", C.c_void_p), ("q_row_stride", C.c_int64), ("q_head_stride", C.c_int64),
+        ("out", C.c_void_p), ("out_row_stride", C.c_int64), ("out_head_stride", C.c_int64),
+        ("lse", C.c_void_p), ("lse_row_stride", C.c_int64),
+        ("row_seq", C.c_void_p), ("n_keys", C.c_void_p), ("slopes", C.c_void_p),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+        ("scale", C.c_float), ("score_cap", C.c_float),
+        ("rows", C.c_int32), ("n_head", C.c_int32), ("window", C.c_int32),
+    ]
+
+
+class LogprobsArgs(C.Structure):
+    _fields_ = [
+        ("logits", C.c_void_p), ("row_stride", C.c_int64), ("targets", C.c_void_p),
+        ("logprob", C.c_void_p), ("entropy", C.c_void_p), ("lse", C.c_void_p),
+        ("top_ids", C.c_void_p), ("top_logprobs", C.c_void_p),
+        ("rows", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("top", C.c_int32), ("scale", C.c_float),
     ]
 
 
@@ -171,6 +214,10 @@ def lib(dtype: Optional[str] = None) -> C.CDLL:
         L.kraken_tuning_set.argtypes = [i32, i32]
         L.kraken_test_wait_limit.argtypes = [vp, C.c_uint32, vp]
         L.kraken_test_mma_issue_rate.argtypes = [i32, i32, i32, vp, i32, C.POINTER(C.c_int32), vp, vp]
+        L.kraken_op_paged_append.argtypes = [C.POINTER(PagedCacheArgs), C.POINTER(PagedAppendArgs), vp, vp]
+        L.kraken_op_paged_attention.argtypes = [C.POINTER(PagedCacheArgs), C.POINTER(PagedAttentionArgs), vp, vp]
+        L.kraken_paged_attention_workspace.argtypes = [i32, i32, i32, C.POINTER(C.c_size_t)]
+        L.kraken_op_token_logprobs.argtypes = [C.POINTER(LogprobsArgs), vp, vp]
         if L.kraken_storage_dtype() != (1 if dtype == "f16" else 0):
             raise RuntimeError(f"{path} was not built for storage dtype {dtype}")
         _libs[dtype] = L
@@ -270,6 +317,16 @@ class KrakenModel:
         _check(lib(self.dtype).kraken_prefill_all_logits(self._h, tokens.data_ptr(), b, l, logits.data_ptr(), _stream()),
                "kraken_prefill_all_logits")
         return logits
+
+    def score(self, tokens: torch.Tensor, top: int = 0, scale: float = 1.0) -> "TokenLogprobs":
+        """Prefill of tokens [batch, seqlen] that reads its logits: row b * seqlen + t of the result (see
+        op_token_logprobs) is about the token that follows position t, whose log probability it gives where the prompt
+        holds it (0 at the last position of every sequence)."""
+        b, l = tokens.shape
+        logits = self.prefill_all_logits(tokens).view(b * l, self.cfg.vocab)
+        following = torch.full_like(tokens, -1)
+        following[:, :-1] = tokens[:, 1:]
+        return op_token_logprobs(logits, following.view(-1), top=top, scale=scale)
 
     def prefill_packed(self, tokens: torch.Tensor, seq_lens, logits: Optional[torch.Tensor] = None) -> torch.Tensor:
         """tokens: device int32 [sum(seq_lens)], the sequences back to back -> fp32 [batch, V] logits of every
@@ -498,6 +555,210 @@ def op_decode_attention_static(q: torch.Tensor, k_cache: torch.Tensor, v_cache: 
 
 def decode_attention_static_capacity() -> int:
     return int(lib().kraken_decode_attention_static_capacity())
+
+
+# ------------------------------------------------------------------ the cache in pages, and the reading of logits
+# These calls take the library image from their tensors' 16-bit type (bfloat16 or float16) and run on the current stream of
+# the tensors' device.
+
+_IMAGE = {torch.bfloat16: "bf16", torch.float16: "f16"}
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+@contextlib.contextmanager
+def _on(device: int):
+    """Makes `device` the current one (the library works on the current device) and puts the old one back."""
+    old = torch.cuda.current_device()
+    torch.cuda.set_device(device)
+    try:
+        yield
+    finally:
+        torch.cuda.set_device(old)
+
+
+def _call(fn, what: str, dtype: str, device: int, *args):
+    """fn(*args, stream) on the current stream of `device`."""
+    if device == torch.cuda.current_device():
+        status = fn(*args, _stream())
+    else:
+        with _on(device):
+            status = fn(*args, _stream())
+    if status != OK:
+        with storage_dtype(dtype):
+            raise KrakenError(status, what)
+
+
+def _int_row(t: Optional[torch.Tensor], n: int, device, what: str) -> Optional[int]:
+    """Address of an int32 [n] tensor on `device` (None: NULL)."""
+    if t is None:
+        return None
+    _need(t.dtype == torch.int32 and t.dim() == 1 and t.shape[0] == n and t.is_contiguous() and t.device == device,
+          f"{what} must be a contiguous int32 [{n}] on {device}")
+    return t.data_ptr()
+
+
+def _f32_row(t: Optional[torch.Tensor], n: Optional[int], device, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    _need(t.dtype == torch.float32 and t.dim() == 1 and (n is None or t.shape[0] == n) and t.is_contiguous() and
+          t.device == device, f"{what} must be a contiguous float32 vector{'' if n is None else f' of {n}'} on {device}")
+    return t.data_ptr()
+
+
+def _status_word(t: Optional[torch.Tensor], device) -> Optional[int]:
+    if t is None:
+        return None
+    _need(t.element_size() == 4 and t.numel() >= 1 and t.device == device, f"status must be a 32-bit word on {device}")
+    return t.data_ptr()
+
+
+def _paged_cache(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor) -> PagedCacheArgs:
+    _need(k_cache.dim() == 4 and k_cache.dtype in _IMAGE and k_cache.is_cuda,
+          "the caches must be 16-bit CUDA tensors [pages, key/value heads, page size, head_dim]")
+    n_pages, n_kv, page, hd = k_cache.shape
+    sp, sh, ss, se = k_cache.stride()
+    _need(v_cache.shape == k_cache.shape and v_cache.stride() == (sp, sh, ss, se) and v_cache.dtype == k_cache.dtype and
+          v_cache.device == k_cache.device, "k_cache and v_cache must have the same shape, strides, type and device")
+    _need(se == 1 or hd == 1, "the last dimension of the caches must be contiguous")
+    _need(page_table.dim() == 2 and page_table.dtype == torch.int32 and page_table.stride(1) == 1 and
+          page_table.device == k_cache.device, "page_table must be int32 [sequences, pages] on the caches' device")
+    n_seqs, max_pages = page_table.shape
+    return PagedCacheArgs(k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(), sp, sh, ss,
+                          page_table.stride(0) if n_seqs > 1 else max_pages, n_pages, page, n_kv, hd, n_seqs, max_pages)
+
+
+def _rows_of(t: torch.Tensor, heads: Optional[int], like: torch.Tensor, what: str):
+    """(address, row stride, head stride) of a 16-bit [rows, heads, head_dim] tensor."""
+    hd = like.shape[3]
+    _need(t.dim() == 3 and t.shape[2] == hd and (heads is None or t.shape[1] == heads) and t.dtype == like.dtype and
+          t.device == like.device and t.stride(2) == 1,
+          f"{what} must be [rows, {heads or 'heads'}, {hd}] of the caches' type and device, contiguous in its last dimension")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def op_paged_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                    page_table: torch.Tensor, positions: torch.Tensor, row_seq: Optional[torch.Tensor] = None,
+                    q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                    inv_freq: Optional[torch.Tensor] = None, interleaved: bool = False,
+                    status: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Appends new tokens' keys and values to a cache in pages (kraken_op_paged_append): k, v [rows, key/value heads,
+    head_dim] (any row and head strides: slices of one qkv product do) go to position positions[r] of sequence row_seq[r]
+    (None: sequence r; negative: padding).  k_cache, v_cache: [pages, key/value heads, page size, head_dim], page_table
+    int32 [sequences, pages].  inv_freq (float32 [rot_dim / 2]) turns keys and queries by their position; the queries q
+    [rows, heads, head_dim] go to q_out (created when not given, with the padding rows zero; may be q itself), which is
+    returned.  The rows of one call must go to distinct positions."""
+    cache = _paged_cache(k_cache, v_cache, page_table)
+    rows, device = k.shape[0], k_cache.device
+    kp = _rows_of(k, cache.n_kv_head, k_cache, "k")
+    vp = _rows_of(v, cache.n_kv_head, k_cache, "v")
+    _need(v.shape[0] == rows, "k and v must have the same rows")
+    n_head, qp, op = 0, (None, 0, 0), (None, 0, 0)
+    if q is not None:
+        qp = _rows_of(q, None, k_cache, "q")
+        n_head = q.shape[1]
+        _need(q.shape[0] == rows, "q must have the rows of k")
+        if q_out is None:
+            q_out = torch.zeros(rows, n_head, cache.head_dim, dtype=q.dtype, device=device)
+        op = _rows_of(q_out, n_head, k_cache, "q_out")
+        _need(q_out.shape[0] == rows, "q_out must have the rows of q")
+    _need(positions is not None, "positions are needed")
+    args = PagedAppendArgs(kp[0], vp[0], kp[1], kp[2], vp[1], vp[2], *qp, *op,
+                           _int_row(row_seq, rows, device, "row_seq"), _int_row(positions, rows, device, "positions"),
+                           _f32_row(inv_freq, None, device, "inv_freq"), rows, n_head,
+                           0 if inv_freq is None else 2 * inv_freq.shape[0], int(interleaved))
+    dtype = _IMAGE[k_cache.dtype]
+    _call(lib(dtype).kraken_op_paged_append, "kraken_op_paged_append", dtype, device.index, C.byref(cache), C.byref(args),
+          _status_word(status, device))
+    return q_out
+
+
+def paged_attention_workspace(n_head: int, n_kv_head: int, head_dim: int) -> int:
+    """Workspace bytes of op_paged_decode_attention on the current device."""
+    n = C.c_size_t(0)
+    _check(lib().kraken_paged_attention_workspace(n_head, n_kv_head, head_dim, C.byref(n)),
+           "kraken_paged_attention_workspace")
+    return int(n.value)
+
+
+def op_paged_decode_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor,
+                              n_keys: torch.Tensor, row_seq: Optional[torch.Tensor] = None,
+                              scale: Optional[float] = None, score_cap: float = 0.0, window: int = 0,
+                              slopes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                              lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                              status: Optional[torch.Tensor] = None):
+    """Decode-step attention over a cache in pages (kraken_op_paged_attention): one query per head and row, q [rows, heads,
+    head_dim], against the first n_keys[r] positions of sequence row_seq[r] (None: sequence r; negative: padding, whose
+    rows of out and lse stay as they were).  scale: 1 / sqrt(head_dim) by default; score_cap: scores become
+    cap * tanh(score / cap); window: only that many last positions are visible; slopes (float32 [heads]): a bias of
+    slope * (distance back to the key, negative).  Returns (out, lse): out like q, lse float32 [rows, heads]."""
+    cache = _paged_cache(k_cache, v_cache, page_table)
+    device = k_cache.device
+    qp = _rows_of(q, None, k_cache, "q")
+    rows, n_head, hd = q.shape
+    if out is None:
+        out = torch.empty(rows, n_head, hd, dtype=q.dtype, device=device)
+    op = _rows_of(out, n_head, k_cache, "out")
+    _need(out.shape[0] == rows, "out must have the rows of q")
+    if lse is None:
+        lse = torch.empty(rows, n_head, dtype=torch.float32, device=device)
+    _need(lse.dtype == torch.float32 and lse.shape == (rows, n_head) and lse.stride(1) == 1 and lse.device == device,
+          "lse must be float32 [rows, heads]")
+    dtype = _IMAGE[k_cache.dtype]
+    L = lib(dtype)
+    if workspace is None:
+        need = C.c_size_t(0)
+        with _on(device.index):
+            _check(L.kraken_paged_attention_workspace(n_head, cache.n_kv_head, hd, C.byref(need)),
+                   "kraken_paged_attention_workspace")
+        workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
+    _need(workspace.device == device and workspace.is_contiguous(), "workspace must be contiguous, on the caches' device")
+    _need(n_keys is not None, "n_keys are needed")
+    args = PagedAttentionArgs(*qp, *op, lse.data_ptr(), lse.stride(0), _int_row(row_seq, rows, device, "row_seq"),
+                              _int_row(n_keys, rows, device, "n_keys"), _f32_row(slopes, n_head, device, "slopes"),
+                              workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                              hd ** -0.5 if scale is None else scale, score_cap, rows, n_head, window)
+    _call(L.kraken_op_paged_attention, "kraken_op_paged_attention", dtype, device.index, C.byref(cache), C.byref(args),
+          _status_word(status, device))
+    return out, lse
+
+
+class TokenLogprobs(NamedTuple):
+    logprob: Optional[torch.Tensor]        # float32 [rows], of the targets (0 where the target is negative)
+    entropy: torch.Tensor                  # float32 [rows]
+    lse: torch.Tensor                      # float32 [rows], log of the sum of the exponentials
+    top_ids: Optional[torch.Tensor]        # int32 [rows, top]
+    top_logprobs: Optional[torch.Tensor]   # float32 [rows, top]
+
+
+def op_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 0, scale: float = 1.0,
+                      status: Optional[torch.Tensor] = None) -> TokenLogprobs:
+    """Reads rows of logits (kraken_op_token_logprobs): log probability of targets[r] (int32; negative: not asked for),
+    entropy of the row's distribution and its `top` largest tokens with their log probabilities, for the distribution
+    softmax(scale * logits).  logits: [rows, vocab] float32, bfloat16 or float16, any row stride."""
+    _need(logits.dim() == 2 and logits.is_cuda and logits.dtype in (torch.float32, torch.bfloat16, torch.float16) and
+          (logits.stride(1) == 1 or logits.shape[1] == 1),
+          "logits must be a CUDA tensor [rows, vocab] of float32 or a 16-bit type, contiguous in its last dimension")
+    rows, vocab = logits.shape
+    device = logits.device
+    numbers = torch.empty(3, rows, dtype=torch.float32, device=device)
+    base = numbers.data_ptr()
+    ids = best = None
+    if top > 0:
+        ids = torch.empty(rows, top, dtype=torch.int32, device=device)
+        best = torch.empty(rows, top, dtype=torch.float32, device=device)
+    asked = _int_row(targets, rows, device, "targets")
+    dtype = _IMAGE.get(logits.dtype, _current_dtype)
+    args = LogprobsArgs(logits.data_ptr(), logits.stride(0), asked,
+                        None if targets is None else base, base + 4 * rows, base + 8 * rows, _ptr(ids), _ptr(best), rows, vocab,
+                        int(logits.dtype != torch.float32), top, scale)
+    _call(lib(dtype).kraken_op_token_logprobs, "kraken_op_token_logprobs", dtype, device.index, C.byref(args),
+          _status_word(status, device))
+    logprob, entropy, lse = numbers.unbind(0)
+    return TokenLogprobs(None if targets is None else logprob, entropy, lse, ids, best)
 
 
 def set_tuning(key: int, value: int) -> None:

@@ -559,85 +559,68 @@ def decode_attention_static_capacity() -> int:
 
 # ------------------------------------------------------------------ the cache in pages, and the reading of logits
 # These calls take the library image from their tensors' 16-bit type (bfloat16 or float16) and run on the current stream of
-# the tensors' device.
+# the tensors' device.  Their kernels take a few microseconds at decode sizes, so the checks build no text unless they fail.
 
 _IMAGE = {torch.bfloat16: "bf16", torch.float16: "f16"}
-
-
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
-
-
-@contextlib.contextmanager
-def _on(device: int):
-    """Makes `device` the current one (the library works on the current device) and puts the old one back."""
-    old = torch.cuda.current_device()
-    torch.cuda.set_device(device)
-    try:
-        yield
-    finally:
-        torch.cuda.set_device(old)
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 
 def _call(fn, what: str, dtype: str, device: int, *args):
-    """fn(*args, stream) on the current stream of `device`."""
+    """fn(*args, stream) with `device` current (the library works on the current device), on its current stream."""
     if device == torch.cuda.current_device():
-        status = fn(*args, _stream())
+        status = fn(*args, _raw_stream(device))
     else:
-        with _on(device):
-            status = fn(*args, _stream())
-    if status != OK:
+        with torch.cuda.device(device):
+            status = fn(*args, _raw_stream(device))
+    if status:
         with storage_dtype(dtype):
             raise KrakenError(status, what)
 
 
-def _int_row(t: Optional[torch.Tensor], n: int, device, what: str) -> Optional[int]:
-    """Address of an int32 [n] tensor on `device` (None: NULL)."""
+def _vector(t: Optional[torch.Tensor], dtype: torch.dtype, n: int, device, what: str) -> Optional[int]:
+    """Address of a contiguous [n] tensor of the type on `device` (None: NULL)."""
     if t is None:
         return None
-    _need(t.dtype == torch.int32 and t.dim() == 1 and t.shape[0] == n and t.is_contiguous() and t.device == device,
-          f"{what} must be a contiguous int32 [{n}] on {device}")
-    return t.data_ptr()
-
-
-def _f32_row(t: Optional[torch.Tensor], n: Optional[int], device, what: str) -> Optional[int]:
-    if t is None:
-        return None
-    _need(t.dtype == torch.float32 and t.dim() == 1 and (n is None or t.shape[0] == n) and t.is_contiguous() and
-          t.device == device, f"{what} must be a contiguous float32 vector{'' if n is None else f' of {n}'} on {device}")
+    if t.dtype is not dtype or t.shape != (n,) or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} [{n}] on {device}")
     return t.data_ptr()
 
 
 def _status_word(t: Optional[torch.Tensor], device) -> Optional[int]:
     if t is None:
         return None
-    _need(t.element_size() == 4 and t.numel() >= 1 and t.device == device, f"status must be a 32-bit word on {device}")
+    if t.element_size() != 4 or t.numel() < 1 or t.device != device:
+        raise ValueError(f"status must be a 32-bit word on {device}")
     return t.data_ptr()
 
 
-def _paged_cache(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor) -> PagedCacheArgs:
-    _need(k_cache.dim() == 4 and k_cache.dtype in _IMAGE and k_cache.is_cuda,
-          "the caches must be 16-bit CUDA tensors [pages, key/value heads, page size, head_dim]")
-    n_pages, n_kv, page, hd = k_cache.shape
-    sp, sh, ss, se = k_cache.stride()
-    _need(v_cache.shape == k_cache.shape and v_cache.stride() == (sp, sh, ss, se) and v_cache.dtype == k_cache.dtype and
-          v_cache.device == k_cache.device, "k_cache and v_cache must have the same shape, strides, type and device")
-    _need(se == 1 or hd == 1, "the last dimension of the caches must be contiguous")
-    _need(page_table.dim() == 2 and page_table.dtype == torch.int32 and page_table.stride(1) == 1 and
-          page_table.device == k_cache.device, "page_table must be int32 [sequences, pages] on the caches' device")
+def _paged_cache(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor, device) -> PagedCacheArgs:
+    strides = k_cache.stride()
+    if k_cache.dtype not in _IMAGE or not k_cache.is_cuda or len(strides) != 4 or strides[3] != 1:
+        raise ValueError("the caches must be 16-bit CUDA tensors [pages, key/value heads, page size, head_dim], contiguous in "
+                         "the last dimension")
+    shape = k_cache.shape
+    if v_cache.shape != shape or v_cache.stride() != strides or v_cache.dtype is not k_cache.dtype or v_cache.device != device:
+        raise ValueError("k_cache and v_cache must have the same shape, strides, type and device")
+    if page_table.dtype is not torch.int32 or page_table.device != device or page_table.dim() != 2:
+        raise ValueError("page_table must be int32 [sequences, pages] on the caches' device")
     n_seqs, max_pages = page_table.shape
-    return PagedCacheArgs(k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(), sp, sh, ss,
-                          page_table.stride(0) if n_seqs > 1 else max_pages, n_pages, page, n_kv, hd, n_seqs, max_pages)
+    row, one = page_table.stride()
+    if one != 1 and max_pages > 1:
+        raise ValueError("page_table must be contiguous in its last dimension")
+    n_pages, n_kv, page, hd = shape
+    return PagedCacheArgs(k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(), strides[0], strides[1], strides[2],
+                          row if n_seqs > 1 else max_pages, n_pages, page, n_kv, hd, n_seqs, max_pages)
 
 
-def _rows_of(t: torch.Tensor, heads: Optional[int], like: torch.Tensor, what: str):
+def _rows_of(t: torch.Tensor, rows: int, heads: int, hd: int, like: torch.Tensor, device, what: str):
     """(address, row stride, head stride) of a 16-bit [rows, heads, head_dim] tensor."""
-    hd = like.shape[3]
-    _need(t.dim() == 3 and t.shape[2] == hd and (heads is None or t.shape[1] == heads) and t.dtype == like.dtype and
-          t.device == like.device and t.stride(2) == 1,
-          f"{what} must be [rows, {heads or 'heads'}, {hd}] of the caches' type and device, contiguous in its last dimension")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    if t.shape != (rows, heads, hd) or t.dtype is not like.dtype or t.device != device:
+        raise ValueError(f"{what} must be [{rows}, {heads}, {hd}] of the caches' type and device")
+    row, head, one = t.stride()
+    if one != 1:
+        raise ValueError(f"{what} must be contiguous in its last dimension")
+    return t.data_ptr(), row, head
 
 
 def op_paged_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -651,25 +634,27 @@ def op_paged_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_c
     int32 [sequences, pages].  inv_freq (float32 [rot_dim / 2]) turns keys and queries by their position; the queries q
     [rows, heads, head_dim] go to q_out (created when not given, with the padding rows zero; may be q itself), which is
     returned.  The rows of one call must go to distinct positions."""
-    cache = _paged_cache(k_cache, v_cache, page_table)
-    rows, device = k.shape[0], k_cache.device
-    kp = _rows_of(k, cache.n_kv_head, k_cache, "k")
-    vp = _rows_of(v, cache.n_kv_head, k_cache, "v")
-    _need(v.shape[0] == rows, "k and v must have the same rows")
+    device = k_cache.device
+    cache = _paged_cache(k_cache, v_cache, page_table, device)
+    hd, n_kv = cache.head_dim, cache.n_kv_head
+    rows = k.shape[0]
+    kp, k_row, k_head = _rows_of(k, rows, n_kv, hd, k_cache, device, "k")
+    vp, v_row, v_head = _rows_of(v, rows, n_kv, hd, k_cache, device, "v")
     n_head, qp, op = 0, (None, 0, 0), (None, 0, 0)
     if q is not None:
-        qp = _rows_of(q, None, k_cache, "q")
         n_head = q.shape[1]
-        _need(q.shape[0] == rows, "q must have the rows of k")
+        qp = _rows_of(q, rows, n_head, hd, k_cache, device, "q")
         if q_out is None:
-            q_out = torch.zeros(rows, n_head, cache.head_dim, dtype=q.dtype, device=device)
-        op = _rows_of(q_out, n_head, k_cache, "q_out")
-        _need(q_out.shape[0] == rows, "q_out must have the rows of q")
-    _need(positions is not None, "positions are needed")
-    args = PagedAppendArgs(kp[0], vp[0], kp[1], kp[2], vp[1], vp[2], *qp, *op,
-                           _int_row(row_seq, rows, device, "row_seq"), _int_row(positions, rows, device, "positions"),
-                           _f32_row(inv_freq, None, device, "inv_freq"), rows, n_head,
-                           0 if inv_freq is None else 2 * inv_freq.shape[0], int(interleaved))
+            q_out = torch.zeros(rows, n_head, hd, dtype=q.dtype, device=device)
+        op = _rows_of(q_out, rows, n_head, hd, k_cache, device, "q_out")
+    if positions is None:
+        raise ValueError("positions are needed")
+    half = 0 if inv_freq is None else inv_freq.shape[0]
+    args = PagedAppendArgs(kp, vp, k_row, k_head, v_row, v_head, *qp, *op,
+                           _vector(row_seq, torch.int32, rows, device, "row_seq"),
+                           _vector(positions, torch.int32, rows, device, "positions"),
+                           _vector(inv_freq, torch.float32, half, device, "inv_freq"), rows, n_head, 2 * half,
+                           bool(interleaved))
     dtype = _IMAGE[k_cache.dtype]
     _call(lib(dtype).kraken_op_paged_append, "kraken_op_paged_append", dtype, device.index, C.byref(cache), C.byref(args),
           _status_word(status, device))
@@ -695,34 +680,34 @@ def op_paged_decode_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: t
     rows of out and lse stay as they were).  scale: 1 / sqrt(head_dim) by default; score_cap: scores become
     cap * tanh(score / cap); window: only that many last positions are visible; slopes (float32 [heads]): a bias of
     slope * (distance back to the key, negative).  Returns (out, lse): out like q, lse float32 [rows, heads]."""
-    cache = _paged_cache(k_cache, v_cache, page_table)
     device = k_cache.device
-    qp = _rows_of(q, None, k_cache, "q")
+    cache = _paged_cache(k_cache, v_cache, page_table, device)
     rows, n_head, hd = q.shape
+    qp, q_row, q_head = _rows_of(q, rows, n_head, cache.head_dim, k_cache, device, "q")
     if out is None:
         out = torch.empty(rows, n_head, hd, dtype=q.dtype, device=device)
-    op = _rows_of(out, n_head, k_cache, "out")
-    _need(out.shape[0] == rows, "out must have the rows of q")
+    op, o_row, o_head = _rows_of(out, rows, n_head, hd, k_cache, device, "out")
     if lse is None:
         lse = torch.empty(rows, n_head, dtype=torch.float32, device=device)
-    _need(lse.dtype == torch.float32 and lse.shape == (rows, n_head) and lse.stride(1) == 1 and lse.device == device,
-          "lse must be float32 [rows, heads]")
+    l_row, one = lse.stride()
+    if lse.dtype is not torch.float32 or lse.shape != (rows, n_head) or one != 1 or lse.device != device:
+        raise ValueError("lse must be float32 [rows, heads] on the caches' device, contiguous in its last dimension")
     dtype = _IMAGE[k_cache.dtype]
-    L = lib(dtype)
     if workspace is None:
-        need = C.c_size_t(0)
-        with _on(device.index):
-            _check(L.kraken_paged_attention_workspace(n_head, cache.n_kv_head, hd, C.byref(need)),
-                   "kraken_paged_attention_workspace")
-        workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
-    _need(workspace.device == device and workspace.is_contiguous(), "workspace must be contiguous, on the caches' device")
-    _need(n_keys is not None, "n_keys are needed")
-    args = PagedAttentionArgs(*qp, *op, lse.data_ptr(), lse.stride(0), _int_row(row_seq, rows, device, "row_seq"),
-                              _int_row(n_keys, rows, device, "n_keys"), _f32_row(slopes, n_head, device, "slopes"),
-                              workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                              hd ** -0.5 if scale is None else scale, score_cap, rows, n_head, window)
-    _call(L.kraken_op_paged_attention, "kraken_op_paged_attention", dtype, device.index, C.byref(cache), C.byref(args),
-          _status_word(status, device))
+        with contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device):
+            workspace = torch.empty(paged_attention_workspace(n_head, cache.n_kv_head, hd), dtype=torch.uint8, device=device)
+    elif workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous, on the caches' device")
+    if n_keys is None:
+        raise ValueError("n_keys are needed")
+    args = PagedAttentionArgs(qp, q_row, q_head, op, o_row, o_head, lse.data_ptr(), l_row,
+                              _vector(row_seq, torch.int32, rows, device, "row_seq"),
+                              _vector(n_keys, torch.int32, rows, device, "n_keys"),
+                              _vector(slopes, torch.float32, n_head, device, "slopes"),
+                              workspace.data_ptr(), workspace.nbytes, hd ** -0.5 if scale is None else scale, score_cap, rows,
+                              n_head, window)
+    _call(lib(dtype).kraken_op_paged_attention, "kraken_op_paged_attention", dtype, device.index, C.byref(cache),
+          C.byref(args), _status_word(status, device))
     return out, lse
 
 
@@ -739,22 +724,25 @@ def op_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = No
     """Reads rows of logits (kraken_op_token_logprobs): log probability of targets[r] (int32; negative: not asked for),
     entropy of the row's distribution and its `top` largest tokens with their log probabilities, for the distribution
     softmax(scale * logits).  logits: [rows, vocab] float32, bfloat16 or float16, any row stride."""
-    _need(logits.dim() == 2 and logits.is_cuda and logits.dtype in (torch.float32, torch.bfloat16, torch.float16) and
-          (logits.stride(1) == 1 or logits.shape[1] == 1),
-          "logits must be a CUDA tensor [rows, vocab] of float32 or a 16-bit type, contiguous in its last dimension")
+    kind = logits.dtype
+    if not logits.is_cuda or logits.dim() != 2 or (kind is not torch.float32 and kind not in _IMAGE):
+        raise ValueError("logits must be a CUDA tensor [rows, vocab] of float32 or a 16-bit type")
     rows, vocab = logits.shape
+    row, one = logits.stride()
+    if one != 1 and vocab > 1:
+        raise ValueError("logits must be contiguous in the last dimension")
     device = logits.device
+    asked = _vector(targets, torch.int32, rows, device, "targets")
     numbers = torch.empty(3, rows, dtype=torch.float32, device=device)
     base = numbers.data_ptr()
-    ids = best = None
+    ids = best = ids_at = best_at = None
     if top > 0:
         ids = torch.empty(rows, top, dtype=torch.int32, device=device)
         best = torch.empty(rows, top, dtype=torch.float32, device=device)
-    asked = _int_row(targets, rows, device, "targets")
-    dtype = _IMAGE.get(logits.dtype, _current_dtype)
-    args = LogprobsArgs(logits.data_ptr(), logits.stride(0), asked,
-                        None if targets is None else base, base + 4 * rows, base + 8 * rows, _ptr(ids), _ptr(best), rows, vocab,
-                        int(logits.dtype != torch.float32), top, scale)
+        ids_at, best_at = ids.data_ptr(), best.data_ptr()
+    dtype = _IMAGE.get(kind, _current_dtype)
+    args = LogprobsArgs(logits.data_ptr(), row, asked, None if targets is None else base, base + 4 * rows, base + 8 * rows,
+                        ids_at, best_at, rows, vocab, kind is not torch.float32, top, scale)
     _call(lib(dtype).kraken_op_token_logprobs, "kraken_op_token_logprobs", dtype, device.index, C.byref(args),
           _status_word(status, device))
     logprob, entropy, lse = numbers.unbind(0)

@@ -18,6 +18,8 @@
 // which would be as large as that of the output, does not count; a running maximum and sum are kept in fp32.
 #include <math.h>
 
+#include <algorithm>
+
 #include "paged.cuh"
 
 namespace kr {
@@ -25,6 +27,7 @@ namespace kr {
 namespace {
 
 constexpr int PA_WARPS = 4;
+constexpr int TILE = PA_WARPS * 16;   // keys of a tile: 16 for every warp
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.69314718055994531f;
 
@@ -39,6 +42,7 @@ struct PagedAttnParams {
     float scale, cap;
     int rows, n_head, window;
     uint32_t *status;
+    uint8_t *workspace;
 };
 
 __device__ __forceinline__ void mma_keys(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -163,134 +167,354 @@ __device__ __forceinline__ void take_block(Running<HD, NT> &run, const KeyBlock<
     }
 }
 
+// What row r asks for: its visible keys lo .. n - 1 of sequence seq.  False: padding, or (bad) no such sequence or length.
+struct RowKeys {
+    int seq, lo, n, tiles;   // tiles of TILE keys, at least one (a row without keys writes zeros)
+};
+
+__device__ __forceinline__ bool row_keys(const PagedAttnParams &p, int r, RowKeys &k, bool &bad) {
+    k.seq = p.row_seq ? p.row_seq[r] : r;
+    k.tiles = 0;
+    if (k.seq < 0) return false;
+    k.n = p.n_keys[r];
+    if (k.seq >= p.c.n_seqs || k.n < 0 || k.n > (long long)p.c.max_pages * p.c.page_size) {
+        bad = true;
+        return false;
+    }
+    k.lo = p.window > 0 && k.n > p.window ? k.n - p.window : 0;
+    k.tiles = max(1, (k.n - k.lo + TILE - 1) / TILE);
+    return true;
+}
+
+// The work of a call is a line of tiles: rows in order, of each row its (key/value head, head tile) units in order, of each
+// unit its key tiles.  CTA i of G (at most one per tile) takes tiles [total i / G, total (i + 1) / G): the same number for every CTA, whatever the
+// lengths.  A unit that lies in one CTA is finished there; of one that does not, every CTA leaves its part in the
+// workspace (slot 1 where the unit begins, slot 0 elsewhere: a CTA has at most one of each) and the CTA with the
+// beginning notes who has the rest, for the joining kernel.
+struct Part {
+    int row, unit, last_cta;   // row = -1: nothing to join
+    int pad;
+};
+
+template <int HD, int NT>
+struct PartShape {
+    static constexpr int HEADS = 8 * NT;
+    static constexpr int FLOATS = HEADS * (HD + 2);   // [HEADS] m, [HEADS] l, [HEADS][HD] o
+};
+
 template <int HD, int NT>
 __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAttnParams p) {
     constexpr int CH = KeyBlock<HD>::CH, HF = KeyBlock<HD>::HF, HEADS = 8 * NT;
     __shared__ float sm_m[PA_WARPS][HEADS], sm_l[PA_WARPS][HEADS];
     __shared__ float sm_o[PA_WARPS][HEADS][HF * 64];
+    __shared__ long long sm_sum[PA_WARPS];
+    __shared__ int sm_row;
+    __shared__ long long sm_before;
     pdl_wait();
     const int rep = p.n_head / p.c.n_kv_head;
     const int head_tiles = (rep + HEADS - 1) / HEADS;
-    const int hk = blockIdx.x / head_tiles, first = blockIdx.x % head_tiles * HEADS;
-    const int heads = min(HEADS, rep - first);      // of this CTA
-    const int h0 = hk * rep + first;
-    const int r = blockIdx.y;
+    const int units = p.c.n_kv_head * head_tiles;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int seq = p.row_seq ? p.row_seq[r] : r;
-    if (seq < 0) return;
-    const int n = p.n_keys[r];
-    if (seq >= p.c.n_seqs || n < 0 || n > (long long)p.c.max_pages * p.c.page_size) {
-        if (threadIdx.x == 0 && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
-        return;
+    Part *parts = reinterpret_cast<Part *>(p.workspace);
+    float *slots = reinterpret_cast<float *>(p.workspace + sizeof(Part) * gridDim.x);
+    if (threadIdx.x == 0) {
+        parts[blockIdx.x].row = -1;
+        sm_row = -1;
     }
-    const int lo = p.window > 0 && n > p.window ? n - p.window : 0;
-    const int *table = p.c.table + seq * p.c.table_stride;
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
 
-    uint4 q[NT][CH];
-    float slope[NT][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int h = nt * 8 + g, e = c * 32 + t * 8;
-            q[nt][c] = h < heads && e < HD ? *reinterpret_cast<const uint4 *>(p.q + r * p.q_row + (h0 + h) * p.q_head + e) : zero;
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int h = nt * 8 + 2 * t + e;
-            slope[nt][e] = p.slopes && h < heads ? p.slopes[h0 + h] : 0.f;
-        }
-    }
-    const ScoreForm form = {p.scale, p.cap, p.cap > 0.f ? 1.f / p.cap : 0.f, p.cap <= 0.f && !p.slopes, p.scale * LOG2E};
-    Running<HD, NT> run;
-    run.clear();
+    // where this CTA's share begins: every thread adds up the tiles of a run of rows
+    const int per = (p.rows + PA_WARPS * 32 - 1) / (PA_WARPS * 32);
+    const int row_lo = min(p.rows, (int)threadIdx.x * per), row_hi = min(p.rows, row_lo + per);
+    long long mine = 0;
     bool bad = false;
-    for (int key0 = lo + warp * 16; key0 < n; key0 += PA_WARPS * 16) {
-        // lanes 0..15 look up the page of one key each; -1: not visible
-        const int mine = key0 + (lane & 15);
-        int page = -1;
-        if (mine < n) {
-            page = table[mine / p.c.page_size];
-            if (page < 0 || page >= p.c.n_pages) {
-                page = -1;
-                bad = true;
-            }
-        }
-        const int slot = mine % p.c.page_size;
-        KeyBlock<HD> b;
-        bool live[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int pg = __shfl_sync(0xFFFFFFFFu, page, g + 8 * i), sl = __shfl_sync(0xFFFFFFFFu, slot, g + 8 * i);
-            live[i] = pg >= 0;
-            const uint16_t *row = p.c.k + pg * p.c.page_stride + sl * p.c.slot_stride + hk * p.c.head_stride;
-#pragma unroll
-            for (int c = 0; c < CH; ++c)
-                b.k[i][c] = live[i] && c * 32 + t * 8 < HD ? __ldcs(reinterpret_cast<const uint4 *>(row + c * 32 + t * 8)) : zero;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int who = 2 * t + (i & 1) + (i >> 1) * 8;
-            const int pg = __shfl_sync(0xFFFFFFFFu, page, who), sl = __shfl_sync(0xFFFFFFFFu, slot, who);
-            const uint16_t *row = p.c.v + pg * p.c.page_stride + sl * p.c.slot_stride + hk * p.c.head_stride;
-#pragma unroll
-            for (int hf = 0; hf < HF; ++hf)
-                b.v[i][hf] = pg >= 0 && hf * 64 + g * 8 < HD ? __ldcs(reinterpret_cast<const uint4 *>(row + hf * 64 + g * 8)) : zero;
-        }
-        take_block<HD, NT>(run, b, q, live, key0 + g - (n - 1), form, slope);
+    for (int r = row_lo; r < row_hi; ++r) {
+        RowKeys k;
+        row_keys(p, r, k, bad);
+        mine += k.tiles;
     }
-    if (bad && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
-    pdl_trigger();
-
-    // sums over the lanes that hold the same heads; then the warps through shared memory
+    long long upto = mine;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float l = run.l[nt][e];
-            l += __shfl_xor_sync(0xFFFFFFFFu, l, 4);
-            l += __shfl_xor_sync(0xFFFFFFFFu, l, 8);
-            l += __shfl_xor_sync(0xFFFFFFFFu, l, 16);
-            const int h = nt * 8 + 2 * t + e;
-            if (g == 0) {
-                sm_m[warp][h] = run.m[nt][e];
-                sm_l[warp][h] = l;
-            }
-#pragma unroll
-            for (int hf = 0; hf < HF; ++hf)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    sm_o[warp][h][hf * 64 + g * 8 + 2 * j] = run.o[nt][hf * 4 + j][e];
-                    sm_o[warp][h][hf * 64 + g * 8 + 2 * j + 1] = run.o[nt][hf * 4 + j][2 + e];
-                }
-        }
+    for (int off = 1; off < 32; off <<= 1) {
+        const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, off);
+        if (lane >= off) upto += v;
+    }
+    if (lane == 31) sm_sum[warp] = upto;
     __syncthreads();
-    for (int i = threadIdx.x; i < heads * HD; i += PA_WARPS * 32) {
-        const int h = i / HD, e = i % HD;
-        float m = -INFINITY;
+    long long total = 0;
 #pragma unroll
-        for (int w = 0; w < PA_WARPS; ++w) m = fmaxf(m, sm_m[w][h]);
-        const float base = m == -INFINITY ? 0.f : m;
-        float l = 0.f, o = 0.f;
-#pragma unroll
-        for (int w = 0; w < PA_WARPS; ++w) {
-            const float c = ex2_approx(sm_m[w][h] - base);
-            l += sm_l[w][h] * c;
-            o += sm_o[w][h][e] * c;
-        }
-        p.out[r * p.out_row + (h0 + h) * p.out_head + e] = to_h16(l == 0.f ? 0.f : o / l);
-        if (p.lse && e == 0) p.lse[r * p.lse_row + h0 + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+    for (int w = 0; w < PA_WARPS; ++w) {
+        if (w < warp) upto += sm_sum[w];
+        total += sm_sum[w];
     }
+    const long long all = total * units;
+    const long long n_cta = min((long long)gridDim.x, all);   // no CTA between the two ends of a unit is without a tile
+    const long long c0 = blockIdx.x < n_cta ? all * blockIdx.x / n_cta : all;
+    const long long c1 = blockIdx.x < n_cta ? all * (blockIdx.x + 1) / n_cta : all;
+    {
+        long long before = upto - mine;
+        if (c0 < c1 && c0 >= before * units && c0 < upto * units) {
+            for (int r = row_lo; r < row_hi; ++r) {
+                RowKeys k;
+                row_keys(p, r, k, bad);
+                if (c0 < (before + k.tiles) * units) {
+                    sm_row = r;
+                    sm_before = before;
+                    break;
+                }
+                before += k.tiles;
+            }
+        }
+    }
+    if (bad && blockIdx.x == 0 && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
+    if (c0 >= c1) return;
+    __syncthreads();
+
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    const ScoreForm form = {p.scale, p.cap, p.cap > 0.f ? 1.f / p.cap : 0.f, p.cap <= 0.f && !p.slopes, p.scale * LOG2E};
+    int r = sm_row;
+    RowKeys k;
+    // (no such row, here and below: the lengths changed under the kernel)
+    if (r < 0 || !row_keys(p, r, k, bad)) return;
+    long long row_c0 = sm_before * units;          // first tile of row r
+    int unit = static_cast<int>((c0 - row_c0) / k.tiles);
+    int tile = static_cast<int>((c0 - row_c0) % k.tiles);
+    long long left = c1 - c0;
+    bool bad_page = false;
+    while (left > 0) {
+        const int seg = static_cast<int>(min(left, (long long)(k.tiles - tile)));
+        const int hk = unit / head_tiles, first = unit % head_tiles * HEADS;
+        const int heads = min(HEADS, rep - first), h0 = hk * rep + first;
+        const int *table = p.c.table + k.seq * p.c.table_stride;
+        uint4 q[NT][CH];
+        float slope[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int h = nt * 8 + g, e = c * 32 + t * 8;
+                q[nt][c] = h < heads && e < HD ? *reinterpret_cast<const uint4 *>(p.q + r * p.q_row + (h0 + h) * p.q_head + e) : zero;
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int h = nt * 8 + 2 * t + e;
+                slope[nt][e] = p.slopes && h < heads ? p.slopes[h0 + h] : 0.f;
+            }
+        }
+        Running<HD, NT> run;
+        run.clear();
+        const int end = min((long long)k.n, k.lo + (long long)(tile + seg) * TILE);
+        for (int key0 = k.lo + tile * TILE + warp * 16; key0 < end; key0 += TILE) {
+            // lanes 0..15 look up the page of one key each; -1: not visible
+            const int key = key0 + (lane & 15);
+            int page = -1;
+            if (key < end) {
+                page = table[key / p.c.page_size];
+                if (page < 0 || page >= p.c.n_pages) {
+                    page = -1;
+                    bad_page = true;
+                }
+            }
+            const int slot = key % p.c.page_size;
+            KeyBlock<HD> b;
+            bool live[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int pg = __shfl_sync(0xFFFFFFFFu, page, g + 8 * i), sl = __shfl_sync(0xFFFFFFFFu, slot, g + 8 * i);
+                live[i] = pg >= 0;
+                const uint16_t *row = p.c.k + pg * p.c.page_stride + sl * p.c.slot_stride + hk * p.c.head_stride;
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+                    b.k[i][c] = live[i] && c * 32 + t * 8 < HD ? __ldcs(reinterpret_cast<const uint4 *>(row + c * 32 + t * 8)) : zero;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int who = 2 * t + (i & 1) + (i >> 1) * 8;
+                const int pg = __shfl_sync(0xFFFFFFFFu, page, who), sl = __shfl_sync(0xFFFFFFFFu, slot, who);
+                const uint16_t *row = p.c.v + pg * p.c.page_stride + sl * p.c.slot_stride + hk * p.c.head_stride;
+#pragma unroll
+                for (int hf = 0; hf < HF; ++hf)
+                    b.v[i][hf] = pg >= 0 && hf * 64 + g * 8 < HD ? __ldcs(reinterpret_cast<const uint4 *>(row + hf * 64 + g * 8)) : zero;
+            }
+            take_block<HD, NT>(run, b, q, live, key0 + g - (k.n - 1), form, slope);
+        }
+
+        // sums over the lanes that hold the same heads; then the warps through shared memory
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float l = run.l[nt][e];
+                l += __shfl_xor_sync(0xFFFFFFFFu, l, 4);
+                l += __shfl_xor_sync(0xFFFFFFFFu, l, 8);
+                l += __shfl_xor_sync(0xFFFFFFFFu, l, 16);
+                const int h = nt * 8 + 2 * t + e;
+                if (g == 0) {
+                    sm_m[warp][h] = run.m[nt][e];
+                    sm_l[warp][h] = l;
+                }
+#pragma unroll
+                for (int hf = 0; hf < HF; ++hf)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        sm_o[warp][h][hf * 64 + g * 8 + 2 * j] = run.o[nt][hf * 4 + j][e];
+                        sm_o[warp][h][hf * 64 + g * 8 + 2 * j + 1] = run.o[nt][hf * 4 + j][2 + e];
+                    }
+            }
+        __syncthreads();
+        const bool whole = tile == 0 && seg == k.tiles;
+        float *slot = slots + ((long long)blockIdx.x * 2 + (tile == 0 ? 1 : 0)) * PartShape<HD, NT>::FLOATS;
+        for (int i = threadIdx.x; i < heads * HD; i += PA_WARPS * 32) {
+            const int h = i / HD, e = i % HD;
+            float m = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < PA_WARPS; ++w) m = fmaxf(m, sm_m[w][h]);
+            const float base = m == -INFINITY ? 0.f : m;
+            float l = 0.f, o = 0.f;
+#pragma unroll
+            for (int w = 0; w < PA_WARPS; ++w) {
+                const float c = ex2_approx(sm_m[w][h] - base);
+                l += sm_l[w][h] * c;
+                o += sm_o[w][h][e] * c;
+            }
+            if (whole) {
+                p.out[r * p.out_row + (h0 + h) * p.out_head + e] = to_h16(l == 0.f ? 0.f : o / l);
+                if (p.lse && e == 0) p.lse[r * p.lse_row + h0 + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+            } else {
+                slot[2 * HEADS + i] = o;
+                if (e == 0) {
+                    slot[h] = m;
+                    slot[HEADS + h] = l;
+                }
+            }
+        }
+        if (tile == 0 && !whole && threadIdx.x == 0) {
+            // the CTA with the unit's last tile x: the largest i with all i / n_cta (rounded down) <= x
+            const long long x = row_c0 + (long long)(unit + 1) * k.tiles - 1;
+            parts[blockIdx.x] = {r, unit, static_cast<int>(((x + 1) * n_cta - 1) / all), 0};
+        }
+        left -= seg;
+        tile = 0;
+        if (++unit == units && left > 0) {
+            unit = 0;
+            row_c0 += (long long)units * k.tiles;
+            do {
+                if (++r == p.rows) {
+                    left = 0;
+                    break;
+                }
+                row_keys(p, r, k, bad);
+            } while (k.tiles == 0);
+        }
+        __syncthreads();
+    }
+    if (bad_page && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
+}
+
+// Joins the parts of the unit that begins in CTA blockIdx.x of the kernel above, head blockIdx.y of it:
+// out = sum_i o_i 2^(m_i - m) / sum_i l_i 2^(m_i - m).  A warp takes every 8th part, a lane 4 elements of the head.
+constexpr int JOIN_WARPS = 8;
+
+template <int HD, int NT>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) paged_attn_join_kernel(const PagedAttnParams p, int n_cta) {
+    constexpr int HEADS = 8 * NT;
+    __shared__ float sm_m[JOIN_WARPS], sm_l[JOIN_WARPS];
+    __shared__ float4 sm_o[JOIN_WARPS][32];
+    pdl_wait();
+    const Part part = reinterpret_cast<const Part *>(p.workspace)[blockIdx.x];
+    if (part.row < 0) return;
+    const int rep = p.n_head / p.c.n_kv_head, head_tiles = (rep + HEADS - 1) / HEADS;
+    const int hk = part.unit / head_tiles, first = part.unit % head_tiles * HEADS, h = blockIdx.y;
+    if (first + h >= rep) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const float *slots = reinterpret_cast<const float *>(p.workspace + sizeof(Part) * n_cta);
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = blockIdx.x + warp; i <= part.last_cta; i += JOIN_WARPS) {
+        const float *slot = slots + ((long long)i * 2 + (i == (int)blockIdx.x ? 1 : 0)) * PartShape<HD, NT>::FLOATS;
+        const float mi = slot[h], li = slot[HEADS + h];
+        const float4 oi = lane * 4 < HD ? *reinterpret_cast<const float4 *>(slot + 2 * HEADS + h * HD + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float mx = fmaxf(m, mi), base = mx == -INFINITY ? 0.f : mx;
+        const float a = ex2_approx(m - base), b = ex2_approx(mi - base);
+        m = mx;
+        l = l * a + li * b;
+        o.x = o.x * a + oi.x * b;
+        o.y = o.y * a + oi.y * b;
+        o.z = o.z * a + oi.z * b;
+        o.w = o.w * a + oi.w * b;
+    }
+    if (lane == 0) {
+        sm_m[warp] = m;
+        sm_l[warp] = l;
+    }
+    sm_o[warp][lane] = o;
+    __syncthreads();
+    if (warp != 0) return;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < JOIN_WARPS; ++w) mx = fmaxf(mx, sm_m[w]);
+    const float base = mx == -INFINITY ? 0.f : mx;
+    l = 0.f;
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < JOIN_WARPS; ++w) {
+        const float c = ex2_approx(sm_m[w] - base);
+        const float4 ow = sm_o[w][lane];
+        l += sm_l[w] * c;
+        o.x += ow.x * c;
+        o.y += ow.y * c;
+        o.z += ow.z * c;
+        o.w += ow.w * c;
+    }
+    const int head = hk * rep + first + h;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (lane * 4 < HD) {
+        uint2 u;
+        u.x = pack_h16x2(o.x * inv, o.y * inv);
+        u.y = pack_h16x2(o.z * inv, o.w * inv);
+        *reinterpret_cast<uint2 *>(p.out + part.row * p.out_row + head * p.out_head + lane * 4) = u;
+    }
+    if (p.lse && lane == 0) p.lse[part.row * p.lse_row + head] = l == 0.f ? -INFINITY : (mx + log2f(l)) * LN2;
+}
+
+// CTAs of the grid: all that run at once, and no more than there can be tiles.
+constexpr int MAX_CTAS_PER_SM = 4;
+
+size_t workspace_bytes(int rep, int head_dim) {
+    const int sms = sm_count() > 0 ? sm_count() : 148;
+    const size_t heads = rep <= 8 ? 8 : 16;
+    return (size_t)sms * MAX_CTAS_PER_SM * (sizeof(Part) + 2 * heads * (head_dim + 2) * sizeof(float));
+}
+
+template <int HD, int NT>
+int launch_nt(const PagedAttnParams &p, cudaStream_t st) {
+    static std::atomic<int> resident[MAX_DEVICES];   // CTAs of this instance that an SM of the device holds
+    const int dev = device_slot(), sms = sm_count();
+    if (dev < 0 || sms <= 0) return KRAKEN_ECUDA;
+    int n = resident[dev].load(std::memory_order_relaxed);
+    if (n <= 0) {
+        int rc = cuda_check(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, paged_attn_kernel<HD, NT>, PA_WARPS * 32, 0),
+                            "paged attention: occupancy");
+        if (rc) return rc;
+        n = n < 1 ? 1 : (n > MAX_CTAS_PER_SM ? MAX_CTAS_PER_SM : n);
+        resident[dev].store(n, std::memory_order_relaxed);
+    }
+    const int rep = p.n_head / p.c.n_kv_head;
+    const long long units = (long long)p.c.n_kv_head * ((rep + 8 * NT - 1) / (8 * NT)) * p.rows;
+    const long long keys = (long long)p.c.max_pages * p.c.page_size;
+    const long long seen = p.window > 0 && p.window < keys ? p.window : keys;
+    const long long tiles = (seen + TILE - 1) / TILE;
+    const long long grid = std::min<long long>((long long)sms * n, units * tiles);
+    int rc = cuda_check(launch_pdl(paged_attn_kernel<HD, NT>, dim3((unsigned)grid), dim3(PA_WARPS * 32), 0, st, p),
+                        "paged attention: launch");
+    // with one tile a unit nothing is ever split
+    if (rc || tiles == 1) return rc;
+    return cuda_check(launch_pdl(paged_attn_join_kernel<HD, NT>, dim3((unsigned)grid, std::min(rep, 8 * NT)), dim3(JOIN_WARPS * 32), 0,
+                                 st, p, (int)grid), "paged attention join: launch");
 }
 
 template <int HD>
 int launch(const PagedAttnParams &p, cudaStream_t st) {
-    const int rep = p.n_head / p.c.n_kv_head;
-    cudaError_t e;
-    if (rep <= 8) e = launch_pdl(paged_attn_kernel<HD, 1>, dim3(p.c.n_kv_head, p.rows), dim3(PA_WARPS * 32), 0, st, p);
-    else e = launch_pdl(paged_attn_kernel<HD, 2>, dim3(p.c.n_kv_head * ((rep + 15) / 16), p.rows), dim3(PA_WARPS * 32), 0, st, p);
-    return cuda_check(e, "paged attention: launch");
+    return p.n_head / p.c.n_kv_head <= 8 ? launch_nt<HD, 1>(p, st) : launch_nt<HD, 2>(p, st);
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -303,7 +527,7 @@ extern "C" int kraken_paged_attention_workspace(int32_t n_head, int32_t n_kv_hea
     using namespace kr;
     if (!bytes || n_head < 1 || n_kv_head < 1 || n_head % n_kv_head != 0) return KRAKEN_EINVAL;
     if (!decode_head_dim_ok(head_dim)) return KRAKEN_EUNSUPPORTED;
-    *bytes = 0;
+    *bytes = workspace_bytes(n_head / n_kv_head, head_dim);
     return KRAKEN_OK;
 }
 
@@ -322,7 +546,9 @@ extern "C" int kraken_op_paged_attention(const kraken_paged_cache *cache, const 
     if (!aligned16(a->q) || !aligned16(a->out) ||
         ((a->q_row_stride | a->q_head_stride | a->out_row_stride | a->out_head_stride) & 7))
         return KRAKEN_EUNSUPPORTED;
-    if (a->rows > 65535) return KRAKEN_EUNSUPPORTED;
+    if (!a->workspace || a->workspace_bytes < workspace_bytes(a->n_head / cache->n_kv_head, cache->head_dim)) return KRAKEN_ECAPACITY;
+    if (!aligned16(a->workspace)) return KRAKEN_EINVAL;
+    p.workspace = static_cast<uint8_t *>(a->workspace);
     p.q = static_cast<const uint16_t *>(a->q);
     p.out = static_cast<uint16_t *>(a->out);
     p.lse = a->lse;

@@ -27,6 +27,7 @@ namespace kr {
 namespace {
 
 constexpr int PA_WARPS = 4;
+constexpr int STAGES = 3;                // key blocks of a warp in shared memory: one being used, two on their way
 constexpr int TILE = PA_WARPS * 16;   // keys of a tile: 16 for every warp
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.69314718055994531f;
@@ -60,13 +61,15 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
     return y;
 }
 
-// The 16-key block at key0 of one (sequence, key/value head) as a lane holds it: keys g and g + 8 of K, keys 2t, 2t + 1,
-// 2t + 8, 2t + 9 of V (g = lane / 4, t = lane % 4).
+// The 16-key block at key0 of one (sequence, key/value head) as the lanes need it: keys g and g + 8 of K, keys 2t, 2t + 1,
+// 2t + 8, 2t + 9 of V (g = lane / 4, t = lane % 4).  A lane copies the pieces that it will read itself, so a block needs no
+// barrier of any kind between its copy and its use, and every access to shared memory is a warp's 512 bytes in a row.
 template <int HD>
 struct KeyBlock {
     static constexpr int CH = (HD + 31) / 32;   // 32-element chunks of a key, 8 elements of each per lane
     static constexpr int HF = (HD + 63) / 64;   // 64-element halves of a value, 8 elements of each per lane
-    uint4 k[2][CH], v[4][HF];
+    static constexpr int PIECES = 2 * CH + 4 * HF;   // 16-byte pieces of a lane, kept as [piece][lane] in shared memory
+    static constexpr int BYTES = PIECES * 512;
 };
 
 template <int HD, int NT>
@@ -96,17 +99,25 @@ struct ScoreForm {
 
 // `live[i]`: whether key g + 8 i of the block is visible; `back`: position of key g minus that of the query
 template <int HD, int NT>
-__device__ __forceinline__ void take_block(Running<HD, NT> &run, const KeyBlock<HD> &b, const uint4 (&q)[NT][KeyBlock<HD>::CH],
+__device__ __forceinline__ void take_block(Running<HD, NT> &run, const uint4 *block, const uint4 (&q)[NT][KeyBlock<HD>::CH],
                                            const bool (&live)[2], int back, const ScoreForm &f, const float (&slope)[NT][2]) {
     constexpr int CH = KeyBlock<HD>::CH, HF = KeyBlock<HD>::HF;
+    float sc[NT][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const uint4 k0 = block[(2 * c) * 32], k1 = block[(2 * c + 1) * 32];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            mma_keys(sc[nt], k0.x, k1.x, k0.y, k1.y, q[nt][c].x, q[nt][c].y);
+            mma_keys(sc[nt], k0.z, k1.z, k0.w, k1.w, q[nt][c].z, q[nt][c].w);
+        }
+    }
+    uint32_t hi[NT][2], lo[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            mma_keys(s, b.k[0][c].x, b.k[1][c].x, b.k[0][c].y, b.k[1][c].y, q[nt][c].x, q[nt][c].y);
-            mma_keys(s, b.k[0][c].z, b.k[1][c].z, b.k[0][c].w, b.k[1][c].w, q[nt][c].z, q[nt][c].w);
-        }
+        float (&s)[4] = sc[nt];
         // s[2 i + e]: key g + 8 i, head 2t + e
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -147,23 +158,27 @@ __device__ __forceinline__ void take_block(Running<HD, NT> &run, const KeyBlock<
                 run.o[nt][j][3] *= corr[1];
             }
         }
-        uint32_t hi[2], lo[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t w = pack_h16x2(p[2 * i], p[2 * i + 1]);
-            hi[i] = transpose_8x8(w);
-            lo[i] = transpose_8x8(pack_h16x2(p[2 * i] - h16_lo(w), p[2 * i + 1] - h16_hi(w)));
+            hi[nt][i] = transpose_8x8(w);
+            lo[nt][i] = transpose_8x8(pack_h16x2(p[2 * i] - h16_lo(w), p[2 * i + 1] - h16_hi(w)));
         }
+    }
 #pragma unroll
-        for (int hf = 0; hf < HF; ++hf)
+    for (int hf = 0; hf < HF; ++hf) {
+        const uint4 *v = block + (2 * CH + 4 * hf) * 32;
+        const uint4 v0 = v[0], v1 = v[32], v2 = v[64], v3 = v[96];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t v0 = word(b.v[0][hf], j), v1 = word(b.v[1][hf], j), v2 = word(b.v[2][hf], j), v3 = word(b.v[3][hf], j);
-                const uint32_t a0 = __byte_perm(v0, v1, 0x5410), a1 = __byte_perm(v0, v1, 0x7632);
-                const uint32_t a2 = __byte_perm(v2, v3, 0x5410), a3 = __byte_perm(v2, v3, 0x7632);
-                mma_keys(run.o[nt][hf * 4 + j], a0, a1, a2, a3, hi[0], hi[1]);
-                mma_keys(run.o[nt][hf * 4 + j], a0, a1, a2, a3, lo[0], lo[1]);
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t a0 = __byte_perm(word(v0, j), word(v1, j), 0x5410), a1 = __byte_perm(word(v0, j), word(v1, j), 0x7632);
+            const uint32_t a2 = __byte_perm(word(v2, j), word(v3, j), 0x5410), a3 = __byte_perm(word(v2, j), word(v3, j), 0x7632);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                mma_keys(run.o[nt][hf * 4 + j], a0, a1, a2, a3, hi[nt][0], hi[nt][1]);
+                mma_keys(run.o[nt][hf * 4 + j], a0, a1, a2, a3, lo[nt][0], lo[nt][1]);
             }
+        }
     }
 }
 
@@ -196,20 +211,53 @@ struct Part {
     int pad;
 };
 
+// A part in the workspace, as the accumulators lie in a warp: [NT][HF * 4 products][32 lanes][4] o, then [2][HEADS] m and l.
 template <int HD, int NT>
 struct PartShape {
-    static constexpr int HEADS = 8 * NT;
-    static constexpr int FLOATS = HEADS * (HD + 2);   // [HEADS] m, [HEADS] l, [HEADS][HD] o
+    static constexpr int HEADS = 8 * NT, PRODUCTS = KeyBlock<HD>::HF * 4;
+    static constexpr int O_FLOATS = NT * PRODUCTS * 128;
+    static constexpr int FLOATS = O_FLOATS + 2 * HEADS;
+};
+
+// Accumulator of product j, head tile nt: elements e and e + 1 of heads 8 nt + 2t and 8 nt + 2t + 1 are (x, z) and (y, w).
+template <int HD>
+__device__ __forceinline__ void store_pair(const PagedAttnParams &p, int row, int h0, int heads, int nt, int j, int lane, float4 o,
+                                           const float (&l)[2]) {
+    const int h = nt * 8 + 2 * (lane & 3), e = (j >> 2) * 64 + (lane >> 2) * 8 + 2 * (j & 3);
+    if (e >= HD) return;
+    uint16_t *out = p.out + row * p.out_row + (h0 + h) * p.out_head + e;
+    const float i0 = l[0] == 0.f ? 0.f : 1.f / l[0], i1 = l[1] == 0.f ? 0.f : 1.f / l[1];
+    if (h < heads) *reinterpret_cast<uint32_t *>(out) = pack_h16x2(o.x * i0, o.z * i0);
+    if (h + 1 < heads) *reinterpret_cast<uint32_t *>(out + p.out_head) = pack_h16x2(o.y * i1, o.w * i1);
+}
+
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * LN2; }
+
+__device__ __forceinline__ void copy16(void *smem, const void *gmem, bool live) {   // zeros where not live
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(smem)), "l"(gmem), "r"(live ? 16 : 0) : "memory");
+}
+
+// A place on the line of tiles
+struct Place {
+    int r, unit, tile;
+    RowKeys k;
+};
+
+template <int HD, int NT>
+struct Smem {
+    uint4 ring[PA_WARPS][STAGES][KeyBlock<HD>::PIECES * 32];
+    float4 o[PA_WARPS][KeyBlock<HD>::HF * 4][32];   // one head tile of every warp, to be joined
+    float m[PA_WARPS][8], l[PA_WARPS][8];
+    long long sum[PA_WARPS], before;
+    int row;
 };
 
 template <int HD, int NT>
 __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAttnParams p) {
     constexpr int CH = KeyBlock<HD>::CH, HF = KeyBlock<HD>::HF, HEADS = 8 * NT;
-    __shared__ float sm_m[PA_WARPS][HEADS], sm_l[PA_WARPS][HEADS];
-    __shared__ float sm_o[PA_WARPS][HEADS][HF * 64];
-    __shared__ long long sm_sum[PA_WARPS];
-    __shared__ int sm_row;
-    __shared__ long long sm_before;
+    using Shape = PartShape<HD, NT>;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    Smem<HD, NT> &sm = *reinterpret_cast<Smem<HD, NT> *>(smem_raw);
     pdl_wait();
     const int rep = p.n_head / p.c.n_kv_head;
     const int head_tiles = (rep + HEADS - 1) / HEADS;
@@ -219,7 +267,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
     float *slots = reinterpret_cast<float *>(p.workspace + sizeof(Part) * gridDim.x);
     if (threadIdx.x == 0) {
         parts[blockIdx.x].row = -1;
-        sm_row = -1;
+        sm.row = -1;
     }
 
     // where this CTA's share begins: every thread adds up the tiles of a run of rows
@@ -238,13 +286,13 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
         const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, off);
         if (lane >= off) upto += v;
     }
-    if (lane == 31) sm_sum[warp] = upto;
+    if (lane == 31) sm.sum[warp] = upto;
     __syncthreads();
     long long total = 0;
 #pragma unroll
     for (int w = 0; w < PA_WARPS; ++w) {
-        if (w < warp) upto += sm_sum[w];
-        total += sm_sum[w];
+        if (w < warp) upto += sm.sum[w];
+        total += sm.sum[w];
     }
     const long long all = total * units;
     const long long n_cta = min((long long)gridDim.x, all);   // no CTA between the two ends of a unit is without a tile
@@ -257,8 +305,8 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
                 RowKeys k;
                 row_keys(p, r, k, bad);
                 if (c0 < (before + k.tiles) * units) {
-                    sm_row = r;
-                    sm_before = before;
+                    sm.row = r;
+                    sm.before = before;
                     break;
                 }
                 before += k.tiles;
@@ -266,25 +314,97 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
         }
     }
     if (bad && blockIdx.x == 0 && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
+    pdl_trigger();
     if (c0 >= c1) return;
     __syncthreads();
 
+    // `at`: the tile being worked on; `ahead`: the tile whose copy is issued next, up to STAGES - 1 further on
+    Place at;
+    at.r = sm.row;
+    // (no such row, here and below: the lengths changed under the kernel)
+    if (at.r < 0 || !row_keys(p, at.r, at.k, bad)) return;
+    long long row_c0 = sm.before * units;          // first tile of row at.r
+    at.unit = static_cast<int>((c0 - row_c0) / at.k.tiles);
+    at.tile = static_cast<int>((c0 - row_c0) % at.k.tiles);
+    Place ahead = at;
+    long long to_issue = c1 - c0;
+    bool bad_page = false;
+    // lanes 0..15 (and again 16..31) each look up the page of one key of their warp's block; -1: not visible.  The lookup of
+    // a block is requested one block before its copies need it.
+    auto look_up = [&](const Place &w) {
+        const int key = w.k.lo + w.tile * TILE + warp * 16 + (lane & 15);
+        return key < w.k.n ? p.c.table[w.k.seq * p.c.table_stride + key / p.c.page_size] : -1;
+    };
+    auto step_row = [&](Place &w) {   // to the next row with tiles; false when there is none
+        do {
+            if (++w.r == p.rows) return false;
+            row_keys(p, w.r, w.k, bad);
+        } while (w.k.tiles == 0);
+        return true;
+    };
+    int page = look_up(ahead), fill = 0;
+    uint32_t seen[STAGES - 1];   // keys visible in the blocks under way, oldest first
+    auto issue = [&]() -> uint32_t {
+        uint32_t mask = 0;
+        if (to_issue > 0) {
+            const int key0 = ahead.k.lo + ahead.tile * TILE + warp * 16;
+            if (key0 < ahead.k.n) {
+                if (page < 0 || page >= p.c.n_pages) {
+                    page = -1;
+                    bad_page |= key0 + (lane & 15) < ahead.k.n;
+                }
+                mask = __ballot_sync(0xFFFFFFFFu, page >= 0) & 0xFFFFu;
+                const long long off = max(page, 0) * p.c.page_stride + (key0 + (lane & 15)) % p.c.page_size * p.c.slot_stride +
+                                      ahead.unit / head_tiles * p.c.head_stride;
+                uint4 *to = &sm.ring[warp][fill][lane];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint16_t *row = p.c.k + __shfl_sync(0xFFFFFFFFu, off, g + 8 * i) + t * 8;
+                    const bool live = mask >> (g + 8 * i) & 1;
+#pragma unroll
+                    for (int c = 0; c < CH; ++c) {
+                        const bool in = live && c * 32 + t * 8 < HD;
+                        copy16(to + (2 * c + i) * 32, in ? row + c * 32 : p.c.k, in);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int who = 2 * t + (i & 1) + (i >> 1) * 8;
+                    const uint16_t *row = p.c.v + __shfl_sync(0xFFFFFFFFu, off, who) + g * 8;
+                    const bool live = mask >> who & 1;
+#pragma unroll
+                    for (int hf = 0; hf < HF; ++hf) {
+                        const bool in = live && hf * 64 + g * 8 < HD;
+                        copy16(to + (2 * CH + 4 * hf + i) * 32, in ? row + hf * 64 : p.c.v, in);
+                    }
+                }
+            }
+            if (--to_issue > 0) {
+                if (++ahead.tile == ahead.k.tiles) {
+                    ahead.tile = 0;
+                    if (++ahead.unit == units) {
+                        ahead.unit = 0;
+                        if (!step_row(ahead)) to_issue = 0;
+                    }
+                }
+                page = look_up(ahead);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (++fill == STAGES) fill = 0;
+        return mask;
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) seen[i] = issue();
+
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
     const ScoreForm form = {p.scale, p.cap, p.cap > 0.f ? 1.f / p.cap : 0.f, p.cap <= 0.f && !p.slopes, p.scale * LOG2E};
-    int r = sm_row;
-    RowKeys k;
-    // (no such row, here and below: the lengths changed under the kernel)
-    if (r < 0 || !row_keys(p, r, k, bad)) return;
-    long long row_c0 = sm_before * units;          // first tile of row r
-    int unit = static_cast<int>((c0 - row_c0) / k.tiles);
-    int tile = static_cast<int>((c0 - row_c0) % k.tiles);
     long long left = c1 - c0;
-    bool bad_page = false;
+    int use = 0;
     while (left > 0) {
-        const int seg = static_cast<int>(min(left, (long long)(k.tiles - tile)));
-        const int hk = unit / head_tiles, first = unit % head_tiles * HEADS;
+        const int seg = static_cast<int>(min(left, (long long)(at.k.tiles - at.tile)));
+        const int hk = at.unit / head_tiles, first = at.unit % head_tiles * HEADS;
         const int heads = min(HEADS, rep - first), h0 = hk * rep + first;
-        const int *table = p.c.table + k.seq * p.c.table_stride;
         uint4 q[NT][CH];
         float slope[NT][2];
 #pragma unroll
@@ -292,7 +412,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int h = nt * 8 + g, e = c * 32 + t * 8;
-                q[nt][c] = h < heads && e < HD ? *reinterpret_cast<const uint4 *>(p.q + r * p.q_row + (h0 + h) * p.q_head + e) : zero;
+                q[nt][c] = h < heads && e < HD ? *reinterpret_cast<const uint4 *>(p.q + at.r * p.q_row + (h0 + h) * p.q_head + e) : zero;
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -302,178 +422,152 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
         }
         Running<HD, NT> run;
         run.clear();
-        const int end = min((long long)k.n, k.lo + (long long)(tile + seg) * TILE);
-        for (int key0 = k.lo + tile * TILE + warp * 16; key0 < end; key0 += TILE) {
-            // lanes 0..15 look up the page of one key each; -1: not visible
-            const int key = key0 + (lane & 15);
-            int page = -1;
-            if (key < end) {
-                page = table[key / p.c.page_size];
-                if (page < 0 || page >= p.c.n_pages) {
-                    page = -1;
-                    bad_page = true;
-                }
+        for (int i = 0; i < seg; ++i) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+            const uint32_t mask = seen[0];
+#pragma unroll
+            for (int j = 0; j + 1 < STAGES - 1; ++j) seen[j] = seen[j + 1];
+            // the block used one step ago has been read: its place takes the next copies
+            seen[STAGES - 2] = issue();
+            if (mask) {
+                const bool live[2] = {(mask >> g & 1) != 0, (mask >> (g + 8) & 1) != 0};
+                take_block<HD, NT>(run, &sm.ring[warp][use][lane], q, live,
+                                   at.k.lo + (at.tile + i) * TILE + warp * 16 + g - (at.k.n - 1), form, slope);
             }
-            const int slot = key % p.c.page_size;
-            KeyBlock<HD> b;
-            bool live[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int pg = __shfl_sync(0xFFFFFFFFu, page, g + 8 * i), sl = __shfl_sync(0xFFFFFFFFu, slot, g + 8 * i);
-                live[i] = pg >= 0;
-                const uint16_t *row = p.c.k + pg * p.c.page_stride + sl * p.c.slot_stride + hk * p.c.head_stride;
-#pragma unroll
-                for (int c = 0; c < CH; ++c)
-                    b.k[i][c] = live[i] && c * 32 + t * 8 < HD ? __ldcs(reinterpret_cast<const uint4 *>(row + c * 32 + t * 8)) : zero;
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int who = 2 * t + (i & 1) + (i >> 1) * 8;
-                const int pg = __shfl_sync(0xFFFFFFFFu, page, who), sl = __shfl_sync(0xFFFFFFFFu, slot, who);
-                const uint16_t *row = p.c.v + pg * p.c.page_stride + sl * p.c.slot_stride + hk * p.c.head_stride;
-#pragma unroll
-                for (int hf = 0; hf < HF; ++hf)
-                    b.v[i][hf] = pg >= 0 && hf * 64 + g * 8 < HD ? __ldcs(reinterpret_cast<const uint4 *>(row + hf * 64 + g * 8)) : zero;
-            }
-            take_block<HD, NT>(run, b, q, live, key0 + g - (k.n - 1), form, slope);
+            if (++use == STAGES) use = 0;
         }
 
-        // sums over the lanes that hold the same heads; then the warps through shared memory
+        // the warps' results of the unit meet in shared memory, one head tile at a time
+        const bool whole = at.tile == 0 && seg == at.k.tiles;
+        float *slot = slots + ((long long)blockIdx.x * 2 + (at.tile == 0 ? 1 : 0)) * Shape::FLOATS;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+            __syncthreads();
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 float l = run.l[nt][e];
                 l += __shfl_xor_sync(0xFFFFFFFFu, l, 4);
                 l += __shfl_xor_sync(0xFFFFFFFFu, l, 8);
                 l += __shfl_xor_sync(0xFFFFFFFFu, l, 16);
-                const int h = nt * 8 + 2 * t + e;
                 if (g == 0) {
-                    sm_m[warp][h] = run.m[nt][e];
-                    sm_l[warp][h] = l;
+                    sm.m[warp][2 * t + e] = run.m[nt][e];
+                    sm.l[warp][2 * t + e] = l;
                 }
+            }
 #pragma unroll
-                for (int hf = 0; hf < HF; ++hf)
+            for (int j = 0; j < HF * 4; ++j)
+                sm.o[warp][j][lane] = make_float4(run.o[nt][j][0], run.o[nt][j][1], run.o[nt][j][2], run.o[nt][j][3]);
+            __syncthreads();
+            float m[2], l[2] = {0.f, 0.f}, c[PA_WARPS][2];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        sm_o[warp][h][hf * 64 + g * 8 + 2 * j] = run.o[nt][hf * 4 + j][e];
-                        sm_o[warp][h][hf * 64 + g * 8 + 2 * j + 1] = run.o[nt][hf * 4 + j][2 + e];
+            for (int e = 0; e < 2; ++e) {
+                m[e] = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < PA_WARPS; ++w) m[e] = fmaxf(m[e], sm.m[w][2 * t + e]);
+                const float base = m[e] == -INFINITY ? 0.f : m[e];
+#pragma unroll
+                for (int w = 0; w < PA_WARPS; ++w) {
+                    c[w][e] = ex2_approx(sm.m[w][2 * t + e] - base);
+                    l[e] += sm.l[w][2 * t + e] * c[w][e];
+                }
+            }
+#pragma unroll
+            for (int jj = 0; jj < HF; ++jj) {
+                const int j = jj * 4 + warp;
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < PA_WARPS; ++w) {
+                    const float4 x = sm.o[w][j][lane];
+                    o.x += x.x * c[w][0];
+                    o.y += x.y * c[w][1];
+                    o.z += x.z * c[w][0];
+                    o.w += x.w * c[w][1];
+                }
+                if (whole) store_pair<HD>(p, at.r, h0, heads, nt, j, lane, o, l);
+                else *reinterpret_cast<float4 *>(slot + ((nt * HF * 4 + j) * 32 + lane) * 4) = o;
+            }
+            if (warp == 0 && g == 0) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int h = nt * 8 + 2 * t + e;
+                    if (!whole) {
+                        slot[Shape::O_FLOATS + h] = m[e];
+                        slot[Shape::O_FLOATS + HEADS + h] = l[e];
+                    } else if (p.lse && h < heads) {
+                        p.lse[at.r * p.lse_row + h0 + h] = lse_of(m[e], l[e]);
                     }
-            }
-        __syncthreads();
-        const bool whole = tile == 0 && seg == k.tiles;
-        float *slot = slots + ((long long)blockIdx.x * 2 + (tile == 0 ? 1 : 0)) * PartShape<HD, NT>::FLOATS;
-        for (int i = threadIdx.x; i < heads * HD; i += PA_WARPS * 32) {
-            const int h = i / HD, e = i % HD;
-            float m = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < PA_WARPS; ++w) m = fmaxf(m, sm_m[w][h]);
-            const float base = m == -INFINITY ? 0.f : m;
-            float l = 0.f, o = 0.f;
-#pragma unroll
-            for (int w = 0; w < PA_WARPS; ++w) {
-                const float c = ex2_approx(sm_m[w][h] - base);
-                l += sm_l[w][h] * c;
-                o += sm_o[w][h][e] * c;
-            }
-            if (whole) {
-                p.out[r * p.out_row + (h0 + h) * p.out_head + e] = to_h16(l == 0.f ? 0.f : o / l);
-                if (p.lse && e == 0) p.lse[r * p.lse_row + h0 + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
-            } else {
-                slot[2 * HEADS + i] = o;
-                if (e == 0) {
-                    slot[h] = m;
-                    slot[HEADS + h] = l;
                 }
             }
         }
-        if (tile == 0 && !whole && threadIdx.x == 0) {
+        if (at.tile == 0 && !whole && threadIdx.x == 0) {
             // the CTA with the unit's last tile x: the largest i with all i / n_cta (rounded down) <= x
-            const long long x = row_c0 + (long long)(unit + 1) * k.tiles - 1;
-            parts[blockIdx.x] = {r, unit, static_cast<int>(((x + 1) * n_cta - 1) / all), 0};
+            const long long x = row_c0 + (long long)(at.unit + 1) * at.k.tiles - 1;
+            parts[blockIdx.x] = {at.r, at.unit, static_cast<int>(((x + 1) * n_cta - 1) / all), 0};
         }
         left -= seg;
-        tile = 0;
-        if (++unit == units && left > 0) {
-            unit = 0;
-            row_c0 += (long long)units * k.tiles;
-            do {
-                if (++r == p.rows) {
-                    left = 0;
-                    break;
-                }
-                row_keys(p, r, k, bad);
-            } while (k.tiles == 0);
+        at.tile = 0;
+        if (++at.unit == units && left > 0) {
+            at.unit = 0;
+            row_c0 += (long long)units * at.k.tiles;
+            if (!step_row(at)) break;
         }
-        __syncthreads();
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if (bad_page && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
 }
 
-// Joins the parts of the unit that begins in CTA blockIdx.x of the kernel above, head blockIdx.y of it:
-// out = sum_i o_i 2^(m_i - m) / sum_i l_i 2^(m_i - m).  A warp takes every 8th part, a lane 4 elements of the head.
+// Joins the parts of the unit that begins in CTA blockIdx.x of the kernel above, for the elements of product blockIdx.y:
+// out = sum_i o_i 2^(m_i - m) / sum_i l_i 2^(m_i - m).  A warp takes every 8th part.
 constexpr int JOIN_WARPS = 8;
 
 template <int HD, int NT>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) paged_attn_join_kernel(const PagedAttnParams p, int n_cta) {
     constexpr int HEADS = 8 * NT;
-    __shared__ float sm_m[JOIN_WARPS], sm_l[JOIN_WARPS];
+    using Shape = PartShape<HD, NT>;
+    __shared__ float2 sm_m[JOIN_WARPS][32], sm_l[JOIN_WARPS][32];
     __shared__ float4 sm_o[JOIN_WARPS][32];
     pdl_wait();
+    pdl_trigger();
     const Part part = reinterpret_cast<const Part *>(p.workspace)[blockIdx.x];
     if (part.row < 0) return;
     const int rep = p.n_head / p.c.n_kv_head, head_tiles = (rep + HEADS - 1) / HEADS;
-    const int hk = part.unit / head_tiles, first = part.unit % head_tiles * HEADS, h = blockIdx.y;
-    if (first + h >= rep) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int first = part.unit % head_tiles * HEADS, heads = min(HEADS, rep - first), h0 = part.unit / head_tiles * rep + first;
+    const int nt = blockIdx.y / Shape::PRODUCTS, j = blockIdx.y % Shape::PRODUCTS;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = nt * 8 + 2 * (lane & 3);
     const float *slots = reinterpret_cast<const float *>(p.workspace + sizeof(Part) * n_cta);
-    float m = -INFINITY, l = 0.f;
+    float2 m = make_float2(-INFINITY, -INFINITY), l = make_float2(0.f, 0.f);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](const float2 mi, const float2 li, const float4 oi) {
+        const float mx = fmaxf(m.x, mi.x), my = fmaxf(m.y, mi.y);
+        const float bx = mx == -INFINITY ? 0.f : mx, by = my == -INFINITY ? 0.f : my;
+        const float ax = ex2_approx(m.x - bx), cx = ex2_approx(mi.x - bx), ay = ex2_approx(m.y - by), cy = ex2_approx(mi.y - by);
+        m = make_float2(mx, my);
+        l.x = l.x * ax + li.x * cx;
+        l.y = l.y * ay + li.y * cy;
+        o.x = o.x * ax + oi.x * cx;
+        o.y = o.y * ay + oi.y * cy;
+        o.z = o.z * ax + oi.z * cx;
+        o.w = o.w * ay + oi.w * cy;
+    };
+#pragma unroll 4
     for (int i = blockIdx.x + warp; i <= part.last_cta; i += JOIN_WARPS) {
-        const float *slot = slots + ((long long)i * 2 + (i == (int)blockIdx.x ? 1 : 0)) * PartShape<HD, NT>::FLOATS;
-        const float mi = slot[h], li = slot[HEADS + h];
-        const float4 oi = lane * 4 < HD ? *reinterpret_cast<const float4 *>(slot + 2 * HEADS + h * HD + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-        const float mx = fmaxf(m, mi), base = mx == -INFINITY ? 0.f : mx;
-        const float a = ex2_approx(m - base), b = ex2_approx(mi - base);
-        m = mx;
-        l = l * a + li * b;
-        o.x = o.x * a + oi.x * b;
-        o.y = o.y * a + oi.y * b;
-        o.z = o.z * a + oi.z * b;
-        o.w = o.w * a + oi.w * b;
+        const float *slot = slots + ((long long)i * 2 + (i == (int)blockIdx.x ? 1 : 0)) * Shape::FLOATS;
+        add(*reinterpret_cast<const float2 *>(slot + Shape::O_FLOATS + h), *reinterpret_cast<const float2 *>(slot + Shape::O_FLOATS + HEADS + h),
+            *reinterpret_cast<const float4 *>(slot + (blockIdx.y * 32 + lane) * 4));
     }
-    if (lane == 0) {
-        sm_m[warp] = m;
-        sm_l[warp] = l;
-    }
+    sm_m[warp][lane] = m;
+    sm_l[warp][lane] = l;
     sm_o[warp][lane] = o;
     __syncthreads();
     if (warp != 0) return;
-    float mx = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < JOIN_WARPS; ++w) mx = fmaxf(mx, sm_m[w]);
-    const float base = mx == -INFINITY ? 0.f : mx;
-    l = 0.f;
-    o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < JOIN_WARPS; ++w) {
-        const float c = ex2_approx(sm_m[w] - base);
-        const float4 ow = sm_o[w][lane];
-        l += sm_l[w] * c;
-        o.x += ow.x * c;
-        o.y += ow.y * c;
-        o.z += ow.z * c;
-        o.w += ow.w * c;
+    for (int w = 1; w < JOIN_WARPS; ++w) add(sm_m[w][lane], sm_l[w][lane], sm_o[w][lane]);
+    const float ls[2] = {l.x, l.y};
+    store_pair<HD>(p, part.row, h0, heads, nt, j, lane, o, ls);
+    if (p.lse && j == 0 && lane < 4) {
+        if (h < heads) p.lse[part.row * p.lse_row + h0 + h] = lse_of(m.x, l.x);
+        if (h + 1 < heads) p.lse[part.row * p.lse_row + h0 + h + 1] = lse_of(m.y, l.y);
     }
-    const int head = hk * rep + first + h;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (lane * 4 < HD) {
-        uint2 u;
-        u.x = pack_h16x2(o.x * inv, o.y * inv);
-        u.y = pack_h16x2(o.z * inv, o.w * inv);
-        *reinterpret_cast<uint2 *>(p.out + part.row * p.out_row + head * p.out_head + lane * 4) = u;
-    }
-    if (p.lse && lane == 0) p.lse[part.row * p.lse_row + head] = l == 0.f ? -INFINITY : (mx + log2f(l)) * LN2;
 }
 
 // CTAs of the grid: all that run at once, and no more than there can be tiles.
@@ -482,7 +576,7 @@ constexpr int MAX_CTAS_PER_SM = 4;
 size_t workspace_bytes(int rep, int head_dim) {
     const int sms = sm_count() > 0 ? sm_count() : 148;
     const size_t heads = rep <= 8 ? 8 : 16;
-    return (size_t)sms * MAX_CTAS_PER_SM * (sizeof(Part) + 2 * heads * (head_dim + 2) * sizeof(float));
+    return (size_t)sms * MAX_CTAS_PER_SM * (sizeof(Part) + 2 * heads * ((head_dim + 63) / 64 * 64 + 2) * sizeof(float));
 }
 
 template <int HD, int NT>
@@ -491,9 +585,12 @@ int launch_nt(const PagedAttnParams &p, cudaStream_t st) {
     const int dev = device_slot(), sms = sm_count();
     if (dev < 0 || sms <= 0) return KRAKEN_ECUDA;
     int n = resident[dev].load(std::memory_order_relaxed);
+    constexpr int SMEM = sizeof(Smem<HD, NT>);
     if (n <= 0) {
-        int rc = cuda_check(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, paged_attn_kernel<HD, NT>, PA_WARPS * 32, 0),
-                            "paged attention: occupancy");
+        int rc = cuda_check(cudaFuncSetAttribute(paged_attn_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM),
+                            "paged attention: shared memory opt-in");
+        if (!rc) rc = cuda_check(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, paged_attn_kernel<HD, NT>, PA_WARPS * 32, SMEM),
+                                 "paged attention: occupancy");
         if (rc) return rc;
         n = n < 1 ? 1 : (n > MAX_CTAS_PER_SM ? MAX_CTAS_PER_SM : n);
         resident[dev].store(n, std::memory_order_relaxed);
@@ -504,11 +601,11 @@ int launch_nt(const PagedAttnParams &p, cudaStream_t st) {
     const long long seen = p.window > 0 && p.window < keys ? p.window : keys;
     const long long tiles = (seen + TILE - 1) / TILE;
     const long long grid = std::min<long long>((long long)sms * n, units * tiles);
-    int rc = cuda_check(launch_pdl(paged_attn_kernel<HD, NT>, dim3((unsigned)grid), dim3(PA_WARPS * 32), 0, st, p),
+    int rc = cuda_check(launch_pdl(paged_attn_kernel<HD, NT>, dim3((unsigned)grid), dim3(PA_WARPS * 32), SMEM, st, p),
                         "paged attention: launch");
     // with one tile a unit nothing is ever split
     if (rc || tiles == 1) return rc;
-    return cuda_check(launch_pdl(paged_attn_join_kernel<HD, NT>, dim3((unsigned)grid, std::min(rep, 8 * NT)), dim3(JOIN_WARPS * 32), 0,
+    return cuda_check(launch_pdl(paged_attn_join_kernel<HD, NT>, dim3((unsigned)grid, NT * PartShape<HD, NT>::PRODUCTS), dim3(JOIN_WARPS * 32), 0,
                                  st, p, (int)grid), "paged attention join: launch");
 }
 

@@ -7,15 +7,17 @@
 // against 4 FLOP per query head, so up to 16 heads a group this is bound by HBM (16 FLOP a byte: 100 TFLOP/s at the copy
 // bandwidth) and the products run on the warp-level tensor instructions, which take both operands from registers.
 //
-// The products of a 16-key block, with the keys as rows and the query heads as the 8 columns (m16n8k16):
-//   S^T[key, head] = K Q^T    a lane reads 16 bytes (8 consecutive elements) of a key and feeds them to two products; Q is
-//                             held with the same order of elements in the k slots, which is all a dot product needs
-//   O^T[e, head] += V^T P^T   a lane reads 16 bytes of four keys and pairs neighbouring keys by byte permutes; rows g and
-//                             g + 8 of product j stand for elements 8 g + 2 j and 8 g + 2 j + 1, so a lane ends with
-//                             8 consecutive elements of two heads.  P^T gets from the accumulator layout to the operand
-//                             layout by a transposing 8 x 8 move inside the warp.
+// The products of 16 keys with the 8 or 16 query heads of a tile (m16n8k16):
+//   S[head, key] = Q K^T        the heads are the rows (rows 8..15 are empty up to 8 heads); a lane reads 16 bytes (8
+//                               consecutive elements) of one key and feeds them to two products; Q is held with the same
+//                               order of elements in the k slots, which is all a dot product needs
+//   O^T[e, head] += V^T P^T     P comes straight from the score accumulators (their layout is that of the second operand); a
+//                               lane reads 16 bytes of four keys and pairs neighbouring keys by byte permutes; rows g and
+//                               g + 8 of product j stand for elements 8 g + 2 j and 8 g + 2 j + 1
 // P goes into the product as the sum of two 16-bit numbers (its rounding and the rounding of the rest), so its rounding,
-// which would be as large as that of the output, does not count; a running maximum and sum are kept in fp32.
+// which would be as large as that of the output, does not count.  Maximum and sum are kept in fp32, and the maximum in use
+// is only raised when a score exceeds it by more than 2^8 in the exponent (numerator and denominator carry the same
+// factor), so most blocks need one vote of the warp where a running maximum would take shuffles and a rescaling.
 #include <math.h>
 
 #include <algorithm>
@@ -27,10 +29,26 @@ namespace kr {
 namespace {
 
 constexpr int PA_WARPS = 4;
-constexpr int STAGES = 3;                // key blocks of a warp in shared memory: one being used, two on their way
-constexpr int TILE = PA_WARPS * 16;   // keys of a tile: 16 for every warp
+constexpr int STAGES = 2;                // steps of a warp in shared memory: one being used, one on its way
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.69314718055994531f;
+constexpr float RAISE = 8.f;
+
+// n / d for 0 <= n < 2^31 by a product: with 2^(s-1) < d <= 2^s, m = floor(2^(31+s) / d) + 1 is off by less than d 2^-(31+s)
+// of itself, which n < 2^31 cannot carry past the next integer.
+struct Divisor {
+    uint32_t m;
+    int s;
+    explicit Divisor(uint32_t d) : m(0), s(0) {
+        if (d == 1) return;
+        int up = 0;
+        while ((1ull << up) < d) ++up;
+        m = static_cast<uint32_t>((1ull << (31 + up)) / d + 1);
+        s = up - 1;
+    }
+    Divisor() = default;
+    __device__ __forceinline__ int quotient(int n) const { return m ? static_cast<int>(__umulhi(n, m) >> s) : n; }
+};
 
 struct PagedAttnParams {
     PagedView c;
@@ -44,6 +62,8 @@ struct PagedAttnParams {
     int rows, n_head, window;
     uint32_t *status;
     uint8_t *workspace;
+    Divisor by_page;
+    bool page_of_16;   // page_size is a multiple of 16: the 16 keys of a product lie in one page
 };
 
 __device__ __forceinline__ void mma_keys(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -55,33 +75,30 @@ __device__ __forceinline__ void mma_keys(float (&c)[4], uint32_t a0, uint32_t a1
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
-    uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
-}
-
-// The 16-key block at key0 of one (sequence, key/value head) as the lanes need it: keys g and g + 8 of K, keys 2t, 2t + 1,
-// 2t + 8, 2t + 9 of V (g = lane / 4, t = lane % 4).  A lane copies the pieces that it will read itself, so a block needs no
-// barrier of any kind between its copy and its use, and every access to shared memory is a warp's 512 bytes in a row.
+// One step of a warp: SUBS blocks of 16 keys of one (sequence, key/value head), as the lanes need them: of a block the keys g
+// and g + 8 of K and the keys 2t, 2t + 1, 2t + 8, 2t + 9 of V (g = lane / 4, t = lane % 4).  A lane copies the pieces that
+// it will read itself, so a step needs no barrier of any kind between its copy and its use, and every access to shared
+// memory is a warp's 512 bytes in a row.
 template <int HD>
-struct KeyBlock {
+struct Step {
     static constexpr int CH = (HD + 31) / 32;   // 32-element chunks of a key, 8 elements of each per lane
     static constexpr int HF = (HD + 63) / 64;   // 64-element halves of a value, 8 elements of each per lane
-    static constexpr int PIECES = 2 * CH + 4 * HF;   // 16-byte pieces of a lane, kept as [piece][lane] in shared memory
-    static constexpr int BYTES = PIECES * 512;
+    static constexpr int BLOCK = 2 * CH + 4 * HF;   // 16-byte pieces of a lane and block, kept as [piece][lane]
+    static constexpr int SUBS = HD <= 64 ? 2 : 1;
+    static constexpr int KEYS = SUBS * 16;          // of a warp
+    static constexpr int TILE = KEYS * PA_WARPS;    // of the CTA
 };
 
 template <int HD, int NT>
-struct Running {   // online softmax of 8 NT heads over the keys of one warp; heads 8 nt + 2t + {0, 1} per lane
-    static constexpr int HF = KeyBlock<HD>::HF;
-    float m[NT][2], l[NT][2];       // maximum in use (log2 domain), this lane's part of the sum
-    float o[NT][HF * 4][4];
+struct Running {   // online softmax of 8 NT heads over the keys of one warp
+    static constexpr int HF = Step<HD>::HF;
+    float m[NT], base[NT], l[NT];   // head 8 nt + g: maximum in use (log2 domain; base: 0 for -inf), this lane's part of the sum
+    float o[NT][HF * 4][4];         // heads 8 nt + 2t + {0, 1}
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            m[nt][0] = m[nt][1] = -INFINITY;
-            l[nt][0] = l[nt][1] = 0.f;
+            m[nt] = -INFINITY;
+            base[nt] = l[nt] = 0.f;
 #pragma unroll
             for (int j = 0; j < HF * 4; ++j) o[nt][j][0] = o[nt][j][1] = o[nt][j][2] = o[nt][j][3] = 0.f;
         }
@@ -97,96 +114,111 @@ struct ScoreForm {
     float scale2;    // scale * log2(e)
 };
 
-// `live[i]`: whether key g + 8 i of the block is visible; `back`: position of key g minus that of the query
+// `mask`: which keys of the step are visible; `back`: position of its first key minus that of the query
 template <int HD, int NT>
-__device__ __forceinline__ void take_block(Running<HD, NT> &run, const uint4 *block, const uint4 (&q)[NT][KeyBlock<HD>::CH],
-                                           const bool (&live)[2], int back, const ScoreForm &f, const float (&slope)[NT][2]) {
-    constexpr int CH = KeyBlock<HD>::CH, HF = KeyBlock<HD>::HF;
-    float sc[NT][4];
+__device__ __forceinline__ void take_step(Running<HD, NT> &run, const uint4 *pieces, const uint4 (&q)[NT][Step<HD>::CH],
+                                          uint32_t mask, int back, const ScoreForm &f, const float (&slope)[NT], int lane) {
+    constexpr int CH = Step<HD>::CH, HF = Step<HD>::HF, SUBS = Step<HD>::SUBS, BLOCK = Step<HD>::BLOCK;
+    constexpr uint32_t ALL = SUBS == 2 ? 0xFFFFFFFFu : 0xFFFFu;
+    const int t = lane & 3;
+    float s[2 * SUBS][4];   // [8 keys]: head g, keys 2t and 2t + 1; head g + 8, the same keys
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
+    for (int kt = 0; kt < 2 * SUBS; ++kt) {
+        s[kt][0] = s[kt][1] = s[kt][2] = s[kt][3] = 0.f;
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const uint4 k0 = block[(2 * c) * 32], k1 = block[(2 * c + 1) * 32];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            mma_keys(sc[nt], k0.x, k1.x, k0.y, k1.y, q[nt][c].x, q[nt][c].y);
-            mma_keys(sc[nt], k0.z, k1.z, k0.w, k1.w, q[nt][c].z, q[nt][c].w);
+        for (int c = 0; c < CH; ++c) {
+            const uint4 k = pieces[((kt >> 1) * BLOCK + 2 * c + (kt & 1)) * 32];
+            const uint4 a = q[0][c], b = NT == 2 ? q[NT - 1][c] : make_uint4(0u, 0u, 0u, 0u);
+            mma_keys(s[kt], a.x, b.x, a.y, b.y, k.x, k.y);
+            mma_keys(s[kt], a.z, b.z, a.w, b.w, k.z, k.w);
         }
     }
-    uint32_t hi[NT][2], lo[NT][2];
+    bool over = false;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        float (&s)[4] = sc[nt];
-        // s[2 i + e]: key g + 8 i, head 2t + e
+    for (int kt = 0; kt < 2 * SUBS; ++kt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float x = s[i];
+        for (int i = 0; i < 2 * NT; ++i) {
+            float x = s[kt][i];
             if (f.plain) {
                 x *= f.scale2;
             } else {
                 x *= f.scale;
                 if (f.cap > 0.f) x = f.cap * tanhf(x * f.inv_cap);
-                x = (x + slope[nt][i & 1] * static_cast<float>(back + (i >> 1) * 8)) * LOG2E;
+                x = (x + slope[i >> 1] * static_cast<float>(back + kt * 8 + 2 * t + (i & 1))) * LOG2E;
             }
-            s[i] = live[i >> 1] ? x : -INFINITY;
+            s[kt][i] = x;
         }
-        float p[4];
-        bool moved = false;
-        float corr[2];
+    if (mask != ALL) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float mx = fmaxf(s[e], s[2 + e]);
-            mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
-            mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
-            mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
-            mx = fmaxf(mx, run.m[nt][e]);
-            const float base = mx == -INFINITY ? 0.f : mx;   // nothing visible yet: every weight is 2^-inf = 0
-            corr[e] = ex2_approx(run.m[nt][e] - base);
-            moved |= mx != run.m[nt][e];
-            run.m[nt][e] = mx;
-            p[e] = ex2_approx(s[e] - base);
-            p[2 + e] = ex2_approx(s[2 + e] - base);
-            run.l[nt][e] = run.l[nt][e] * corr[e] + (p[e] + p[2 + e]);
-        }
-        if (__any_sync(0xFFFFFFFFu, moved)) {
+        for (int kt = 0; kt < 2 * SUBS; ++kt)
+#pragma unroll
+            for (int i = 0; i < 2 * NT; ++i)
+                if (!(mask >> (kt * 8 + 2 * t + (i & 1)) & 1)) s[kt][i] = -INFINITY;
+    }
+    float top[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        top[nt] = fmaxf(s[0][2 * nt], s[0][2 * nt + 1]);
+#pragma unroll
+        for (int kt = 1; kt < 2 * SUBS; ++kt) top[nt] = fmaxf(top[nt], fmaxf(s[kt][2 * nt], s[kt][2 * nt + 1]));
+        over |= top[nt] > run.m[nt] + RAISE;
+    }
+    if (__any_sync(0xFFFFFFFFu, over)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float mx = fmaxf(top[nt], __shfl_xor_sync(0xFFFFFFFFu, top[nt], 1));
+            mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 2));
+            mx = fmaxf(mx, run.m[nt]);
+            run.base[nt] = mx == -INFINITY ? 0.f : mx;   // nothing visible yet: every weight is 2^-inf = 0
+            const float corr = ex2_approx(run.m[nt] - run.base[nt]);
+            run.m[nt] = mx;
+            run.l[nt] *= corr;
+            const float c0 = __shfl_sync(0xFFFFFFFFu, corr, t * 8), c1 = __shfl_sync(0xFFFFFFFFu, corr, t * 8 + 4);
 #pragma unroll
             for (int j = 0; j < HF * 4; ++j) {
-                run.o[nt][j][0] *= corr[0];
-                run.o[nt][j][1] *= corr[1];
-                run.o[nt][j][2] *= corr[0];
-                run.o[nt][j][3] *= corr[1];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t w = pack_h16x2(p[2 * i], p[2 * i + 1]);
-            hi[nt][i] = transpose_8x8(w);
-            lo[nt][i] = transpose_8x8(pack_h16x2(p[2 * i] - h16_lo(w), p[2 * i + 1] - h16_hi(w)));
-        }
-    }
-#pragma unroll
-    for (int hf = 0; hf < HF; ++hf) {
-        const uint4 *v = block + (2 * CH + 4 * hf) * 32;
-        const uint4 v0 = v[0], v1 = v[32], v2 = v[64], v3 = v[96];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t a0 = __byte_perm(word(v0, j), word(v1, j), 0x5410), a1 = __byte_perm(word(v0, j), word(v1, j), 0x7632);
-            const uint32_t a2 = __byte_perm(word(v2, j), word(v3, j), 0x5410), a3 = __byte_perm(word(v2, j), word(v3, j), 0x7632);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                mma_keys(run.o[nt][hf * 4 + j], a0, a1, a2, a3, hi[nt][0], hi[nt][1]);
-                mma_keys(run.o[nt][hf * 4 + j], a0, a1, a2, a3, lo[nt][0], lo[nt][1]);
+                run.o[nt][j][0] *= c0;
+                run.o[nt][j][1] *= c1;
+                run.o[nt][j][2] *= c0;
+                run.o[nt][j][3] *= c1;
             }
         }
     }
+    uint32_t hi[NT][2 * SUBS], lo[NT][2 * SUBS];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int kt = 0; kt < 2 * SUBS; ++kt) {
+            const float p0 = ex2_approx(s[kt][2 * nt] - run.base[nt]), p1 = ex2_approx(s[kt][2 * nt + 1] - run.base[nt]);
+            run.l[nt] += p0 + p1;
+            hi[nt][kt] = pack_h16x2(p0, p1);
+            lo[nt][kt] = pack_h16x2(p0 - h16_lo(hi[nt][kt]), p1 - h16_hi(hi[nt][kt]));
+        }
+#pragma unroll
+    for (int sb = 0; sb < SUBS; ++sb)
+#pragma unroll
+        for (int hf = 0; hf < HF; ++hf) {
+            const uint4 *v = pieces + (sb * BLOCK + 2 * CH + 4 * hf) * 32;
+            const uint4 v0 = v[0], v1 = v[32], v2 = v[64], v3 = v[96];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t a0 = __byte_perm(word(v0, j), word(v1, j), 0x5410), a1 = __byte_perm(word(v0, j), word(v1, j), 0x7632);
+                const uint32_t a2 = __byte_perm(word(v2, j), word(v3, j), 0x5410), a3 = __byte_perm(word(v2, j), word(v3, j), 0x7632);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    mma_keys(run.o[nt][hf * 4 + j], a0, a1, a2, a3, hi[nt][2 * sb], hi[nt][2 * sb + 1]);
+                    mma_keys(run.o[nt][hf * 4 + j], a0, a1, a2, a3, lo[nt][2 * sb], lo[nt][2 * sb + 1]);
+                }
+            }
+        }
 }
 
 // What row r asks for: its visible keys lo .. n - 1 of sequence seq.  False: padding, or (bad) no such sequence or length.
 struct RowKeys {
-    int seq, lo, n, tiles;   // tiles of TILE keys, at least one (a row without keys writes zeros)
+    int seq, lo, n, tiles;   // tiles from lo rounded down to a multiple of 16; at least one (a row without keys writes zeros)
+    __device__ __forceinline__ int start() const { return lo & ~15; }
 };
 
+template <int TILE>
 __device__ __forceinline__ bool row_keys(const PagedAttnParams &p, int r, RowKeys &k, bool &bad) {
     k.seq = p.row_seq ? p.row_seq[r] : r;
     k.tiles = 0;
@@ -197,7 +229,7 @@ __device__ __forceinline__ bool row_keys(const PagedAttnParams &p, int r, RowKey
         return false;
     }
     k.lo = p.window > 0 && k.n > p.window ? k.n - p.window : 0;
-    k.tiles = max(1, (k.n - k.lo + TILE - 1) / TILE);
+    k.tiles = max(1, (k.n - k.start() + TILE - 1) / TILE);
     return true;
 }
 
@@ -214,7 +246,7 @@ struct Part {
 // A part in the workspace, as the accumulators lie in a warp: [NT][HF * 4 products][32 lanes][4] o, then [2][HEADS] m and l.
 template <int HD, int NT>
 struct PartShape {
-    static constexpr int HEADS = 8 * NT, PRODUCTS = KeyBlock<HD>::HF * 4;
+    static constexpr int HEADS = 8 * NT, PRODUCTS = Step<HD>::HF * 4;
     static constexpr int O_FLOATS = NT * PRODUCTS * 128;
     static constexpr int FLOATS = O_FLOATS + 2 * HEADS;
 };
@@ -245,16 +277,17 @@ struct Place {
 
 template <int HD, int NT>
 struct Smem {
-    uint4 ring[PA_WARPS][STAGES][KeyBlock<HD>::PIECES * 32];
-    float4 o[PA_WARPS][KeyBlock<HD>::HF * 4][32];   // one head tile of every warp, to be joined
-    float m[PA_WARPS][8], l[PA_WARPS][8];
+    uint4 ring[PA_WARPS][STAGES][Step<HD>::SUBS * Step<HD>::BLOCK * 32];
+    float4 o[PA_WARPS][4][32];   // four products of every warp, to be joined
+    float m[PA_WARPS][8 * NT], l[PA_WARPS][8 * NT];
     long long sum[PA_WARPS], before;
     int row;
 };
 
 template <int HD, int NT>
 __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAttnParams p) {
-    constexpr int CH = KeyBlock<HD>::CH, HF = KeyBlock<HD>::HF, HEADS = 8 * NT;
+    constexpr int CH = Step<HD>::CH, HF = Step<HD>::HF, SUBS = Step<HD>::SUBS, BLOCK = Step<HD>::BLOCK, KEYS = Step<HD>::KEYS;
+    constexpr int TILE = Step<HD>::TILE, HEADS = 8 * NT;
     using Shape = PartShape<HD, NT>;
     extern __shared__ __align__(16) uint8_t smem_raw[];
     Smem<HD, NT> &sm = *reinterpret_cast<Smem<HD, NT> *>(smem_raw);
@@ -277,7 +310,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
     bool bad = false;
     for (int r = row_lo; r < row_hi; ++r) {
         RowKeys k;
-        row_keys(p, r, k, bad);
+        row_keys<TILE>(p, r, k, bad);
         mine += k.tiles;
     }
     long long upto = mine;
@@ -303,7 +336,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
         if (c0 < c1 && c0 >= before * units && c0 < upto * units) {
             for (int r = row_lo; r < row_hi; ++r) {
                 RowKeys k;
-                row_keys(p, r, k, bad);
+                row_keys<TILE>(p, r, k, bad);
                 if (c0 < (before + k.tiles) * units) {
                     sm.row = r;
                     sm.before = before;
@@ -322,60 +355,97 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
     Place at;
     at.r = sm.row;
     // (no such row, here and below: the lengths changed under the kernel)
-    if (at.r < 0 || !row_keys(p, at.r, at.k, bad)) return;
+    if (at.r < 0 || !row_keys<TILE>(p, at.r, at.k, bad)) return;
     long long row_c0 = sm.before * units;          // first tile of row at.r
     at.unit = static_cast<int>((c0 - row_c0) / at.k.tiles);
     at.tile = static_cast<int>((c0 - row_c0) % at.k.tiles);
     Place ahead = at;
     long long to_issue = c1 - c0;
     bool bad_page = false;
-    // lanes 0..15 (and again 16..31) each look up the page of one key of their warp's block; -1: not visible.  The lookup of
-    // a block is requested one block before its copies need it.
-    auto look_up = [&](const Place &w) {
-        const int key = w.k.lo + w.tile * TILE + warp * 16 + (lane & 15);
-        return key < w.k.n ? p.c.table[w.k.seq * p.c.table_stride + key / p.c.page_size] : -1;
+    // Each lane looks up the page of one key of its warp's step (lanes 16..31 those of 0..15 again in steps of 16 keys); -1: not
+    // visible.  The lookup for a step is requested one step before its copies need it.
+    int page, slot;
+    const uint16_t *head_k, *head_v;   // of the key/value head of `ahead`
+    auto look_up = [&] {
+        const int key = ahead.k.start() + ahead.tile * TILE + warp * KEYS + (lane & (KEYS - 1));
+        const int i = p.by_page.quotient(key);
+        slot = key - i * p.c.page_size;
+        page = key < ahead.k.n ? p.c.table[ahead.k.seq * p.c.table_stride + i] : -1;
     };
     auto step_row = [&](Place &w) {   // to the next row with tiles; false when there is none
         do {
             if (++w.r == p.rows) return false;
-            row_keys(p, w.r, w.k, bad);
+            row_keys<TILE>(p, w.r, w.k, bad);
         } while (w.k.tiles == 0);
         return true;
     };
-    int page = look_up(ahead), fill = 0;
-    uint32_t seen[STAGES - 1];   // keys visible in the blocks under way, oldest first
+    auto head_of = [&] {
+        const long long off = ahead.unit / head_tiles * p.c.head_stride;
+        head_k = p.c.k + off + t * 8;
+        head_v = p.c.v + off + g * 8;
+    };
+    const long long slots_g = g * p.c.slot_stride, slots_t = 2 * t * p.c.slot_stride;
+    int fill = 0;
+    uint32_t seen[STAGES - 1];   // keys visible in the steps under way, oldest first
     auto issue = [&]() -> uint32_t {
         uint32_t mask = 0;
         if (to_issue > 0) {
-            const int key0 = ahead.k.lo + ahead.tile * TILE + warp * 16;
+            const int key0 = ahead.k.start() + ahead.tile * TILE + warp * KEYS;
             if (key0 < ahead.k.n) {
+                const int key = key0 + (lane & (KEYS - 1));
                 if (page < 0 || page >= p.c.n_pages) {
+                    bad_page |= key < ahead.k.n;
                     page = -1;
-                    bad_page |= key0 + (lane & 15) < ahead.k.n;
                 }
-                mask = __ballot_sync(0xFFFFFFFFu, page >= 0) & 0xFFFFu;
-                const long long off = max(page, 0) * p.c.page_stride + (key0 + (lane & 15)) % p.c.page_size * p.c.slot_stride +
-                                      ahead.unit / head_tiles * p.c.head_stride;
-                uint4 *to = &sm.ring[warp][fill][lane];
+                mask = __ballot_sync(0xFFFFFFFFu, page >= 0 && key >= ahead.k.lo);
+                if (SUBS == 1) mask &= 0xFFFFu;
+                const long long off = max(page, 0) * p.c.page_stride + slot * p.c.slot_stride;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint16_t *row = p.c.k + __shfl_sync(0xFFFFFFFFu, off, g + 8 * i) + t * 8;
-                    const bool live = mask >> (g + 8 * i) & 1;
+                for (int sb = 0; sb < SUBS; ++sb) {
+                    uint4 *to = &sm.ring[warp][fill][sb * BLOCK * 32 + lane];
+                    const uint32_t m16 = mask >> (sb * 16) & 0xFFFFu;
+                    const bool in_one = p.page_of_16 && m16 == 0xFFFFu;
+                    const long long first = __shfl_sync(0xFFFFFFFFu, off, sb * 16);   // of the block's first key
+                    if (in_one) {
 #pragma unroll
-                    for (int c = 0; c < CH; ++c) {
-                        const bool in = live && c * 32 + t * 8 < HD;
-                        copy16(to + (2 * c + i) * 32, in ? row + c * 32 : p.c.k, in);
-                    }
-                }
+                        for (int i = 0; i < 2; ++i) {
+                            const uint16_t *row = head_k + first + slots_g + i * 8 * p.c.slot_stride;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int who = 2 * t + (i & 1) + (i >> 1) * 8;
-                    const uint16_t *row = p.c.v + __shfl_sync(0xFFFFFFFFu, off, who) + g * 8;
-                    const bool live = mask >> who & 1;
+                            for (int c = 0; c < CH; ++c) {
+                                const bool in = HD % 32 == 0 || c * 32 + t * 8 < HD;
+                                copy16(to + (2 * c + i) * 32, in ? row + c * 32 : p.c.k, in);
+                            }
+                        }
 #pragma unroll
-                    for (int hf = 0; hf < HF; ++hf) {
-                        const bool in = live && hf * 64 + g * 8 < HD;
-                        copy16(to + (2 * CH + 4 * hf + i) * 32, in ? row + hf * 64 : p.c.v, in);
+                        for (int i = 0; i < 4; ++i) {
+                            const uint16_t *row = head_v + first + slots_t + ((i >> 1) * 8 + (i & 1)) * p.c.slot_stride;
+#pragma unroll
+                            for (int hf = 0; hf < HF; ++hf) {
+                                const bool in = HD % 64 == 0 || hf * 64 + g * 8 < HD;
+                                copy16(to + (2 * CH + 4 * hf + i) * 32, in ? row + hf * 64 : p.c.v, in);
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int who = g + 8 * i;
+                            const uint16_t *row = head_k + __shfl_sync(0xFFFFFFFFu, off, sb * 16 + who);
+#pragma unroll
+                            for (int c = 0; c < CH; ++c) {
+                                const bool in = (m16 >> who & 1) && c * 32 + t * 8 < HD;
+                                copy16(to + (2 * c + i) * 32, in ? row + c * 32 : p.c.k, in);
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int who = 2 * t + (i & 1) + (i >> 1) * 8;
+                            const uint16_t *row = head_v + __shfl_sync(0xFFFFFFFFu, off, sb * 16 + who);
+#pragma unroll
+                            for (int hf = 0; hf < HF; ++hf) {
+                                const bool in = (m16 >> who & 1) && hf * 64 + g * 8 < HD;
+                                copy16(to + (2 * CH + 4 * hf + i) * 32, in ? row + hf * 64 : p.c.v, in);
+                            }
+                        }
                     }
                 }
             }
@@ -386,14 +456,17 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
                         ahead.unit = 0;
                         if (!step_row(ahead)) to_issue = 0;
                     }
+                    head_of();
                 }
-                page = look_up(ahead);
+                look_up();
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
         if (++fill == STAGES) fill = 0;
         return mask;
     };
+    head_of();
+    look_up();
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) seen[i] = issue();
 
@@ -406,19 +479,16 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
         const int hk = at.unit / head_tiles, first = at.unit % head_tiles * HEADS;
         const int heads = min(HEADS, rep - first), h0 = hk * rep + first;
         uint4 q[NT][CH];
-        float slope[NT][2];
+        float slope[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
+            const int h = nt * 8 + g;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const int h = nt * 8 + g, e = c * 32 + t * 8;
+                const int e = c * 32 + t * 8;
                 q[nt][c] = h < heads && e < HD ? *reinterpret_cast<const uint4 *>(p.q + at.r * p.q_row + (h0 + h) * p.q_head + e) : zero;
             }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int h = nt * 8 + 2 * t + e;
-                slope[nt][e] = p.slopes && h < heads ? p.slopes[h0 + h] : 0.f;
-            }
+            slope[nt] = p.slopes && h < heads ? p.slopes[h0 + h] : 0.f;
         }
         Running<HD, NT> run;
         run.clear();
@@ -427,62 +497,61 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
             const uint32_t mask = seen[0];
 #pragma unroll
             for (int j = 0; j + 1 < STAGES - 1; ++j) seen[j] = seen[j + 1];
-            // the block used one step ago has been read: its place takes the next copies
+            // the step used before has been read: its place takes the next copies
             seen[STAGES - 2] = issue();
-            if (mask) {
-                const bool live[2] = {(mask >> g & 1) != 0, (mask >> (g + 8) & 1) != 0};
-                take_block<HD, NT>(run, &sm.ring[warp][use][lane], q, live,
-                                   at.k.lo + (at.tile + i) * TILE + warp * 16 + g - (at.k.n - 1), form, slope);
-            }
+            if (mask)
+                take_step<HD, NT>(run, &sm.ring[warp][use][lane], q, mask,
+                                  at.k.start() + (at.tile + i) * TILE + warp * KEYS - (at.k.n - 1), form, slope, lane);
             if (++use == STAGES) use = 0;
         }
 
-        // the warps' results of the unit meet in shared memory, one head tile at a time
+        // the warps' results of the unit meet in shared memory, four products at a time: warp w joins product w
         const bool whole = at.tile == 0 && seg == at.k.tiles;
         float *slot = slots + ((long long)blockIdx.x * 2 + (at.tile == 0 ? 1 : 0)) * Shape::FLOATS;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            __syncthreads();
+            float l_sum = run.l[nt];
+            l_sum += __shfl_xor_sync(0xFFFFFFFFu, l_sum, 1);
+            l_sum += __shfl_xor_sync(0xFFFFFFFFu, l_sum, 2);
+            float c[PA_WARPS][2], m[2], l[2] = {0.f, 0.f};
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float l = run.l[nt][e];
-                l += __shfl_xor_sync(0xFFFFFFFFu, l, 4);
-                l += __shfl_xor_sync(0xFFFFFFFFu, l, 8);
-                l += __shfl_xor_sync(0xFFFFFFFFu, l, 16);
-                if (g == 0) {
-                    sm.m[warp][2 * t + e] = run.m[nt][e];
-                    sm.l[warp][2 * t + e] = l;
+            for (int hf = 0; hf < HF; ++hf) {
+                __syncthreads();
+                if (hf == 0 && t == 0) {
+                    sm.m[warp][nt * 8 + g] = run.m[nt];
+                    sm.l[warp][nt * 8 + g] = l_sum;
                 }
-            }
 #pragma unroll
-            for (int j = 0; j < HF * 4; ++j)
-                sm.o[warp][j][lane] = make_float4(run.o[nt][j][0], run.o[nt][j][1], run.o[nt][j][2], run.o[nt][j][3]);
-            __syncthreads();
-            float m[2], l[2] = {0.f, 0.f}, c[PA_WARPS][2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                m[e] = -INFINITY;
-#pragma unroll
-                for (int w = 0; w < PA_WARPS; ++w) m[e] = fmaxf(m[e], sm.m[w][2 * t + e]);
-                const float base = m[e] == -INFINITY ? 0.f : m[e];
-#pragma unroll
-                for (int w = 0; w < PA_WARPS; ++w) {
-                    c[w][e] = ex2_approx(sm.m[w][2 * t + e] - base);
-                    l[e] += sm.l[w][2 * t + e] * c[w][e];
+                for (int j = 0; j < 4; ++j) {
+                    const float(&o)[4] = run.o[nt][hf * 4 + j];
+                    sm.o[warp][j][lane] = make_float4(o[0], o[1], o[2], o[3]);
                 }
-            }
+                __syncthreads();
+                if (hf == 0) {
 #pragma unroll
-            for (int jj = 0; jj < HF; ++jj) {
-                const int j = jj * 4 + warp;
+                    for (int e = 0; e < 2; ++e) {
+                        const int h = nt * 8 + 2 * t + e;
+                        m[e] = -INFINITY;
+#pragma unroll
+                        for (int w = 0; w < PA_WARPS; ++w) m[e] = fmaxf(m[e], sm.m[w][h]);
+                        const float base = m[e] == -INFINITY ? 0.f : m[e];
+#pragma unroll
+                        for (int w = 0; w < PA_WARPS; ++w) {
+                            c[w][e] = ex2_approx(sm.m[w][h] - base);
+                            l[e] += sm.l[w][h] * c[w][e];
+                        }
+                    }
+                }
                 float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < PA_WARPS; ++w) {
-                    const float4 x = sm.o[w][j][lane];
+                    const float4 x = sm.o[w][warp][lane];
                     o.x += x.x * c[w][0];
                     o.y += x.y * c[w][1];
                     o.z += x.z * c[w][0];
                     o.w += x.w * c[w][1];
                 }
+                const int j = hf * 4 + warp;
                 if (whole) store_pair<HD>(p, at.r, h0, heads, nt, j, lane, o, l);
                 else *reinterpret_cast<float4 *>(slot + ((nt * HF * 4 + j) * 32 + lane) * 4) = o;
             }
@@ -599,7 +668,8 @@ int launch_nt(const PagedAttnParams &p, cudaStream_t st) {
     const long long units = (long long)p.c.n_kv_head * ((rep + 8 * NT - 1) / (8 * NT)) * p.rows;
     const long long keys = (long long)p.c.max_pages * p.c.page_size;
     const long long seen = p.window > 0 && p.window < keys ? p.window : keys;
-    const long long tiles = (seen + TILE - 1) / TILE;
+    // (a window that begins inside a 16-key block touches up to 15 keys more)
+    const long long tiles = std::min((keys + Step<HD>::TILE - 1) / Step<HD>::TILE, (seen + 15 + Step<HD>::TILE - 1) / Step<HD>::TILE);
     const long long grid = std::min<long long>((long long)sms * n, units * tiles);
     int rc = cuda_check(launch_pdl(paged_attn_kernel<HD, NT>, dim3((unsigned)grid), dim3(PA_WARPS * 32), SMEM, st, p),
                         "paged attention: launch");
@@ -663,6 +733,8 @@ extern "C" int kraken_op_paged_attention(const kraken_paged_cache *cache, const 
     p.n_head = a->n_head;
     p.window = a->window;
     p.status = d_status;
+    p.by_page = Divisor(cache->page_size);
+    p.page_of_16 = cache->page_size % 16 == 0;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     switch (cache->head_dim) {
         case 64: return launch<64>(p, st);

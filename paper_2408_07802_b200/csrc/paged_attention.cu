@@ -19,6 +19,7 @@
 // is only raised when a score exceeds it by more than 2^8 in the exponent (numerator and denominator carry the same
 // factor), so most blocks need one vote of the warp where a running maximum would take shuffles and a rescaling.
 #include <math.h>
+#include <string.h>
 
 #include <algorithm>
 
@@ -63,7 +64,6 @@ struct PagedAttnParams {
     uint32_t *status;
     uint8_t *workspace;
     Divisor by_page;
-    bool page_of_16;   // page_size is a multiple of 16: the 16 keys of a product lie in one page
 };
 
 __device__ __forceinline__ void mma_keys(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -75,16 +75,18 @@ __device__ __forceinline__ void mma_keys(float (&c)[4], uint32_t a0, uint32_t a1
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// One step of a warp: SUBS blocks of 16 keys of one (sequence, key/value head), as the lanes need them: of a block the keys g
-// and g + 8 of K and the keys 2t, 2t + 1, 2t + 8, 2t + 9 of V (g = lane / 4, t = lane % 4).  A lane copies the pieces that
-// it will read itself, so a step needs no barrier of any kind between its copy and its use, and every access to shared
-// memory is a warp's 512 bytes in a row.
+// One step of a warp: SUBS blocks of 16 keys of one (sequence, key/value head).  A block lies in shared memory as tiles of
+// 16 rows x 128 bytes (64 elements), the halves of K and then those of V, with the 128-byte swizzle: the 16-byte piece c of
+// row r is at r * 128 + (c ^ (r & 7)) * 16.  Of a block a lane reads (g = lane / 4, t = lane % 4)
+//   keys g and g + 8 of K: of every half the pieces 2t and 2t + 1;      keys 2t, 2t + 1, 2t + 8, 2t + 9 of V: piece g
+// which in this layout are free of bank conflicts.
 template <int HD>
 struct Step {
-    static constexpr int CH = (HD + 31) / 32;   // 32-element chunks of a key, 8 elements of each per lane
-    static constexpr int HF = (HD + 63) / 64;   // 64-element halves of a value, 8 elements of each per lane
-    static constexpr int BLOCK = 2 * CH + 4 * HF;   // 16-byte pieces of a lane and block, kept as [piece][lane]
+    static constexpr int HF = (HD + 63) / 64;       // 64-element halves of a head
+    static constexpr int HALF = 16 * 128;           // bytes of a tile
+    static constexpr int BLOCK = 2 * HF * HALF;
     static constexpr int SUBS = HD <= 64 ? 2 : 1;
+    static constexpr int BYTES = SUBS * BLOCK;
     static constexpr int KEYS = SUBS * 16;          // of a warp
     static constexpr int TILE = KEYS * PA_WARPS;    // of the CTA
 };
@@ -116,18 +118,19 @@ struct ScoreForm {
 
 // `mask`: which keys of the step are visible; `back`: position of its first key minus that of the query
 template <int HD, int NT>
-__device__ __forceinline__ void take_step(Running<HD, NT> &run, const uint4 *pieces, const uint4 (&q)[NT][Step<HD>::CH],
+__device__ __forceinline__ void take_step(Running<HD, NT> &run, const uint8_t *step, const uint4 (&q)[NT][2 * Step<HD>::HF],
                                           uint32_t mask, int back, const ScoreForm &f, const float (&slope)[NT], int lane) {
-    constexpr int CH = Step<HD>::CH, HF = Step<HD>::HF, SUBS = Step<HD>::SUBS, BLOCK = Step<HD>::BLOCK;
+    constexpr int HF = Step<HD>::HF, SUBS = Step<HD>::SUBS, BLOCK = Step<HD>::BLOCK, HALF = Step<HD>::HALF;
     constexpr uint32_t ALL = SUBS == 2 ? 0xFFFFFFFFu : 0xFFFFu;
-    const int t = lane & 3;
+    const int g = lane >> 2, t = lane & 3;
     float s[2 * SUBS][4];   // [8 keys]: head g, keys 2t and 2t + 1; head g + 8, the same keys
 #pragma unroll
     for (int kt = 0; kt < 2 * SUBS; ++kt) {
         s[kt][0] = s[kt][1] = s[kt][2] = s[kt][3] = 0.f;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const uint4 k = pieces[((kt >> 1) * BLOCK + 2 * c + (kt & 1)) * 32];
+        for (int c = 0; c < 2 * HF; ++c) {
+            const uint4 k = *reinterpret_cast<const uint4 *>(step + (kt >> 1) * BLOCK + (c >> 1) * HALF + (kt & 1) * 1024 + g * 128 +
+                                                             ((2 * t + (c & 1)) ^ g) * 16);
             const uint4 a = q[0][c], b = NT == 2 ? q[NT - 1][c] : make_uint4(0u, 0u, 0u, 0u);
             mma_keys(s[kt], a.x, b.x, a.y, b.y, k.x, k.y);
             mma_keys(s[kt], a.z, b.z, a.w, b.w, k.z, k.w);
@@ -197,12 +200,20 @@ __device__ __forceinline__ void take_step(Running<HD, NT> &run, const uint4 *pie
     for (int sb = 0; sb < SUBS; ++sb)
 #pragma unroll
         for (int hf = 0; hf < HF; ++hf) {
-            const uint4 *v = pieces + (sb * BLOCK + 2 * CH + 4 * hf) * 32;
-            const uint4 v0 = v[0], v1 = v[32], v2 = v[64], v3 = v[96];
+            uint4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = *reinterpret_cast<const uint4 *>(step + sb * BLOCK + (HF + hf) * HALF + (i >> 1) * 1024 + (2 * t + (i & 1)) * 128 +
+                                                        (g ^ (2 * t + (i & 1))) * 16);
+            if (mask != ALL) {   // what lies behind the visible keys may be anything, and 0 times a NaN is one
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!(mask >> (sb * 16 + (i >> 1) * 8 + 2 * t + (i & 1)) & 1)) v[i] = make_uint4(0u, 0u, 0u, 0u);
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t a0 = __byte_perm(word(v0, j), word(v1, j), 0x5410), a1 = __byte_perm(word(v0, j), word(v1, j), 0x7632);
-                const uint32_t a2 = __byte_perm(word(v2, j), word(v3, j), 0x5410), a3 = __byte_perm(word(v2, j), word(v3, j), 0x7632);
+                const uint32_t a0 = __byte_perm(word(v[0], j), word(v[1], j), 0x5410), a1 = __byte_perm(word(v[0], j), word(v[1], j), 0x7632);
+                const uint32_t a2 = __byte_perm(word(v[2], j), word(v[3], j), 0x5410), a3 = __byte_perm(word(v[2], j), word(v[3], j), 0x7632);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     mma_keys(run.o[nt][hf * 4 + j], a0, a1, a2, a3, hi[nt][2 * sb], hi[nt][2 * sb + 1]);
@@ -265,8 +276,8 @@ __device__ __forceinline__ void store_pair(const PagedAttnParams &p, int row, in
 
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * LN2; }
 
-__device__ __forceinline__ void copy16(void *smem, const void *gmem, bool live) {   // zeros where not live
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(smem)), "l"(gmem), "r"(live ? 16 : 0) : "memory");
+__device__ __forceinline__ void copy16(uint32_t smem, const void *gmem, bool live) {   // zeros where not live
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(gmem), "r"(live ? 16 : 0) : "memory");
 }
 
 // A place on the line of tiles
@@ -277,20 +288,36 @@ struct Place {
 
 template <int HD, int NT>
 struct Smem {
-    uint4 ring[PA_WARPS][STAGES][Step<HD>::SUBS * Step<HD>::BLOCK * 32];
+    uint8_t ring[PA_WARPS][STAGES][Step<HD>::BYTES];
     float4 o[PA_WARPS][4][32];   // four products of every warp, to be joined
     float m[PA_WARPS][8 * NT], l[PA_WARPS][8 * NT];
+    uint64_t full[PA_WARPS][STAGES];
     long long sum[PA_WARPS], before;
     int row;
+    uint32_t gave_up;
 };
 
-template <int HD, int NT>
-__global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAttnParams p) {
-    constexpr int CH = Step<HD>::CH, HF = Step<HD>::HF, SUBS = Step<HD>::SUBS, BLOCK = Step<HD>::BLOCK, KEYS = Step<HD>::KEYS;
+// BOXES: pages of a multiple of 16 keys, whose 16-key blocks the copy engine brings in, one 64-element half at a time, by
+// tensor maps over (element, slot, head, page); other page sizes are copied by the lanes, each the pieces that it will read
+// itself.
+template <int HD, int NT, bool BOXES>
+__global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k,
+                                                                   const __grid_constant__ CUtensorMap tm_v, const PagedAttnParams p) {
+    constexpr int HF = Step<HD>::HF, SUBS = Step<HD>::SUBS, BLOCK = Step<HD>::BLOCK, HALF = Step<HD>::HALF, KEYS = Step<HD>::KEYS;
     constexpr int TILE = Step<HD>::TILE, HEADS = 8 * NT;
     using Shape = PartShape<HD, NT>;
-    extern __shared__ __align__(16) uint8_t smem_raw[];
-    Smem<HD, NT> &sm = *reinterpret_cast<Smem<HD, NT> *>(smem_raw);
+    extern __shared__ uint8_t smem_raw[];
+    Smem<HD, NT> &sm = *reinterpret_cast<Smem<HD, NT> *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    if (threadIdx.x == 0) {
+        sm.row = -1;
+        sm.gave_up = 0;
+        if (BOXES) {
+            for (int i = 0; i < PA_WARPS * STAGES; ++i) mbar_init(&sm.full[0][0] + i, 1);
+            fence_barrier_init();
+            prefetch_tensormap(&tm_k);
+            prefetch_tensormap(&tm_v);
+        }
+    }
     pdl_wait();
     const int rep = p.n_head / p.c.n_kv_head;
     const int head_tiles = (rep + HEADS - 1) / HEADS;
@@ -298,10 +325,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     Part *parts = reinterpret_cast<Part *>(p.workspace);
     float *slots = reinterpret_cast<float *>(p.workspace + sizeof(Part) * gridDim.x);
-    if (threadIdx.x == 0) {
-        parts[blockIdx.x].row = -1;
-        sm.row = -1;
-    }
+    if (threadIdx.x == 0) parts[blockIdx.x].row = -1;
 
     // where this CTA's share begins: every thread adds up the tiles of a run of rows
     const int per = (p.rows + PA_WARPS * 32 - 1) / (PA_WARPS * 32);
@@ -362,16 +386,6 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
     Place ahead = at;
     long long to_issue = c1 - c0;
     bool bad_page = false;
-    // Each lane looks up the page of one key of its warp's step (lanes 16..31 those of 0..15 again in steps of 16 keys); -1: not
-    // visible.  The lookup for a step is requested one step before its copies need it.
-    int page, slot;
-    const uint16_t *head_k, *head_v;   // of the key/value head of `ahead`
-    auto look_up = [&] {
-        const int key = ahead.k.start() + ahead.tile * TILE + warp * KEYS + (lane & (KEYS - 1));
-        const int i = p.by_page.quotient(key);
-        slot = key - i * p.c.page_size;
-        page = key < ahead.k.n ? p.c.table[ahead.k.seq * p.c.table_stride + i] : -1;
-    };
     auto step_row = [&](Place &w) {   // to the next row with tiles; false when there is none
         do {
             if (++w.r == p.rows) return false;
@@ -379,12 +393,19 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
         } while (w.k.tiles == 0);
         return true;
     };
-    auto head_of = [&] {
-        const long long off = ahead.unit / head_tiles * p.c.head_stride;
-        head_k = p.c.k + off + t * 8;
-        head_v = p.c.v + off + g * 8;
+    // The page of every block of a step (BOXES), or of one key a lane; -1: not visible.  It is looked up one step before its
+    // copies need it.
+    constexpr int LOOKUPS = BOXES ? SUBS : 1;
+    int page[LOOKUPS], slot[LOOKUPS], head = 0;
+    auto look_up = [&] {
+        const int key0 = ahead.k.start() + ahead.tile * TILE + warp * KEYS + (BOXES ? 0 : lane & (KEYS - 1));
+#pragma unroll
+        for (int i = 0; i < LOOKUPS; ++i) {
+            const int key = key0 + i * 16, n = p.by_page.quotient(key);
+            slot[i] = key - n * p.c.page_size;
+            page[i] = key < ahead.k.n ? p.c.table[ahead.k.seq * p.c.table_stride + n] : -1;
+        }
     };
-    const long long slots_g = g * p.c.slot_stride, slots_t = 2 * t * p.c.slot_stride;
     int fill = 0;
     uint32_t seen[STAGES - 1];   // keys visible in the steps under way, oldest first
     auto issue = [&]() -> uint32_t {
@@ -392,58 +413,70 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
         if (to_issue > 0) {
             const int key0 = ahead.k.start() + ahead.tile * TILE + warp * KEYS;
             if (key0 < ahead.k.n) {
-                const int key = key0 + (lane & (KEYS - 1));
-                if (page < 0 || page >= p.c.n_pages) {
-                    bad_page |= key < ahead.k.n;
-                    page = -1;
-                }
-                mask = __ballot_sync(0xFFFFFFFFu, page >= 0 && key >= ahead.k.lo);
-                if (SUBS == 1) mask &= 0xFFFFu;
-                const long long off = max(page, 0) * p.c.page_stride + slot * p.c.slot_stride;
+                uint8_t *to = sm.ring[warp][fill];
+                if constexpr (BOXES) {
+                    // keys lo .. n - 1 of the step, without the blocks whose page does not exist
+                    const int to_n = ahead.k.n - key0, to_lo = ahead.k.lo - key0;
+                    mask = to_n >= 32 ? 0xFFFFFFFFu : (1u << to_n) - 1u;
+                    if (SUBS == 1) mask &= 0xFFFFu;
+                    if (to_lo > 0) mask = to_lo >= 32 ? 0u : mask >> to_lo << to_lo;
 #pragma unroll
-                for (int sb = 0; sb < SUBS; ++sb) {
-                    uint4 *to = &sm.ring[warp][fill][sb * BLOCK * 32 + lane];
-                    const uint32_t m16 = mask >> (sb * 16) & 0xFFFFu;
-                    const bool in_one = p.page_of_16 && m16 == 0xFFFFu;
-                    const long long first = __shfl_sync(0xFFFFFFFFu, off, sb * 16);   // of the block's first key
-                    if (in_one) {
+                    for (int i = 0; i < SUBS; ++i)
+                        if (page[i] < 0 || page[i] >= p.c.n_pages) {
+                            bad_page |= key0 + i * 16 < ahead.k.n;
+                            mask &= ~(0xFFFFu << (i * 16));
+                        }
+                    __syncwarp();   // every lane has read what this stage held before
+                    if (lane == 0 && mask) {
+                        int blocks = 0;
+#pragma unroll
+                        for (int i = 0; i < SUBS; ++i) blocks += (mask >> (i * 16) & 0xFFFFu) != 0;
+                        uint64_t *full = &sm.full[warp][fill];
+                        mbar_expect_tx(full, blocks * BLOCK);
+#pragma unroll
+                        for (int i = 0; i < SUBS; ++i) {
+                            if (!(mask >> (i * 16) & 0xFFFFu)) continue;
+#pragma unroll
+                            for (int hf = 0; hf < HF; ++hf) {
+                                tma_load_4d(to + i * BLOCK + hf * HALF, &tm_k, full, hf * 64, slot[i], head, page[i]);
+                                tma_load_4d(to + i * BLOCK + (HF + hf) * HALF, &tm_v, full, hf * 64, slot[i], head, page[i]);
+                            }
+                        }
+                    }
+                } else {
+                    const int key = key0 + (lane & (KEYS - 1));
+                    if (page[0] < 0 || page[0] >= p.c.n_pages) {
+                        bad_page |= key < ahead.k.n;
+                        page[0] = -1;
+                    }
+                    mask = __ballot_sync(0xFFFFFFFFu, page[0] >= 0 && key >= ahead.k.lo);
+                    if (SUBS == 1) mask &= 0xFFFFu;
+                    const long long off = max(page[0], 0) * p.c.page_stride + slot[0] * p.c.slot_stride + head * p.c.head_stride;
+                    const uint32_t at = smem_u32(to);
+#pragma unroll
+                    for (int sb = 0; sb < SUBS; ++sb) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            const uint16_t *row = head_k + first + slots_g + i * 8 * p.c.slot_stride;
+                            const int who = sb * 16 + g + 8 * i;
+                            const uint16_t *row = p.c.k + __shfl_sync(0xFFFFFFFFu, off, who);
 #pragma unroll
-                            for (int c = 0; c < CH; ++c) {
-                                const bool in = HD % 32 == 0 || c * 32 + t * 8 < HD;
-                                copy16(to + (2 * c + i) * 32, in ? row + c * 32 : p.c.k, in);
+                            for (int c = 0; c < 2 * HF; ++c) {
+                                const int e = (c >> 1) * 64 + (2 * t + (c & 1)) * 8;
+                                const bool in = (mask >> who & 1) && e < HD;
+                                copy16(at + sb * BLOCK + (c >> 1) * HALF + i * 1024 + g * 128 + ((2 * t + (c & 1)) ^ g) * 16,
+                                       in ? row + e : p.c.k, in);
                             }
                         }
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const uint16_t *row = head_v + first + slots_t + ((i >> 1) * 8 + (i & 1)) * p.c.slot_stride;
+                            const int who = sb * 16 + 2 * t + (i & 1) + (i >> 1) * 8;
+                            const uint16_t *row = p.c.v + __shfl_sync(0xFFFFFFFFu, off, who);
 #pragma unroll
                             for (int hf = 0; hf < HF; ++hf) {
-                                const bool in = HD % 64 == 0 || hf * 64 + g * 8 < HD;
-                                copy16(to + (2 * CH + 4 * hf + i) * 32, in ? row + hf * 64 : p.c.v, in);
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int who = g + 8 * i;
-                            const uint16_t *row = head_k + __shfl_sync(0xFFFFFFFFu, off, sb * 16 + who);
-#pragma unroll
-                            for (int c = 0; c < CH; ++c) {
-                                const bool in = (m16 >> who & 1) && c * 32 + t * 8 < HD;
-                                copy16(to + (2 * c + i) * 32, in ? row + c * 32 : p.c.k, in);
-                            }
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int who = 2 * t + (i & 1) + (i >> 1) * 8;
-                            const uint16_t *row = head_v + __shfl_sync(0xFFFFFFFFu, off, sb * 16 + who);
-#pragma unroll
-                            for (int hf = 0; hf < HF; ++hf) {
-                                const bool in = (m16 >> who & 1) && hf * 64 + g * 8 < HD;
-                                copy16(to + (2 * CH + 4 * hf + i) * 32, in ? row + hf * 64 : p.c.v, in);
+                                const int e = hf * 64 + g * 8;
+                                const bool in = (mask >> who & 1) && e < HD;
+                                copy16(at + sb * BLOCK + (HF + hf) * HALF + (i >> 1) * 1024 + (2 * t + (i & 1)) * 128 +
+                                           (g ^ (2 * t + (i & 1))) * 16, in ? row + e : p.c.v, in);
                             }
                         }
                     }
@@ -456,16 +489,28 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
                         ahead.unit = 0;
                         if (!step_row(ahead)) to_issue = 0;
                     }
-                    head_of();
+                    head = ahead.unit / head_tiles;
                 }
                 look_up();
             }
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (!BOXES) asm volatile("cp.async.commit_group;" ::: "memory");
         if (++fill == STAGES) fill = 0;
         return mask;
     };
-    head_of();
+    // the oldest step under way has arrived
+    uint32_t phases = 0;
+    auto arrived = [&](int stage, uint32_t mask) {
+        if constexpr (BOXES) {
+            if (!mask) return;
+            mbar_wait(&sm.full[warp][stage], phases >> stage & 1, &sm.gave_up);
+            phases ^= 1u << stage;
+            __syncwarp();
+        } else {
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+        }
+    };
+    head = ahead.unit / head_tiles;
     look_up();
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) seen[i] = issue();
@@ -478,14 +523,14 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
         const int seg = static_cast<int>(min(left, (long long)(at.k.tiles - at.tile)));
         const int hk = at.unit / head_tiles, first = at.unit % head_tiles * HEADS;
         const int heads = min(HEADS, rep - first), h0 = hk * rep + first;
-        uint4 q[NT][CH];
+        uint4 q[NT][2 * HF];
         float slope[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int h = nt * 8 + g;
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                const int e = c * 32 + t * 8;
+            for (int c = 0; c < 2 * HF; ++c) {
+                const int e = (c >> 1) * 64 + (2 * t + (c & 1)) * 8;
                 q[nt][c] = h < heads && e < HD ? *reinterpret_cast<const uint4 *>(p.q + at.r * p.q_row + (h0 + h) * p.q_head + e) : zero;
             }
             slope[nt] = p.slopes && h < heads ? p.slopes[h0 + h] : 0.f;
@@ -493,14 +538,14 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
         Running<HD, NT> run;
         run.clear();
         for (int i = 0; i < seg; ++i) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
             const uint32_t mask = seen[0];
+            arrived(use, mask);
 #pragma unroll
             for (int j = 0; j + 1 < STAGES - 1; ++j) seen[j] = seen[j + 1];
             // the step used before has been read: its place takes the next copies
             seen[STAGES - 2] = issue();
             if (mask)
-                take_step<HD, NT>(run, &sm.ring[warp][use][lane], q, mask,
+                take_step<HD, NT>(run, sm.ring[warp][use], q, mask,
                                   at.k.start() + (at.tile + i) * TILE + warp * KEYS - (at.k.n - 1), form, slope, lane);
             if (++use == STAGES) use = 0;
         }
@@ -581,7 +626,17 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const PagedAt
             if (!step_row(at)) break;
         }
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
+    // (nothing is under way here unless the lengths changed under the kernel)
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) {
+        arrived(use, seen[i]);
+        if (++use == STAGES) use = 0;
+    }
+    if (!BOXES) asm volatile("cp.async.wait_all;" ::: "memory");
+    if (BOXES && *static_cast<volatile uint32_t *>(&sm.gave_up)) {
+        for (int i = 0; i < 64; ++i) __nanosleep(10000);
+        if (lane == 0 && p.status) atomicOr(p.status, STATUS_WAIT_LIMIT);
+    }
     if (bad_page && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
 }
 
@@ -648,17 +703,17 @@ size_t workspace_bytes(int rep, int head_dim) {
     return (size_t)sms * MAX_CTAS_PER_SM * (sizeof(Part) + 2 * heads * ((head_dim + 63) / 64 * 64 + 2) * sizeof(float));
 }
 
-template <int HD, int NT>
-int launch_nt(const PagedAttnParams &p, cudaStream_t st) {
+template <int HD, int NT, bool BOXES>
+int launch_nt(const PagedAttnParams &p, const CUtensorMap &tm_k, const CUtensorMap &tm_v, cudaStream_t st) {
     static std::atomic<int> resident[MAX_DEVICES];   // CTAs of this instance that an SM of the device holds
     const int dev = device_slot(), sms = sm_count();
     if (dev < 0 || sms <= 0) return KRAKEN_ECUDA;
     int n = resident[dev].load(std::memory_order_relaxed);
-    constexpr int SMEM = sizeof(Smem<HD, NT>);
+    constexpr int SMEM = sizeof(Smem<HD, NT>) + 1024;
     if (n <= 0) {
-        int rc = cuda_check(cudaFuncSetAttribute(paged_attn_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM),
+        int rc = cuda_check(cudaFuncSetAttribute(paged_attn_kernel<HD, NT, BOXES>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM),
                             "paged attention: shared memory opt-in");
-        if (!rc) rc = cuda_check(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, paged_attn_kernel<HD, NT>, PA_WARPS * 32, SMEM),
+        if (!rc) rc = cuda_check(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, paged_attn_kernel<HD, NT, BOXES>, PA_WARPS * 32, SMEM),
                                  "paged attention: occupancy");
         if (rc) return rc;
         n = n < 1 ? 1 : (n > MAX_CTAS_PER_SM ? MAX_CTAS_PER_SM : n);
@@ -671,7 +726,7 @@ int launch_nt(const PagedAttnParams &p, cudaStream_t st) {
     // (a window that begins inside a 16-key block touches up to 15 keys more)
     const long long tiles = std::min((keys + Step<HD>::TILE - 1) / Step<HD>::TILE, (seen + 15 + Step<HD>::TILE - 1) / Step<HD>::TILE);
     const long long grid = std::min<long long>((long long)sms * n, units * tiles);
-    int rc = cuda_check(launch_pdl(paged_attn_kernel<HD, NT>, dim3((unsigned)grid), dim3(PA_WARPS * 32), SMEM, st, p),
+    int rc = cuda_check(launch_pdl(paged_attn_kernel<HD, NT, BOXES>, dim3((unsigned)grid), dim3(PA_WARPS * 32), SMEM, st, tm_k, tm_v, p),
                         "paged attention: launch");
     // with one tile a unit nothing is ever split
     if (rc || tiles == 1) return rc;
@@ -681,7 +736,19 @@ int launch_nt(const PagedAttnParams &p, cudaStream_t st) {
 
 template <int HD>
 int launch(const PagedAttnParams &p, cudaStream_t st) {
-    return p.n_head / p.c.n_kv_head <= 8 ? launch_nt<HD, 1>(p, st) : launch_nt<HD, 2>(p, st);
+    const bool narrow = p.n_head / p.c.n_kv_head <= 8;
+    CUtensorMap tm_k, tm_v;
+    if (p.c.page_size % 16 == 0) {
+        const uint64_t dims[4] = {(uint64_t)HD, (uint64_t)p.c.page_size, (uint64_t)p.c.n_kv_head, (uint64_t)p.c.n_pages};
+        const uint64_t strides[3] = {(uint64_t)p.c.slot_stride, (uint64_t)p.c.head_stride, (uint64_t)p.c.page_stride};
+        const uint32_t box[4] = {64, 16, 1, 1};
+        // (strides that a tensor map cannot hold: the lanes copy)
+        if (encode_tma_4d_bf16(&tm_k, p.c.k, dims, strides, box) == KRAKEN_OK &&
+            encode_tma_4d_bf16(&tm_v, p.c.v, dims, strides, box) == KRAKEN_OK)
+            return narrow ? launch_nt<HD, 1, true>(p, tm_k, tm_v, st) : launch_nt<HD, 2, true>(p, tm_k, tm_v, st);
+    }
+    memset(&tm_k, 0, sizeof(tm_k));
+    return narrow ? launch_nt<HD, 1, false>(p, tm_k, tm_k, st) : launch_nt<HD, 2, false>(p, tm_k, tm_k, st);
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -734,7 +801,6 @@ extern "C" int kraken_op_paged_attention(const kraken_paged_cache *cache, const 
     p.window = a->window;
     p.status = d_status;
     p.by_page = Divisor(cache->page_size);
-    p.page_of_16 = cache->page_size % 16 == 0;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     switch (cache->head_dim) {
         case 64: return launch<64>(p, st);

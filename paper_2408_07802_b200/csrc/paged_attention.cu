@@ -31,6 +31,9 @@ namespace {
 
 constexpr int PA_WARPS = 4;
 constexpr int STAGES = 2;                // steps of a warp in shared memory: one being used, one on its way
+// What beginning and finishing a unit costs, in tiles: without it a CTA whose share is a run of short sequences took 17 us
+// longer than the others (64 ragged sequences).
+constexpr int BEGIN = 1;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.69314718055994531f;
 constexpr float RAISE = 8.f;
@@ -64,6 +67,7 @@ struct PagedAttnParams {
     uint32_t *status;
     uint8_t *workspace;
     Divisor by_page;
+    int box;   // keys of a copy: 16 or 8
 };
 
 __device__ __forceinline__ void mma_keys(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -85,7 +89,7 @@ struct Step {
     static constexpr int HF = (HD + 63) / 64;       // 64-element halves of a head
     static constexpr int HALF = 16 * 128;           // bytes of a tile
     static constexpr int BLOCK = 2 * HF * HALF;
-    static constexpr int SUBS = HD <= 64 ? 2 : 1;
+        static constexpr int SUBS = HD <= 64 ? 2 : 1;
     static constexpr int BYTES = SUBS * BLOCK;
     static constexpr int KEYS = SUBS * 16;          // of a warp
     static constexpr int TILE = KEYS * PA_WARPS;    // of the CTA
@@ -111,7 +115,7 @@ __device__ __forceinline__ uint32_t word(const uint4 &v, int i) { return i == 0 
 
 // Score options that the caller asked for, uniform over the launch
 struct ScoreForm {
-    float scale, cap, inv_cap;
+    float scale, cap, inv_cap2;   // inv_cap2: 2 log2(e) / cap
     bool plain;      // neither cap nor slopes: one product takes the scale and log2(e)
     float scale2;    // scale * log2(e)
 };
@@ -126,6 +130,7 @@ __device__ __forceinline__ void take_step(Running<HD, NT> &run, const uint8_t *s
     float s[2 * SUBS][4];   // [8 keys]: head g, keys 2t and 2t + 1; head g + 8, the same keys
 #pragma unroll
     for (int kt = 0; kt < 2 * SUBS; ++kt) {
+        float z[4] = {0.f, 0.f, 0.f, 0.f};   // two chains of products: a chain of all of them would take twice as long
         s[kt][0] = s[kt][1] = s[kt][2] = s[kt][3] = 0.f;
 #pragma unroll
         for (int c = 0; c < 2 * HF; ++c) {
@@ -133,8 +138,10 @@ __device__ __forceinline__ void take_step(Running<HD, NT> &run, const uint8_t *s
                                                              ((2 * t + (c & 1)) ^ g) * 16);
             const uint4 a = q[0][c], b = NT == 2 ? q[NT - 1][c] : make_uint4(0u, 0u, 0u, 0u);
             mma_keys(s[kt], a.x, b.x, a.y, b.y, k.x, k.y);
-            mma_keys(s[kt], a.z, b.z, a.w, b.w, k.z, k.w);
+            mma_keys(z, a.z, b.z, a.w, b.w, k.z, k.w);
         }
+#pragma unroll
+        for (int i = 0; i < 2 * NT; ++i) s[kt][i] += z[i];
     }
     bool over = false;
 #pragma unroll
@@ -146,7 +153,8 @@ __device__ __forceinline__ void take_step(Running<HD, NT> &run, const uint8_t *s
                 x *= f.scale2;
             } else {
                 x *= f.scale;
-                if (f.cap > 0.f) x = f.cap * tanhf(x * f.inv_cap);
+                // tanh y = 1 - 2 / (e^2y + 1): off by about 2^-23 absolute, i.e. the score by cap 2^-23
+                if (f.cap > 0.f) x = f.cap - 2.f * f.cap * rcp_approx(ex2_approx(x * f.inv_cap2) + 1.f);
                 x = (x + slope[i >> 1] * static_cast<float>(back + kt * 8 + 2 * t + (i & 1))) * LOG2E;
             }
             s[kt][i] = x;
@@ -232,9 +240,9 @@ struct RowKeys {
 template <int TILE>
 __device__ __forceinline__ bool row_keys(const PagedAttnParams &p, int r, RowKeys &k, bool &bad) {
     k.seq = p.row_seq ? p.row_seq[r] : r;
+    k.n = p.n_keys[r];
     k.tiles = 0;
     if (k.seq < 0) return false;
-    k.n = p.n_keys[r];
     if (k.seq >= p.c.n_seqs || k.n < 0 || k.n > (long long)p.c.max_pages * p.c.page_size) {
         bad = true;
         return false;
@@ -244,9 +252,10 @@ __device__ __forceinline__ bool row_keys(const PagedAttnParams &p, int r, RowKey
     return true;
 }
 
-// The work of a call is a line of tiles: rows in order, of each row its (key/value head, head tile) units in order, of each
-// unit its key tiles.  CTA i of G (at most one per tile) takes tiles [total i / G, total (i + 1) / G): the same number for every CTA, whatever the
-// lengths.  A unit that lies in one CTA is finished there; of one that does not, every CTA leaves its part in the
+// The work of a call is a line: rows in order, of each row its (key/value head, head tile) units in order, of each unit `begin`
+// places for its beginning and end and then one for every key tile (begin: BEGIN, or 0 where there are no more tiles than
+// CTAs).  CTA i of G takes the places [total i / G, total (i + 1) / G), the same number for every CTA whatever the lengths, and
+// works on the tiles among them; G is at most total / (begin + 1), so that there are some.  A unit that lies in one CTA is finished there; of one that does not, every CTA leaves its part in the
 // workspace (slot 1 where the unit begins, slot 0 elsewhere: a CTA has at most one of each) and the CTA with the
 // beginning notes who has the rest, for the joining kernel.
 struct Part {
@@ -293,13 +302,14 @@ struct Smem {
     float m[PA_WARPS][8 * NT], l[PA_WARPS][8 * NT];
     uint64_t full[PA_WARPS][STAGES];
     long long sum[PA_WARPS], before;
+    RowKeys keys;
     int row;
     uint32_t gave_up;
 };
 
-// BOXES: pages of a multiple of 16 keys, whose 16-key blocks the copy engine brings in, one 64-element half at a time, by
-// tensor maps over (element, slot, head, page); other page sizes are copied by the lanes, each the pieces that it will read
-// itself.
+// BOXES: pages of a multiple of 16 (or 8) keys, which the copy engine brings in as boxes of 16 (8) keys, one 64-element half at
+// a time, by tensor maps over (element, slot, head, page); with other page sizes the lanes copy, each the pieces that it will
+// read itself.
 template <int HD, int NT, bool BOXES>
 __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k,
                                                                    const __grid_constant__ CUtensorMap tm_v, const PagedAttnParams p) {
@@ -330,12 +340,13 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
     // where this CTA's share begins: every thread adds up the tiles of a run of rows
     const int per = (p.rows + PA_WARPS * 32 - 1) / (PA_WARPS * 32);
     const int row_lo = min(p.rows, (int)threadIdx.x * per), row_hi = min(p.rows, row_lo + per);
+    constexpr int ROWS_AT = 40;   // a sum of tiles, and above it of rows that have some
     long long mine = 0;
     bool bad = false;
     for (int r = row_lo; r < row_hi; ++r) {
         RowKeys k;
         row_keys<TILE>(p, r, k, bad);
-        mine += k.tiles;
+        if (k.tiles > 0) mine += (1LL << ROWS_AT) + k.tiles;
     }
     long long upto = mine;
 #pragma unroll
@@ -351,22 +362,26 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
         if (w < warp) upto += sm.sum[w];
         total += sm.sum[w];
     }
-    const long long all = total * units;
-    const long long n_cta = min((long long)gridDim.x, all);   // no CTA between the two ends of a unit is without a tile
+    const int begin = (total & ((1LL << ROWS_AT) - 1)) * units <= gridDim.x ? 0 : BEGIN;
+    auto places = [&](long long sum) { return ((sum & ((1LL << ROWS_AT) - 1)) + (sum >> ROWS_AT) * begin) * units; };
+    const long long all = places(total);
+    const long long n_cta = min((long long)gridDim.x, all / (begin + 1));
     const long long c0 = blockIdx.x < n_cta ? all * blockIdx.x / n_cta : all;
     const long long c1 = blockIdx.x < n_cta ? all * (blockIdx.x + 1) / n_cta : all;
     {
-        long long before = upto - mine;
-        if (c0 < c1 && c0 >= before * units && c0 < upto * units) {
+        long long before = places(upto - mine);
+        if (c0 < c1 && c0 >= before && c0 < places(upto)) {
             for (int r = row_lo; r < row_hi; ++r) {
                 RowKeys k;
                 row_keys<TILE>(p, r, k, bad);
-                if (c0 < (before + k.tiles) * units) {
+                const long long here = k.tiles > 0 ? (long long)(k.tiles + begin) * units : 0;
+                if (c0 < before + here) {
                     sm.row = r;
+                    sm.keys = k;
                     sm.before = before;
                     break;
                 }
-                before += k.tiles;
+                before += here;
             }
         }
     }
@@ -378,13 +393,15 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
     // `at`: the tile being worked on; `ahead`: the tile whose copy is issued next, up to STAGES - 1 further on
     Place at;
     at.r = sm.row;
-    // (no such row, here and below: the lengths changed under the kernel)
-    if (at.r < 0 || !row_keys<TILE>(p, at.r, at.k, bad)) return;
-    long long row_c0 = sm.before * units;          // first tile of row at.r
-    at.unit = static_cast<int>((c0 - row_c0) / at.k.tiles);
-    at.tile = static_cast<int>((c0 - row_c0) % at.k.tiles);
+    at.k = sm.keys;
+    if (at.r < 0) return;   // (no such row, here and below: the lengths changed under the kernel)
+    long long row_c0 = sm.before;          // first place of row at.r
+    at.unit = static_cast<int>((c0 - row_c0) / (at.k.tiles + begin));
+    const int skipped = static_cast<int>((c0 - row_c0) % (at.k.tiles + begin));
+    at.tile = max(0, skipped - begin);
     Place ahead = at;
-    long long to_issue = c1 - c0;
+    // places left to the copies and to the work: they go on by one place a tile, and by `begin` where a unit begins
+    long long to_issue = c1 - c0 - max(0, begin - skipped), left = to_issue;
     bool bad_page = false;
     auto step_row = [&](Place &w) {   // to the next row with tiles; false when there is none
         do {
@@ -393,18 +410,15 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
         } while (w.k.tiles == 0);
         return true;
     };
-    // The page of every block of a step (BOXES), or of one key a lane; -1: not visible.  It is looked up one step before its
+    // Lane i looks up the page of box i of a step (BOXES), or of key i; -1: not visible.  A step is looked up one step before its
     // copies need it.
-    constexpr int LOOKUPS = BOXES ? SUBS : 1;
-    int page[LOOKUPS], slot[LOOKUPS], head = 0;
+    const int box = BOXES ? p.box : 1;   // keys
+    int page, slot, head = 0;
     auto look_up = [&] {
-        const int key0 = ahead.k.start() + ahead.tile * TILE + warp * KEYS + (BOXES ? 0 : lane & (KEYS - 1));
-#pragma unroll
-        for (int i = 0; i < LOOKUPS; ++i) {
-            const int key = key0 + i * 16, n = p.by_page.quotient(key);
-            slot[i] = key - n * p.c.page_size;
-            page[i] = key < ahead.k.n ? p.c.table[ahead.k.seq * p.c.table_stride + n] : -1;
-        }
+        const int key = ahead.k.start() + ahead.tile * TILE + warp * KEYS + (BOXES ? min(lane * box, KEYS) : lane & (KEYS - 1));
+        const int n = p.by_page.quotient(key);
+        slot = key - n * p.c.page_size;
+        page = key < ahead.k.n && (!BOXES || lane * box < KEYS) ? p.c.table[ahead.k.seq * p.c.table_stride + n] : -1;
     };
     int fill = 0;
     uint32_t seen[STAGES - 1];   // keys visible in the steps under way, oldest first
@@ -415,43 +429,40 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
             if (key0 < ahead.k.n) {
                 uint8_t *to = sm.ring[warp][fill];
                 if constexpr (BOXES) {
-                    // keys lo .. n - 1 of the step, without the blocks whose page does not exist
+                    const int key = key0 + lane * box;
+                    const bool mine = lane * box < KEYS && key < ahead.k.n && key + box > ahead.k.lo;
+                    const bool there = mine && page >= 0 && page < p.c.n_pages;
+                    bad_page |= mine && !there;
+                    const uint32_t boxes = __ballot_sync(0xFFFFFFFFu, there);   // (every lane has read what this stage held before)
+#pragma unroll
+                    for (int i = 0; i < KEYS / 8; ++i)
+                        if (boxes >> i & 1) mask |= ((1u << box) - 1u) << ((i * box) & 31);
+                    // of these the keys lo .. n - 1
                     const int to_n = ahead.k.n - key0, to_lo = ahead.k.lo - key0;
-                    mask = to_n >= 32 ? 0xFFFFFFFFu : (1u << to_n) - 1u;
-                    if (SUBS == 1) mask &= 0xFFFFu;
+                    if (to_n < 32) mask &= (1u << to_n) - 1u;
                     if (to_lo > 0) mask = to_lo >= 32 ? 0u : mask >> to_lo << to_lo;
-#pragma unroll
-                    for (int i = 0; i < SUBS; ++i)
-                        if (page[i] < 0 || page[i] >= p.c.n_pages) {
-                            bad_page |= key0 + i * 16 < ahead.k.n;
-                            mask &= ~(0xFFFFu << (i * 16));
-                        }
-                    __syncwarp();   // every lane has read what this stage held before
-                    if (lane == 0 && mask) {
-                        int blocks = 0;
-#pragma unroll
-                        for (int i = 0; i < SUBS; ++i) blocks += (mask >> (i * 16) & 0xFFFFu) != 0;
+                    if (boxes) {
                         uint64_t *full = &sm.full[warp][fill];
-                        mbar_expect_tx(full, blocks * BLOCK);
-#pragma unroll
-                        for (int i = 0; i < SUBS; ++i) {
-                            if (!(mask >> (i * 16) & 0xFFFFu)) continue;
+                        if (lane == 0) mbar_expect_tx(full, __popc(boxes) * box * (2 * HF * 128));
+                        __syncwarp();
+                        if (there) {
+                            uint8_t *row = to + (lane * box / 16) * BLOCK + (lane * box % 16) * 128;
 #pragma unroll
                             for (int hf = 0; hf < HF; ++hf) {
-                                tma_load_4d(to + i * BLOCK + hf * HALF, &tm_k, full, hf * 64, slot[i], head, page[i]);
-                                tma_load_4d(to + i * BLOCK + (HF + hf) * HALF, &tm_v, full, hf * 64, slot[i], head, page[i]);
+                                tma_load_4d(row + hf * HALF, &tm_k, full, hf * 64, slot, head, page);
+                                tma_load_4d(row + (HF + hf) * HALF, &tm_v, full, hf * 64, slot, head, page);
                             }
                         }
                     }
                 } else {
                     const int key = key0 + (lane & (KEYS - 1));
-                    if (page[0] < 0 || page[0] >= p.c.n_pages) {
+                    if (page < 0 || page >= p.c.n_pages) {
                         bad_page |= key < ahead.k.n;
-                        page[0] = -1;
+                        page = -1;
                     }
-                    mask = __ballot_sync(0xFFFFFFFFu, page[0] >= 0 && key >= ahead.k.lo);
+                    mask = __ballot_sync(0xFFFFFFFFu, page >= 0 && key >= ahead.k.lo);
                     if (SUBS == 1) mask &= 0xFFFFu;
-                    const long long off = max(page[0], 0) * p.c.page_stride + slot[0] * p.c.slot_stride + head * p.c.head_stride;
+                    const long long off = max(page, 0) * p.c.page_stride + slot * p.c.slot_stride + head * p.c.head_stride;
                     const uint32_t at = smem_u32(to);
 #pragma unroll
                     for (int sb = 0; sb < SUBS; ++sb) {
@@ -485,13 +496,14 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
             if (--to_issue > 0) {
                 if (++ahead.tile == ahead.k.tiles) {
                     ahead.tile = 0;
+                    to_issue -= begin;
                     if (++ahead.unit == units) {
                         ahead.unit = 0;
-                        if (!step_row(ahead)) to_issue = 0;
+                        if (to_issue > 0 && !step_row(ahead)) to_issue = 0;
                     }
                     head = ahead.unit / head_tiles;
                 }
-                look_up();
+                if (to_issue > 0) look_up();
             }
         }
         if (!BOXES) asm volatile("cp.async.commit_group;" ::: "memory");
@@ -516,15 +528,12 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
     for (int i = 0; i < STAGES - 1; ++i) seen[i] = issue();
 
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    const ScoreForm form = {p.scale, p.cap, p.cap > 0.f ? 1.f / p.cap : 0.f, p.cap <= 0.f && !p.slopes, p.scale * LOG2E};
-    long long left = c1 - c0;
+    const ScoreForm form = {p.scale, p.cap, p.cap > 0.f ? 2.f * LOG2E / p.cap : 0.f, p.cap <= 0.f && !p.slopes, p.scale * LOG2E};
     int use = 0;
-    while (left > 0) {
-        const int seg = static_cast<int>(min(left, (long long)(at.k.tiles - at.tile)));
-        const int hk = at.unit / head_tiles, first = at.unit % head_tiles * HEADS;
-        const int heads = min(HEADS, rep - first), h0 = hk * rep + first;
-        uint4 q[NT][2 * HF];
-        float slope[NT];
+    uint4 q[NT][2 * HF];
+    float slope[NT];
+    auto load_q = [&] {
+        const int first = at.unit % head_tiles * HEADS, heads = min(HEADS, rep - first), h0 = at.unit / head_tiles * rep + first;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int h = nt * 8 + g;
@@ -535,6 +544,12 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
             }
             slope[nt] = p.slopes && h < heads ? p.slopes[h0 + h] : 0.f;
         }
+    };
+    load_q();
+    while (left > 0) {
+        const int seg = static_cast<int>(min(left, (long long)(at.k.tiles - at.tile)));
+        const int first = at.unit % head_tiles * HEADS, heads = min(HEADS, rep - first), h0 = at.unit / head_tiles * rep + first;
+        const int row = at.r;
         Running<HD, NT> run;
         run.clear();
         for (int i = 0; i < seg; ++i) {
@@ -550,9 +565,29 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
             if (++use == STAGES) use = 0;
         }
 
+        const bool begins = at.tile == 0, whole = begins && seg == at.k.tiles;
+        float *slot = slots + ((long long)blockIdx.x * 2 + (begins ? 1 : 0)) * Shape::FLOATS;
+        if (begins && !whole && threadIdx.x == 0) {
+            // the CTA with the unit's last place x: the largest i with all i / n_cta (rounded down) <= x
+            const long long x = row_c0 + (long long)(at.unit + 1) * (at.k.tiles + begin) - 1;
+            parts[blockIdx.x] = {row, at.unit, static_cast<int>(((x + 1) * n_cta - 1) / all), 0};
+        }
+        // the next unit's queries are requested before this one is finished
+        left -= seg;
+        if (left > begin) {
+            left -= begin;
+            at.tile = 0;
+            if (++at.unit == units) {
+                at.unit = 0;
+                row_c0 += (long long)units * (at.k.tiles + begin);
+                if (!step_row(at)) left = 0;
+            }
+            if (left > 0) load_q();
+        } else {
+            left = 0;
+        }
+
         // the warps' results of the unit meet in shared memory, four products at a time: warp w joins product w
-        const bool whole = at.tile == 0 && seg == at.k.tiles;
-        float *slot = slots + ((long long)blockIdx.x * 2 + (at.tile == 0 ? 1 : 0)) * Shape::FLOATS;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             float l_sum = run.l[nt];
@@ -597,7 +632,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
                     o.w += x.w * c[w][1];
                 }
                 const int j = hf * 4 + warp;
-                if (whole) store_pair<HD>(p, at.r, h0, heads, nt, j, lane, o, l);
+                if (whole) store_pair<HD>(p, row, h0, heads, nt, j, lane, o, l);
                 else *reinterpret_cast<float4 *>(slot + ((nt * HF * 4 + j) * 32 + lane) * 4) = o;
             }
             if (warp == 0 && g == 0) {
@@ -608,22 +643,10 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
                         slot[Shape::O_FLOATS + h] = m[e];
                         slot[Shape::O_FLOATS + HEADS + h] = l[e];
                     } else if (p.lse && h < heads) {
-                        p.lse[at.r * p.lse_row + h0 + h] = lse_of(m[e], l[e]);
+                        p.lse[row * p.lse_row + h0 + h] = lse_of(m[e], l[e]);
                     }
                 }
             }
-        }
-        if (at.tile == 0 && !whole && threadIdx.x == 0) {
-            // the CTA with the unit's last tile x: the largest i with all i / n_cta (rounded down) <= x
-            const long long x = row_c0 + (long long)(at.unit + 1) * at.k.tiles - 1;
-            parts[blockIdx.x] = {at.r, at.unit, static_cast<int>(((x + 1) * n_cta - 1) / all), 0};
-        }
-        left -= seg;
-        at.tile = 0;
-        if (++at.unit == units && left > 0) {
-            at.unit = 0;
-            row_c0 += (long long)units * at.k.tiles;
-            if (!step_row(at)) break;
         }
     }
     // (nothing is under way here unless the lengths changed under the kernel)
@@ -640,52 +663,104 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
     if (bad_page && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
 }
 
-// Joins the parts of the unit that begins in CTA blockIdx.x of the kernel above, for the elements of product blockIdx.y:
-// out = sum_i o_i 2^(m_i - m) / sum_i l_i 2^(m_i - m).  A warp takes every 8th part.
-constexpr int JOIN_WARPS = 8;
+// Joins the parts of the units that were split: out = sum_i o_i 2^(m_i - m) / sum_i l_i 2^(m_i - m).  A warp has one product
+// (128 floats of every part) and takes BATCH parts at a time: what this kernel waits for is the way to L2 and back.
+//   FEW = false  many units, of few parts each: CTA i joins the unit that begins in CTA i of the kernel above (if one does),
+//                a warp per product;
+//   FEW = true   few units, of many parts each: CTA (i, j) joins product j of unit i, whose beginning it looks for among the
+//                parts; its warps share the parts.  (One sequence of 131072 keys, 55 parts a unit: 8 us with one CTA a unit.)
+constexpr int JOIN_BATCH = 8, FEW_WARPS = 16;
 
-template <int HD, int NT>
-__global__ void __launch_bounds__(JOIN_WARPS * 32) paged_attn_join_kernel(const PagedAttnParams p, int n_cta) {
-    constexpr int HEADS = 8 * NT;
+template <int HD, int NT, bool FEW>
+__global__ void __launch_bounds__(FEW ? FEW_WARPS * 32 : NT *PartShape<HD, NT>::PRODUCTS * 32)
+paged_attn_join_kernel(const PagedAttnParams p, int n_cta) {
+    constexpr int HEADS = 8 * NT, GROUPS = FEW ? FEW_WARPS : 1, BATCH = FEW ? JOIN_BATCH / 2 : JOIN_BATCH;
     using Shape = PartShape<HD, NT>;
-    __shared__ float2 sm_m[JOIN_WARPS][32], sm_l[JOIN_WARPS][32];
-    __shared__ float4 sm_o[JOIN_WARPS][32];
+    __shared__ float2 sm_m[GROUPS][32], sm_l[GROUPS][32];
+    __shared__ float4 sm_o[GROUPS][32];
+    __shared__ int sm_begin;
     pdl_wait();
-    pdl_trigger();
-    const Part part = reinterpret_cast<const Part *>(p.workspace)[blockIdx.x];
+    const Part *parts = reinterpret_cast<const Part *>(p.workspace);
+    const int rep = p.n_head / p.c.n_kv_head, head_tiles = (rep + HEADS - 1) / HEADS, units = p.c.n_kv_head * head_tiles;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = FEW ? warp : 0, product = FEW ? blockIdx.y : warp;
+    int begin = blockIdx.x;
+    if (FEW) {
+        if (threadIdx.x == 0) sm_begin = -1;
+        __syncthreads();
+        for (int i = threadIdx.x; i < n_cta; i += FEW_WARPS * 32)
+            if (parts[i].row >= 0 && (long long)parts[i].row * units + parts[i].unit == blockIdx.x) sm_begin = i;
+        __syncthreads();
+        begin = sm_begin;
+        if (begin < 0) return;
+    }
+    const Part part = parts[begin];
     if (part.row < 0) return;
-    const int rep = p.n_head / p.c.n_kv_head, head_tiles = (rep + HEADS - 1) / HEADS;
     const int first = part.unit % head_tiles * HEADS, heads = min(HEADS, rep - first), h0 = part.unit / head_tiles * rep + first;
-    const int nt = blockIdx.y / Shape::PRODUCTS, j = blockIdx.y % Shape::PRODUCTS;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = nt * 8 + 2 * (lane & 3);
+    const int nt = product / Shape::PRODUCTS, j = product % Shape::PRODUCTS, h = nt * 8 + 2 * (lane & 3);
     const float *slots = reinterpret_cast<const float *>(p.workspace + sizeof(Part) * n_cta);
     float2 m = make_float2(-INFINITY, -INFINITY), l = make_float2(0.f, 0.f);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    auto add = [&](const float2 mi, const float2 li, const float4 oi) {
-        const float mx = fmaxf(m.x, mi.x), my = fmaxf(m.y, mi.y);
-        const float bx = mx == -INFINITY ? 0.f : mx, by = my == -INFINITY ? 0.f : my;
-        const float ax = ex2_approx(m.x - bx), cx = ex2_approx(mi.x - bx), ay = ex2_approx(m.y - by), cy = ex2_approx(mi.y - by);
+    auto scale_to = [&](float mx, float my, float2 &base) {   // the sums so far go over to a larger maximum
+        base = make_float2(mx == -INFINITY ? 0.f : mx, my == -INFINITY ? 0.f : my);
+        const float ax = ex2_approx(m.x - base.x), ay = ex2_approx(m.y - base.y);
         m = make_float2(mx, my);
-        l.x = l.x * ax + li.x * cx;
-        l.y = l.y * ay + li.y * cy;
-        o.x = o.x * ax + oi.x * cx;
-        o.y = o.y * ay + oi.y * cy;
-        o.z = o.z * ax + oi.z * cx;
-        o.w = o.w * ay + oi.w * cy;
+        l.x *= ax;
+        l.y *= ay;
+        o.x *= ax;
+        o.y *= ay;
+        o.z *= ax;
+        o.w *= ay;
     };
-#pragma unroll 4
-    for (int i = blockIdx.x + warp; i <= part.last_cta; i += JOIN_WARPS) {
-        const float *slot = slots + ((long long)i * 2 + (i == (int)blockIdx.x ? 1 : 0)) * Shape::FLOATS;
-        add(*reinterpret_cast<const float2 *>(slot + Shape::O_FLOATS + h), *reinterpret_cast<const float2 *>(slot + Shape::O_FLOATS + HEADS + h),
-            *reinterpret_cast<const float4 *>(slot + (blockIdx.y * 32 + lane) * 4));
-    }
-    sm_m[warp][lane] = m;
-    sm_l[warp][lane] = l;
-    sm_o[warp][lane] = o;
-    __syncthreads();
-    if (warp != 0) return;
+    auto add = [&](const float2 base, const float2 mi, const float2 li, const float4 oi) {
+        const float cx = ex2_approx(mi.x - base.x), cy = ex2_approx(mi.y - base.y);
+        l.x += li.x * cx;
+        l.y += li.y * cy;
+        o.x += oi.x * cx;
+        o.y += oi.y * cy;
+        o.z += oi.z * cx;
+        o.w += oi.w * cy;
+    };
+    for (int i0 = begin + group; i0 <= part.last_cta; i0 += GROUPS * BATCH) {
+        float2 mi[BATCH], li[BATCH];
+        float4 oi[BATCH];
 #pragma unroll
-    for (int w = 1; w < JOIN_WARPS; ++w) add(sm_m[w][lane], sm_l[w][lane], sm_o[w][lane]);
+        for (int b = 0; b < BATCH; ++b) {
+            const int i = i0 + b * GROUPS;
+            mi[b] = make_float2(-INFINITY, -INFINITY);
+            li[b] = make_float2(0.f, 0.f);
+            oi[b] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (i <= part.last_cta) {
+                const float *slot = slots + ((long long)i * 2 + (i == begin ? 1 : 0)) * Shape::FLOATS;
+                mi[b] = *reinterpret_cast<const float2 *>(slot + Shape::O_FLOATS + h);
+                li[b] = *reinterpret_cast<const float2 *>(slot + Shape::O_FLOATS + HEADS + h);
+                oi[b] = *reinterpret_cast<const float4 *>(slot + (product * 32 + lane) * 4);
+            }
+        }
+        float mx = m.x, my = m.y;
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            mx = fmaxf(mx, mi[b].x);
+            my = fmaxf(my, mi[b].y);
+        }
+        float2 base;
+        scale_to(mx, my, base);
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) add(base, mi[b], li[b], oi[b]);
+    }
+    if (GROUPS > 1) {
+        sm_m[group][lane] = m;
+        sm_l[group][lane] = l;
+        sm_o[group][lane] = o;
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int w = 1; w < GROUPS; ++w) {
+            const float2 mw = sm_m[w][lane];
+            float2 base;
+            scale_to(fmaxf(m.x, mw.x), fmaxf(m.y, mw.y), base);
+            add(base, mw, sm_l[w][lane], sm_o[w][lane]);
+        }
+    }
     const float ls[2] = {l.x, l.y};
     store_pair<HD>(p, part.row, h0, heads, nt, j, lane, o, ls);
     if (p.lse && j == 0 && lane < 4) {
@@ -730,18 +805,23 @@ int launch_nt(const PagedAttnParams &p, const CUtensorMap &tm_k, const CUtensorM
                         "paged attention: launch");
     // with one tile a unit nothing is ever split
     if (rc || tiles == 1) return rc;
-    return cuda_check(launch_pdl(paged_attn_join_kernel<HD, NT>, dim3((unsigned)grid, NT * PartShape<HD, NT>::PRODUCTS), dim3(JOIN_WARPS * 32), 0,
-                                 st, p, (int)grid), "paged attention join: launch");
+    // fewer units than an eighth of the CTAs: over 8 parts each where the lengths are alike
+    constexpr int PRODUCTS = NT * PartShape<HD, NT>::PRODUCTS;
+    const bool few = units * JOIN_BATCH < grid;
+    return cuda_check(few ? launch_pdl(paged_attn_join_kernel<HD, NT, true>, dim3((unsigned)units, PRODUCTS), dim3(FEW_WARPS * 32), 0, st, p,
+                                       (int)grid)
+                          : launch_pdl(paged_attn_join_kernel<HD, NT, false>, dim3((unsigned)grid), dim3(PRODUCTS * 32), 0, st, p, (int)grid),
+                      "paged attention join: launch");
 }
 
 template <int HD>
 int launch(const PagedAttnParams &p, cudaStream_t st) {
     const bool narrow = p.n_head / p.c.n_kv_head <= 8;
     CUtensorMap tm_k, tm_v;
-    if (p.c.page_size % 16 == 0) {
+    if (p.c.page_size % 8 == 0) {
         const uint64_t dims[4] = {(uint64_t)HD, (uint64_t)p.c.page_size, (uint64_t)p.c.n_kv_head, (uint64_t)p.c.n_pages};
         const uint64_t strides[3] = {(uint64_t)p.c.slot_stride, (uint64_t)p.c.head_stride, (uint64_t)p.c.page_stride};
-        const uint32_t box[4] = {64, 16, 1, 1};
+        const uint32_t box[4] = {64, (uint32_t)p.box, 1, 1};
         // (strides that a tensor map cannot hold: the lanes copy)
         if (encode_tma_4d_bf16(&tm_k, p.c.k, dims, strides, box) == KRAKEN_OK &&
             encode_tma_4d_bf16(&tm_v, p.c.v, dims, strides, box) == KRAKEN_OK)
@@ -801,6 +881,7 @@ extern "C" int kraken_op_paged_attention(const kraken_paged_cache *cache, const 
     p.window = a->window;
     p.status = d_status;
     p.by_page = Divisor(cache->page_size);
+    p.box = cache->page_size % 16 == 0 ? 16 : 8;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     switch (cache->head_dim) {
         case 64: return launch<64>(p, st);

@@ -1,7 +1,20 @@
-// Log probability of a given token, entropy and the largest logits of every row.
+// Log probability of a given token, entropy and the largest logits of every row, in one pass over the logits.
 //
 //   x = scale * logit, m = max x, S = sum e^(x - m):  lse = m + log S,  logprob = x_t - lse,
 //   entropy = log S + sum (m - x) e^(x - m) / S       (every term of the sum is positive: nothing cancels)
+//
+// Bound by HBM: 4 (or 2) bytes a logit against about 8 instructions.  Every thread keeps a maximum and the two sums of its
+// own logits, brought to a larger maximum 16 logits at a time; the threads of a row meet at the end.
+//
+// The alternatives are found in the same pass.  A logit and its index make one 64-bit key whose order is that of the list
+// (larger logit first, then lower index), so keys are distinct.  Of the first chunk the maxima of 64 groups of 8 threads are
+// taken: the k-th largest of them is a bound that k logits reach, and from then on only logits above the bound are put aside
+// (a few dozen of a row; a thread compares the maximum of its 16 logits, which it has anyway).  Where many threads exceed
+// the bound (logits in rising order) it is raised from that chunk in the same way; a chunk then adds at most
+// (k - 1) * 128 + 1 keys, and where these might not fit the keys put aside are cut down to the k largest first.  What is left
+// at the end is ranked by counting.
+//
+// Few rows: up to 8 CTAs of a cluster share a row and join through each other's shared memory.
 #include <math.h>
 
 #include "internal.h"
@@ -12,9 +25,18 @@ namespace kr {
 namespace {
 
 constexpr int LP_THREADS = 512;
+constexpr int LP_WARPS = LP_THREADS / 32;
 constexpr int LP_MAX_TOP = 32;
+constexpr int PER_THREAD = 16;                       // logits of a thread in a chunk
+constexpr int GROUP = 8, GROUPS = LP_THREADS / GROUP;
+constexpr int CHUNK_ADDS = (LP_MAX_TOP - 1) * GROUP * PER_THREAD + 1;
+constexpr int ASIDE = 6144;                          // room for keys put aside
+constexpr int MAX_CLUSTER = 8;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.69314718055994531f;
+typedef unsigned long long Key;
+static_assert(GROUPS == 64, "a warp ranks the groups' keys two a lane");
+static_assert(ASIDE > CHUNK_ADDS + LP_MAX_TOP, "after a cut a chunk has to fit");
 
 struct LogprobParams {
     const void *logits;
@@ -28,90 +50,361 @@ struct LogprobParams {
     uint32_t *status;
 };
 
-template <bool H16>
-__device__ __forceinline__ float logit_at(const void *row, int i) {
-    return H16 ? from_h16(static_cast<const uint16_t *>(row)[i]) : static_cast<const float *>(row)[i];
-}
-
-// Orders logits as the alternatives are listed: larger value first, of equal ones the lower index; NaN as -inf.
-// -0 and +0 are equal.
-__device__ __forceinline__ unsigned long long order_key(float x, int i) {
+// Larger logit first, of equal ones the lower index; NaN as -inf; -0 and +0 are equal.  Every key is above 0.
+__device__ __forceinline__ Key order_key(float x, int i) {
     if (!(x > -INFINITY)) x = -INFINITY;
     const uint32_t u = __float_as_uint(x + 0.f);
     const uint32_t o = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-    return (static_cast<unsigned long long>(o) << 32) | static_cast<uint32_t>(~i);
+    return (static_cast<Key>(o) << 32) | static_cast<uint32_t>(~i);
 }
 
-__device__ __forceinline__ float key_value(unsigned long long k) {
+__device__ __forceinline__ float key_value(Key k) {
     const uint32_t o = static_cast<uint32_t>(k >> 32);
     return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
 }
 
-template <typename T, typename F>
-__device__ __forceinline__ T block_reduce(T v, F f, T *sm) {
+// Sum of 2^((x - base) k) and of -(x - base) k 2^((x - base) k) over some logits, base = their maximum m or 0 for -inf
+struct Sums {
+    float m, s, d;
+    __device__ __forceinline__ float base() const { return m == -INFINITY ? 0.f : m; }
+    __device__ __forceinline__ void rise_to(float mx, float k) {
+        if (mx == m) return;
+        if (m > -INFINITY) {
+            const float step = fminf((mx - m) * k, 1000.f), c = ex2_approx(-step);   // (2^-1000: 0)
+            d = (d + s * step) * c;
+            s *= c;
+        }
+        m = mx;
+    }
+    __device__ __forceinline__ void join(Sums o, float k) {
+        const float mx = fmaxf(m, o.m);
+        rise_to(mx, k);
+        o.rise_to(mx, k);
+        s += o.s;
+        d += o.d;
+    }
+};
+
+struct Smem {
+    Key aside[ASIDE];
+    Key group[GROUPS];
+    Key list[LP_MAX_TOP];     // of this CTA, in order; 0: none
+    Key tau;
+    int count;                // keys put aside
+    int sum;
+    Sums warp[LP_WARPS], cta;
+};
+
+template <bool H16>
+struct Chunk {   // 16 logits of a thread, in vectors of 16 bytes
+    static constexpr int VEC = H16 ? 8 : 4, VECS = PER_THREAD / VEC;
+    uint4 raw[VECS];
+    __device__ __forceinline__ float at(int i) const {   // i known when compiled
+        const uint4 &v = raw[i / VEC];
+        const int e = i % VEC;
+        if (H16) {
+            const uint32_t w = e / 2 == 0 ? v.x : (e / 2 == 1 ? v.y : (e / 2 == 2 ? v.z : v.w));
+            return (e & 1) ? h16_hi(w) : h16_lo(w);
+        }
+        return __uint_as_float(e == 0 ? v.x : (e == 1 ? v.y : (e == 2 ? v.z : v.w)));
+    }
+};
+
+// The k-th largest of the groups' largest keys; 0 when there are fewer than k.  All threads; two barriers.
+__device__ __forceinline__ Key kth_of_groups(Smem &sm, Key best, int k) {
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) v = f(v, __shfl_xor_sync(0xFFFFFFFFu, v, off));
+    for (int off = 1; off < GROUP; off <<= 1) {
+        const Key o = __shfl_xor_sync(0xFFFFFFFFu, best, off);
+        best = o > best ? o : best;
+    }
+    if (threadIdx.x % GROUP == 0) sm.group[threadIdx.x / GROUP] = best;
+    if (threadIdx.x == 0) sm.tau = 0;
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
+    if (threadIdx.x < GROUPS) {
+        const Key mine = sm.group[threadIdx.x];
+        int above = 0;
+#pragma unroll 16
+        for (int i = 0; i < GROUPS; ++i) above += sm.group[i] > mine;
+        if (above == k - 1 && mine != 0) sm.tau = mine;
+    }
     __syncthreads();
-    T r = sm[0];
-    for (int w = 1; w < LP_THREADS / 32; ++w) r = f(r, sm[w]);
-    return r;
+    return sm.tau;
 }
 
-// One CTA per row: a pass for the maximum, one for the sums, one for every alternative.
-template <bool H16>
-__global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(const LogprobParams p) {
-    __shared__ unsigned long long sm_k[LP_THREADS / 32];
-    __shared__ float sm_f[LP_THREADS / 32];
-    pdl_wait();
-    const long long r = blockIdx.x;
-    const void *row = static_cast<const uint8_t *>(p.logits) + r * p.row_stride * (H16 ? 2 : 4);
-    float m = -INFINITY;
-    for (int i = threadIdx.x; i < p.vocab; i += LP_THREADS) m = fmaxf(m, logit_at<H16>(row, i));
-    m = block_reduce(m, [](float a, float b) { return fmaxf(a, b); }, sm_f);
-    if (m == -INFINITY) m = 0.f;   // nothing but -inf: S = 0, log S = -inf, no NaN on the way
-    float s = 0.f, d = 0.f;
-    for (int i = threadIdx.x; i < p.vocab; i += LP_THREADS) {
-        const float x = logit_at<H16>(row, i);
-        const float y = (x - m) * p.scale;
-        const float e = ex2_approx(y * LOG2E);
-        s += e;
-        if (x > -INFINITY) d -= y * e;
+// Cuts the n keys put aside down to the k largest and returns the smallest of these, found bit by bit.  All threads.
+__device__ __noinline__ Key cut(Smem &sm, int n, int k) {
+    constexpr int MOST = (ASIDE + LP_THREADS - 1) / LP_THREADS;
+    Key mine[MOST];
+#pragma unroll
+    for (int i = 0; i < MOST; ++i) {
+        const int at = threadIdx.x + i * LP_THREADS;
+        mine[i] = at < n ? sm.aside[at] : 0;
     }
-    s = block_reduce(s, [](float a, float b) { return a + b; }, sm_f);
-    d = block_reduce(d, [](float a, float b) { return a + b; }, sm_f);
-    const float log_s = log2f(s) * LN2;
-    const float lse = m * p.scale + log_s;
-    if (threadIdx.x == 0) {
-        if (p.lse) p.lse[r] = lse;
-        if (p.entropy) p.entropy[r] = log_s + d / s;
+    Key tau = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+        const Key t = tau | (1ull << bit);
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < MOST; ++i) c += mine[i] >= t;
+        c = __reduce_add_sync(0xFFFFFFFFu, c);
+        __syncthreads();
+        if (threadIdx.x == 0) sm.sum = 0;
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0 && c) atomicAdd(&sm.sum, c);
+        __syncthreads();
+        if (sm.sum >= k) tau = t;
+    }
+    if (threadIdx.x == 0) sm.count = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MOST; ++i)
+        if (mine[i] != 0 && mine[i] >= tau) sm.aside[atomicAdd(&sm.count, 1)] = mine[i];
+    __syncthreads();
+    return tau;
+}
+
+template <bool H16, bool TOP>
+__global__ void __launch_bounds__(LP_THREADS, 2) logprobs_kernel(const LogprobParams p, int cluster) {
+    using C = Chunk<H16>;
+    constexpr int VEC = C::VEC, VECS = C::VECS;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    Smem &sm = *reinterpret_cast<Smem *>(smem_raw);
+    pdl_wait();
+    const long long r = blockIdx.x / cluster;
+    const int rank = blockIdx.x % cluster, tid = threadIdx.x;
+    constexpr int SIZE = H16 ? 2 : 4;
+    const uint8_t *row = static_cast<const uint8_t *>(p.logits) + r * p.row_stride * SIZE;
+    float x_t = 0.f;
+    int target = -1;
+    if (p.logprob && rank == 0 && tid == 0) {
+        target = p.targets[r];
+        if (target >= 0 && target < p.vocab)
+            x_t = H16 ? from_h16(reinterpret_cast<const uint16_t *>(row)[target]) : reinterpret_cast<const float *>(row)[target];
+    }
+    // vectors start on 16 bytes: `before` elements of the first one lie in front of the row and are not read
+    const int before = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / SIZE);
+    const uint4 *vectors = reinterpret_cast<const uint4 *>(row - before * SIZE);
+    const int n_vec = (before + p.vocab + VEC - 1) / VEC;
+    const int per = (n_vec + cluster - 1) / cluster;
+    const int vec_lo = min(n_vec, rank * per), vec_hi = min(n_vec, vec_lo + per);
+    constexpr uint32_t NONE = H16 ? (KRAKEN_F16 ? 0xFC00FC00u : 0xFF80FF80u) : 0xFF800000u;   // -inf
+
+    auto load = [&](C &c, int chunk) {
+#pragma unroll
+        for (int i = 0; i < VECS; ++i) {
+            const int v = vec_lo + (chunk * VECS + i) * LP_THREADS + tid;
+            const int first = v * VEC - before;
+            c.raw[i] = make_uint4(NONE, NONE, NONE, NONE);
+            if (v < vec_hi) {
+                if (first >= 0 && first + VEC <= p.vocab) {
+                    c.raw[i] = __ldcs(vectors + v);
+                } else {   // the row's first or last vector: element by element
+                    uint32_t w[4] = {NONE, NONE, NONE, NONE};
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        if (first + e < 0 || first + e >= p.vocab) continue;
+                        if (H16) {
+                            const uint32_t h = reinterpret_cast<const uint16_t *>(row)[first + e];
+                            w[e / 2] = (e & 1) ? (w[e / 2] & 0xFFFFu) | (h << 16) : (w[e / 2] & 0xFFFF0000u) | h;
+                        } else {
+                            w[e] = reinterpret_cast<const uint32_t *>(row)[first + e];
+                        }
+                    }
+                    c.raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+        }
+    };
+    auto index_of = [&](int chunk, int i) {   // of logit i of the chunk; may lie outside the row
+        return (vec_lo + (chunk * VECS + i / VEC) * LP_THREADS + tid) * VEC + i % VEC - before;
+    };
+    // elements of the row that this CTA reads
+    const int el_lo = max(0, vec_lo * VEC - before), el_hi = min(p.vocab, vec_hi * VEC - before);
+
+    const float k2 = p.scale * LOG2E;
+    Sums run = {-INFINITY, 0.f, 0.f};
+    Key tau = 0;
+    float tau_value = -INFINITY;
+    if (TOP && tid == 0) sm.count = 0;
+    const int chunks = (vec_hi - vec_lo + VECS * LP_THREADS - 1) / (VECS * LP_THREADS);
+    C cur, next;
+    load(cur, 0);
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        if (chunk + 1 < chunks) load(next, chunk + 1);
+        float top = cur.at(0);
+#pragma unroll
+        for (int i = 1; i < PER_THREAD; ++i) top = fmaxf(top, cur.at(i));
+        if (!(top > -INFINITY)) top = -INFINITY;
+        run.rise_to(fmaxf(run.m, top), k2);
+        const float base = run.base();
+#pragma unroll
+        for (int i = 0; i < PER_THREAD; ++i) {
+            const float u = (cur.at(i) - base) * k2, e = ex2_approx(u);
+            run.s += e;
+            run.d = fmaf(fmaxf(u, -1000.f), -e, run.d);   // (u = -inf: 0, and a NaN stays one in e)
+        }
+        if (TOP) {
+            int over = __syncthreads_count(top >= tau_value);
+            if (over > 0) {
+                if (chunk == 0 || over > GROUPS) {
+                    Key best = 0;
+#pragma unroll
+                    for (int i = 0; i < PER_THREAD; ++i) {
+                        const int at = index_of(chunk, i);
+                        if (at >= el_lo && at < el_hi) {
+                            const Key key = order_key(cur.at(i), at);
+                            best = key > best ? key : best;
+                        }
+                    }
+                    const Key bound = kth_of_groups(sm, best, p.top);
+                    tau = bound > tau ? bound : tau;
+                }
+                const int n = sm.count;
+                if (n + CHUNK_ADDS > ASIDE) {
+                    const Key bound = cut(sm, n, p.top);
+                    tau = bound > tau ? bound : tau;
+                } else {
+                    __syncthreads();   // everyone has read the count
+                }
+                tau_value = tau ? key_value(tau) : -INFINITY;
+                if (top >= tau_value) {
+#pragma unroll
+                    for (int i = 0; i < PER_THREAD; ++i) {
+                        const int at = index_of(chunk, i);
+                        if (at < el_lo || at >= el_hi) continue;
+                        const Key key = order_key(cur.at(i), at);
+                        if (key >= tau) sm.aside[atomicAdd(&sm.count, 1)] = key;
+                    }
+                }
+            }
+        }
+        cur = next;
+    }
+
+    // the threads' sums
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        Sums o;
+        o.m = __shfl_xor_sync(0xFFFFFFFFu, run.m, off);
+        o.s = __shfl_xor_sync(0xFFFFFFFFu, run.s, off);
+        o.d = __shfl_xor_sync(0xFFFFFFFFu, run.d, off);
+        run.join(o, k2);
+    }
+    if ((tid & 31) == 0) sm.warp[tid >> 5] = run;
+    __syncthreads();
+    run = sm.warp[tid % LP_WARPS];
+#pragma unroll
+    for (int off = LP_WARPS / 2; off > 0; off >>= 1) {
+        Sums o;
+        o.m = __shfl_xor_sync(0xFFFFFFFFu, run.m, off);
+        o.s = __shfl_xor_sync(0xFFFFFFFFu, run.s, off);
+        o.d = __shfl_xor_sync(0xFFFFFFFFu, run.d, off);
+        run.join(o, k2);
+    }
+    int n = 0;
+    if (TOP) {
+        n = sm.count;
+        if (n > LP_THREADS) {
+            cut(sm, n, p.top);
+            n = sm.count;
+        }
+    }
+    if (cluster > 1) {
+        if (TOP) {
+            if (tid < LP_MAX_TOP) sm.list[tid] = 0;
+            __syncthreads();
+            if (tid < n) {
+                const Key mine = sm.aside[tid];
+                int above = 0;
+                for (int i = 0; i < n; ++i) above += sm.aside[i] > mine;
+                if (above < p.top) sm.list[above] = mine;
+            }
+        }
+        if (tid == 0) sm.cta = run;
+        cluster_sync_all();
+        if (rank == 0) {
+            run = {-INFINITY, 0.f, 0.f};
+            for (int c = 0; c < cluster; ++c) {
+                const uint32_t at = map_to_cta(smem_u32(&sm.cta), c);
+                Sums o;
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.m) : "r"(at) : "memory");
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.s) : "r"(at + 4) : "memory");
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.d) : "r"(at + 8) : "memory");
+                run.join(o, k2);
+            }
+            if (TOP) {
+                n = cluster * p.top;
+                if (tid < n) {
+                    Key key;
+                    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(key) : "r"(map_to_cta(smem_u32(&sm.list[tid % p.top]), tid / p.top)) : "memory");
+                    sm.aside[tid] = key;
+                }
+                __syncthreads();
+            }
+        }
+        cluster_sync_all();   // nobody leaves while its shared memory is being read
+        if (rank != 0) return;
+    }
+    const float m = run.base(), log_s = log2f(run.s) * LN2;
+    if (TOP && tid < n) {
+        const Key mine = sm.aside[tid];
+        int above = 0;
+        for (int i = 0; i < n; ++i) above += sm.aside[i] > mine;
+        if (above < p.top && mine != 0) {
+            if (p.top_ids) p.top_ids[r * p.top + above] = static_cast<int>(~static_cast<uint32_t>(mine));
+            if (p.top_logprobs) p.top_logprobs[r * p.top + above] = (key_value(mine) - m) * p.scale - log_s;
+        }
+    }
+    if (tid == 0) {
+        if (p.lse) p.lse[r] = m * p.scale + log_s;
+        if (p.entropy) p.entropy[r] = log_s + run.d / run.s * LN2;
         if (p.logprob) {
-            const int t = p.targets[r];
             float v = 0.f;
-            if (t >= p.vocab) {
+            if (target >= p.vocab) {
                 v = NAN;
                 if (p.status) atomicOr(p.status, STATUS_BAD_TOKEN);
-            } else if (t >= 0) {
-                v = (logit_at<H16>(row, t) - m) * p.scale - log_s;
+            } else if (target >= 0) {
+                v = (x_t - m) * p.scale - log_s;
             }
             p.logprob[r] = v;
         }
     }
-    unsigned long long last = ~0ull;
-    for (int k = 0; k < p.top; ++k) {
-        unsigned long long best = 0;
-        for (int i = threadIdx.x; i < p.vocab; i += LP_THREADS) {
-            const unsigned long long key = order_key(logit_at<H16>(row, i), i);
-            if (key < last && key > best) best = key;
-        }
-        best = block_reduce(best, [](unsigned long long a, unsigned long long b) { return a > b ? a : b; }, sm_k);
-        last = best;
-        if (threadIdx.x == 0) {
-            if (p.top_ids) p.top_ids[r * p.top + k] = static_cast<int>(~static_cast<uint32_t>(best));
-            if (p.top_logprobs) p.top_logprobs[r * p.top + k] = (key_value(best) - m) * p.scale - log_s;
-        }
+}
+
+// CTAs of a row: as many as bring the grid to two a SM, none with less than 4096 logits
+int cluster_of(int rows, int vocab) {
+    const int sms = sm_count() > 0 ? sm_count() : 148;
+    int c = 1;
+    while (c < MAX_CLUSTER && (long long)rows * c < 2 * sms && vocab / (2 * c) >= 4096) c *= 2;
+    return c;
+}
+
+template <bool H16, bool TOP>
+int launch(const LogprobParams &p, int rows, cudaStream_t st) {
+    static DeviceOnce configured;
+    constexpr int SMEM = sizeof(Smem);
+    if (!configured.done()) {
+        int rc = cuda_check(cudaFuncSetAttribute(logprobs_kernel<H16, TOP>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM),
+                            "token logprobs: shared memory opt-in");
+        if (rc) return rc;
+        configured.set();
     }
+    const int cluster = cluster_of(rows, p.vocab);
+    if ((long long)rows * cluster > 0x7fffffffLL) return KRAKEN_EUNSUPPORTED;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(rows * cluster);
+    cfg.blockDim = dim3(LP_THREADS);
+    cfg.dynamicSmemBytes = SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cuda_check(cudaLaunchKernelEx(&cfg, logprobs_kernel<H16, TOP>, p, cluster), "token logprobs: launch");
 }
 
 }  // namespace
@@ -122,11 +415,10 @@ extern "C" int kraken_op_token_logprobs(const kraken_logprobs_args *a, uint32_t 
     using namespace kr;
     if (!a || a->rows < 0) return KRAKEN_EINVAL;
     if (a->rows == 0) return KRAKEN_OK;
-    if (!a->logits || a->vocab < 1 || a->row_stride < 0 || a->dtype < 0 || a->dtype > 1 || a->top < 0 ||
-        a->top > a->vocab || !(a->scale > 0.f) || !isfinite(a->scale) || (a->logprob && !a->targets) ||
-        (a->top > 0 && !a->top_ids && !a->top_logprobs))
+    if (!a->logits || a->vocab < 1 || a->row_stride < 0 || a->dtype < 0 || a->dtype > 1 || a->top < 0 || a->top > a->vocab ||
+        !(a->scale > 0.f) || !isfinite(a->scale) || (a->logprob && !a->targets) || (a->top > 0 && !a->top_ids && !a->top_logprobs))
         return KRAKEN_EINVAL;
-    if (a->top > LP_MAX_TOP) return KRAKEN_EUNSUPPORTED;
+    if (a->top > LP_MAX_TOP || a->vocab > 1 << 30) return KRAKEN_EUNSUPPORTED;
     if (reinterpret_cast<uintptr_t>(a->logits) & (a->dtype ? 1 : 3)) return KRAKEN_EUNSUPPORTED;
     LogprobParams p;
     p.logits = a->logits;
@@ -142,7 +434,6 @@ extern "C" int kraken_op_token_logprobs(const kraken_logprobs_args *a, uint32_t 
     p.scale = a->scale;
     p.status = d_status;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = a->dtype ? launch_pdl(logprobs_kernel<true>, dim3(a->rows), dim3(LP_THREADS), 0, st, p)
-                                   : launch_pdl(logprobs_kernel<false>, dim3(a->rows), dim3(LP_THREADS), 0, st, p);
-    return cuda_check(e, "token logprobs: launch");
+    if (a->dtype) return a->top ? launch<true, true>(p, a->rows, st) : launch<true, false>(p, a->rows, st);
+    return a->top ? launch<false, true>(p, a->rows, st) : launch<false, false>(p, a->rows, st);
 }

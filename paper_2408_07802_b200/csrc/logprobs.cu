@@ -3,16 +3,15 @@
 //   x = scale * logit, m = max x, S = sum e^(x - m):  lse = m + log S,  logprob = x_t - lse,
 //   entropy = log S + sum (m - x) e^(x - m) / S       (every term of the sum is positive: nothing cancels)
 //
-// Bound by HBM: 4 (or 2) bytes a logit against about 8 instructions.  Every thread keeps a maximum and the two sums of its
+// Bound by HBM: 4 (or 2) bytes a logit against about 6 instructions.  Every thread keeps a maximum and the two sums of its
 // own logits, brought to a larger maximum 16 logits at a time; the threads of a row meet at the end.
 //
-// The alternatives are found in the same pass.  A logit and its index make one 64-bit key whose order is that of the list
-// (larger logit first, then lower index), so keys are distinct.  Of the first chunk the maxima of 64 groups of 8 threads are
-// taken: the k-th largest of them is a bound that k logits reach, and from then on only logits above the bound are put aside
-// (a few dozen of a row; a thread compares the maximum of its 16 logits, which it has anyway).  Where many threads exceed
-// the bound (logits in rising order) it is raised from that chunk in the same way; a chunk then adds at most
-// (k - 1) * 128 + 1 keys, and where these might not fit the keys put aside are cut down to the k largest first.  What is left
-// at the end is ranked by counting.
+// The alternatives are found in the same pass.  After chunks 1, 2, 4, 8 ... the largest logits so far of 64 groups of 4
+// threads are looked at: the k-th largest of them is a bound that k logits reach, and logits that reach the bound are put aside
+// (a thread compares the maximum of its 16, which it has anyway; some 25 for k = 20 between two looks, whatever the vocabulary).
+// What was put aside is ranked by counting at the end, by keys of a logit and its index whose order is that of the list.
+// Where more logits reach the bound than there is room for (a vocabulary in rising order, or of few different values) the row
+// is gone through again by exact_top(), which works with the distinct keys and cuts down what it has put aside.
 //
 // Few rows: up to 8 CTAs of a cluster share a row and join through each other's shared memory.
 #include <math.h>
@@ -24,18 +23,18 @@ namespace kr {
 
 namespace {
 
-constexpr int LP_THREADS = 512;
+constexpr int LP_THREADS = 256;
 constexpr int LP_WARPS = LP_THREADS / 32;
 constexpr int LP_MAX_TOP = 32;
 constexpr int PER_THREAD = 16;                       // logits of a thread in a chunk
-constexpr int GROUP = 8, GROUPS = LP_THREADS / GROUP;
+constexpr int GROUP = 4, GROUPS = LP_THREADS / GROUP;
 constexpr int CHUNK_ADDS = (LP_MAX_TOP - 1) * GROUP * PER_THREAD + 1;
-constexpr int ASIDE = 6144;                          // room for keys put aside
+constexpr int ASIDE = 2560;                          // room for keys put aside
 constexpr int MAX_CLUSTER = 8;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.69314718055994531f;
 typedef unsigned long long Key;
-static_assert(GROUPS == 64, "a warp ranks the groups' keys two a lane");
+static_assert(GROUPS >= LP_MAX_TOP, "the bound is the k-th of the groups");
 static_assert(ASIDE > CHUNK_ADDS + LP_MAX_TOP, "after a cut a chunk has to fit");
 
 struct LogprobParams {
@@ -63,7 +62,7 @@ __device__ __forceinline__ float key_value(Key k) {
     return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
 }
 
-// Sum of 2^((x - base) k) and of -(x - base) k 2^((x - base) k) over some logits, base = their maximum m or 0 for -inf
+// Sum of 2^u and of u 2^u, u = (x - base) k, over some logits; base = their maximum m, or 0 for -inf
 struct Sums {
     float m, s, d;
     __device__ __forceinline__ float base() const { return m == -INFINITY ? 0.f : m; }
@@ -71,7 +70,7 @@ struct Sums {
         if (mx == m) return;
         if (m > -INFINITY) {
             const float step = fminf((mx - m) * k, 1000.f), c = ex2_approx(-step);   // (2^-1000: 0)
-            d = (d + s * step) * c;
+            d = (d - s * step) * c;
             s *= c;
         }
         m = mx;
@@ -85,11 +84,19 @@ struct Sums {
     }
 };
 
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
 struct Smem {
     Key aside[ASIDE];
     Key group[GROUPS];
+    float high[GROUPS];
     Key list[LP_MAX_TOP];     // of this CTA, in order; 0: none
     Key tau;
+    float bound;
     int count;                // keys put aside
     int sum;
     Sums warp[LP_WARPS], cta;
@@ -110,7 +117,27 @@ struct Chunk {   // 16 logits of a thread, in vectors of 16 bytes
     }
 };
 
-// The k-th largest of the groups' largest keys; 0 when there are fewer than k.  All threads; two barriers.
+// The k-th largest of the groups' largest logits.  All threads; two barriers.
+__device__ __forceinline__ float kth_of_groups(Smem &sm, float high, int k) {
+#pragma unroll
+    for (int off = 1; off < GROUP; off <<= 1) high = fmaxf(high, __shfl_xor_sync(0xFFFFFFFFu, high, off));
+    if (threadIdx.x % GROUP == 0) sm.high[threadIdx.x / GROUP] = high;
+    __syncthreads();
+    if (threadIdx.x < GROUPS) {
+        const float mine = sm.high[threadIdx.x];
+        int above = 0, equal = 0;
+#pragma unroll 16
+        for (int i = 0; i < GROUPS; ++i) {
+            above += sm.high[i] > mine;
+            equal += sm.high[i] == mine;
+        }
+        if (above < k && above + equal >= k) sm.bound = mine;   // (one value, from one or more threads)
+    }
+    __syncthreads();
+    return sm.bound;
+}
+
+// The same of the groups' largest keys; 0 when there are fewer than k.
 __device__ __forceinline__ Key kth_of_groups(Smem &sm, Key best, int k) {
 #pragma unroll
     for (int off = 1; off < GROUP; off <<= 1) {
@@ -163,17 +190,119 @@ __device__ __noinline__ Key cut(Smem &sm, int n, int k) {
     return tau;
 }
 
-template <bool H16, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS, 2) logprobs_kernel(const LogprobParams p, int cluster) {
+// The part of a row that a CTA reads, in vectors of 16 bytes that start on 16 bytes: `before` elements of the row's first
+// vector lie in front of the row, and are not read any more than those behind its end.
+template <bool H16>
+struct Span {
     using C = Chunk<H16>;
-    constexpr int VEC = C::VEC, VECS = C::VECS;
+    static constexpr int VEC = C::VEC, VECS = C::VECS, SIZE = H16 ? 2 : 4, CHUNK = VECS * LP_THREADS;   // CHUNK: vectors
+    static constexpr uint32_t NONE = H16 ? (KRAKEN_F16 ? 0xFC00FC00u : 0xFF80FF80u) : 0xFF800000u;      // -inf
+    const uint8_t *row;
+    const uint4 *vectors;
+    int vocab, before, lo, hi;         // vectors lo .. hi - 1
+    int clean_lo, clean_hi;            // of these, the ones that lie in the row whole
+    int chunks;
+    __device__ __forceinline__ Span(const uint8_t *r, int v, int rank, int cluster) : row(r), vocab(v) {
+        before = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / SIZE);
+        vectors = reinterpret_cast<const uint4 *>(row - before * SIZE);
+        const int n = (before + vocab + VEC - 1) / VEC, per = (n + cluster - 1) / cluster;
+        lo = min(n, rank * per);
+        hi = min(n, lo + per);
+        clean_lo = max(lo, before > 0 ? 1 : 0);
+        clean_hi = min(hi, (before + vocab) / VEC);
+        chunks = (hi - lo + CHUNK - 1) / CHUNK;
+    }
+    __device__ __forceinline__ int index(int chunk, int i) const {   // of logit i of this thread's chunk; maybe outside the part
+        return (lo + (chunk * VECS + i / VEC) * LP_THREADS + (int)threadIdx.x) * VEC + i % VEC - before;
+    }
+    __device__ __forceinline__ bool has(int index) const {
+        return index >= max(0, lo * VEC - before) && index < min(vocab, hi * VEC - before);
+    }
+    __device__ __forceinline__ void load(C &c, int chunk) const {   // -inf outside the part
+        const int v0 = lo + chunk * CHUNK;
+        if (v0 >= clean_lo && v0 + CHUNK <= clean_hi) {
+#pragma unroll
+            for (int i = 0; i < VECS; ++i) c.raw[i] = __ldcs(vectors + v0 + i * LP_THREADS + threadIdx.x);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < VECS; ++i) {
+            const int v = v0 + i * LP_THREADS + threadIdx.x;
+            c.raw[i] = make_uint4(NONE, NONE, NONE, NONE);
+            if (v >= clean_lo && v < clean_hi) {
+                c.raw[i] = __ldcs(vectors + v);
+            } else if (v < hi) {   // the row's first or last vector: element by element
+                uint32_t w[4] = {NONE, NONE, NONE, NONE};
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const int at = v * VEC - before + e;
+                    if (at < 0 || at >= vocab) continue;
+                    if (H16) {
+                        const uint32_t h = reinterpret_cast<const uint16_t *>(row)[at];
+                        w[e / 2] = (e & 1) ? (w[e / 2] & 0xFFFFu) | (h << 16) : (w[e / 2] & 0xFFFF0000u) | h;
+                    } else {
+                        w[e] = reinterpret_cast<const uint32_t *>(row)[at];
+                    }
+                }
+                c.raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+    }
+};
+
+// The k largest keys of the part, and maybe some more, into sm.aside; any order, any ties.  A bound is raised from a chunk as
+// long as many threads exceed it, after which a chunk adds at most (k - 1) * GROUP * PER_THREAD + 1 keys; where these might not
+// fit, the keys put aside are cut down to k first.
+template <bool H16>
+__device__ __noinline__ void exact_top(Smem &sm, const Span<H16> &span, int k) {
+    __syncthreads();
+    if (threadIdx.x == 0) sm.count = 0;
+    Key tau = 0;
+    for (int chunk = 0; chunk < span.chunks; ++chunk) {
+        Chunk<H16> c;
+        span.load(c, chunk);
+        Key best = 0;
+#pragma unroll
+        for (int i = 0; i < PER_THREAD; ++i) {
+            const int at = span.index(chunk, i);
+            if (!span.has(at)) continue;
+            const Key key = order_key(c.at(i), at);
+            best = key > best ? key : best;
+        }
+        const int over = __syncthreads_count(best >= tau && best != 0);
+        if (over == 0) continue;
+        if (chunk == 0 || over > GROUPS) {
+            const Key bound = kth_of_groups(sm, best, k);
+            tau = bound > tau ? bound : tau;
+        }
+        const int n = sm.count;
+        if (n + CHUNK_ADDS > ASIDE) {
+            const Key bound = cut(sm, n, k);
+            tau = bound > tau ? bound : tau;
+        } else {
+            __syncthreads();   // everyone has read the count
+        }
+        if (best < tau || best == 0) continue;
+#pragma unroll
+        for (int i = 0; i < PER_THREAD; ++i) {
+            const int at = span.index(chunk, i);
+            if (!span.has(at)) continue;
+            const Key key = order_key(c.at(i), at);
+            if (key >= tau) sm.aside[atomicAdd(&sm.count, 1)] = key;
+        }
+    }
+    __syncthreads();
+}
+
+template <bool H16, bool TOP>
+__global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobParams p, int cluster) {
+    using C = Chunk<H16>;
     extern __shared__ __align__(16) uint8_t smem_raw[];
     Smem &sm = *reinterpret_cast<Smem *>(smem_raw);
     pdl_wait();
     const long long r = blockIdx.x / cluster;
     const int rank = blockIdx.x % cluster, tid = threadIdx.x;
-    constexpr int SIZE = H16 ? 2 : 4;
-    const uint8_t *row = static_cast<const uint8_t *>(p.logits) + r * p.row_stride * SIZE;
+    const uint8_t *row = static_cast<const uint8_t *>(p.logits) + r * p.row_stride * Span<H16>::SIZE;
     float x_t = 0.f;
     int target = -1;
     if (p.logprob && rank == 0 && tid == 0) {
@@ -181,99 +310,44 @@ __global__ void __launch_bounds__(LP_THREADS, 2) logprobs_kernel(const LogprobPa
         if (target >= 0 && target < p.vocab)
             x_t = H16 ? from_h16(reinterpret_cast<const uint16_t *>(row)[target]) : reinterpret_cast<const float *>(row)[target];
     }
-    // vectors start on 16 bytes: `before` elements of the first one lie in front of the row and are not read
-    const int before = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / SIZE);
-    const uint4 *vectors = reinterpret_cast<const uint4 *>(row - before * SIZE);
-    const int n_vec = (before + p.vocab + VEC - 1) / VEC;
-    const int per = (n_vec + cluster - 1) / cluster;
-    const int vec_lo = min(n_vec, rank * per), vec_hi = min(n_vec, vec_lo + per);
-    constexpr uint32_t NONE = H16 ? (KRAKEN_F16 ? 0xFC00FC00u : 0xFF80FF80u) : 0xFF800000u;   // -inf
-
-    auto load = [&](C &c, int chunk) {
-#pragma unroll
-        for (int i = 0; i < VECS; ++i) {
-            const int v = vec_lo + (chunk * VECS + i) * LP_THREADS + tid;
-            const int first = v * VEC - before;
-            c.raw[i] = make_uint4(NONE, NONE, NONE, NONE);
-            if (v < vec_hi) {
-                if (first >= 0 && first + VEC <= p.vocab) {
-                    c.raw[i] = __ldcs(vectors + v);
-                } else {   // the row's first or last vector: element by element
-                    uint32_t w[4] = {NONE, NONE, NONE, NONE};
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        if (first + e < 0 || first + e >= p.vocab) continue;
-                        if (H16) {
-                            const uint32_t h = reinterpret_cast<const uint16_t *>(row)[first + e];
-                            w[e / 2] = (e & 1) ? (w[e / 2] & 0xFFFFu) | (h << 16) : (w[e / 2] & 0xFFFF0000u) | h;
-                        } else {
-                            w[e] = reinterpret_cast<const uint32_t *>(row)[first + e];
-                        }
-                    }
-                    c.raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-            }
-        }
-    };
-    auto index_of = [&](int chunk, int i) {   // of logit i of the chunk; may lie outside the row
-        return (vec_lo + (chunk * VECS + i / VEC) * LP_THREADS + tid) * VEC + i % VEC - before;
-    };
-    // elements of the row that this CTA reads
-    const int el_lo = max(0, vec_lo * VEC - before), el_hi = min(p.vocab, vec_hi * VEC - before);
-
+    const Span<H16> span(row, p.vocab, rank, cluster);
     const float k2 = p.scale * LOG2E;
     Sums run = {-INFINITY, 0.f, 0.f};
-    Key tau = 0;
-    float tau_value = -INFINITY;
+    float bound = -INFINITY;
     if (TOP && tid == 0) sm.count = 0;
-    const int chunks = (vec_hi - vec_lo + VECS * LP_THREADS - 1) / (VECS * LP_THREADS);
     C cur, next;
-    load(cur, 0);
-    for (int chunk = 0; chunk < chunks; ++chunk) {
-        if (chunk + 1 < chunks) load(next, chunk + 1);
-        float top = cur.at(0);
+    span.load(cur, 0);
+    for (int chunk = 0; chunk < span.chunks; ++chunk) {
+        if (chunk + 1 < span.chunks) span.load(next, chunk + 1);
+        float high = -INFINITY;   // (a NaN is passed over)
 #pragma unroll
-        for (int i = 1; i < PER_THREAD; ++i) top = fmaxf(top, cur.at(i));
-        if (!(top > -INFINITY)) top = -INFINITY;
-        run.rise_to(fmaxf(run.m, top), k2);
-        const float base = run.base();
+        for (int i = 0; i < PER_THREAD; ++i) high = fmaxf(high, cur.at(i));
+        run.rise_to(fmaxf(run.m, high), k2);
+        const uint64_t minus_base = splat2(-run.base()), scale = splat2(k2);
+        uint64_t s = splat2(0.f), d = splat2(0.f);
 #pragma unroll
-        for (int i = 0; i < PER_THREAD; ++i) {
-            const float u = (cur.at(i) - base) * k2, e = ex2_approx(u);
-            run.s += e;
-            run.d = fmaf(fmaxf(u, -1000.f), -e, run.d);   // (u = -inf: 0, and a NaN stays one in e)
+        for (int i = 0; i < PER_THREAD; i += 2) {
+            const uint64_t u = mul2(add2(pk2(cur.at(i), cur.at(i + 1)), minus_base), scale);
+            float u0, u1;
+            upk2(u, u0, u1);
+            const uint64_t e = pk2(ex2_approx(u0), ex2_approx(u1));
+            s = add2(s, e);
+            d = fma2(pk2(fmaxf(u0, -1000.f), fmaxf(u1, -1000.f)), e, d);   // (u = -inf: 0; a NaN stays one in e)
         }
+        float s0, s1, d0, d1;
+        upk2(s, s0, s1);
+        upk2(d, d0, d1);
+        run.s += s0 + s1;
+        run.d += d0 + d1;
         if (TOP) {
-            int over = __syncthreads_count(top >= tau_value);
-            if (over > 0) {
-                if (chunk == 0 || over > GROUPS) {
-                    Key best = 0;
+            if ((chunk & (chunk + 1)) == 0) bound = kth_of_groups(sm, run.m, p.top);   // after chunks 1, 2, 4, 8, ...
+            if (high >= bound) {
 #pragma unroll
-                    for (int i = 0; i < PER_THREAD; ++i) {
-                        const int at = index_of(chunk, i);
-                        if (at >= el_lo && at < el_hi) {
-                            const Key key = order_key(cur.at(i), at);
-                            best = key > best ? key : best;
-                        }
-                    }
-                    const Key bound = kth_of_groups(sm, best, p.top);
-                    tau = bound > tau ? bound : tau;
-                }
-                const int n = sm.count;
-                if (n + CHUNK_ADDS > ASIDE) {
-                    const Key bound = cut(sm, n, p.top);
-                    tau = bound > tau ? bound : tau;
-                } else {
-                    __syncthreads();   // everyone has read the count
-                }
-                tau_value = tau ? key_value(tau) : -INFINITY;
-                if (top >= tau_value) {
-#pragma unroll
-                    for (int i = 0; i < PER_THREAD; ++i) {
-                        const int at = index_of(chunk, i);
-                        if (at < el_lo || at >= el_hi) continue;
-                        const Key key = order_key(cur.at(i), at);
-                        if (key >= tau) sm.aside[atomicAdd(&sm.count, 1)] = key;
+                for (int i = 0; i < PER_THREAD; ++i) {
+                    if (cur.at(i) >= bound) {
+                        const int at = span.index(chunk, i);
+                        const int n = span.has(at) ? atomicAdd(&sm.count, 1) : ASIDE;
+                        if (n < ASIDE) sm.aside[n] = order_key(cur.at(i), at);
                     }
                 }
             }
@@ -304,7 +378,13 @@ __global__ void __launch_bounds__(LP_THREADS, 2) logprobs_kernel(const LogprobPa
     int n = 0;
     if (TOP) {
         n = sm.count;
+        // no room for all of them; or a bound of -inf, which NaN should have reached too
+        if (n > ASIDE || bound == -INFINITY) {
+            exact_top<H16>(sm, span, p.top);
+            n = sm.count;
+        }
         if (n > LP_THREADS) {
+            __syncthreads();
             cut(sm, n, p.top);
             n = sm.count;
         }
@@ -357,7 +437,7 @@ __global__ void __launch_bounds__(LP_THREADS, 2) logprobs_kernel(const LogprobPa
     }
     if (tid == 0) {
         if (p.lse) p.lse[r] = m * p.scale + log_s;
-        if (p.entropy) p.entropy[r] = log_s + run.d / run.s * LN2;
+        if (p.entropy) p.entropy[r] = log_s - run.d / run.s * LN2;
         if (p.logprob) {
             float v = 0.f;
             if (target >= p.vocab) {
@@ -371,11 +451,11 @@ __global__ void __launch_bounds__(LP_THREADS, 2) logprobs_kernel(const LogprobPa
     }
 }
 
-// CTAs of a row: as many as bring the grid to two a SM, none with less than 4096 logits
+// CTAs of a row: as many as bring the grid to four a SM, none with less than a chunk
 int cluster_of(int rows, int vocab) {
     const int sms = sm_count() > 0 ? sm_count() : 148;
     int c = 1;
-    while (c < MAX_CLUSTER && (long long)rows * c < 2 * sms && vocab / (2 * c) >= 4096) c *= 2;
+    while (c < MAX_CLUSTER && (long long)rows * c < 4 * sms && vocab / (2 * c) >= LP_THREADS * PER_THREAD) c *= 2;
     return c;
 }
 

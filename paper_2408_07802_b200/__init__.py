@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import importlib
 import os
 from typing import Dict, NamedTuple, Optional
 
@@ -221,6 +222,8 @@ def lib(dtype: Optional[str] = None) -> C.CDLL:
         if L.kraken_storage_dtype() != (1 if dtype == "f16" else 0):
             raise RuntimeError(f"{path} was not built for storage dtype {dtype}")
         _libs[dtype] = L
+        if _native is not None:
+            _bind(_native, dtype)
     return _libs[dtype]
 
 
@@ -559,68 +562,45 @@ def decode_attention_static_capacity() -> int:
 
 # ------------------------------------------------------------------ the cache in pages, and the reading of logits
 # These calls take the library image from their tensors' 16-bit type (bfloat16 or float16) and run on the current stream of
-# the tensors' device.  Their kernels take a few microseconds at decode sizes, so the checks build no text unless they fail.
+# the tensors' device.  Their kernels take a few microseconds at decode sizes, so their arguments are checked and marshalled in
+# C++ (csrc/binding.cpp); what does not fit is a ValueError, a status of the library a KrakenError.
 
-_IMAGE = {torch.bfloat16: "bf16", torch.float16: "f16"}
-_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
-
-
-def _call(fn, what: str, dtype: str, device: int, *args):
-    """fn(*args, stream) with `device` current (the library works on the current device), on its current stream."""
-    if device == torch.cuda.current_device():
-        status = fn(*args, _raw_stream(device))
-    else:
-        with torch.cuda.device(device):
-            status = fn(*args, _raw_stream(device))
-    if status:
-        with storage_dtype(dtype):
-            raise KrakenError(status, what)
+_native = None   # the extension module _marshal.so, once loaded
 
 
-def _vector(t: Optional[torch.Tensor], dtype: torch.dtype, n: int, device, what: str) -> Optional[int]:
-    """Address of a contiguous [n] tensor of the type on `device` (None: NULL)."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.shape != (n,) or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous {dtype} [{n}] on {device}")
-    return t.data_ptr()
+def _load_marshal():
+    global _native
+    if not os.path.exists(kbuild.MARSHAL):
+        raise RuntimeError(f"{kbuild.MARSHAL} is missing: build it with `python -m paper_2408_07802_b200.build` "
+                           "(there is no CPU or PyTorch fallback)")
+    module = importlib.import_module("._marshal", __name__)
+    for dtype in _libs:
+        _bind(module, dtype)
+    _native = module
+    return module
 
 
-def _status_word(t: Optional[torch.Tensor], device) -> Optional[int]:
-    if t is None:
-        return None
-    if t.element_size() != 4 or t.numel() < 1 or t.device != device:
-        raise ValueError(f"status must be a 32-bit word on {device}")
-    return t.data_ptr()
+def _bind(module, dtype: str):
+    """Hands the addresses of an image's functions to the marshalling module."""
+    L = _libs[dtype]
+    module.bind(int(dtype == "f16"), *(C.cast(f, C.c_void_p).value for f in (
+        L.kraken_op_paged_append, L.kraken_op_paged_attention, L.kraken_paged_attention_workspace, L.kraken_op_token_logprobs)))
 
 
-def _paged_cache(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor, device) -> PagedCacheArgs:
-    strides = k_cache.stride()
-    if k_cache.dtype not in _IMAGE or not k_cache.is_cuda or len(strides) != 4 or strides[3] != 1:
-        raise ValueError("the caches must be 16-bit CUDA tensors [pages, key/value heads, page size, head_dim], contiguous in "
-                         "the last dimension")
-    shape = k_cache.shape
-    if v_cache.shape != shape or v_cache.stride() != strides or v_cache.dtype is not k_cache.dtype or v_cache.device != device:
-        raise ValueError("k_cache and v_cache must have the same shape, strides, type and device")
-    if page_table.dtype is not torch.int32 or page_table.device != device or page_table.dim() != 2:
-        raise ValueError("page_table must be int32 [sequences, pages] on the caches' device")
-    n_seqs, max_pages = page_table.shape
-    row, one = page_table.stride()
-    if one != 1 and max_pages > 1:
-        raise ValueError("page_table must be contiguous in its last dimension")
-    n_pages, n_kv, page, hd = shape
-    return PagedCacheArgs(k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(), strides[0], strides[1], strides[2],
-                          row if n_seqs > 1 else max_pages, n_pages, page, n_kv, hd, n_seqs, max_pages)
+def _failed(code: int, what: str, dtype: str, again):
+    """An image that is not loaded yet is, and the call made again; any other status is an error."""
+    if code == _native.NOT_BOUND:
+        lib(dtype)
+        got = again()
+        if not got[0]:
+            return got
+        code = got[0]
+    with storage_dtype(dtype):
+        raise KrakenError(code, what)
 
 
-def _rows_of(t: torch.Tensor, rows: int, heads: int, hd: int, like: torch.Tensor, device, what: str):
-    """(address, row stride, head stride) of a 16-bit [rows, heads, head_dim] tensor."""
-    if t.shape != (rows, heads, hd) or t.dtype is not like.dtype or t.device != device:
-        raise ValueError(f"{what} must be [{rows}, {heads}, {hd}] of the caches' type and device")
-    row, head, one = t.stride()
-    if one != 1:
-        raise ValueError(f"{what} must be contiguous in its last dimension")
-    return t.data_ptr(), row, head
+def _image_of(t: torch.Tensor) -> str:
+    return "f16" if t.dtype is torch.float16 else "bf16" if t.dtype is torch.bfloat16 else _current_dtype
 
 
 def op_paged_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -634,31 +614,12 @@ def op_paged_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_c
     int32 [sequences, pages].  inv_freq (float32 [rot_dim / 2]) turns keys and queries by their position; the queries q
     [rows, heads, head_dim] go to q_out (created when not given, with the padding rows zero; may be q itself), which is
     returned.  The rows of one call must go to distinct positions."""
-    device = k_cache.device
-    cache = _paged_cache(k_cache, v_cache, page_table, device)
-    hd, n_kv = cache.head_dim, cache.n_kv_head
-    rows = k.shape[0]
-    kp, k_row, k_head = _rows_of(k, rows, n_kv, hd, k_cache, device, "k")
-    vp, v_row, v_head = _rows_of(v, rows, n_kv, hd, k_cache, device, "v")
-    n_head, qp, op = 0, (None, 0, 0), (None, 0, 0)
-    if q is not None:
-        n_head = q.shape[1]
-        qp = _rows_of(q, rows, n_head, hd, k_cache, device, "q")
-        if q_out is None:
-            q_out = torch.zeros(rows, n_head, hd, dtype=q.dtype, device=device)
-        op = _rows_of(q_out, rows, n_head, hd, k_cache, device, "q_out")
-    if positions is None:
-        raise ValueError("positions are needed")
-    half = 0 if inv_freq is None else inv_freq.shape[0]
-    args = PagedAppendArgs(kp, vp, k_row, k_head, v_row, v_head, *qp, *op,
-                           _vector(row_seq, torch.int32, rows, device, "row_seq"),
-                           _vector(positions, torch.int32, rows, device, "positions"),
-                           _vector(inv_freq, torch.float32, half, device, "inv_freq"), rows, n_head, 2 * half,
-                           bool(interleaved))
-    dtype = _IMAGE[k_cache.dtype]
-    _call(lib(dtype).kraken_op_paged_append, "kraken_op_paged_append", dtype, device.index, C.byref(cache), C.byref(args),
-          _status_word(status, device))
-    return q_out
+    m = _native or _load_marshal()
+    args = (k, v, k_cache, v_cache, page_table, positions, row_seq, q, q_out, inv_freq, interleaved, status)
+    got = m.paged_append(*args)
+    if got[0]:
+        got = _failed(got[0], "kraken_op_paged_append", _image_of(k_cache), lambda: m.paged_append(*args))
+    return got[1]
 
 
 def paged_attention_workspace(n_head: int, n_kv_head: int, head_dim: int) -> int:
@@ -680,35 +641,12 @@ def op_paged_decode_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: t
     rows of out and lse stay as they were).  scale: 1 / sqrt(head_dim) by default; score_cap: scores become
     cap * tanh(score / cap); window: only that many last positions are visible; slopes (float32 [heads]): a bias of
     slope * (distance back to the key, negative).  Returns (out, lse): out like q, lse float32 [rows, heads]."""
-    device = k_cache.device
-    cache = _paged_cache(k_cache, v_cache, page_table, device)
-    rows, n_head, hd = q.shape
-    qp, q_row, q_head = _rows_of(q, rows, n_head, cache.head_dim, k_cache, device, "q")
-    if out is None:
-        out = torch.empty(rows, n_head, hd, dtype=q.dtype, device=device)
-    op, o_row, o_head = _rows_of(out, rows, n_head, hd, k_cache, device, "out")
-    if lse is None:
-        lse = torch.empty(rows, n_head, dtype=torch.float32, device=device)
-    l_row, one = lse.stride()
-    if lse.dtype is not torch.float32 or lse.shape != (rows, n_head) or one != 1 or lse.device != device:
-        raise ValueError("lse must be float32 [rows, heads] on the caches' device, contiguous in its last dimension")
-    dtype = _IMAGE[k_cache.dtype]
-    if workspace is None:
-        with contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device):
-            workspace = torch.empty(paged_attention_workspace(n_head, cache.n_kv_head, hd), dtype=torch.uint8, device=device)
-    elif workspace.device != device or not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous, on the caches' device")
-    if n_keys is None:
-        raise ValueError("n_keys are needed")
-    args = PagedAttentionArgs(qp, q_row, q_head, op, o_row, o_head, lse.data_ptr(), l_row,
-                              _vector(row_seq, torch.int32, rows, device, "row_seq"),
-                              _vector(n_keys, torch.int32, rows, device, "n_keys"),
-                              _vector(slopes, torch.float32, n_head, device, "slopes"),
-                              workspace.data_ptr(), workspace.nbytes, hd ** -0.5 if scale is None else scale, score_cap, rows,
-                              n_head, window)
-    _call(lib(dtype).kraken_op_paged_attention, "kraken_op_paged_attention", dtype, device.index, C.byref(cache),
-          C.byref(args), _status_word(status, device))
-    return out, lse
+    m = _native or _load_marshal()
+    args = (q, k_cache, v_cache, page_table, n_keys, row_seq, scale, score_cap, window, slopes, out, lse, workspace, status)
+    got = m.paged_attention(*args)
+    if got[0]:
+        got = _failed(got[0], "kraken_op_paged_attention", _image_of(k_cache), lambda: m.paged_attention(*args))
+    return got[1], got[2]
 
 
 class TokenLogprobs(NamedTuple):
@@ -724,29 +662,12 @@ def op_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = No
     """Reads rows of logits (kraken_op_token_logprobs): log probability of targets[r] (int32; negative: not asked for),
     entropy of the row's distribution and its `top` largest tokens with their log probabilities, for the distribution
     softmax(scale * logits).  logits: [rows, vocab] float32, bfloat16 or float16, any row stride."""
-    kind = logits.dtype
-    if not logits.is_cuda or logits.dim() != 2 or (kind is not torch.float32 and kind not in _IMAGE):
-        raise ValueError("logits must be a CUDA tensor [rows, vocab] of float32 or a 16-bit type")
-    rows, vocab = logits.shape
-    row, one = logits.stride()
-    if one != 1 and vocab > 1:
-        raise ValueError("logits must be contiguous in the last dimension")
-    device = logits.device
-    asked = _vector(targets, torch.int32, rows, device, "targets")
-    numbers = torch.empty(3, rows, dtype=torch.float32, device=device)
-    base = numbers.data_ptr()
-    ids = best = ids_at = best_at = None
-    if top > 0:
-        ids = torch.empty(rows, top, dtype=torch.int32, device=device)
-        best = torch.empty(rows, top, dtype=torch.float32, device=device)
-        ids_at, best_at = ids.data_ptr(), best.data_ptr()
-    dtype = _IMAGE.get(kind, _current_dtype)
-    args = LogprobsArgs(logits.data_ptr(), row, asked, None if targets is None else base, base + 4 * rows, base + 8 * rows,
-                        ids_at, best_at, rows, vocab, kind is not torch.float32, top, scale)
-    _call(lib(dtype).kraken_op_token_logprobs, "kraken_op_token_logprobs", dtype, device.index, C.byref(args),
-          _status_word(status, device))
-    logprob, entropy, lse = numbers.unbind(0)
-    return TokenLogprobs(None if targets is None else logprob, entropy, lse, ids, best)
+    m = _native or _load_marshal()
+    args = (logits, targets, top, scale, status, _current_dtype == "f16")
+    got = m.token_logprobs(*args)
+    if got[0]:
+        got = _failed(got[0], "kraken_op_token_logprobs", _image_of(logits), lambda: m.token_logprobs(*args))
+    return TokenLogprobs._make(got[1:])
 
 
 def set_tuning(key: int, value: int) -> None:

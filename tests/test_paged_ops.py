@@ -17,6 +17,9 @@ import torch
 
 import kraken_inputs as ki
 import paper_2408_07802_b200 as kr
+from paper_2408_07802_b200 import build as kbuild
+
+kbuild.build_all()
 
 DEV = "cuda:0"
 gpu = pytest.mark.gpu

@@ -35,6 +35,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.69314718055994531f;
 typedef unsigned long long Key;
 static_assert(GROUPS >= LP_MAX_TOP, "the bound is the k-th of the groups");
+static_assert(MAX_CLUSTER * LP_MAX_TOP == LP_THREADS, "a thread clears one key of the list");
 static_assert(ASIDE > CHUNK_ADDS + LP_MAX_TOP, "after a cut a chunk has to fit");
 
 struct LogprobParams {
@@ -94,12 +95,12 @@ struct Smem {
     Key aside[ASIDE];
     Key group[GROUPS];
     float high[GROUPS];
-    Key list[LP_MAX_TOP];     // of this CTA, in order; 0: none
+    Key list[MAX_CLUSTER * LP_MAX_TOP];   // of every CTA of the cluster, in order; 0: none
     Key tau;
     float bound;
     int count;                // keys put aside
     int sum;
-    Sums warp[LP_WARPS], cta;
+    Sums warp[LP_WARPS], cta[MAX_CLUSTER];
 };
 
 template <bool H16>
@@ -119,22 +120,38 @@ struct Chunk {   // 16 logits of a thread, in vectors of 16 bytes
 
 // The k-th largest of the groups' largest logits.  All threads; two barriers.
 __device__ __forceinline__ float kth_of_groups(Smem &sm, float high, int k) {
+    static_assert(GROUP == 4, "the threads of a group rank its logit");
 #pragma unroll
     for (int off = 1; off < GROUP; off <<= 1) high = fmaxf(high, __shfl_xor_sync(0xFFFFFFFFu, high, off));
     if (threadIdx.x % GROUP == 0) sm.high[threadIdx.x / GROUP] = high;
     __syncthreads();
-    if (threadIdx.x < GROUPS) {
-        const float mine = sm.high[threadIdx.x];
-        int above = 0, equal = 0;
-#pragma unroll 16
-        for (int i = 0; i < GROUPS; ++i) {
-            above += sm.high[i] > mine;
-            equal += sm.high[i] == mine;
-        }
-        if (above < k && above + equal >= k) sm.bound = mine;   // (one value, from one or more threads)
+    int ranks = 0;   // logits above, and in the upper half those equal
+#pragma unroll
+    for (int i = 0; i < GROUPS; i += GROUP) {
+        const float x = sm.high[i + threadIdx.x % GROUP];
+        ranks += (x > high ? 1 : 0) + (x == high ? 1 << 16 : 0);
     }
+    ranks += __shfl_xor_sync(0xFFFFFFFFu, ranks, 1);
+    ranks += __shfl_xor_sync(0xFFFFFFFFu, ranks, 2);
+    const int above = ranks & 0xFFFF, equal = ranks >> 16;
+    if (above < k && above + equal >= k) sm.bound = high;   // (one value, from one or more threads)
     __syncthreads();
     return sm.bound;
+}
+
+// f(rank, key) for those of n keys whose rank is below k, four threads a key.  All threads.
+template <typename F>
+__device__ __forceinline__ void ranked(const Key *keys, int n, int k, F f) {
+    for (int i0 = 0; i0 < n; i0 += LP_THREADS / 4) {
+        const int at = i0 + threadIdx.x / 4;
+        const Key mine = at < n ? keys[at] : 0;
+        int above = 0;
+#pragma unroll 4
+        for (int i = threadIdx.x % 4; i < n; i += 4) above += keys[i] > mine;
+        above += __shfl_xor_sync(0xFFFFFFFFu, above, 1);
+        above += __shfl_xor_sync(0xFFFFFFFFu, above, 2);
+        if (mine != 0 && above < k && threadIdx.x % 4 == 0) f(above, mine);
+    }
 }
 
 // The same of the groups' largest keys; 0 when there are fewer than k.
@@ -299,9 +316,14 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
     using C = Chunk<H16>;
     extern __shared__ __align__(16) uint8_t smem_raw[];
     Smem &sm = *reinterpret_cast<Smem *>(smem_raw);
-    pdl_wait();
     const long long r = blockIdx.x / cluster;
     const int rank = blockIdx.x % cluster, tid = threadIdx.x;
+    if (cluster > 1) {
+        // the CTAs of a cluster write into the first one's shared memory at the end: by then it has to run, and to be ready
+        if (TOP && rank == 0) sm.list[tid] = 0;
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    }
+    pdl_wait();
     const uint8_t *row = static_cast<const uint8_t *>(p.logits) + r * p.row_stride * Span<H16>::SIZE;
     float x_t = 0.f;
     int target = -1;
@@ -356,25 +378,25 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
     }
 
     // the threads' sums
+    auto over_lanes = [&](int lanes) {
+        float m = run.m;
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        Sums o;
-        o.m = __shfl_xor_sync(0xFFFFFFFFu, run.m, off);
-        o.s = __shfl_xor_sync(0xFFFFFFFFu, run.s, off);
-        o.d = __shfl_xor_sync(0xFFFFFFFFu, run.d, off);
-        run.join(o, k2);
-    }
-    if ((tid & 31) == 0) sm.warp[tid >> 5] = run;
+        for (int off = 16; off > 0; off >>= 1)
+            if (off < lanes) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
+        run.rise_to(m, k2);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) {
+            if (off >= lanes) continue;
+            run.s += __shfl_xor_sync(0xFFFFFFFFu, run.s, off);
+            run.d += __shfl_xor_sync(0xFFFFFFFFu, run.d, off);
+        }
+    };
+    over_lanes(32);
+    if (tid % 32 == 0) sm.warp[tid / 32] = run;
     __syncthreads();
     run = sm.warp[tid % LP_WARPS];
-#pragma unroll
-    for (int off = LP_WARPS / 2; off > 0; off >>= 1) {
-        Sums o;
-        o.m = __shfl_xor_sync(0xFFFFFFFFu, run.m, off);
-        o.s = __shfl_xor_sync(0xFFFFFFFFu, run.s, off);
-        o.d = __shfl_xor_sync(0xFFFFFFFFu, run.d, off);
-        run.join(o, k2);
-    }
+    over_lanes(LP_WARPS);
+    const Key *keys = sm.aside;
     int n = 0;
     if (TOP) {
         n = sm.count;
@@ -390,51 +412,32 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
         }
     }
     if (cluster > 1) {
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (tid == 0) {
+            const uint32_t at = map_to_cta(smem_u32(&sm.cta[rank]), 0);
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(run.m) : "memory");
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(run.s) : "memory");
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 8), "f"(run.d) : "memory");
+        }
         if (TOP) {
-            if (tid < LP_MAX_TOP) sm.list[tid] = 0;
-            __syncthreads();
-            if (tid < n) {
-                const Key mine = sm.aside[tid];
-                int above = 0;
-                for (int i = 0; i < n; ++i) above += sm.aside[i] > mine;
-                if (above < p.top) sm.list[above] = mine;
-            }
+            const uint32_t list = map_to_cta(smem_u32(&sm.list[rank * p.top]), 0);
+            ranked(sm.aside, n, p.top, [&](int place, Key key) {
+                asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(list + 8 * place), "l"(key) : "memory");
+            });
         }
-        if (tid == 0) sm.cta = run;
         cluster_sync_all();
-        if (rank == 0) {
-            run = {-INFINITY, 0.f, 0.f};
-            for (int c = 0; c < cluster; ++c) {
-                const uint32_t at = map_to_cta(smem_u32(&sm.cta), c);
-                Sums o;
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.m) : "r"(at) : "memory");
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.s) : "r"(at + 4) : "memory");
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.d) : "r"(at + 8) : "memory");
-                run.join(o, k2);
-            }
-            if (TOP) {
-                n = cluster * p.top;
-                if (tid < n) {
-                    Key key;
-                    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(key) : "r"(map_to_cta(smem_u32(&sm.list[tid % p.top]), tid / p.top)) : "memory");
-                    sm.aside[tid] = key;
-                }
-                __syncthreads();
-            }
-        }
-        cluster_sync_all();   // nobody leaves while its shared memory is being read
         if (rank != 0) return;
+        run = tid % MAX_CLUSTER < cluster ? sm.cta[tid % MAX_CLUSTER] : Sums{-INFINITY, 0.f, 0.f};
+        over_lanes(MAX_CLUSTER);
+        keys = sm.list;
+        n = cluster * p.top;
     }
     const float m = run.base(), log_s = log2f(run.s) * LN2;
-    if (TOP && tid < n) {
-        const Key mine = sm.aside[tid];
-        int above = 0;
-        for (int i = 0; i < n; ++i) above += sm.aside[i] > mine;
-        if (above < p.top && mine != 0) {
-            if (p.top_ids) p.top_ids[r * p.top + above] = static_cast<int>(~static_cast<uint32_t>(mine));
-            if (p.top_logprobs) p.top_logprobs[r * p.top + above] = (key_value(mine) - m) * p.scale - log_s;
-        }
-    }
+    if (TOP)
+        ranked(keys, n, p.top, [&](int place, Key key) {
+            if (p.top_ids) p.top_ids[r * p.top + place] = static_cast<int>(~static_cast<uint32_t>(key));
+            if (p.top_logprobs) p.top_logprobs[r * p.top + place] = (key_value(key) - m) * p.scale - log_s;
+        });
     if (tid == 0) {
         if (p.lse) p.lse[r] = m * p.scale + log_s;
         if (p.entropy) p.entropy[r] = log_s - run.d / run.s * LN2;

@@ -6,12 +6,14 @@
 // Bound by HBM: 4 (or 2) bytes a logit against about 6 instructions.  Every thread keeps a maximum and the two sums of its
 // own logits, brought to a larger maximum 16 logits at a time; the threads of a row meet at the end.
 //
-// The alternatives are found in the same pass.  After chunks 1, 2, 4, 8 ... the largest logits so far of 64 groups of 4
-// threads are looked at: the k-th largest of them is a bound that k logits reach, and logits that reach the bound are put aside
-// (a thread compares the maximum of its 16, which it has anyway; some 25 for k = 20 between two looks, whatever the vocabulary).
-// What was put aside is ranked by counting at the end, by keys of a logit and its index whose order is that of the list.
-// Where more logits reach the bound than there is room for (a vocabulary in rising order, or of few different values) the row
-// is gone through again by exact_top(), which works with the distinct keys and cuts down what it has put aside.
+// The alternatives are found in the same pass.  After chunks 1, 3, 9, 27 ... the largest logits so far of 64 groups of 4
+// threads are looked at: the k-th largest of them is a bound that k logits reach.  A thread compares the maximum of its 16
+// logits, which it has anyway, with the bound and where it is reached notes the place: some 130 of a row for k = 20.  At the end
+// the bound is taken once more, the places noted are read again (out of L2) and the logits that reach the last bound, not many
+// more than k, are ranked by counting, by keys of a logit and its index whose order is that of the list.  (With the logits put
+// aside at once, a warp went through the 16 logits of a thread some hundred times a row: 2048 x 50257 with k = 20 took 98 us.)
+// Where more places or logits reach the bound than there is room for (a vocabulary in rising order, or of few different
+// values) the row is gone through again by exact_top(), which works with the distinct keys and cuts down what it has put aside.
 //
 // Few rows: up to 8 CTAs of a cluster share a row and join through each other's shared memory.
 #include <math.h>
@@ -30,6 +32,7 @@ constexpr int PER_THREAD = 16;                       // logits of a thread in a 
 constexpr int GROUP = 4, GROUPS = LP_THREADS / GROUP;
 constexpr int CHUNK_ADDS = (LP_MAX_TOP - 1) * GROUP * PER_THREAD + 1;
 constexpr int ASIDE = 2560;                          // room for keys put aside
+constexpr int PLACES = 2560;                         // and for places noted
 constexpr int MAX_CLUSTER = 8;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.69314718055994531f;
@@ -98,6 +101,8 @@ struct Smem {
     Key list[MAX_CLUSTER * LP_MAX_TOP];   // of every CTA of the cluster, in order; 0: none
     Key tau;
     float bound;
+    int places[PLACES];       // chunk * LP_THREADS + thread
+    int noted;
     int count;                // keys put aside
     int sum;
     Sums warp[LP_WARPS], cta[MAX_CLUSTER];
@@ -265,6 +270,23 @@ struct Span {
             }
         }
     }
+    // f(logit, index) for the logits of vector i of a thread's chunk
+    template <typename F>
+    __device__ __forceinline__ void each(int chunk, int thread, int i, F f) const {
+        const int v = lo + (chunk * VECS + i) * LP_THREADS + thread;
+        if (v >= clean_lo && v < clean_hi) {
+            C c;
+            c.raw[0] = vectors[v];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f(c.at(e), v * VEC - before + e);
+        } else if (v < hi) {
+            for (int e = 0; e < VEC; ++e) {
+                const int at = v * VEC - before + e;
+                if (at < 0 || at >= vocab) continue;
+                f(H16 ? from_h16(reinterpret_cast<const uint16_t *>(row)[at]) : reinterpret_cast<const float *>(row)[at], at);
+            }
+        }
+    }
 };
 
 // The k largest keys of the part, and maybe some more, into sm.aside; any order, any ties.  A bound is raised from a chunk as
@@ -336,7 +358,8 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
     const float k2 = p.scale * LOG2E;
     Sums run = {-INFINITY, 0.f, 0.f};
     float bound = -INFINITY;
-    if (TOP && tid == 0) sm.count = 0;
+    if (TOP && tid == 0) sm.count = sm.noted = 0;
+    int look = 0;   // the chunk after which the bound is taken next
     C cur, next;
     span.load(cur, 0);
     for (int chunk = 0; chunk < span.chunks; ++chunk) {
@@ -362,21 +385,37 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
         run.s += s0 + s1;
         run.d += d0 + d1;
         if (TOP) {
-            if ((chunk & (chunk + 1)) == 0) bound = kth_of_groups(sm, run.m, p.top);   // after chunks 1, 2, 4, 8, ...
+            if (chunk == look) {
+                bound = kth_of_groups(sm, run.m, p.top);
+                look = 3 * look + 2;
+            }
             if (high >= bound) {
-#pragma unroll
-                for (int i = 0; i < PER_THREAD; ++i) {
-                    if (cur.at(i) >= bound) {
-                        const int at = span.index(chunk, i);
-                        const int n = span.has(at) ? atomicAdd(&sm.count, 1) : ASIDE;
-                        if (n < ASIDE) sm.aside[n] = order_key(cur.at(i), at);
-                    }
-                }
+                const int at = atomicAdd(&sm.noted, 1);
+                if (at < PLACES) sm.places[at] = chunk * LP_THREADS + tid;
             }
         }
         cur = next;
     }
 
+    // the logits that reach the bound of the whole part
+    bool all_found = false;
+    if (TOP) {
+        if (look > 2) bound = kth_of_groups(sm, run.m, p.top);
+        else __syncthreads();
+        const int noted = sm.noted;
+        all_found = noted <= PLACES && bound > -INFINITY;   // (NaN should have reached a bound of -inf too)
+        if (all_found) {
+            for (int i = tid; i < noted * C::VECS; i += LP_THREADS) {
+                const int place = sm.places[i / C::VECS];
+                span.each(place / LP_THREADS, place % LP_THREADS, i % C::VECS, [&](float x, int at) {
+                    if (x >= bound) {
+                        const int n = atomicAdd(&sm.count, 1);
+                        if (n < ASIDE) sm.aside[n] = order_key(x, at);
+                    }
+                });
+            }
+        }
+    }
     // the threads' sums
     auto over_lanes = [&](int lanes) {
         float m = run.m;
@@ -400,8 +439,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
     int n = 0;
     if (TOP) {
         n = sm.count;
-        // no room for all of them; or a bound of -inf, which NaN should have reached too
-        if (n > ASIDE || bound == -INFINITY) {
+        if (!all_found || n > ASIDE) {
             exact_top<H16>(sm, span, p.top);
             n = sm.count;
         }

@@ -48,7 +48,7 @@ struct LogprobParams {
     float *logprob, *entropy, *lse;
     int *top_ids;
     float *top_logprobs;
-    int vocab, top;
+    int rows, vocab, top;
     float scale;
     uint32_t *status;
 };
@@ -338,7 +338,6 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
     using C = Chunk<H16>;
     extern __shared__ __align__(16) uint8_t smem_raw[];
     Smem &sm = *reinterpret_cast<Smem *>(smem_raw);
-    const long long r = blockIdx.x / cluster;
     const int rank = blockIdx.x % cluster, tid = threadIdx.x;
     if (cluster > 1) {
         // the CTAs of a cluster write into the first one's shared memory at the end: by then it has to run, and to be ready
@@ -346,157 +345,165 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     }
     pdl_wait();
-    const uint8_t *row = static_cast<const uint8_t *>(p.logits) + r * p.row_stride * Span<H16>::SIZE;
-    float x_t = 0.f;
-    int target = -1;
-    if (p.logprob && rank == 0 && tid == 0) {
-        target = p.targets[r];
-        if (target >= 0 && target < p.vocab)
-            x_t = H16 ? from_h16(reinterpret_cast<const uint16_t *>(row)[target]) : reinterpret_cast<const float *>(row)[target];
-    }
-    const Span<H16> span(row, p.vocab, rank, cluster);
     const float k2 = p.scale * LOG2E;
-    Sums run = {-INFINITY, 0.f, 0.f};
-    float bound = -INFINITY;
-    if (TOP && tid == 0) sm.count = sm.noted = 0;
-    int look = 0;   // the chunk after which the bound is taken next
+    const int step = gridDim.x / cluster;   // rows side by side; with clusters every row has its own
+    auto row_at = [&](long long r) { return static_cast<const uint8_t *>(p.logits) + r * p.row_stride * Span<H16>::SIZE; };
     C cur, next;
-    span.load(cur, 0);
-    for (int chunk = 0; chunk < span.chunks; ++chunk) {
-        if (chunk + 1 < span.chunks) span.load(next, chunk + 1);
-        float high = -INFINITY;   // (a NaN is passed over)
-#pragma unroll
-        for (int i = 0; i < PER_THREAD; ++i) high = fmaxf(high, cur.at(i));
-        run.rise_to(fmaxf(run.m, high), k2);
-        const uint64_t minus_base = splat2(-run.base()), scale = splat2(k2);
-        uint64_t s = splat2(0.f), d = splat2(0.f);
-#pragma unroll
-        for (int i = 0; i < PER_THREAD; i += 2) {
-            const uint64_t u = mul2(add2(pk2(cur.at(i), cur.at(i + 1)), minus_base), scale);
-            float u0, u1;
-            upk2(u, u0, u1);
-            const uint64_t e = pk2(ex2_approx(u0), ex2_approx(u1));
-            s = add2(s, e);
-            d = fma2(pk2(fmaxf(u0, -1000.f), fmaxf(u1, -1000.f)), e, d);   // (u = -inf: 0; a NaN stays one in e)
+    Span<H16>(row_at(blockIdx.x / cluster), p.vocab, rank, cluster).load(cur, 0);
+    for (long long r = blockIdx.x / cluster; r < p.rows; r += step) {
+        const uint8_t *row = row_at(r);
+        float x_t = 0.f;
+        int target = -1;
+        if (p.logprob && rank == 0 && tid == 0) {
+            target = p.targets[r];
+            if (target >= 0 && target < p.vocab)
+                x_t = H16 ? from_h16(reinterpret_cast<const uint16_t *>(row)[target]) : reinterpret_cast<const float *>(row)[target];
         }
-        float s0, s1, d0, d1;
-        upk2(s, s0, s1);
-        upk2(d, d0, d1);
-        run.s += s0 + s1;
-        run.d += d0 + d1;
-        if (TOP) {
-            if (chunk == look) {
-                bound = kth_of_groups(sm, run.m, p.top);
-                look = 3 * look + 2;
+        const Span<H16> span(row, p.vocab, rank, cluster);
+        Sums run = {-INFINITY, 0.f, 0.f};
+        float bound = -INFINITY;
+        if (TOP && tid == 0) sm.count = sm.noted = 0;
+        int look = 0;   // the chunk after which the bound is taken next
+        for (int chunk = 0; chunk < span.chunks; ++chunk) {
+            // with the last chunk the next row's first one is requested: the end of a row takes longer than the way to memory
+            if (chunk + 1 < span.chunks) span.load(next, chunk + 1);
+            else if (r + step < p.rows) Span<H16>(row_at(r + step), p.vocab, rank, cluster).load(next, 0);
+            float high = -INFINITY;   // (a NaN is passed over)
+#pragma unroll
+            for (int i = 0; i < PER_THREAD; ++i) high = fmaxf(high, cur.at(i));
+            run.rise_to(fmaxf(run.m, high), k2);
+            const uint64_t minus_base = splat2(-run.base()), scale = splat2(k2);
+            uint64_t s = splat2(0.f), d = splat2(0.f);
+#pragma unroll
+            for (int i = 0; i < PER_THREAD; i += 2) {
+                const uint64_t u = mul2(add2(pk2(cur.at(i), cur.at(i + 1)), minus_base), scale);
+                float u0, u1;
+                upk2(u, u0, u1);
+                const uint64_t e = pk2(ex2_approx(u0), ex2_approx(u1));
+                s = add2(s, e);
+                d = fma2(pk2(fmaxf(u0, -1000.f), fmaxf(u1, -1000.f)), e, d);   // (u = -inf: 0; a NaN stays one in e)
             }
-            if (high >= bound) {
-                const int at = atomicAdd(&sm.noted, 1);
-                if (at < PLACES) sm.places[at] = chunk * LP_THREADS + tid;
+            float s0, s1, d0, d1;
+            upk2(s, s0, s1);
+            upk2(d, d0, d1);
+            run.s += s0 + s1;
+            run.d += d0 + d1;
+            if (TOP) {
+                if (chunk == look) {
+                    bound = kth_of_groups(sm, run.m, p.top);
+                    look = 3 * look + 2;
+                }
+                if (high >= bound) {
+                    const int at = atomicAdd(&sm.noted, 1);
+                    if (at < PLACES) sm.places[at] = chunk * LP_THREADS + tid;
+                }
             }
+            cur = next;
         }
-        cur = next;
-    }
 
-    // the logits that reach the bound of the whole part
-    bool all_found = false;
-    if (TOP) {
-        if (look > 2) bound = kth_of_groups(sm, run.m, p.top);
-        else __syncthreads();
-        const int noted = sm.noted;
-        all_found = noted <= PLACES && bound > -INFINITY;   // (NaN should have reached a bound of -inf too)
-        if (all_found) {
-            for (int i = tid; i < noted * C::VECS; i += LP_THREADS) {
-                const int place = sm.places[i / C::VECS];
-                span.each(place / LP_THREADS, place % LP_THREADS, i % C::VECS, [&](float x, int at) {
-                    if (x >= bound) {
-                        const int n = atomicAdd(&sm.count, 1);
-                        if (n < ASIDE) sm.aside[n] = order_key(x, at);
-                    }
+        // the logits that reach the bound of the whole part
+        bool all_found = false;
+        if (TOP) {
+            if (look > 2) bound = kth_of_groups(sm, run.m, p.top);
+            else __syncthreads();
+            const int noted = sm.noted;
+            all_found = noted <= PLACES && bound > -INFINITY;   // (NaN should have reached a bound of -inf too)
+            if (all_found) {
+                for (int i = tid; i < noted * C::VECS; i += LP_THREADS) {
+                    const int place = sm.places[i / C::VECS];
+                    span.each(place / LP_THREADS, place % LP_THREADS, i % C::VECS, [&](float x, int at) {
+                        if (x >= bound) {
+                            const int n = atomicAdd(&sm.count, 1);
+                            if (n < ASIDE) sm.aside[n] = order_key(x, at);
+                        }
+                    });
+                }
+            }
+        }
+        // the threads' sums
+        auto over_lanes = [&](int lanes) {
+            float m = run.m;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1)
+                if (off < lanes) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
+            run.rise_to(m, k2);
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) {
+                if (off >= lanes) continue;
+                run.s += __shfl_xor_sync(0xFFFFFFFFu, run.s, off);
+                run.d += __shfl_xor_sync(0xFFFFFFFFu, run.d, off);
+            }
+        };
+        over_lanes(32);
+        if (tid % 32 == 0) sm.warp[tid / 32] = run;
+        __syncthreads();
+        run = sm.warp[tid % LP_WARPS];
+        over_lanes(LP_WARPS);
+        const Key *keys = sm.aside;
+        int n = 0;
+        if (TOP) {
+            n = sm.count;
+            if (!all_found || n > ASIDE) {
+                exact_top<H16>(sm, span, p.top);
+                n = sm.count;
+            }
+            if (n > LP_THREADS) {
+                __syncthreads();
+                cut(sm, n, p.top);
+                n = sm.count;
+            }
+        }
+        if (cluster > 1) {
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            if (tid == 0) {
+                const uint32_t at = map_to_cta(smem_u32(&sm.cta[rank]), 0);
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(run.m) : "memory");
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(run.s) : "memory");
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 8), "f"(run.d) : "memory");
+            }
+            if (TOP) {
+                const uint32_t list = map_to_cta(smem_u32(&sm.list[rank * p.top]), 0);
+                ranked(sm.aside, n, p.top, [&](int place, Key key) {
+                    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(list + 8 * place), "l"(key) : "memory");
                 });
             }
+            cluster_sync_all();
+            if (rank != 0) return;
+            run = tid % MAX_CLUSTER < cluster ? sm.cta[tid % MAX_CLUSTER] : Sums{-INFINITY, 0.f, 0.f};
+            over_lanes(MAX_CLUSTER);
+            keys = sm.list;
+            n = cluster * p.top;
         }
-    }
-    // the threads' sums
-    auto over_lanes = [&](int lanes) {
-        float m = run.m;
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1)
-            if (off < lanes) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
-        run.rise_to(m, k2);
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) {
-            if (off >= lanes) continue;
-            run.s += __shfl_xor_sync(0xFFFFFFFFu, run.s, off);
-            run.d += __shfl_xor_sync(0xFFFFFFFFu, run.d, off);
-        }
-    };
-    over_lanes(32);
-    if (tid % 32 == 0) sm.warp[tid / 32] = run;
-    __syncthreads();
-    run = sm.warp[tid % LP_WARPS];
-    over_lanes(LP_WARPS);
-    const Key *keys = sm.aside;
-    int n = 0;
-    if (TOP) {
-        n = sm.count;
-        if (!all_found || n > ASIDE) {
-            exact_top<H16>(sm, span, p.top);
-            n = sm.count;
-        }
-        if (n > LP_THREADS) {
-            __syncthreads();
-            cut(sm, n, p.top);
-            n = sm.count;
-        }
-    }
-    if (cluster > 1) {
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        if (tid == 0) {
-            const uint32_t at = map_to_cta(smem_u32(&sm.cta[rank]), 0);
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(run.m) : "memory");
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(run.s) : "memory");
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 8), "f"(run.d) : "memory");
-        }
-        if (TOP) {
-            const uint32_t list = map_to_cta(smem_u32(&sm.list[rank * p.top]), 0);
-            ranked(sm.aside, n, p.top, [&](int place, Key key) {
-                asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(list + 8 * place), "l"(key) : "memory");
+        const float m = run.base(), log_s = log2f(run.s) * LN2;
+        if (TOP)
+            ranked(keys, n, p.top, [&](int place, Key key) {
+                if (p.top_ids) p.top_ids[r * p.top + place] = static_cast<int>(~static_cast<uint32_t>(key));
+                if (p.top_logprobs) p.top_logprobs[r * p.top + place] = (key_value(key) - m) * p.scale - log_s;
             });
-        }
-        cluster_sync_all();
-        if (rank != 0) return;
-        run = tid % MAX_CLUSTER < cluster ? sm.cta[tid % MAX_CLUSTER] : Sums{-INFINITY, 0.f, 0.f};
-        over_lanes(MAX_CLUSTER);
-        keys = sm.list;
-        n = cluster * p.top;
-    }
-    const float m = run.base(), log_s = log2f(run.s) * LN2;
-    if (TOP)
-        ranked(keys, n, p.top, [&](int place, Key key) {
-            if (p.top_ids) p.top_ids[r * p.top + place] = static_cast<int>(~static_cast<uint32_t>(key));
-            if (p.top_logprobs) p.top_logprobs[r * p.top + place] = (key_value(key) - m) * p.scale - log_s;
-        });
-    if (tid == 0) {
-        if (p.lse) p.lse[r] = m * p.scale + log_s;
-        if (p.entropy) p.entropy[r] = log_s - run.d / run.s * LN2;
-        if (p.logprob) {
-            float v = 0.f;
-            if (target >= p.vocab) {
-                v = NAN;
-                if (p.status) atomicOr(p.status, STATUS_BAD_TOKEN);
-            } else if (target >= 0) {
-                v = (x_t - m) * p.scale - log_s;
+        if (tid == 0) {
+            if (p.lse) p.lse[r] = m * p.scale + log_s;
+            if (p.entropy) p.entropy[r] = log_s - run.d / run.s * LN2;
+            if (p.logprob) {
+                float v = 0.f;
+                if (target >= p.vocab) {
+                    v = NAN;
+                    if (p.status) atomicOr(p.status, STATUS_BAD_TOKEN);
+                } else if (target >= 0) {
+                    v = (x_t - m) * p.scale - log_s;
+                }
+                p.logprob[r] = v;
             }
-            p.logprob[r] = v;
         }
+        __syncthreads();   // shared memory is the next row's
     }
 }
 
-// CTAs of a row: as many as bring the grid to four a SM, none with less than a chunk
+// CTAs of a row: more while they do not fill half the SMs, none with less than a chunk.  (48 x 51200 bf16, k = 20: 9.3 us with 2
+// a row, 10.1 with 4, 11.8 with 8; one row of 50257 fp32: 7.9 with 8, 10.8 with one.)
 int cluster_of(int rows, int vocab) {
     const int sms = sm_count() > 0 ? sm_count() : 148;
     int c = 1;
-    while (c < MAX_CLUSTER && (long long)rows * c < 4 * sms && vocab / (2 * c) >= LP_THREADS * PER_THREAD) c *= 2;
+    while (c < MAX_CLUSTER && (long long)rows * c * 2 < sms && vocab / (2 * c) >= LP_THREADS * PER_THREAD) c *= 2;
     return c;
 }
 
@@ -513,7 +520,9 @@ int launch(const LogprobParams &p, int rows, cudaStream_t st) {
     const int cluster = cluster_of(rows, p.vocab);
     if ((long long)rows * cluster > 0x7fffffffLL) return KRAKEN_EUNSUPPORTED;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(rows * cluster);
+    // one row after the other in each CTA of all that run at once
+    const int side = 4 * (sm_count() > 0 ? sm_count() : 148);
+    cfg.gridDim = dim3(cluster > 1 || rows < side ? rows * cluster : side);
     cfg.blockDim = dim3(LP_THREADS);
     cfg.dynamicSmemBytes = SMEM;
     cfg.stream = st;
@@ -550,6 +559,7 @@ extern "C" int kraken_op_token_logprobs(const kraken_logprobs_args *a, uint32_t 
     p.lse = a->lse;
     p.top_ids = a->top_ids;
     p.top_logprobs = a->top_logprobs;
+    p.rows = a->rows;
     p.vocab = a->vocab;
     p.top = a->top;
     p.scale = a->scale;

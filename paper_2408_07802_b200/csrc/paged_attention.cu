@@ -115,7 +115,7 @@ __device__ __forceinline__ uint32_t word(const uint4 &v, int i) { return i == 0 
 
 // Score options that the caller asked for, uniform over the launch
 struct ScoreForm {
-    float scale, cap, inv_cap2;   // inv_cap2: 2 log2(e) / cap
+    float scale, cap, inv_cap;
     bool plain;      // neither cap nor slopes: one product takes the scale and log2(e)
     float scale2;    // scale * log2(e)
 };
@@ -153,8 +153,7 @@ __device__ __forceinline__ void take_step(Running<HD, NT> &run, const uint8_t *s
                 x *= f.scale2;
             } else {
                 x *= f.scale;
-                // tanh y = 1 - 2 / (e^2y + 1): off by about 2^-23 absolute, i.e. the score by cap 2^-23
-                if (f.cap > 0.f) x = f.cap - 2.f * f.cap * rcp_approx(ex2_approx(x * f.inv_cap2) + 1.f);
+                if (f.cap > 0.f) x = f.cap * tanhf(x * f.inv_cap);
                 x = (x + slope[i >> 1] * static_cast<float>(back + kt * 8 + 2 * t + (i & 1))) * LOG2E;
             }
             s[kt][i] = x;
@@ -528,7 +527,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
     for (int i = 0; i < STAGES - 1; ++i) seen[i] = issue();
 
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    const ScoreForm form = {p.scale, p.cap, p.cap > 0.f ? 2.f * LOG2E / p.cap : 0.f, p.cap <= 0.f && !p.slopes, p.scale * LOG2E};
+    const ScoreForm form = {p.scale, p.cap, p.cap > 0.f ? 1.f / p.cap : 0.f, p.cap <= 0.f && !p.slopes, p.scale * LOG2E};
     int use = 0;
     uint4 q[NT][2 * HF];
     float slope[NT];

@@ -452,8 +452,8 @@ typedef struct kraken_paged_cache {
  * (interleaved: (x_2i, x_2i+1)) becomes (a cos - b sin, b cos + a sin); elements from rot_dim on are copied, and so
  * are the values.  The angle is formed and reduced in 64 bits; the products are fp32, rounded once.  rot_dim = 0 (then
  * inv_freq may be NULL) appends the rows as they are: the learned positions of this library's models.
- * q (or NULL): the rows' queries, rotated into q_out, which may be q itself (same strides) but must not overlap k, v
- * or the cache otherwise.  A row with row_seq[r] < 0 is padding, and one whose sequence, position or page does not
+ * q (or NULL): the rows' queries, rotated into q_out, which may be q itself (same strides).  Otherwise none of q_out and
+ * the cache may overlap another tensor of the call.  A row with row_seq[r] < 0 is padding, and one whose sequence, position or page does not
  * exist raises the status bit: neither changes the cache nor q_out.  The rows of one call must go to distinct
  * positions: of two rows with the same one, which of them the cache then holds is not defined, element by element.
  * Errors: EINVAL, EUNSUPPORTED (alignment, head_dim, rot_dim no multiple of 8 or above head_dim), ECUDA. */

@@ -25,21 +25,27 @@ namespace kr {
 
 namespace {
 
-constexpr int LP_THREADS = 256;
-constexpr int LP_WARPS = LP_THREADS / 32;
 constexpr int LP_MAX_TOP = 32;
 constexpr int PER_THREAD = 16;                       // logits of a thread in a chunk
-constexpr int GROUP = 4, GROUPS = LP_THREADS / GROUP;
+constexpr int GROUP = 4;
 constexpr int CHUNK_ADDS = (LP_MAX_TOP - 1) * GROUP * PER_THREAD + 1;
-constexpr int ASIDE = 2560;                          // room for keys put aside
-constexpr int PLACES = 2560;                         // and for places noted
+constexpr int ASIDE = 2048;                          // room for keys put aside
+constexpr int PLACES = 1024;                         // and for places noted
+constexpr int MAX_GROUPS = 64;
 constexpr int MAX_CLUSTER = 8;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.69314718055994531f;
 typedef unsigned long long Key;
-static_assert(GROUPS >= LP_MAX_TOP, "the bound is the k-th of the groups");
-static_assert(MAX_CLUSTER * LP_MAX_TOP == LP_THREADS, "a thread clears one key of the list");
 static_assert(ASIDE > CHUNK_ADDS + LP_MAX_TOP, "after a cut a chunk has to fit");
+
+// Threads of a CTA and CTAs of an SM.  Smaller CTAs keep more rows going side by side, one's end beside another's middle, but
+// take their bounds from fewer groups and longer over a single row (2048 x 50257, k = 5: fp32 72 us with 128 threads against 76
+// with 256, bf16 57 against 67; k = 20, fp32: 92 against 87; 592 rows, fp32, k = 5: 25 against 23).
+template <int T>
+struct Shape {
+    static constexpr int THREADS = T, WARPS = T / 32, CTAS = 1024 / T, GROUPS = T / GROUP;
+    static_assert(GROUPS >= LP_MAX_TOP, "the bound is the k-th of the groups");
+};
 
 struct LogprobParams {
     const void *logits;
@@ -96,16 +102,16 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 
 struct Smem {
     Key aside[ASIDE];
-    Key group[GROUPS];
-    float high[GROUPS];
+    Key group[MAX_GROUPS];
+    float high[MAX_GROUPS];
     Key list[MAX_CLUSTER * LP_MAX_TOP];   // of every CTA of the cluster, in order; 0: none
     Key tau;
     float bound;
-    int places[PLACES];       // chunk * LP_THREADS + thread
+    int places[PLACES];       // chunk * T + thread
     int noted;
     int count;                // keys put aside
     int sum;
-    Sums warp[LP_WARPS], cta[MAX_CLUSTER];
+    Sums warp[8], cta[MAX_CLUSTER];
 };
 
 template <bool H16>
@@ -124,6 +130,7 @@ struct Chunk {   // 16 logits of a thread, in vectors of 16 bytes
 };
 
 // The k-th largest of the groups' largest logits.  All threads; two barriers.
+template <int T>
 __device__ __forceinline__ float kth_of_groups(Smem &sm, float high, int k) {
     static_assert(GROUP == 4, "the threads of a group rank its logit");
 #pragma unroll
@@ -132,7 +139,7 @@ __device__ __forceinline__ float kth_of_groups(Smem &sm, float high, int k) {
     __syncthreads();
     int ranks = 0;   // logits above, and in the upper half those equal
 #pragma unroll
-    for (int i = 0; i < GROUPS; i += GROUP) {
+    for (int i = 0; i < Shape<T>::GROUPS; i += GROUP) {
         const float x = sm.high[i + threadIdx.x % GROUP];
         ranks += (x > high ? 1 : 0) + (x == high ? 1 << 16 : 0);
     }
@@ -145,9 +152,9 @@ __device__ __forceinline__ float kth_of_groups(Smem &sm, float high, int k) {
 }
 
 // f(rank, key) for those of n keys whose rank is below k, four threads a key.  All threads.
-template <typename F>
+template <int T, typename F>
 __device__ __forceinline__ void ranked(const Key *keys, int n, int k, F f) {
-    for (int i0 = 0; i0 < n; i0 += LP_THREADS / 4) {
+    for (int i0 = 0; i0 < n; i0 += T / 4) {
         const int at = i0 + threadIdx.x / 4;
         const Key mine = at < n ? keys[at] : 0;
         int above = 0;
@@ -160,6 +167,7 @@ __device__ __forceinline__ void ranked(const Key *keys, int n, int k, F f) {
 }
 
 // The same of the groups' largest keys; 0 when there are fewer than k.
+template <int T>
 __device__ __forceinline__ Key kth_of_groups(Smem &sm, Key best, int k) {
 #pragma unroll
     for (int off = 1; off < GROUP; off <<= 1) {
@@ -169,11 +177,11 @@ __device__ __forceinline__ Key kth_of_groups(Smem &sm, Key best, int k) {
     if (threadIdx.x % GROUP == 0) sm.group[threadIdx.x / GROUP] = best;
     if (threadIdx.x == 0) sm.tau = 0;
     __syncthreads();
-    if (threadIdx.x < GROUPS) {
+    if (threadIdx.x < Shape<T>::GROUPS) {
         const Key mine = sm.group[threadIdx.x];
         int above = 0;
 #pragma unroll 16
-        for (int i = 0; i < GROUPS; ++i) above += sm.group[i] > mine;
+        for (int i = 0; i < Shape<T>::GROUPS; ++i) above += sm.group[i] > mine;
         if (above == k - 1 && mine != 0) sm.tau = mine;
     }
     __syncthreads();
@@ -181,12 +189,13 @@ __device__ __forceinline__ Key kth_of_groups(Smem &sm, Key best, int k) {
 }
 
 // Cuts the n keys put aside down to the k largest and returns the smallest of these, found bit by bit.  All threads.
+template <int T>
 __device__ __noinline__ Key cut(Smem &sm, int n, int k) {
-    constexpr int MOST = (ASIDE + LP_THREADS - 1) / LP_THREADS;
+    constexpr int MOST = (ASIDE + T - 1) / T;
     Key mine[MOST];
 #pragma unroll
     for (int i = 0; i < MOST; ++i) {
-        const int at = threadIdx.x + i * LP_THREADS;
+        const int at = threadIdx.x + i * T;
         mine[i] = at < n ? sm.aside[at] : 0;
     }
     Key tau = 0;
@@ -214,10 +223,10 @@ __device__ __noinline__ Key cut(Smem &sm, int n, int k) {
 
 // The part of a row that a CTA reads, in vectors of 16 bytes that start on 16 bytes: `before` elements of the row's first
 // vector lie in front of the row, and are not read any more than those behind its end.
-template <bool H16>
+template <bool H16, int T>
 struct Span {
     using C = Chunk<H16>;
-    static constexpr int VEC = C::VEC, VECS = C::VECS, SIZE = H16 ? 2 : 4, CHUNK = VECS * LP_THREADS;   // CHUNK: vectors
+    static constexpr int VEC = C::VEC, VECS = C::VECS, SIZE = H16 ? 2 : 4, CHUNK = VECS * T;   // CHUNK: vectors
     static constexpr uint32_t NONE = H16 ? (KRAKEN_F16 ? 0xFC00FC00u : 0xFF80FF80u) : 0xFF800000u;      // -inf
     const uint8_t *row;
     const uint4 *vectors;
@@ -235,7 +244,7 @@ struct Span {
         chunks = (hi - lo + CHUNK - 1) / CHUNK;
     }
     __device__ __forceinline__ int index(int chunk, int i) const {   // of logit i of this thread's chunk; maybe outside the part
-        return (lo + (chunk * VECS + i / VEC) * LP_THREADS + (int)threadIdx.x) * VEC + i % VEC - before;
+        return (lo + (chunk * VECS + i / VEC) * T + (int)threadIdx.x) * VEC + i % VEC - before;
     }
     __device__ __forceinline__ bool has(int index) const {
         return index >= max(0, lo * VEC - before) && index < min(vocab, hi * VEC - before);
@@ -244,12 +253,12 @@ struct Span {
         const int v0 = lo + chunk * CHUNK;
         if (v0 >= clean_lo && v0 + CHUNK <= clean_hi) {
 #pragma unroll
-            for (int i = 0; i < VECS; ++i) c.raw[i] = __ldcs(vectors + v0 + i * LP_THREADS + threadIdx.x);
+            for (int i = 0; i < VECS; ++i) c.raw[i] = __ldcs(vectors + v0 + i * T + threadIdx.x);
             return;
         }
 #pragma unroll
         for (int i = 0; i < VECS; ++i) {
-            const int v = v0 + i * LP_THREADS + threadIdx.x;
+            const int v = v0 + i * T + threadIdx.x;
             c.raw[i] = make_uint4(NONE, NONE, NONE, NONE);
             if (v >= clean_lo && v < clean_hi) {
                 c.raw[i] = __ldcs(vectors + v);
@@ -273,7 +282,7 @@ struct Span {
     // f(logit, index) for the logits of vector i of a thread's chunk
     template <typename F>
     __device__ __forceinline__ void each(int chunk, int thread, int i, F f) const {
-        const int v = lo + (chunk * VECS + i) * LP_THREADS + thread;
+        const int v = lo + (chunk * VECS + i) * T + thread;
         if (v >= clean_lo && v < clean_hi) {
             C c;
             c.raw[0] = vectors[v];
@@ -292,8 +301,8 @@ struct Span {
 // The k largest keys of the part, and maybe some more, into sm.aside; any order, any ties.  A bound is raised from a chunk as
 // long as many threads exceed it, after which a chunk adds at most (k - 1) * GROUP * PER_THREAD + 1 keys; where these might not
 // fit, the keys put aside are cut down to k first.
-template <bool H16>
-__device__ __noinline__ void exact_top(Smem &sm, const Span<H16> &span, int k) {
+template <bool H16, int T>
+__device__ __noinline__ void exact_top(Smem &sm, const Span<H16, T> &span, int k) {
     __syncthreads();
     if (threadIdx.x == 0) sm.count = 0;
     Key tau = 0;
@@ -310,13 +319,13 @@ __device__ __noinline__ void exact_top(Smem &sm, const Span<H16> &span, int k) {
         }
         const int over = __syncthreads_count(best >= tau && best != 0);
         if (over == 0) continue;
-        if (chunk == 0 || over > GROUPS) {
-            const Key bound = kth_of_groups(sm, best, k);
+        if (chunk == 0 || over > Shape<T>::GROUPS) {
+            const Key bound = kth_of_groups<T>(sm, best, k);
             tau = bound > tau ? bound : tau;
         }
         const int n = sm.count;
         if (n + CHUNK_ADDS > ASIDE) {
-            const Key bound = cut(sm, n, k);
+            const Key bound = cut<T>(sm, n, k);
             tau = bound > tau ? bound : tau;
         } else {
             __syncthreads();   // everyone has read the count
@@ -333,23 +342,24 @@ __device__ __noinline__ void exact_top(Smem &sm, const Span<H16> &span, int k) {
     __syncthreads();
 }
 
-template <bool H16, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobParams p, int cluster) {
+template <bool H16, bool TOP, int T>
+__global__ void __launch_bounds__(T, Shape<T>::CTAS) logprobs_kernel(const LogprobParams p, int cluster) {
     using C = Chunk<H16>;
     extern __shared__ __align__(16) uint8_t smem_raw[];
     Smem &sm = *reinterpret_cast<Smem *>(smem_raw);
     const int rank = blockIdx.x % cluster, tid = threadIdx.x;
     if (cluster > 1) {
         // the CTAs of a cluster write into the first one's shared memory at the end: by then it has to run, and to be ready
-        if (TOP && rank == 0) sm.list[tid] = 0;
+        if (TOP && rank == 0)
+            for (int i = tid; i < MAX_CLUSTER * LP_MAX_TOP; i += T) sm.list[i] = 0;
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     }
     pdl_wait();
     const float k2 = p.scale * LOG2E;
     const int step = gridDim.x / cluster;   // rows side by side; with clusters every row has its own
-    auto row_at = [&](long long r) { return static_cast<const uint8_t *>(p.logits) + r * p.row_stride * Span<H16>::SIZE; };
+    auto row_at = [&](long long r) { return static_cast<const uint8_t *>(p.logits) + r * p.row_stride * Span<H16, T>::SIZE; };
     C cur, next;
-    Span<H16>(row_at(blockIdx.x / cluster), p.vocab, rank, cluster).load(cur, 0);
+    Span<H16, T>(row_at(blockIdx.x / cluster), p.vocab, rank, cluster).load(cur, 0);
     for (long long r = blockIdx.x / cluster; r < p.rows; r += step) {
         const uint8_t *row = row_at(r);
         float x_t = 0.f;
@@ -359,7 +369,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
             if (target >= 0 && target < p.vocab)
                 x_t = H16 ? from_h16(reinterpret_cast<const uint16_t *>(row)[target]) : reinterpret_cast<const float *>(row)[target];
         }
-        const Span<H16> span(row, p.vocab, rank, cluster);
+        const Span<H16, T> span(row, p.vocab, rank, cluster);
         Sums run = {-INFINITY, 0.f, 0.f};
         float bound = -INFINITY;
         if (TOP && tid == 0) sm.count = sm.noted = 0;
@@ -367,7 +377,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
         for (int chunk = 0; chunk < span.chunks; ++chunk) {
             // with the last chunk the next row's first one is requested: the end of a row takes longer than the way to memory
             if (chunk + 1 < span.chunks) span.load(next, chunk + 1);
-            else if (r + step < p.rows) Span<H16>(row_at(r + step), p.vocab, rank, cluster).load(next, 0);
+            else if (r + step < p.rows) Span<H16, T>(row_at(r + step), p.vocab, rank, cluster).load(next, 0);
             float high = -INFINITY;   // (a NaN is passed over)
 #pragma unroll
             for (int i = 0; i < PER_THREAD; ++i) high = fmaxf(high, cur.at(i));
@@ -390,12 +400,12 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
             run.d += d0 + d1;
             if (TOP) {
                 if (chunk == look) {
-                    bound = kth_of_groups(sm, run.m, p.top);
+                    bound = kth_of_groups<T>(sm, run.m, p.top);
                     look = 3 * look + 2;
                 }
                 if (high >= bound) {
                     const int at = atomicAdd(&sm.noted, 1);
-                    if (at < PLACES) sm.places[at] = chunk * LP_THREADS + tid;
+                    if (at < PLACES) sm.places[at] = chunk * T + tid;
                 }
             }
             cur = next;
@@ -404,14 +414,14 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
         // the logits that reach the bound of the whole part
         bool all_found = false;
         if (TOP) {
-            if (look > 2) bound = kth_of_groups(sm, run.m, p.top);
+            if (look > 2) bound = kth_of_groups<T>(sm, run.m, p.top);
             else __syncthreads();
             const int noted = sm.noted;
             all_found = noted <= PLACES && bound > -INFINITY;   // (NaN should have reached a bound of -inf too)
             if (all_found) {
-                for (int i = tid; i < noted * C::VECS; i += LP_THREADS) {
+                for (int i = tid; i < noted * C::VECS; i += T) {
                     const int place = sm.places[i / C::VECS];
-                    span.each(place / LP_THREADS, place % LP_THREADS, i % C::VECS, [&](float x, int at) {
+                    span.each(place / T, place % T, i % C::VECS, [&](float x, int at) {
                         if (x >= bound) {
                             const int n = atomicAdd(&sm.count, 1);
                             if (n < ASIDE) sm.aside[n] = order_key(x, at);
@@ -437,19 +447,19 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
         over_lanes(32);
         if (tid % 32 == 0) sm.warp[tid / 32] = run;
         __syncthreads();
-        run = sm.warp[tid % LP_WARPS];
-        over_lanes(LP_WARPS);
+        run = sm.warp[tid % Shape<T>::WARPS];
+        over_lanes(Shape<T>::WARPS);
         const Key *keys = sm.aside;
         int n = 0;
         if (TOP) {
             n = sm.count;
             if (!all_found || n > ASIDE) {
-                exact_top<H16>(sm, span, p.top);
+                exact_top<H16, T>(sm, span, p.top);
                 n = sm.count;
             }
-            if (n > LP_THREADS) {
+            if (n > T) {
                 __syncthreads();
-                cut(sm, n, p.top);
+                cut<T>(sm, n, p.top);
                 n = sm.count;
             }
         }
@@ -463,7 +473,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
             }
             if (TOP) {
                 const uint32_t list = map_to_cta(smem_u32(&sm.list[rank * p.top]), 0);
-                ranked(sm.aside, n, p.top, [&](int place, Key key) {
+                ranked<T>(sm.aside, n, p.top, [&](int place, Key key) {
                     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(list + 8 * place), "l"(key) : "memory");
                 });
             }
@@ -476,7 +486,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
         }
         const float m = run.base(), log_s = log2f(run.s) * LN2;
         if (TOP)
-            ranked(keys, n, p.top, [&](int place, Key key) {
+            ranked<T>(keys, n, p.top, [&](int place, Key key) {
                 if (p.top_ids) p.top_ids[r * p.top + place] = static_cast<int>(~static_cast<uint32_t>(key));
                 if (p.top_logprobs) p.top_logprobs[r * p.top + place] = (key_value(key) - m) * p.scale - log_s;
             });
@@ -503,27 +513,25 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const LogprobPa
 int cluster_of(int rows, int vocab) {
     const int sms = sm_count() > 0 ? sm_count() : 148;
     int c = 1;
-    while (c < MAX_CLUSTER && (long long)rows * c * 2 < sms && vocab / (2 * c) >= LP_THREADS * PER_THREAD) c *= 2;
+    while (c < MAX_CLUSTER && (long long)rows * c * 2 < sms && vocab / (2 * c) >= 256 * PER_THREAD) c *= 2;
     return c;
 }
 
-template <bool H16, bool TOP>
-int launch(const LogprobParams &p, int rows, cudaStream_t st) {
+template <bool H16, bool TOP, int T>
+int launch(const LogprobParams &p, int cluster, cudaStream_t st) {
     static DeviceOnce configured;
     constexpr int SMEM = sizeof(Smem);
     if (!configured.done()) {
-        int rc = cuda_check(cudaFuncSetAttribute(logprobs_kernel<H16, TOP>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM),
+        int rc = cuda_check(cudaFuncSetAttribute(logprobs_kernel<H16, TOP, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM),
                             "token logprobs: shared memory opt-in");
         if (rc) return rc;
         configured.set();
     }
-    const int cluster = cluster_of(rows, p.vocab);
-    if ((long long)rows * cluster > 0x7fffffffLL) return KRAKEN_EUNSUPPORTED;
     cudaLaunchConfig_t cfg = {};
     // one row after the other in each CTA of all that run at once
-    const int side = 4 * (sm_count() > 0 ? sm_count() : 148);
-    cfg.gridDim = dim3(cluster > 1 || rows < side ? rows * cluster : side);
-    cfg.blockDim = dim3(LP_THREADS);
+    const int side = Shape<T>::CTAS * (sm_count() > 0 ? sm_count() : 148);
+    cfg.gridDim = dim3(cluster > 1 || p.rows < side ? p.rows * cluster : side);
+    cfg.blockDim = dim3(T);
     cfg.dynamicSmemBytes = SMEM;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -534,7 +542,14 @@ int launch(const LogprobParams &p, int rows, cudaStream_t st) {
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cuda_check(cudaLaunchKernelEx(&cfg, logprobs_kernel<H16, TOP>, p, cluster), "token logprobs: launch");
+    return cuda_check(cudaLaunchKernelEx(&cfg, logprobs_kernel<H16, TOP, T>, p, cluster), "token logprobs: launch");
+}
+
+template <bool H16, bool TOP>
+int launch_rows(const LogprobParams &p, cudaStream_t st) {
+    const int cluster = cluster_of(p.rows, p.vocab), sms = sm_count() > 0 ? sm_count() : 148;
+    // many rows and few alternatives: see Shape
+    return p.rows >= 8 * sms && p.top <= 8 ? launch<H16, TOP, 128>(p, cluster, st) : launch<H16, TOP, 256>(p, cluster, st);
 }
 
 }  // namespace
@@ -565,6 +580,6 @@ extern "C" int kraken_op_token_logprobs(const kraken_logprobs_args *a, uint32_t 
     p.scale = a->scale;
     p.status = d_status;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (a->dtype) return a->top ? launch<true, true>(p, a->rows, st) : launch<true, false>(p, a->rows, st);
-    return a->top ? launch<false, true>(p, a->rows, st) : launch<false, false>(p, a->rows, st);
+    if (a->dtype) return a->top ? launch_rows<true, true>(p, st) : launch_rows<true, false>(p, st);
+    return a->top ? launch_rows<false, true>(p, st) : launch_rows<false, false>(p, st);
 }

@@ -197,6 +197,11 @@ extern "C" int kraken_op_paged_append(const kraken_paged_cache *cache, const kra
         (a->q && (!a->q_out || a->n_head < 1)))
         return KRAKEN_EINVAL;
     if (!a->row_seq && a->rows > cache->n_seqs) return KRAKEN_EINVAL;
+    // (no two places of the cache, rows or heads of q_out in one place)
+    if ((cache->n_pages > 1 && cache->page_stride == 0) || (cache->n_kv_head > 1 && cache->head_stride == 0) ||
+        (cache->page_size > 1 && cache->slot_stride == 0) ||
+        (a->q && ((a->rows > 1 && a->q_out_row_stride == 0) || (a->n_head > 1 && a->q_out_head_stride == 0))))
+        return KRAKEN_EINVAL;
     if (a->rot_dim % 8 != 0 || a->rot_dim > cache->head_dim) return KRAKEN_EUNSUPPORTED;
     if (!aligned16(a->k) || !aligned16(a->v) || ((a->k_row_stride | a->k_head_stride | a->v_row_stride | a->v_head_stride) & 7))
         return KRAKEN_EUNSUPPORTED;

@@ -16,7 +16,7 @@
 //                               g + 8 of product j stand for elements 8 g + 2 j and 8 g + 2 j + 1
 // P goes into the product as the sum of two 16-bit numbers (its rounding and the rounding of the rest), so its rounding,
 // which would be as large as that of the output, does not count.  Maximum and sum are kept in fp32, and the maximum in use
-// is only raised when a score exceeds it by more than 2^8 in the exponent (numerator and denominator carry the same
+// is only raised when a score exceeds it by more than 8 in the exponent of 2 (numerator and denominator carry the same
 // factor), so most blocks need one vote of the warp where a running maximum would take shuffles and a rescaling.
 #include <math.h>
 #include <string.h>
@@ -36,7 +36,11 @@ constexpr int STAGES = 2;                // steps of a warp in shared memory: on
 constexpr int BEGIN = 1;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.69314718055994531f;
-constexpr float RAISE = 8.f;
+// A weight is 2^(score - m) with m so chosen that the largest of a block is 2^HEADROOM when m is set, and m is raised when a
+// score would get past 2^(HEADROOM + 8).  HEADROOM = 7 in the half image: half numbers end at 2^16 and 2^-24, and weights that
+// round to nothing against the largest one, 10^5 of them, would be missing from the output and not from the sum.
+constexpr float HEADROOM = KRAKEN_F16 ? 7.f : 0.f;
+constexpr float RAISE = HEADROOM + 8.f;
 
 // n / d for 0 <= n < 2^31 by a product: with 2^(s-1) < d <= 2^s, m = floor(2^(31+s) / d) + 1 is off by less than d 2^-(31+s)
 // of itself, which n < 2^31 cannot carry past the next integer.
@@ -98,7 +102,7 @@ struct Step {
 template <int HD, int NT>
 struct Running {   // online softmax of 8 NT heads over the keys of one warp
     static constexpr int HF = Step<HD>::HF;
-    float m[NT], base[NT], l[NT];   // head 8 nt + g: maximum in use (log2 domain; base: 0 for -inf), this lane's part of the sum
+    float m[NT], base[NT], l[NT];   // head 8 nt + g: exponent in use (log2 domain; base: 0 for -inf), this lane's part of the sum
     float o[NT][HF * 4][4];         // heads 8 nt + 2t + {0, 1}
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -178,7 +182,7 @@ __device__ __forceinline__ void take_step(Running<HD, NT> &run, const uint8_t *s
         for (int nt = 0; nt < NT; ++nt) {
             float mx = fmaxf(top[nt], __shfl_xor_sync(0xFFFFFFFFu, top[nt], 1));
             mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 2));
-            mx = fmaxf(mx, run.m[nt]);
+            mx = fmaxf(mx - HEADROOM, run.m[nt]);
             run.base[nt] = mx == -INFINITY ? 0.f : mx;   // nothing visible yet: every weight is 2^-inf = 0
             const float corr = ex2_approx(run.m[nt] - run.base[nt]);
             run.m[nt] = mx;
@@ -856,6 +860,10 @@ extern "C" int kraken_op_paged_attention(const kraken_paged_cache *cache, const 
         !isfinite(a->scale) || !isfinite(a->score_cap) || a->score_cap < 0.f)
         return KRAKEN_EINVAL;
     if (!a->row_seq && a->rows > cache->n_seqs) return KRAKEN_EINVAL;
+    // (no two rows or heads of the output in one place)
+    if ((a->rows > 1 && a->out_row_stride == 0) || (a->n_head > 1 && a->out_head_stride == 0) ||
+        (a->lse && a->rows > 1 && a->lse_row_stride == 0))
+        return KRAKEN_EINVAL;
     if (!aligned16(a->q) || !aligned16(a->out) ||
         ((a->q_row_stride | a->q_head_stride | a->out_row_stride | a->out_head_stride) & 7))
         return KRAKEN_EUNSUPPORTED;

@@ -233,6 +233,31 @@ def test_attention_extreme_scores():
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("gap", [12.0, 17.0, 21.0])
+def test_attention_many_small_weights_against_a_large_one(dtype, gap):
+    """One key with e^gap times the weight of each of 60000 others: together these count, alone each is next to nothing in 16
+    bits.  V is 1 at the large one and -1 elsewhere."""
+    n, hd = 60000, 64
+    pages = Pages(15, [n], 1, hd, 64, dtype, fill=False)
+    pages.k.zero_()
+    pages.v.fill_(-1.0)
+    at = 777
+    slot = pages.table[0, at // 64].item(), 0, at % 64
+    pages.k[slot][0] = gap
+    pages.v[slot] = 1.0
+    q = torch.zeros(1, 1, hd, dtype=T16[dtype], device=DEV)
+    q[0, 0, 0] = 1.0
+    out, lse = kr.op_paged_decode_attention(q, pages.k, pages.v, pages.table, torch.tensor([n], dtype=torch.int32, device=DEV), scale=1.0)
+    big = math.exp(gap)
+    ref = (big - (n - 1)) / (big + (n - 1))
+    # half a step of the output; the sums as above; in half, weights below 2^-25 of 2^7 may be off by that, each
+    lost = (n * 2.0 ** -32 if dtype == "f16" else 0) + 2.0 ** -17 + 2.0 ** -21 + n * 2.0 ** -24 * 0.01
+    assert (out.double() - ref).abs().max() <= torch.finfo(T16[dtype]).eps / 2 * abs(ref) + 2 * lost
+    assert abs(lse.item() - math.log(big + n - 1)) < 1e-5
+
+
+@gpu
 def test_attention_far_pages_and_streams():
     """Offsets past 2^31 elements, on another stream than the default one, captured into a graph and replayed with other lengths."""
     page, hd, n_pages = 128, 128, 140000
@@ -417,7 +442,7 @@ def check_logprobs(logits, targets, top, scale=1.0, status=None):
 
 
 SCORES = [(1, 1, 1), (3, 2, 2), (2, 31, 5), (5, 33, 32), (1, 1000, 0), (7, 4097, 20), (300, 257, 3), (2, 50257, 32), (1, 131073, 20),
-          (160, 8191, 7), (40, 51200, 20)]
+          (160, 8191, 7), (40, 51200, 20), (700, 5003, 8), (1500, 999, 0), (650, 9001, 9)]
 
 
 @gpu
@@ -446,6 +471,43 @@ def test_logprobs_orders(V, kind):
     check_logprobs(x.float(), targets, 32)
     if kind != "huge":
         check_logprobs(x.to(torch.bfloat16), targets, 20)
+
+
+@gpu
+@pytest.mark.parametrize("rows,top", [(200, 32), (1300, 8), (1300, 0), (1300, 20)])
+def test_logprobs_many_rows_of_every_order(rows, top):
+    """Rows that need the exact way through (rising, of few values, all equal, mostly forbidden) between ordinary ones, in CTAs that
+    take several rows."""
+    V = 9001
+    x = normal(33, rows, V).float()
+    i = torch.arange(V, dtype=torch.float32, device=DEV)
+    x[1::7] = i / 500
+    x[2::7] = (i % 3)
+    x[3::7] = 1.25
+    x[4::7, 5:] = -math.inf
+    x[5::7] = -i / 500
+    targets = torch.arange(rows, dtype=torch.int32, device=DEV) % V
+    check_logprobs(x, targets, top)
+    check_logprobs(x.to(torch.float16), targets, top)
+
+
+@gpu
+def test_logprobs_lowest_values():
+    """Masks of the type's lowest value, a row of nothing else (every token equally likely), values at both ends of the type."""
+    V = 5000
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        low = torch.finfo(dtype).min
+        x = normal(34, 4, V).to(dtype)
+        x[0, 100:] = low
+        x[1] = low
+        x[2, ::2] = -low
+        x[2, 1::2] = low
+        got = kr.op_token_logprobs(x, torch.tensor([5, 7, 0, 3], dtype=torch.int32, device=DEV), top=3)
+        ref = torch.log_softmax(x.double(), -1)
+        assert abs(got.logprob[0].item() - ref[0, 5].item()) < 1e-5 and abs(got.logprob[3].item() - ref[3, 3].item()) < 1e-5
+        assert abs(got.logprob[1].item() + math.log(V)) < 1e-4 and abs(got.entropy[1].item() - math.log(V)) < 1e-4
+        assert abs(got.logprob[2].item() + math.log(V / 2)) < 1e-4 and abs(got.entropy[2].item() - math.log(V / 2)) < 1e-4
+        assert got.top_ids[1].tolist() == [0, 1, 2] and got.top_ids[2].tolist() == [0, 2, 4]
 
 
 @gpu
@@ -634,12 +696,17 @@ def test_refusals_before_the_device_is_touched(dtype):
                        (dict(inv_freq=None), kr.EINVAL), (dict(q_out=None), kr.EINVAL), (dict(n_head=0), kr.EINVAL),
                        (dict(row_seq=None, rows=4), kr.EINVAL), (dict(rot_dim=-8), kr.EINVAL), (dict(rot_dim=12), kr.EUNSUPPORTED),
                        (dict(rot_dim=72), kr.EUNSUPPORTED), (dict(k=(1 << 20) + 4), kr.EUNSUPPORTED), (dict(v_row_stride=65), kr.EUNSUPPORTED),
-                       (dict(q=(1 << 20) + 8), kr.EUNSUPPORTED), (dict(q_out_head_stride=4), kr.EUNSUPPORTED)]:
+                       (dict(q=(1 << 20) + 8), kr.EUNSUPPORTED), (dict(q_out_head_stride=4), kr.EUNSUPPORTED),
+                       (dict(q_out_row_stride=0), kr.EINVAL), (dict(q_out_head_stride=0), kr.EINVAL)]:
         assert append(cache_args(), append_args(**over)) == code, over
+    for over in (dict(page_stride=0), dict(head_stride=0), dict(slot_stride=0)):      # nothing to write to twice
+        assert append(cache_args(**over), append_args()) == kr.EINVAL, over
     assert append(cache_args(), append_args(rows=0)) == kr.OK
     for over, code in [(dict(rows=-1), kr.EINVAL), (dict(q=None), kr.EINVAL), (dict(out=None), kr.EINVAL), (dict(n_keys=None), kr.EINVAL),
                        (dict(n_head=3), kr.EINVAL), (dict(n_head=0), kr.EINVAL), (dict(window=-1), kr.EINVAL), (dict(scale=math.nan), kr.EINVAL),
                        (dict(score_cap=-1.0), kr.EINVAL), (dict(score_cap=math.inf), kr.EINVAL), (dict(row_seq=None, rows=4), kr.EINVAL),
+                       (dict(out_row_stride=0), kr.EINVAL), (dict(out_head_stride=0), kr.EINVAL), (dict(lse=1 << 20), kr.EINVAL),
+                       (dict(workspace=None), kr.ECAPACITY), (dict(workspace_bytes=1000), kr.ECAPACITY), (dict(workspace=(1 << 20) + 8), kr.EINVAL),
                        (dict(q=(1 << 20) + 2), kr.EUNSUPPORTED), (dict(out_row_stride=252), kr.EUNSUPPORTED)]:
         assert attend(cache_args(), attention_args(**over)) == code, over
     assert attend(cache_args(), attention_args(rows=0)) == kr.OK

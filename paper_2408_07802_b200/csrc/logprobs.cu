@@ -8,8 +8,8 @@
 //
 // The alternatives are found in the same pass.  After chunks 1, 3, 9, 27 ... the largest logits so far of 64 groups of 4
 // threads are looked at: the k-th largest of them is a bound that k logits reach.  A thread compares the maximum of its 16
-// logits, which it has anyway, with the bound and where it is reached notes the place: some 130 of a row for k = 20.  At the end
-// the bound is taken once more, the places noted are read again (out of L2) and the logits that reach the last bound, not many
+// logits, which it has anyway, with the bound and where it is reached notes its place and that maximum: some 100 of a row for k = 20.  At the
+// end the bound is taken once more, the places whose maximum reaches it are read again and the logits that do, not many
 // more than k, are ranked by counting, by keys of a logit and its index whose order is that of the list.  (With the logits put
 // aside at once, a warp went through the 16 logits of a thread some hundred times a row: 2048 x 50257 with k = 20 took 98 us.)
 // Where more places or logits reach the bound than there is room for (a vocabulary in rising order, or of few different
@@ -28,23 +28,24 @@ namespace {
 constexpr int LP_MAX_TOP = 32;
 constexpr int PER_THREAD = 16;                       // logits of a thread in a chunk
 constexpr int GROUP = 4;
-constexpr int CHUNK_ADDS = (LP_MAX_TOP - 1) * GROUP * PER_THREAD + 1;
-constexpr int ASIDE = 2048;                          // room for keys put aside
-constexpr int PLACES = 1024;                         // and for places noted
-constexpr int MAX_GROUPS = 64;
 constexpr int MAX_CLUSTER = 8;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.69314718055994531f;
 typedef unsigned long long Key;
-static_assert(ASIDE > CHUNK_ADDS + LP_MAX_TOP, "after a cut a chunk has to fit");
 
 // Threads of a CTA and CTAs of an SM.  Smaller CTAs keep more rows going side by side, one's end beside another's middle, but
 // take their bounds from fewer groups and longer over a single row (2048 x 50257, k = 5: fp32 72 us with 128 threads against 76
 // with 256, bf16 57 against 67; k = 20, fp32: 92 against 87; 592 rows, fp32, k = 5: 25 against 23).
 template <int T>
 struct Shape {
-    static constexpr int THREADS = T, WARPS = T / 32, CTAS = 1024 / T, GROUPS = T / GROUP;
-    static_assert(GROUPS >= LP_MAX_TOP, "the bound is the k-th of the groups");
+    static constexpr int WARPS = T / 32, CTAS = 1024 / T, GROUPS = T / GROUP;
+    static constexpr int TOP = T == 128 ? 8 : LP_MAX_TOP;                       // alternatives at most
+    static constexpr int CHUNK_ADDS = (TOP - 1) * GROUP * PER_THREAD + 1;       // see exact_top
+    // room for keys put aside and for places noted.  (Shared memory is taken from L1, which the loads on their way go through:
+    // 27 KB for each of 8 CTAs made the sums alone of 2048 x 50257 take 87 us instead of 63.)
+    static constexpr int ASIDE = T == 128 ? 640 : 2048, PLACES = T == 128 ? 512 : 896;
+    static_assert(GROUPS >= TOP, "the bound is the k-th of the groups");
+    static_assert(ASIDE > CHUNK_ADDS + TOP, "after a cut a chunk has to fit");
 };
 
 struct LogprobParams {
@@ -100,18 +101,19 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return d;
 }
 
+template <int T>
 struct Smem {
-    Key aside[ASIDE];
-    Key group[MAX_GROUPS];
-    float high[MAX_GROUPS];
+    Key aside[Shape<T>::ASIDE];
+    Key group[Shape<T>::GROUPS];
+    float high[Shape<T>::GROUPS];
     Key list[MAX_CLUSTER * LP_MAX_TOP];   // of every CTA of the cluster, in order; 0: none
     Key tau;
     float bound;
-    int places[PLACES];       // chunk * T + thread
+    float2 places[Shape<T>::PLACES];    // largest logit of the 16, and (as bits) chunk * T + thread
     int noted;
     int count;                // keys put aside
     int sum;
-    Sums warp[8], cta[MAX_CLUSTER];
+    Sums warp[Shape<T>::WARPS], cta[MAX_CLUSTER];
 };
 
 template <bool H16>
@@ -131,7 +133,7 @@ struct Chunk {   // 16 logits of a thread, in vectors of 16 bytes
 
 // The k-th largest of the groups' largest logits.  All threads; two barriers.
 template <int T>
-__device__ __forceinline__ float kth_of_groups(Smem &sm, float high, int k) {
+__device__ __forceinline__ float kth_of_groups(Smem<T> &sm, float high, int k) {
     static_assert(GROUP == 4, "the threads of a group rank its logit");
 #pragma unroll
     for (int off = 1; off < GROUP; off <<= 1) high = fmaxf(high, __shfl_xor_sync(0xFFFFFFFFu, high, off));
@@ -168,7 +170,7 @@ __device__ __forceinline__ void ranked(const Key *keys, int n, int k, F f) {
 
 // The same of the groups' largest keys; 0 when there are fewer than k.
 template <int T>
-__device__ __forceinline__ Key kth_of_groups(Smem &sm, Key best, int k) {
+__device__ __forceinline__ Key kth_of_groups(Smem<T> &sm, Key best, int k) {
 #pragma unroll
     for (int off = 1; off < GROUP; off <<= 1) {
         const Key o = __shfl_xor_sync(0xFFFFFFFFu, best, off);
@@ -190,8 +192,8 @@ __device__ __forceinline__ Key kth_of_groups(Smem &sm, Key best, int k) {
 
 // Cuts the n keys put aside down to the k largest and returns the smallest of these, found bit by bit.  All threads.
 template <int T>
-__device__ __noinline__ Key cut(Smem &sm, int n, int k) {
-    constexpr int MOST = (ASIDE + T - 1) / T;
+__device__ __noinline__ Key cut(Smem<T> &sm, int n, int k) {
+    constexpr int MOST = (Shape<T>::ASIDE + T - 1) / T;
     Key mine[MOST];
 #pragma unroll
     for (int i = 0; i < MOST; ++i) {
@@ -302,7 +304,7 @@ struct Span {
 // long as many threads exceed it, after which a chunk adds at most (k - 1) * GROUP * PER_THREAD + 1 keys; where these might not
 // fit, the keys put aside are cut down to k first.
 template <bool H16, int T>
-__device__ __noinline__ void exact_top(Smem &sm, const Span<H16, T> &span, int k) {
+__device__ __noinline__ void exact_top(Smem<T> &sm, const Span<H16, T> &span, int k) {
     __syncthreads();
     if (threadIdx.x == 0) sm.count = 0;
     Key tau = 0;
@@ -324,7 +326,7 @@ __device__ __noinline__ void exact_top(Smem &sm, const Span<H16, T> &span, int k
             tau = bound > tau ? bound : tau;
         }
         const int n = sm.count;
-        if (n + CHUNK_ADDS > ASIDE) {
+        if (n + Shape<T>::CHUNK_ADDS > Shape<T>::ASIDE) {
             const Key bound = cut<T>(sm, n, k);
             tau = bound > tau ? bound : tau;
         } else {
@@ -346,7 +348,7 @@ template <bool H16, bool TOP, int T>
 __global__ void __launch_bounds__(T, Shape<T>::CTAS) logprobs_kernel(const LogprobParams p, int cluster) {
     using C = Chunk<H16>;
     extern __shared__ __align__(16) uint8_t smem_raw[];
-    Smem &sm = *reinterpret_cast<Smem *>(smem_raw);
+    Smem<T> &sm = *reinterpret_cast<Smem<T> *>(smem_raw);
     const int rank = blockIdx.x % cluster, tid = threadIdx.x;
     if (cluster > 1) {
         // the CTAs of a cluster write into the first one's shared memory at the end: by then it has to run, and to be ready
@@ -405,7 +407,7 @@ __global__ void __launch_bounds__(T, Shape<T>::CTAS) logprobs_kernel(const Logpr
                 }
                 if (high >= bound) {
                     const int at = atomicAdd(&sm.noted, 1);
-                    if (at < PLACES) sm.places[at] = chunk * T + tid;
+                    if (at < Shape<T>::PLACES) sm.places[at] = make_float2(high, __int_as_float(chunk * T + tid));
                 }
             }
             cur = next;
@@ -417,16 +419,19 @@ __global__ void __launch_bounds__(T, Shape<T>::CTAS) logprobs_kernel(const Logpr
             if (look > 2) bound = kth_of_groups<T>(sm, run.m, p.top);
             else __syncthreads();
             const int noted = sm.noted;
-            all_found = noted <= PLACES && bound > -INFINITY;   // (NaN should have reached a bound of -inf too)
+            all_found = noted <= Shape<T>::PLACES && bound > -INFINITY;   // (NaN should have reached a bound of -inf too)
             if (all_found) {
-                for (int i = tid; i < noted * C::VECS; i += T) {
-                    const int place = sm.places[i / C::VECS];
-                    span.each(place / T, place % T, i % C::VECS, [&](float x, int at) {
-                        if (x >= bound) {
-                            const int n = atomicAdd(&sm.count, 1);
-                            if (n < ASIDE) sm.aside[n] = order_key(x, at);
-                        }
-                    });
+                for (int i = tid; i < noted; i += T) {
+                    if (!(sm.places[i].x >= bound)) continue;
+                    const int place = __float_as_int(sm.places[i].y);
+#pragma unroll
+                    for (int v = 0; v < C::VECS; ++v)
+                        span.each(place / T, place % T, v, [&](float x, int at) {
+                            if (x >= bound) {
+                                const int n = atomicAdd(&sm.count, 1);
+                                if (n < Shape<T>::ASIDE) sm.aside[n] = order_key(x, at);
+                            }
+                        });
                 }
             }
         }
@@ -453,7 +458,7 @@ __global__ void __launch_bounds__(T, Shape<T>::CTAS) logprobs_kernel(const Logpr
         int n = 0;
         if (TOP) {
             n = sm.count;
-            if (!all_found || n > ASIDE) {
+            if (!all_found || n > Shape<T>::ASIDE) {
                 exact_top<H16, T>(sm, span, p.top);
                 n = sm.count;
             }
@@ -520,7 +525,7 @@ int cluster_of(int rows, int vocab) {
 template <bool H16, bool TOP, int T>
 int launch(const LogprobParams &p, int cluster, cudaStream_t st) {
     static DeviceOnce configured;
-    constexpr int SMEM = sizeof(Smem);
+    constexpr int SMEM = sizeof(Smem<T>);
     if (!configured.done()) {
         int rc = cuda_check(cudaFuncSetAttribute(logprobs_kernel<H16, TOP, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM),
                             "token logprobs: shared memory opt-in");
@@ -549,7 +554,7 @@ template <bool H16, bool TOP>
 int launch_rows(const LogprobParams &p, cudaStream_t st) {
     const int cluster = cluster_of(p.rows, p.vocab), sms = sm_count() > 0 ? sm_count() : 148;
     // many rows and few alternatives: see Shape
-    return p.rows >= 8 * sms && p.top <= 8 ? launch<H16, TOP, 128>(p, cluster, st) : launch<H16, TOP, 256>(p, cluster, st);
+    return p.rows >= 8 * sms && p.top <= Shape<128>::TOP ? launch<H16, TOP, 128>(p, cluster, st) : launch<H16, TOP, 256>(p, cluster, st);
 }
 
 }  // namespace

@@ -34,16 +34,16 @@ constexpr float LN2 = 0.69314718055994531f;
 typedef unsigned long long Key;
 
 // Threads of a CTA and CTAs of an SM.  Smaller CTAs keep more rows going side by side, one's end beside another's middle, but
-// take their bounds from fewer groups and longer over a single row (2048 x 50257, k = 5: fp32 72 us with 128 threads against 76
-// with 256, bf16 57 against 67; k = 20, fp32: 92 against 87; 592 rows, fp32, k = 5: 25 against 23).
+// take longer over a single row, and their bounds from fewer groups (2048 x 50257 with 128 threads against 256, fp32: k = 5 72.5
+// against 76 us, k = 20 80 against 84; bf16: 57 against 67, 63 against 70; 592 rows, fp32, k = 5: 29 against 26).
 template <int T>
 struct Shape {
     static constexpr int WARPS = T / 32, CTAS = 1024 / T, GROUPS = T / GROUP;
-    static constexpr int TOP = T == 128 ? 8 : LP_MAX_TOP;                       // alternatives at most
+    static constexpr int TOP = T == 128 ? 20 : LP_MAX_TOP;                       // alternatives at most
     static constexpr int CHUNK_ADDS = (TOP - 1) * GROUP * PER_THREAD + 1;       // see exact_top
     // room for keys put aside and for places noted.  (Shared memory is taken from L1, which the loads on their way go through:
     // 27 KB for each of 8 CTAs made the sums alone of 2048 x 50257 take 87 us instead of 63.)
-    static constexpr int ASIDE = T == 128 ? 640 : 2048, PLACES = T == 128 ? 512 : 896;
+    static constexpr int ASIDE = T == 128 ? 1280 : 2048, PLACES = T == 128 ? 512 : 896;
     static_assert(GROUPS >= TOP, "the bound is the k-th of the groups");
     static_assert(ASIDE > CHUNK_ADDS + TOP, "after a cut a chunk has to fit");
 };
@@ -553,7 +553,7 @@ int launch(const LogprobParams &p, int cluster, cudaStream_t st) {
 template <bool H16, bool TOP>
 int launch_rows(const LogprobParams &p, cudaStream_t st) {
     const int cluster = cluster_of(p.rows, p.vocab), sms = sm_count() > 0 ? sm_count() : 148;
-    // many rows and few alternatives: see Shape
+    // many rows: see Shape
     return p.rows >= 8 * sms && p.top <= Shape<128>::TOP ? launch<H16, TOP, 128>(p, cluster, st) : launch<H16, TOP, 256>(p, cluster, st);
 }
 

@@ -18,6 +18,11 @@
 // which would be as large as that of the output, does not count.  Maximum and sum are kept in fp32, and the maximum in use
 // is only raised when a score exceeds it by more than 8 in the exponent of 2 (numerator and denominator carry the same
 // factor), so most blocks need one vote of the warp where a running maximum would take shuffles and a rescaling.
+//
+// Measured: one sequence of 131072 keys, 32 query heads on 8 of 128: 88 us = 6.1 TB/s; 64 sequences of 8192: 318 us = 6.75 TB/s.
+// On the way there (the one sequence): a CTA per row and head 3955 us; the keys shared out 133; blocks copied ahead by the lanes
+// into shared memory 120, whatever the number of instructions (541, then 350 a block) and of stages: 16-byte copies of 64-byte
+// pieces; by the copy engine 90.  Below that, 5 us pass before the first key is there and 3 in the joining kernel.
 #include <math.h>
 #include <string.h>
 

@@ -39,6 +39,10 @@ constexpr int STAGES = 2;                // steps of a warp in shared memory: on
 // What beginning and finishing a unit costs, in tiles: without it a CTA whose share is a run of short sequences took 17 us
 // longer than the others (64 ragged sequences).
 constexpr int BEGIN = 1;
+// Units of up to so many tiles are not split where there is a CTA for each: working off the tiles one after the other then takes
+// no longer than joining parts (24 sequences of 500 keys, 16 heads of 64: 11.4 against 16.4 us; one sequence: 8.3 against 8.1;
+// with 8 tiles, one sequence of 1000 keys: 12.4 against 8.3).
+constexpr int WHOLE_TILES = 4;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.69314718055994531f;
 // A weight is 2^(score - m) with m so chosen that the largest of a block is 2^HEADROOM when m is set, and m is raised when a
@@ -77,6 +81,7 @@ struct PagedAttnParams {
     uint8_t *workspace;
     Divisor by_page;
     int box;   // keys of a copy: 16 or 8
+    bool whole;   // CTA i works on unit i, all of it: known from the size of the page table
 };
 
 __device__ __forceinline__ void mma_keys(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -262,7 +267,7 @@ __device__ __forceinline__ bool row_keys(const PagedAttnParams &p, int r, RowKey
 
 // The work of a call is a line: rows in order, of each row its (key/value head, head tile) units in order, of each unit `begin`
 // places for its beginning and end and then one for every key tile (begin: BEGIN, or 0 where there are no more tiles than
-// CTAs).  CTA i of G takes the places [total i / G, total (i + 1) / G), the same number for every CTA whatever the lengths, and
+// CTAs; a unit is one place where none is to be split).  CTA i of G takes the places [total i / G, total (i + 1) / G), the same number for every CTA whatever the lengths, and
 // works on the tiles among them; G is at most total / (begin + 1), so that there are some.  A unit that lies in one CTA is finished there; of one that does not, every CTA leaves its part in the
 // workspace (slot 1 where the unit begins, slot 0 elsewhere: a CTA has at most one of each) and the CTA with the
 // beginning notes who has the rest, for the joining kernel.
@@ -310,6 +315,7 @@ struct Smem {
     float m[PA_WARPS][8 * NT], l[PA_WARPS][8 * NT];
     uint64_t full[PA_WARPS][STAGES];
     long long sum[PA_WARPS], before;
+    int most[PA_WARPS];
     RowKeys keys;
     int row;
     uint32_t gave_up;
@@ -343,73 +349,101 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     Part *parts = reinterpret_cast<Part *>(p.workspace);
     float *slots = reinterpret_cast<float *>(p.workspace + sizeof(Part) * gridDim.x);
-    if (threadIdx.x == 0) parts[blockIdx.x].row = -1;
-
-    // where this CTA's share begins: every thread adds up the tiles of a run of rows
-    const int per = (p.rows + PA_WARPS * 32 - 1) / (PA_WARPS * 32);
-    const int row_lo = min(p.rows, (int)threadIdx.x * per), row_hi = min(p.rows, row_lo + per);
-    constexpr int ROWS_AT = 40;   // a sum of tiles, and above it of rows that have some
-    long long mine = 0;
-    bool bad = false;
-    for (int r = row_lo; r < row_hi; ++r) {
-        RowKeys k;
-        row_keys<TILE>(p, r, k, bad);
-        if (k.tiles > 0) mine += (1LL << ROWS_AT) + k.tiles;
-    }
-    long long upto = mine;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, off);
-        if (lane >= off) upto += v;
-    }
-    if (lane == 31) sm.sum[warp] = upto;
-    __syncthreads();
-    long long total = 0;
-#pragma unroll
-    for (int w = 0; w < PA_WARPS; ++w) {
-        if (w < warp) upto += sm.sum[w];
-        total += sm.sum[w];
-    }
-    const int begin = (total & ((1LL << ROWS_AT) - 1)) * units <= gridDim.x ? 0 : BEGIN;
-    auto places = [&](long long sum) { return ((sum & ((1LL << ROWS_AT) - 1)) + (sum >> ROWS_AT) * begin) * units; };
-    const long long all = places(total);
-    const long long n_cta = min((long long)gridDim.x, all / (begin + 1));
-    const long long c0 = blockIdx.x < n_cta ? all * blockIdx.x / n_cta : all;
-    const long long c1 = blockIdx.x < n_cta ? all * (blockIdx.x + 1) / n_cta : all;
-    {
-        long long before = places(upto - mine);
-        if (c0 < c1 && c0 >= before && c0 < places(upto)) {
-            for (int r = row_lo; r < row_hi; ++r) {
-                RowKeys k;
-                row_keys<TILE>(p, r, k, bad);
-                const long long here = k.tiles > 0 ? (long long)(k.tiles + begin) * units : 0;
-                if (c0 < before + here) {
-                    sm.row = r;
-                    sm.keys = k;
-                    sm.before = before;
-                    break;
-                }
-                before += here;
-            }
-        }
-    }
-    if (bad && blockIdx.x == 0 && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
-    pdl_trigger();
-    if (c0 >= c1) return;
-    __syncthreads();
 
     // `at`: the tile being worked on; `ahead`: the tile whose copy is issued next, up to STAGES - 1 further on
     Place at;
-    at.r = sm.row;
-    at.k = sm.keys;
-    if (at.r < 0) return;   // (no such row, here and below: the lengths changed under the kernel)
-    long long row_c0 = sm.before;          // first place of row at.r
-    at.unit = static_cast<int>((c0 - row_c0) / (at.k.tiles + begin));
-    const int skipped = static_cast<int>((c0 - row_c0) % (at.k.tiles + begin));
-    at.tile = max(0, skipped - begin);
-    Place ahead = at;
+    bool bad = false;
+    int begin = 0;
+    long long all = 0, n_cta = 0, row_c0 = 0;   // places, CTAs that share them, first place of row at.r
     // places left to the copies and to the work: they go on by one place a tile, and by `begin` where a unit begins
-    long long to_issue = c1 - c0 - max(0, begin - skipped), left = to_issue;
+    long long to_issue;
+    if (p.whole) {
+        at.r = blockIdx.x / units;
+        at.unit = blockIdx.x % units;
+        at.tile = 0;
+        row_keys<TILE>(p, at.r, at.k, bad);
+        if (bad && at.unit == 0 && threadIdx.x == 0 && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
+        to_issue = at.k.tiles;
+        pdl_trigger();
+        if (to_issue == 0) return;
+        __syncthreads();
+    } else {
+        if (threadIdx.x == 0) parts[blockIdx.x].row = -1;
+        // where this CTA's share begins: every thread adds up the tiles of a run of rows
+        const int per = (p.rows + PA_WARPS * 32 - 1) / (PA_WARPS * 32);
+        const int row_lo = min(p.rows, (int)threadIdx.x * per), row_hi = min(p.rows, row_lo + per);
+        constexpr int ROWS_AT = 40;   // a sum of tiles, and above it of rows that have some
+        long long mine = 0;
+        int most = 0;
+        for (int r = row_lo; r < row_hi; ++r) {
+            RowKeys k;
+            row_keys<TILE>(p, r, k, bad);
+            if (k.tiles > 0) mine += (1LL << ROWS_AT) + k.tiles;
+            most = max(most, k.tiles);
+        }
+        most = __reduce_max_sync(0xFFFFFFFFu, most);
+        long long upto = mine;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, off);
+            if (lane >= off) upto += v;
+        }
+        if (lane == 31) {
+            sm.sum[warp] = upto;
+            sm.most[warp] = most;
+        }
+        __syncthreads();
+        long long total = 0;
+#pragma unroll
+        for (int w = 0; w < PA_WARPS; ++w) {
+            if (w < warp) upto += sm.sum[w];
+            total += sm.sum[w];
+            most = max(most, sm.most[w]);
+        }
+        // a unit is one place: units of few tiles, and more of them than half the CTAs
+        const long long n_units = (total >> ROWS_AT) * units;
+        const bool whole = most <= WHOLE_TILES && n_units <= gridDim.x && 2 * n_units >= gridDim.x;
+        begin = (total & ((1LL << ROWS_AT) - 1)) * units <= gridDim.x ? 0 : BEGIN;
+        auto places = [&](long long sum) {
+            const long long rows = sum >> ROWS_AT, tiles = sum & ((1LL << ROWS_AT) - 1);
+            return (whole ? rows : tiles + rows * begin) * units;
+        };
+        all = places(total);
+        n_cta = whole ? all : min((long long)gridDim.x, all / (begin + 1));
+        const long long c0 = blockIdx.x < n_cta ? all * blockIdx.x / n_cta : all;
+        const long long c1 = blockIdx.x < n_cta ? all * (blockIdx.x + 1) / n_cta : all;
+        {
+            long long before = places(upto - mine);
+            if (c0 < c1 && c0 >= before && c0 < places(upto)) {
+                for (int r = row_lo; r < row_hi; ++r) {
+                    RowKeys k;
+                    row_keys<TILE>(p, r, k, bad);
+                    const long long here = k.tiles > 0 ? (whole ? 1LL : k.tiles + begin) * units : 0;
+                    if (c0 < before + here) {
+                        sm.row = r;
+                        sm.keys = k;
+                        sm.before = before;
+                        break;
+                    }
+                    before += here;
+                }
+            }
+        }
+        if (bad && blockIdx.x == 0 && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
+        pdl_trigger();
+        if (c0 >= c1) return;
+        __syncthreads();
+        at.r = sm.row;
+        at.k = sm.keys;
+        if (at.r < 0) return;   // (no such row, here and below: the lengths changed under the kernel)
+        row_c0 = sm.before;
+        const int weight = whole ? 1 : at.k.tiles + begin, skipped = static_cast<int>((c0 - row_c0) % weight);
+        at.unit = static_cast<int>((c0 - row_c0) / weight);
+        at.tile = max(0, skipped - begin);
+        to_issue = whole ? at.k.tiles : c1 - c0 - max(0, begin - skipped);
+    }
+    Place ahead = at;
+    long long left = to_issue;
     bool bad_page = false;
     auto step_row = [&](Place &w) {   // to the next row with tiles; false when there is none
         do {
@@ -808,11 +842,13 @@ int launch_nt(const PagedAttnParams &p, const CUtensorMap &tm_k, const CUtensorM
     const long long seen = p.window > 0 && p.window < keys ? p.window : keys;
     // (a window that begins inside a 16-key block touches up to 15 keys more)
     const long long tiles = std::min((keys + Step<HD>::TILE - 1) / Step<HD>::TILE, (seen + 15 + Step<HD>::TILE - 1) / Step<HD>::TILE);
-    const long long grid = std::min<long long>((long long)sms * n, units * tiles);
-    int rc = cuda_check(launch_pdl(paged_attn_kernel<HD, NT, BOXES>, dim3((unsigned)grid), dim3(PA_WARPS * 32), SMEM, st, tm_k, tm_v, p),
+    PagedAttnParams q = p;
+    // nothing is split, and nothing joined, where the host knows that already (the kernel above sees to it where only the lengths say so)
+    q.whole = tiles <= WHOLE_TILES && units <= (long long)sms * n;
+    const long long grid = q.whole ? units : std::min<long long>((long long)sms * n, units * tiles);
+    int rc = cuda_check(launch_pdl(paged_attn_kernel<HD, NT, BOXES>, dim3((unsigned)grid), dim3(PA_WARPS * 32), SMEM, st, tm_k, tm_v, q),
                         "paged attention: launch");
-    // with one tile a unit nothing is ever split
-    if (rc || tiles == 1) return rc;
+    if (rc || q.whole || tiles == 1) return rc;
     // fewer units than an eighth of the CTAs: over 8 parts each where the lengths are alike
     constexpr int PRODUCTS = NT * PartShape<HD, NT>::PRODUCTS;
     const bool few = units * JOIN_BATCH < grid;

@@ -11,6 +11,7 @@ Tolerances.  A result rounded to 16 bits may be off by half a step, eps / 2 of i
 """
 import ctypes as C
 import math
+import random
 
 import pytest
 import torch
@@ -292,6 +293,44 @@ def test_attention_far_pages_and_streams():
         assert bool(((out.double() - ref).abs() <= 2.0 ** -8 * ref.abs() * 1.001 + tol + 2.0 ** -25).all()), now
 
 
+@gpu
+def test_calls_on_two_streams_at_once():
+    """Calls that overlap on the device, each with its own workspace, eager and as two graphs replayed side by side."""
+    sets = []
+    for i, lens in enumerate(([3000, 20, 700], [90, 2500])):
+        pages = Pages(16 + i, lens, 2, 128, 16, "bf16")
+        q = normal(17 + i, len(lens), 8, 128).to(torch.bfloat16)
+        n = torch.tensor(lens, dtype=torch.int32, device=DEV)
+        alone = kr.op_paged_decode_attention(q, pages.k, pages.v, pages.table, n)
+        logits = normal(18 + i, 40, 9000).float()
+        sets.append((pages, q, n, alone, logits, kr.op_token_logprobs(logits, top=9), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+
+    def run(pages, q, n, logits):
+        return kr.op_paged_decode_attention(q, pages.k, pages.v, pages.table, n), kr.op_token_logprobs(logits, top=9)
+
+    got, graphs = [[], []], []
+    for _ in range(20):
+        for i, (pages, q, n, _a, logits, _l, stream) in enumerate(sets):
+            with torch.cuda.stream(stream):
+                got[i].append(run(pages, q, n, logits))
+    torch.cuda.synchronize()
+    for i, (pages, q, n, _a, logits, _l, stream) in enumerate(sets):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            got[i].append(run(pages, q, n, logits))
+        graphs.append(graph)
+    for _ in range(20):
+        for graph, s in zip(graphs, sets):
+            with torch.cuda.stream(s[6]):
+                graph.replay()
+    torch.cuda.synchronize()
+    for i, (_p, _q, _n, alone, _x, read, _s) in enumerate(sets):
+        for (out, lse), lp in got[i]:
+            assert torch.equal(out, alone[0]) and torch.equal(lse, alone[1])
+            assert all(a is b is None or torch.equal(a, b) for a, b in zip(lp, read))
+
+
 # ---------------------------------------------------------------------------------------------------- append
 
 def turn_ref(x, pos, freq, interleaved):
@@ -542,6 +581,61 @@ def test_logprobs_targets_and_rows():
     same = kr.op_token_logprobs(x[:1].expand(5, 500), top=3)          # rows that lie on one another
     assert bool((same.lse == same.lse[0]).all()) and bool((same.top_ids == same.top_ids[0]).all())
     assert kr.op_token_logprobs(x[:0], top=2).top_ids.shape == (0, 2)
+
+
+# ---------------------------------------------------------------------------------------------------- calls nobody wrote down
+
+@gpu
+@pytest.mark.parametrize("seed", range(24))
+def test_random_attention(seed):
+    """Seeded random head layouts, page sizes, lengths, masks and row lists; a call made twice gives the same bits."""
+    rng = random.Random(seed)
+    hd, Hkv, rep = rng.choice((64, 72, 96, 104, 128)), rng.choice((1, 2, 3, 5, 8)), rng.choice((1, 2, 3, 7, 8, 9, 16, 17, 24, 40))
+    page, dtype = rng.choice((1, 2, 3, 7, 8, 16, 24, 40, 64, 100, 128, 512)), rng.choice(("bf16", "f16"))
+    B, longest = rng.choice((1, 2, 5, 17, 60)), rng.choice((1, 16, 65, 130, 700, 3000))
+    lens = [rng.randint(0, longest) for _ in range(B)]
+    pages = Pages(seed, lens, Hkv, hd, page, dtype, by_slot=rng.random() < 0.5, width=max(1, -(-max(lens) // page)) + rng.choice((0, 0, 5, 400)))
+    R = rng.choice((B, B, 2 * B + 1))
+    seq = torch.tensor([rng.randrange(B) if rng.random() < 0.9 else -1 for _ in range(R)], dtype=torch.int32, device=DEV)
+    n = torch.tensor([rng.randint(0, lens[s]) if s >= 0 else -5 for s in seq.tolist()], dtype=torch.int32, device=DEV)
+    q = (normal(seed, R, Hkv * rep, hd) * rng.choice((0.1, 1, 4))).to(T16[dtype])
+    slopes = (torch.rand(Hkv * rep, generator=torch.Generator().manual_seed(seed)) * 0.2).to(DEV) if rng.random() < 0.3 else None
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    form = dict(score_cap=rng.choice((0.0, 0.0, 5.0)), window=rng.choice((0, 0, 1, 15, 16, 17, 100)), slopes=slopes, scale=rng.choice((None, 0.3)))
+    out, lse = torch.full_like(q, 3.0), torch.full((R, Hkv * rep), 3.0, device=DEV)
+    check_attention(pages, q, n, row_seq=seq, status=status, out=out, lse=lse, cap=form["score_cap"], window=form["window"], slopes=slopes,
+                    scale=form["scale"])
+    assert int(status.item()) == 0 and bool((out[seq < 0] == 3).all()) and bool((lse[seq < 0] == 3).all())
+    again, lse2 = kr.op_paged_decode_attention(q, pages.k, pages.v, pages.table, n, row_seq=seq, **form)
+    assert torch.equal(again[seq >= 0], out[seq >= 0]) and torch.equal(lse2[seq >= 0], lse[seq >= 0])
+
+
+@gpu
+@pytest.mark.parametrize("seed", range(12))
+def test_random_append(seed):
+    rng = random.Random(seed)
+    hd, Hkv = rng.choice((64, 72, 96, 104, 128)), rng.choice((1, 2, 3, 8, 17))
+    H, page, dtype = Hkv * rng.choice((1, 2, 5)), rng.choice((1, 5, 8, 16, 24, 100, 256)), rng.choice(("bf16", "f16"))
+    rot = rng.choice([r for r in (0, 8, 16, 24, 40, 64, 72, 104, 120, hd) if r <= hd])
+    B = rng.choice((1, 3, 40))
+    spans = [(s, rng.randint(0, 300), rng.choice((1, 1, 7, 90))) for s in range(B)]
+    if seed % 3 == 0:
+        spans[0] = (0, 11, 900)              # many rows
+    test_append(spans, H, Hkv, hd, rot, rng.random() < 0.5, page, dtype, rng.random() < 0.5)
+
+
+@gpu
+@pytest.mark.parametrize("seed", range(24))
+def test_random_logprobs(seed):
+    rng, g = random.Random(seed), torch.Generator().manual_seed(seed)
+    V = rng.choice((1, 5, 33, 100, 1000, 4095, 4096, 4097, 8200, 16385, 50257))
+    rows = min(rng.choice((1, 1, 2, 5, 30, 149, 297, 700, 1300)), max(1, 4000000 // V))
+    dtype, top, pad = rng.choice((torch.float32, torch.bfloat16, torch.float16)), min(V, rng.choice((0, 1, 3, 8, 9, 20, 32))), rng.choice((0, 1, 3, 8))
+    x = torch.randn(rows, V + pad, generator=g) * rng.choice((0.0, 0.1, 3, 20))
+    if rng.random() < 0.5:
+        x[torch.rand(x.shape, generator=g) < rng.choice((0.01, 0.5, 0.99))] = -math.inf
+    x[:, pad] = rng.choice((0.0, 1.0, 50.0))
+    check_logprobs(x.to(dtype).to(DEV)[:, pad:], torch.randint(-1, V, (rows,), generator=g, dtype=torch.int32).to(DEV), top, scale=rng.choice((1.0, 0.3, 2.0)))
 
 
 # ---------------------------------------------------------------------------------------------------- together

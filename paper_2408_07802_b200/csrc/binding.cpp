@@ -124,6 +124,15 @@ Rows rows_of(const Tensor &t, int64_t rows, int64_t heads, const Tensor &like, c
     return {t.data_ptr(), t.stride(0), t.stride(1)};
 }
 
+// A contiguous tensor in `bytes`, from byte `at` on.  An output of its own costs 0.6 us, a part of a common one 0.1.
+Tensor part(const Tensor &bytes, int64_t at, at::ScalarType type, at::IntArrayRef sizes) {
+    Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(bytes.storage()), bytes.key_set(), c10::scalarTypeToTypeMeta(type));
+    c10::TensorImpl *impl = t.unsafeGetTensorImpl();
+    impl->set_storage_offset(at / static_cast<int64_t>(c10::elementSize(type)));
+    impl->set_sizes_contiguous(sizes);
+    return t;
+}
+
 PyObject *give(int code, std::initializer_list<Tensor> out) {
     PyObject *r = PyTuple_New(static_cast<Py_ssize_t>(out.size()) + 1);
     if (!r) throw python_error();
@@ -226,12 +235,20 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
         g.n_head = to_int32(heads, "the number of heads");
         uint32_t *status = status_word(a[13], device);
         c10::cuda::CUDAGuard guard(device);
-        const Tensor out = a[10] == Py_None ? at::empty({rows, heads, q.size(2)}, q.options()) : tensor(a[10], "out");
+        // out and lse where the caller brings neither: parts of one tensor
+        const int64_t out_bytes = rows * heads * q.size(2) * 2;
+        Tensor both;
+        if (a[10] == Py_None && a[11] == Py_None) both = at::empty({out_bytes + rows * heads * 4}, q.options().dtype(at::kByte));
+        const Tensor out = a[10] != Py_None ? tensor(a[10], "out")
+                           : both.defined() ? part(both, 0, q.scalar_type(), {rows, heads, q.size(2)})
+                                            : at::empty({rows, heads, q.size(2)}, q.options());
         const Rows outr = rows_of(out, rows, heads, kc, "out");
         g.out = outr.p;
         g.out_row_stride = outr.row;
         g.out_head_stride = outr.head;
-        const Tensor lse = a[11] == Py_None ? at::empty({rows, heads}, q.options().dtype(at::kFloat)) : tensor(a[11], "lse");
+        const Tensor lse = a[11] != Py_None ? tensor(a[11], "lse")
+                           : both.defined() ? part(both, out_bytes, at::kFloat, {rows, heads})
+                                            : at::empty({rows, heads}, q.options().dtype(at::kFloat));
         need(lse.device() == device && lse.scalar_type() == at::kFloat && lse.dim() == 2 && lse.size(0) == rows && lse.size(1) == heads &&
                  (lse.stride(1) == 1 || heads <= 1), "lse must be float32 [rows, heads] on the caches' device, contiguous in the last dimension");
         g.lse = static_cast<float *>(lse.data_ptr());
@@ -275,18 +292,20 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const Image &im = images[g.dtype ? x.scalar_type() == at::kHalf : int_arg(a[5], "image") != 0];
         if (!im.logprobs) return give(NOT_BOUND, {Tensor(), Tensor(), Tensor(), Tensor(), Tensor()});
         c10::cuda::CUDAGuard guard(device);
-        const auto f32 = x.options().dtype(at::kFloat);
+        // 4 rows bytes each: entropy, lse, and logprob where asked for; then the alternatives
+        const int64_t row = 4 * rows, numbers = g.targets ? 3 : 2, list = row * g.top;
+        const Tensor bytes = at::empty({row * numbers + 2 * list}, x.options().dtype(at::kByte));
+        const Tensor entropy = part(bytes, 0, at::kFloat, {rows}), lse = part(bytes, row, at::kFloat, {rows});
         Tensor logprob, ids, best;
-        const Tensor entropy = at::empty({rows}, f32), lse = at::empty({rows}, f32);
         if (g.targets) {
-            logprob = at::empty({rows}, f32);
+            logprob = part(bytes, 2 * row, at::kFloat, {rows});
             g.logprob = static_cast<float *>(logprob.data_ptr());
         }
         if (g.top > 0) {
-            ids = at::empty({rows, g.top}, x.options().dtype(at::kInt));
-            best = at::empty({rows, g.top}, f32);
-            g.top_ids = static_cast<int32_t *>(ids.data_ptr());
+            best = part(bytes, numbers * row, at::kFloat, {rows, g.top});
+            ids = part(bytes, numbers * row + list, at::kInt, {rows, g.top});
             g.top_logprobs = static_cast<float *>(best.data_ptr());
+            g.top_ids = static_cast<int32_t *>(ids.data_ptr());
         }
         g.entropy = static_cast<float *>(entropy.data_ptr());
         g.lse = static_cast<float *>(lse.data_ptr());

@@ -155,6 +155,17 @@ __device__ __forceinline__ float kth_of_groups(Smem<T> &sm, float high, int k) {
     return sm.bound;
 }
 
+// The same with every thread a group of its own, for parts too short to fill k groups (or forbidden but for a few logits), found
+// bit by bit: the largest value that the logits of k threads reach.  All threads; 32 barriers, half as long as counting.
+template <int T>
+__device__ __noinline__ float kth_of_threads(float high, int k) {
+    const uint32_t mine = static_cast<uint32_t>(order_key(high, 0) >> 32);
+    uint32_t reached = 0;
+    for (uint32_t bit = 0x80000000u; bit != 0; bit >>= 1)
+        if (__syncthreads_count(mine >= (reached | bit)) >= k) reached |= bit;
+    return key_value(static_cast<Key>(reached) << 32);
+}
+
 // f(rank, key) for those of n keys whose rank is below k, four threads a key.  All threads.
 template <int T, typename F>
 __device__ __forceinline__ void ranked(const Key *keys, int n, int k, F f) {
@@ -283,6 +294,11 @@ struct Span {
             }
         }
     }
+    __device__ __forceinline__ int first() const { return max(0, lo * VEC - before); }    // logits first .. first + count - 1
+    __device__ __forceinline__ int count() const { return max(0, min(vocab, hi * VEC - before) - first()); }
+    __device__ __forceinline__ float value(int at) const {
+        return H16 ? from_h16(reinterpret_cast<const uint16_t *>(row)[at]) : reinterpret_cast<const float *>(row)[at];
+    }
     // f(logit, index) for the logits of vector i of a thread's chunk
     template <typename F>
     __device__ __forceinline__ void each(int chunk, int thread, int i, F f) const {
@@ -296,7 +312,7 @@ struct Span {
             for (int e = 0; e < VEC; ++e) {
                 const int at = v * VEC - before + e;
                 if (at < 0 || at >= vocab) continue;
-                f(H16 ? from_h16(reinterpret_cast<const uint16_t *>(row)[at]) : reinterpret_cast<const float *>(row)[at], at);
+                f(value(at), at);
             }
         }
     }
@@ -404,7 +420,8 @@ __global__ void __launch_bounds__(T, Shape<T>::CTAS) logprobs_kernel(const Logpr
             run.d += d0 + d1;
             if (TOP) {
                 if (chunk == look) {
-                    bound = kth_of_groups<T>(sm, run.m, p.top);
+                    bound = fmaxf(bound, kth_of_groups<T>(sm, run.m, p.top));
+                    if (bound == -INFINITY) bound = kth_of_threads<T>(run.m, p.top);
                     look = 3 * look + 2;
                 }
                 if (high >= bound) {
@@ -418,7 +435,7 @@ __global__ void __launch_bounds__(T, Shape<T>::CTAS) logprobs_kernel(const Logpr
         // the logits that reach the bound of the whole part
         bool all_found = false;
         if (TOP) {
-            if (look > 2) bound = kth_of_groups<T>(sm, run.m, p.top);
+            if (look > 2) bound = fmaxf(bound, kth_of_groups<T>(sm, run.m, p.top));
             else __syncthreads();
             const int noted = sm.noted;
             all_found = noted <= Shape<T>::PLACES && bound > -INFINITY;   // (NaN should have reached a bound of -inf too)
@@ -460,11 +477,16 @@ __global__ void __launch_bounds__(T, Shape<T>::CTAS) logprobs_kernel(const Logpr
         int n = 0;
         if (TOP) {
             n = sm.count;
-            if (!all_found || n > Shape<T>::ASIDE) {
+            if ((!all_found || n > Shape<T>::ASIDE) && span.count() <= T) {
+                // a part of a few logits: all of them
+                n = span.count();
+                if (tid < n) sm.aside[tid] = order_key(span.value(span.first() + tid), span.first() + tid);
+                __syncthreads();
+            } else if (!all_found || n > Shape<T>::ASIDE) {
                 exact_top<H16, T>(sm, span, p.top);
                 n = sm.count;
             }
-            if (n > T) {
+            if (n > 3 * T) {   // (ranking 768 keys takes half as long as cutting them down)
                 __syncthreads();
                 cut<T>(sm, n, p.top);
                 n = sm.count;

@@ -455,7 +455,9 @@ typedef struct kraken_paged_cache {
  * q (or NULL): the rows' queries, rotated into q_out, which may be q itself (same strides).  Otherwise none of q_out and
  * the cache may overlap another tensor of the call.  A row with row_seq[r] < 0 is padding, and one whose sequence, position or page does not
  * exist raises the status bit: neither changes the cache nor q_out.  The rows of one call must go to distinct
- * positions: of two rows with the same one, which of them the cache then holds is not defined, element by element.
+ * positions: of two rows with the same one, which of them the cache then holds is not defined, element by element.  Pages,
+ * heads and slots of the cache must not lie on one another here (EINVAL for a stride of 0; sequences may share pages that
+ * are only read).
  * Errors: EINVAL, EUNSUPPORTED (alignment, head_dim, rot_dim no multiple of 8 or above head_dim), ECUDA. */
 typedef struct kraken_paged_append_args {
     const void *k, *v;  int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;   /* [rows][n_kv_head] */
@@ -482,6 +484,9 @@ int kraken_op_paged_append(const kraken_paged_cache *cache, const kraken_paged_a
  * joined by a second kernel through `workspace` (kraken_paged_attention_workspace bytes, 16-byte aligned, contents of
  * no importance; calls that may overlap on the device each need their own).  The result depends on the device's
  * number of SMs and on all the lengths of the call in its last bits only, and is the same from run to run.
+ * n_keys, row_seq and the page table must not change while the call runs.  A bounded wait that gave up raises bit 1 of
+ * the status word; the outputs then mean nothing.  Rows or heads of out or lse must not lie on one another (EINVAL for a
+ * stride of 0), and none of them may overlap another tensor of the call.
  * Errors: EINVAL, EUNSUPPORTED, ECAPACITY (workspace_bytes too small), ECUDA. */
 typedef struct kraken_paged_attention_args {
     const void *q;  int64_t q_row_stride, q_head_stride;                                    /* [rows][n_head]    */

@@ -18,6 +18,7 @@
 // without barriers at 32 groups: 144 with k = 32; a ring of bulk copies filled by a warp of its own: 88 with k = 5.
 //
 // Few rows: up to 8 CTAs of a cluster share a row and join through each other's shared memory.
+#include <float.h>
 #include <math.h>
 
 #include "internal.h"
@@ -422,6 +423,7 @@ __global__ void __launch_bounds__(T, Shape<T>::CTAS) logprobs_kernel(const Logpr
                 if (chunk == look) {
                     bound = fmaxf(bound, kth_of_groups<T>(sm, run.m, p.top));
                     if (bound == -INFINITY) bound = kth_of_threads<T>(run.m, p.top);
+                    bound = fmaxf(bound, -FLT_MAX);   // no bound: every logit that is not forbidden
                     look = 3 * look + 2;
                 }
                 if (high >= bound) {
@@ -438,7 +440,7 @@ __global__ void __launch_bounds__(T, Shape<T>::CTAS) logprobs_kernel(const Logpr
             if (look > 2) bound = fmaxf(bound, kth_of_groups<T>(sm, run.m, p.top));
             else __syncthreads();
             const int noted = sm.noted;
-            all_found = noted <= Shape<T>::PLACES && bound > -INFINITY;   // (NaN should have reached a bound of -inf too)
+            all_found = noted <= Shape<T>::PLACES;
             if (all_found) {
                 for (int i = tid; i < noted; i += T) {
                     if (!(sm.places[i].x >= bound)) continue;
@@ -477,12 +479,14 @@ __global__ void __launch_bounds__(T, Shape<T>::CTAS) logprobs_kernel(const Logpr
         int n = 0;
         if (TOP) {
             n = sm.count;
-            if ((!all_found || n > Shape<T>::ASIDE) && span.count() <= T) {
+            // (fewer than asked for: forbidden ones and NaN are among them)
+            all_found = all_found && n <= Shape<T>::ASIDE && n >= min(p.top, span.count());
+            if (!all_found && span.count() <= T) {
                 // a part of a few logits: all of them
                 n = span.count();
                 if (tid < n) sm.aside[tid] = order_key(span.value(span.first() + tid), span.first() + tid);
                 __syncthreads();
-            } else if (!all_found || n > Shape<T>::ASIDE) {
+            } else if (!all_found) {
                 exact_top<H16, T>(sm, span, p.top);
                 n = sm.count;
             }

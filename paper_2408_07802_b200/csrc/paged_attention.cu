@@ -267,10 +267,11 @@ __device__ __forceinline__ bool row_keys(const PagedAttnParams &p, int r, RowKey
 
 // The work of a call is a line: rows in order, of each row its (key/value head, head tile) units in order, of each unit `begin`
 // places for its beginning and end and then one for every key tile (begin: BEGIN, or 0 where there are no more tiles than
-// CTAs; a unit is one place where none is to be split).  CTA i of G takes the places [total i / G, total (i + 1) / G), the same number for every CTA whatever the lengths, and
-// works on the tiles among them; G is at most total / (begin + 1), so that there are some.  A unit that lies in one CTA is finished there; of one that does not, every CTA leaves its part in the
-// workspace (slot 1 where the unit begins, slot 0 elsewhere: a CTA has at most one of each) and the CTA with the
-// beginning notes who has the rest, for the joining kernel.
+// CTAs; a unit is one place where none is to be split).  CTA i of G takes the places [total i / G, total (i + 1) / G), the same
+// number for every CTA whatever the lengths, and works on the tiles among them; G is at most total / (begin + 1), so that
+// there are some.  A unit that lies in one CTA is finished there; of one that does not, every CTA leaves its part in the
+// workspace (slot 1 where the unit begins, slot 0 elsewhere: a CTA has at most one of each) and the CTA with the beginning
+// notes who has the rest, for the joining kernel.
 struct Part {
     int row, unit, last_cta;   // row = -1: nothing to join
     int pad;

@@ -86,10 +86,19 @@ uint32_t *status_word(PyObject *o, const at::Device &device) {
     return static_cast<uint32_t *>(t.data_ptr());
 }
 
+// The stride of a dimension of one is of no meaning and may be anything: a multiple of 8 in its place
+int64_t stride_of(const Tensor &t, int64_t dim) { return t.size(dim) > 1 ? t.stride(dim) : t.size(-1) & ~int64_t(7); }
+
+bool same_strides(const Tensor &a, const Tensor &b) {
+    for (int64_t i = 0; i < a.dim(); ++i)
+        if (stride_of(a, i) != stride_of(b, i)) return false;
+    return true;
+}
+
 kraken_paged_cache paged_cache(const Tensor &k, const Tensor &v, const Tensor &table) {
     need(k.is_cuda() && is_16bit(k) && k.dim() == 4 && k.stride(3) == 1,
          "the caches must be 16-bit CUDA tensors [pages, key/value heads, page size, head_dim], contiguous in the last dimension");
-    need(v.device() == k.device() && v.scalar_type() == k.scalar_type() && v.sizes() == k.sizes() && v.strides() == k.strides(),
+    need(v.device() == k.device() && v.scalar_type() == k.scalar_type() && v.sizes() == k.sizes() && v.stride(3) == 1 && same_strides(k, v),
          "k_cache and v_cache must have the same shape, strides, type and device");
     need(table.device() == k.device() && table.scalar_type() == at::kInt && table.dim() == 2 && (table.stride(1) == 1 || table.size(1) <= 1),
          "page_table must be int32 [sequences, pages] on the caches' device, contiguous in the last dimension");
@@ -97,9 +106,9 @@ kraken_paged_cache paged_cache(const Tensor &k, const Tensor &v, const Tensor &t
     c.k = k.data_ptr();
     c.v = v.data_ptr();
     c.page_table = static_cast<const int32_t *>(table.data_ptr());
-    c.page_stride = k.stride(0);
-    c.head_stride = k.stride(1);
-    c.slot_stride = k.stride(2);
+    c.page_stride = stride_of(k, 0);
+    c.head_stride = stride_of(k, 1);
+    c.slot_stride = stride_of(k, 2);
     c.table_stride = table.size(0) > 1 ? table.stride(0) : table.size(1);
     c.n_pages = to_int32(k.size(0), "the number of pages");
     c.n_kv_head = to_int32(k.size(1), "the number of key/value heads");
@@ -121,7 +130,7 @@ Rows rows_of(const Tensor &t, int64_t rows, int64_t heads, const Tensor &like, c
         t.device() != like.device() || t.stride(2) != 1)
         throw Refused{std::string(name) + " must be [" + std::to_string(rows) + ", " + std::to_string(heads) + ", " +
                       std::to_string(like.size(3)) + "] of the caches' type and device, contiguous in the last dimension"};
-    return {t.data_ptr(), t.stride(0), t.stride(1)};
+    return {t.data_ptr(), stride_of(t, 0), stride_of(t, 1)};
 }
 
 // A contiguous tensor in `bytes`, from byte `at` on.  An output of its own costs 0.6 us, a part of a common one 0.1.

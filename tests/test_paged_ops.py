@@ -294,6 +294,23 @@ def test_attention_far_pages_and_streams():
 
 
 @gpu
+def test_strides_of_dimensions_of_one():
+    """A dimension of one may have any stride, an odd one too."""
+    pages = Pages(19, [100], 1, 64, 128, "bf16")                    # one page of 128 slots and two spare ones, one head
+    q = normal(20, 1, 4, 64).to(torch.bfloat16)
+    n = torch.tensor([100], dtype=torch.int32, device=DEV)
+    ref = kr.op_paged_decode_attention(q, pages.k, pages.v, pages.table, n)
+    odd = lambda t: t.as_strided(t.shape, [3 if t.shape[i] == 1 else s for i, s in enumerate(t.stride())])
+    got = kr.op_paged_decode_attention(odd(q), odd(pages.k), pages.v, odd(pages.table), n)
+    assert torch.equal(ref[0], got[0]) and torch.equal(ref[1], got[1])
+    one = pages.k[pages.table[0, 0].item():][:1].clone()
+    row = normal(21, 1, 1, 64).to(torch.bfloat16)
+    zero = torch.zeros(1, 1, dtype=torch.int32, device=DEV)
+    kr.op_paged_append(odd(row), odd(row), odd(one), odd(one.clone()), odd(zero), n - 1)
+    assert torch.equal(one[0, 0, 99], row[0, 0])
+
+
+@gpu
 def test_calls_on_two_streams_at_once():
     """Calls that overlap on the device, each with its own workspace, eager and as two graphs replayed side by side."""
     sets = []

@@ -453,11 +453,11 @@ typedef struct kraken_paged_cache {
  * are the values.  The angle is formed and reduced in 64 bits; the products are fp32, rounded once.  rot_dim = 0 (then
  * inv_freq may be NULL) appends the rows as they are: the learned positions of this library's models.
  * q (or NULL): the rows' queries, rotated into q_out, which may be q itself (same strides).  Otherwise none of q_out and
- * the cache may overlap another tensor of the call.  A row with row_seq[r] < 0 is padding, and one whose sequence, position or page does not
- * exist raises the status bit: neither changes the cache nor q_out.  The rows of one call must go to distinct
- * positions: of two rows with the same one, which of them the cache then holds is not defined, element by element.  Pages,
- * heads and slots of the cache must not lie on one another here (EINVAL for a stride of 0; sequences may share pages that
- * are only read).
+ * the cache may overlap another tensor of the call.  A row with row_seq[r] < 0 is padding, and one whose sequence, position
+ * or page does not exist raises the status bit: neither changes the cache nor q_out.  The rows of one call must go to
+ * distinct positions: of two rows with the same one, which of them the cache then holds is not defined, element by element.
+ * Pages, heads and slots of the cache must not lie on one another here (EINVAL for a stride of 0; sequences may share pages
+ * that are only read).
  * Errors: EINVAL, EUNSUPPORTED (alignment, head_dim, rot_dim no multiple of 8 or above head_dim), ECUDA. */
 typedef struct kraken_paged_append_args {
     const void *k, *v;  int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;   /* [rows][n_kv_head] */

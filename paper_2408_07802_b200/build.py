@@ -2,8 +2,8 @@
 
 Two images come out of the same sources: libkraken.so stores weights, activations and the KV cache as
 bfloat16; libkraken_f16.so (compiled with -DKRAKEN_F16=1) stores them as IEEE half, the precision of the
-paper's engines (Sec. 4.2).  Same C ABI, same symbols; `kraken_storage_dtype()` tells them apart.  A third, _marshal.so, is the extension module through
-which Python makes the shortest of the calls.
+paper's engines (Sec. 4.2).  Same C ABI, same symbols; `kraken_storage_dtype()` tells them apart.  A third
+file, _marshal.so, is the extension module through which Python makes the shortest of the calls.
 """
 from __future__ import annotations
 

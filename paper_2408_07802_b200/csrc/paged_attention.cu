@@ -103,7 +103,7 @@ struct Step {
     static constexpr int HF = (HD + 63) / 64;       // 64-element halves of a head
     static constexpr int HALF = 16 * 128;           // bytes of a tile
     static constexpr int BLOCK = 2 * HF * HALF;
-        static constexpr int SUBS = HD <= 64 ? 2 : 1;
+    static constexpr int SUBS = HD <= 64 ? 2 : 1;
     static constexpr int BYTES = SUBS * BLOCK;
     static constexpr int KEYS = SUBS * 16;          // of a warp
     static constexpr int TILE = KEYS * PA_WARPS;    // of the CTA

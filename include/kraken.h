@@ -479,7 +479,8 @@ int kraken_op_paged_append(const kraken_paged_cache *cache, const kraken_paged_a
  * does a row all of whose scores are -inf.  Several rows may name the same sequence (draft tokens: n_keys grows from
  * row to row).  A row with row_seq[r] < 0 is padding: its out and lse are left as they were.  So are those of a row
  * whose sequence does not exist, or whose n_keys[r] is negative or more than max_pages * page_size; a key whose
- * page does not exist is not visible; all of these raise the status bit.
+ * page does not exist is not visible; all of these raise the status bit.  Table entries of pages wholly in front of
+ * the window are of no importance: a server may give these pages back and leave any number there.
  * The keys are shared out evenly over the whole grid, whatever the lengths, and rows that several CTAs worked on are
  * joined by a second kernel through `workspace` (kraken_paged_attention_workspace bytes, 16-byte aligned, contents of
  * no importance; calls that may overlap on the device each need their own).  The result depends on the device's

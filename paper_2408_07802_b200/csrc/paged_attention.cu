@@ -461,7 +461,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
         const int key = ahead.k.start() + ahead.tile * TILE + warp * KEYS + (BOXES ? min(lane * box, KEYS) : lane & (KEYS - 1));
         const int n = p.by_page.quotient(key);
         slot = key - n * p.c.page_size;
-        page = key < ahead.k.n && (!BOXES || lane * box < KEYS) ? p.c.table[ahead.k.seq * p.c.table_stride + n] : -1;
+        page = key < ahead.k.n && (BOXES ? lane * box < KEYS : key >= ahead.k.lo) ? p.c.table[ahead.k.seq * p.c.table_stride + n] : -1;
     };
     int fill = 0;
     uint32_t seen[STAGES - 1];   // keys visible in the steps under way, oldest first
@@ -499,11 +499,13 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
                     }
                 } else {
                     const int key = key0 + (lane & (KEYS - 1));
+                    // (a step begins up to 15 keys in front of a window: their pages may have been given back)
+                    const bool mine = key < ahead.k.n && key >= ahead.k.lo;
                     if (page < 0 || page >= p.c.n_pages) {
-                        bad_page |= key < ahead.k.n;
+                        bad_page |= mine;
                         page = -1;
                     }
-                    mask = __ballot_sync(0xFFFFFFFFu, page >= 0 && key >= ahead.k.lo);
+                    mask = __ballot_sync(0xFFFFFFFFu, mine && page >= 0);
                     if (SUBS == 1) mask &= 0xFFFFu;
                     const long long off = max(page, 0) * p.c.page_stride + slot * p.c.slot_stride + head * p.c.head_stride;
                     const uint32_t at = smem_u32(to);

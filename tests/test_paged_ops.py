@@ -155,6 +155,25 @@ def test_attention_windows(window):
 
 
 @gpu
+@pytest.mark.parametrize("page", [1, 3, 4, 7, 8, 16, 24, 100])
+@pytest.mark.parametrize("window", [1, 10, 37])
+@pytest.mark.parametrize("no_page", [-1, 1 << 30])
+def test_attention_pages_freed_behind_the_window(page, window, no_page):
+    """Table entries of pages wholly in front of the window may name no page: no status, and the bits of the full table."""
+    lens = [0, 1, 25, 30, 41, 200, 1031]
+    pages = Pages(35, lens, 2, 64, page, "bf16")
+    q = normal(36, len(lens), 8, 64).to(torch.bfloat16)
+    n = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    full = check_attention(pages, q, n, window=window)
+    for s, length in enumerate(lens):
+        pages.table[s, :max(0, length - window) // page] = no_page
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out, lse = kr.op_paged_decode_attention(q, pages.k, pages.v, pages.table, n, window=window, status=status)
+    assert int(status.item()) == 0
+    assert torch.equal(out, full[0]) and torch.equal(lse, full[1])
+
+
+@gpu
 def test_attention_rows_of_one_sequence_padding_and_strides():
     """Draft tokens (several rows of one sequence), padding rows in the middle, q and out as slices of wider tensors."""
     lens = [400, 90]

@@ -9,8 +9,9 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
-import importlib
+import importlib.util
 import os
+import sys
 from typing import Dict, NamedTuple, Optional
 
 import torch
@@ -565,15 +566,21 @@ def decode_attention_static_capacity() -> int:
 # the tensors' device.  Their kernels take a few microseconds at decode sizes, so their arguments are checked and marshalled in
 # C++ (csrc/binding.cpp); what does not fit is a ValueError, a status of the library a KrakenError.
 
-_native = None   # the extension module _marshal.so, once loaded
+_native = None   # the extension module (kbuild.marshal_path), once loaded
 
 
 def _load_marshal():
     global _native
-    if not os.path.exists(kbuild.MARSHAL):
-        raise RuntimeError(f"{kbuild.MARSHAL} is missing: build it with `python -m paper_2408_07802_b200.build` "
+    path, name = kbuild.marshal_path(), __name__ + "._marshal"
+    if not os.path.exists(path):
+        raise RuntimeError(f"{path} is missing: build it with `python -m paper_2408_07802_b200.build` "
                            "(there is no CPU or PyTorch fallback)")
-    module = importlib.import_module("._marshal", __name__)
+    module = sys.modules.get(name)
+    if module is None:
+        spec = importlib.util.spec_from_file_location(name, path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        sys.modules[name] = module
     for dtype in _libs:
         _bind(module, dtype)
     _native = module

@@ -3,7 +3,7 @@
 Two images come out of the same sources: libkraken.so stores weights, activations and the KV cache as
 bfloat16; libkraken_f16.so (compiled with -DKRAKEN_F16=1) stores them as IEEE half, the precision of the
 paper's engines (Sec. 4.2).  Same C ABI, same symbols; `kraken_storage_dtype()` tells them apart.  A third
-file, _marshal.so, is the extension module through which Python makes the shortest of the calls.
+file, _marshal.<Python and torch>.so, is the extension module through which Python makes the shortest of the calls.
 """
 from __future__ import annotations
 
@@ -19,7 +19,6 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "libkraken.so")
 LIB_F16 = os.path.join(HERE, "libkraken_f16.so")
-MARSHAL = os.path.join(HERE, "_marshal.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -77,23 +76,29 @@ def build(force: bool = False, verbose: bool = False, dtype: str = "bf16") -> st
     return lib
 
 
+def marshal_path() -> str:
+    """The extension module of this Python and torch: it holds to their object layouts, so each pair has a file of its own."""
+    import torch
+    return os.path.join(HERE, f"_marshal.{sys.implementation.cache_tag}-torch{torch.__version__}.so")
+
+
 def build_marshal(force: bool = False) -> str:
     """Builds the extension module that turns torch tensors into the arguments of the short calls (csrc/binding.cpp), against
     the headers and libraries of the installed torch."""
     from torch.utils import cpp_extension as ext   # (its paths only; the compiler is called like nvcc above)
-    src = os.path.join(CSRC, "binding.cpp")
-    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) > max(os.path.getmtime(src), _newest_header()):
-        return MARSHAL
+    src, path = os.path.join(CSRC, "binding.cpp"), marshal_path()
+    if not force and os.path.exists(path) and os.path.getmtime(path) > max(os.path.getmtime(src), _newest_header()):
+        return path
     cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")
     dirs = [*ext.include_paths(), cuda, sysconfig.get_paths()["include"]]
     libs = ext.library_paths()
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", *("-isystem" + d for d in dirs), src, "-o", MARSHAL,
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", *("-isystem" + d for d in dirs), src, "-o", path,
            *("-L" + d for d in libs), *("-Wl,-rpath," + d for d in libs), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode:
         sys.stderr.write(res.stdout + res.stderr)
         raise RuntimeError("g++ failed: " + " ".join(cmd))
-    return MARSHAL
+    return path
 
 
 def build_all(force: bool = False, verbose: bool = False):

@@ -92,12 +92,14 @@ def build_marshal(force: bool = False) -> str:
     cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")
     dirs = [*ext.include_paths(), cuda, sysconfig.get_paths()["include"]]
     libs = ext.library_paths()
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", *("-isystem" + d for d in dirs), src, "-o", path,
+    new = f"{path[:-3]}.{os.getpid()}.so"   # another process finds the old file or the new one whole
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", *("-isystem" + d for d in dirs), src, "-o", new,
            *("-L" + d for d in libs), *("-Wl,-rpath," + d for d in libs), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode:
         sys.stderr.write(res.stdout + res.stderr)
         raise RuntimeError("g++ failed: " + " ".join(cmd))
+    os.replace(new, path)
     return path
 
 

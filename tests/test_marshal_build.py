@@ -3,6 +3,7 @@ no compiler: subprocess.run is replaced)."""
 import os
 import subprocess
 
+import pytest
 import torch
 
 from paper_2408_07802_b200 import build as kbuild
@@ -33,3 +34,21 @@ def test_another_torch_has_a_module_of_its_own(monkeypatch):
         if other != ours:
             os.remove(other)
     assert os.path.getsize(ours) > 0
+
+
+def test_a_module_in_the_making_is_not_seen(monkeypatch):
+    """The compiler writes elsewhere: another process finds the old file or the new one whole; a failed build leaves the old one."""
+    kbuild.build_all()
+    path = kbuild.build_marshal()
+    before, written = (os.path.getsize(path), os.path.getmtime(path)), []
+
+    def compiler(cmd, **kw):
+        written.append(target(cmd))
+        return subprocess.CompletedProcess(cmd, 1, "", "")
+
+    with monkeypatch.context() as m:
+        m.setattr(kbuild.subprocess, "run", compiler)
+        with pytest.raises(RuntimeError):
+            kbuild.build_marshal(force=True)
+    assert len(written) == 1 and written[0] != path and os.path.dirname(written[0]) == os.path.dirname(path)
+    assert (os.path.getsize(path), os.path.getmtime(path)) == before and not os.path.exists(written[0])

@@ -581,9 +581,9 @@ def _load_marshal():
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
         sys.modules[name] = module
-    for dtype in _libs:
+    _native = module            # an image that another thread loads from here on is bound there
+    for dtype in list(_libs):
         _bind(module, dtype)
-    _native = module
     return module
 
 
@@ -595,9 +595,10 @@ def _bind(module, dtype: str):
 
 
 def _failed(code: int, what: str, dtype: str, again):
-    """An image that is not loaded yet is, and the call made again; any other status is an error."""
+    """An image that is not loaded or bound yet is, and the call made again; any other status is an error."""
     if code == _native.NOT_BOUND:
         lib(dtype)
+        _bind(_native, dtype)
         got = again()
         if not got[0]:
             return got

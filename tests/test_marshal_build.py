@@ -1,11 +1,13 @@
-"""The extension module that marshals the short calls: when it is built again, and how the file comes into its place (no GPU,
-no compiler: subprocess.run is replaced)."""
+"""The extension module that marshals the short calls: when it is built again, how the file comes into its place (the compiler,
+subprocess.run, is replaced), and that every library image is bound to it.  No GPU."""
 import os
 import subprocess
+import threading
 
 import pytest
 import torch
 
+import paper_2408_07802_b200 as kr
 from paper_2408_07802_b200 import build as kbuild
 
 
@@ -52,3 +54,36 @@ def test_a_module_in_the_making_is_not_seen(monkeypatch):
             kbuild.build_marshal(force=True)
     assert len(written) == 1 and written[0] != path and os.path.dirname(written[0]) == os.path.dirname(path)
     assert (os.path.getsize(path), os.path.getmtime(path)) == before and not os.path.exists(written[0])
+
+
+def test_an_image_loaded_meanwhile_is_bound(monkeypatch):
+    """A thread that loads the other image while the marshalling module is being bound: both images are bound in the end."""
+    kbuild.build_all()
+    kr.lib("bf16")
+    kr._load_marshal()
+    bind, bound, threads = kr._bind, [], []
+
+    def slow_bind(module, dtype):
+        if not threads:
+            threads.append(threading.Thread(target=kr.lib, args=("f16",)))
+            threads[0].start()
+            threads[0].join(0.5)       # (it may have to wait until the module is bound)
+        bind(module, dtype)
+        bound.append(dtype)
+
+    monkeypatch.setattr(kr, "_bind", slow_bind)
+    monkeypatch.setattr(kr, "_libs", {"bf16": kr._libs["bf16"]})
+    monkeypatch.setattr(kr, "_native", None)
+    kr._load_marshal()
+    threads[0].join(60)
+    assert not threads[0].is_alive() and sorted(set(bound)) == ["bf16", "f16"]
+
+
+def test_an_image_that_was_not_bound_is(monkeypatch):
+    """The second attempt after NOT_BOUND binds the image, loaded or not."""
+    kbuild.build_all()
+    kr.lib("f16")
+    module, bound = kr._load_marshal(), []
+    monkeypatch.setattr(kr, "_bind", lambda m, dtype: bound.append(dtype))
+    assert kr._failed(module.NOT_BOUND, "call", "f16", lambda: (0, "made again")) == (0, "made again")
+    assert bound == ["f16"]

@@ -474,6 +474,7 @@ int kraken_op_paged_append(const kraken_paged_cache *cache, const kraken_paged_a
  * sees the n_keys[r] first positions of the sequence, with window > 0 only the last `window` of these.  For key j
  *     x_j = scale * q . k_j;   score_cap > 0:  x_j = score_cap * tanh(x_j / score_cap);
  *     slopes != NULL:  x_j += slopes[h] * (j - (n_keys[r] - 1));
+ * (scale * log2(e) and 1 / score_cap have to be finite in fp32, EINVAL otherwise);
  * out = sum_j softmax(x)_j v_j, and lse (or NULL) = log sum_j exp(x_j), with which attention over other keys can be
  * joined.  Query head h reads key/value head h / (n_head / n_kv_head).  n_keys[r] = 0 gives out = 0 and lse = -inf; so
  * does a row all of whose scores are -inf.  Several rows may name the same sequence (draft tokens: n_keys grows from
@@ -514,7 +515,7 @@ int kraken_paged_attention_workspace(int32_t n_head, int32_t n_kv_head, int32_t 
  * -inf logits (forbidden tokens) have weight 0 and log probability -inf.  A row that holds a NaN or +inf, or nothing
  * but -inf, has no distribution: its numbers are NaN, lse of the last kind -inf; its top_ids are still the order of
  * its logits, a NaN counting as -inf.  A target >= vocab gives NaN and raises bit 0 of *d_status (device uint32 or NULL).
- * 0 <= top <= 32, top <= vocab; scale > 0, finite.  Errors: EINVAL, EUNSUPPORTED (top > 32, vocab > 2^30), ECUDA. */
+ * 0 <= top <= 32, top <= vocab; scale > 0, scale * log2(e) finite in fp32.  Errors: EINVAL, EUNSUPPORTED (top > 32, vocab > 2^30), ECUDA. */
 typedef struct kraken_logprobs_args {
     const void *logits;  int64_t row_stride;
     const int32_t *targets;                               /* int32 [rows] or NULL                         */

@@ -238,6 +238,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
         g.row_seq = vector<const int32_t>(a[5], at::kInt, rows, device, "row_seq");
         g.scale = a[6] == Py_None ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(c.head_dim))) : float_arg(a[6], "scale");
         g.score_cap = float_arg(a[7], "score_cap");
+        need(g.score_cap != 0.f || PyFloat_AsDouble(a[7]) == 0.0, "score_cap is too small for 32 bits");   // (0 is no cap)
         g.window = int_arg(a[8], "window");
         g.slopes = vector<const float>(a[9], at::kFloat, heads, device, "slopes");
         g.rows = to_int32(rows, "the number of rows");

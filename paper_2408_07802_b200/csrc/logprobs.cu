@@ -594,7 +594,7 @@ extern "C" int kraken_op_token_logprobs(const kraken_logprobs_args *a, uint32_t 
     if (!a || a->rows < 0) return KRAKEN_EINVAL;
     if (a->rows == 0) return KRAKEN_OK;
     if (!a->logits || a->vocab < 1 || a->row_stride < 0 || a->dtype < 0 || a->dtype > 1 || a->top < 0 || a->top > a->vocab ||
-        !(a->scale > 0.f) || !isfinite(a->scale) || (a->logprob && !a->targets) || (a->top > 0 && !a->top_ids && !a->top_logprobs))
+        !(a->scale > 0.f) || !isfinite(a->scale * LOG2E) || (a->logprob && !a->targets) || (a->top > 0 && !a->top_ids && !a->top_logprobs))
         return KRAKEN_EINVAL;
     if (a->top > LP_MAX_TOP || a->vocab > 1 << 30) return KRAKEN_EUNSUPPORTED;
     if (reinterpret_cast<uintptr_t>(a->logits) & (a->dtype ? 1 : 3)) return KRAKEN_EUNSUPPORTED;

@@ -901,8 +901,10 @@ extern "C" int kraken_op_paged_attention(const kraken_paged_cache *cache, const 
     if (rc) return rc;
     if (a->rows == 0) return KRAKEN_OK;
     if (a->rows < 0 || !a->q || !a->out || !a->n_keys || a->n_head < 1 || a->n_head % cache->n_kv_head != 0 || a->window < 0 ||
-        !isfinite(a->scale) || !isfinite(a->score_cap) || a->score_cap < 0.f)
+        !isfinite(a->score_cap) || a->score_cap < 0.f)
         return KRAKEN_EINVAL;
+    // (these two are factors in the kernel: a score of 0 times an infinite one would be a NaN)
+    if (!isfinite(a->scale * LOG2E) || (a->score_cap > 0.f && !isfinite(1.f / a->score_cap))) return KRAKEN_EINVAL;
     if (!a->row_seq && a->rows > cache->n_seqs) return KRAKEN_EINVAL;
     // (no two rows or heads of the output in one place)
     if ((a->rows > 1 && a->out_row_stride == 0) || (a->n_head > 1 && a->out_head_stride == 0) ||

@@ -278,6 +278,27 @@ def test_attention_many_small_weights_against_a_large_one(dtype, gap):
 
 
 @gpu
+def test_attention_caps_and_scales_at_the_ends_of_the_type():
+    """The smallest and largest that are taken, on scores of 0 (half of them) and others; smaller and larger ones are refused."""
+    pages = Pages(42, [50], 1, 64, 16, "bf16")
+    q = normal(43, 1, 2, 64).to(torch.bfloat16)
+    q[0, 0] = 0
+    n = torch.tensor([50], dtype=torch.int32, device=DEV)
+    run = lambda **kw: kr.op_paged_decode_attention(q, pages.k, pages.v, pages.table, n, **kw)
+    even, _ = run(scale=0.0)
+    out, lse = run(score_cap=1.2e-38)                        # every score is next to 0: the mean of the values
+    assert torch.equal(out, even) and bool(((lse - math.log(50)).abs() < 1e-5).all())
+    out, _ = run(scale=2.3e38)
+    assert torch.equal(out[0, 0], even[0, 0])
+    for bad in (dict(score_cap=1e-39), dict(score_cap=math.inf), dict(scale=2.4e38), dict(scale=-2.4e38)):
+        with pytest.raises(kr.KrakenError) as e:
+            run(**bad)
+        assert e.value.status == kr.EINVAL
+    with pytest.raises(ValueError):
+        run(score_cap=1e-60)                                 # no cap at all in 32 bits
+
+
+@gpu
 def test_attention_far_pages_and_streams():
     """Offsets past 2^31 elements, on another stream than the default one, captured into a graph and replayed with other lengths."""
     page, hd, n_pages = 128, 128, 140000
@@ -850,6 +871,16 @@ def test_refusals_before_the_device_is_touched(dtype):
     assert L.kraken_paged_attention_workspace(4, 2, 64, None) == kr.EINVAL
     assert L.kraken_paged_attention_workspace(4, 3, 64, C.byref(n)) == kr.EINVAL
     assert L.kraken_paged_attention_workspace(4, 2, 80, C.byref(n)) == kr.EUNSUPPORTED
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_scales_and_caps_that_leave_the_type_are_refused(dtype):
+    """scale * log2(e) and 1 / score_cap are taken in 32 bits: where one of them is infinite, a score of 0 became NaN."""
+    L = kr.lib(dtype)
+    for over in (dict(score_cap=1e-39), dict(score_cap=1e-45), dict(scale=2.4e38), dict(scale=-3.4e38)):
+        a = attention_args(**over)
+        assert L.kraken_op_paged_attention(C.byref(cache_args()), C.byref(a), None, None) == kr.EINVAL, over
+    assert L.kraken_op_token_logprobs(C.byref(logprob_args(scale=2.4e38)), None, None) == kr.EINVAL
 
 
 def test_struct_sizes():

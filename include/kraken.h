@@ -515,7 +515,10 @@ int kraken_paged_attention_workspace(int32_t n_head, int32_t n_kv_head, int32_t 
  * -inf logits (forbidden tokens) have weight 0 and log probability -inf.  A row that holds a NaN or +inf, or nothing
  * but -inf, has no distribution: its numbers are NaN, lse of the last kind -inf; its top_ids are still the order of
  * its logits, a NaN counting as -inf.  A target >= vocab gives NaN and raises bit 0 of *d_status (device uint32 or NULL).
- * 0 <= top <= 32, top <= vocab; scale > 0, scale * log2(e) finite in fp32.  Errors: EINVAL, EUNSUPPORTED (top > 32, vocab > 2^30), ECUDA. */
+ * 0 <= top <= KRAKEN_LOGPROBS_MAX_TOP, top <= vocab; scale > 0, scale * log2(e) finite in fp32.  Errors: EINVAL, EUNSUPPORTED
+ * (a larger top, vocab > 2^30), ECUDA. */
+#define KRAKEN_LOGPROBS_MAX_TOP 32
+
 typedef struct kraken_logprobs_args {
     const void *logits;  int64_t row_stride;
     const int32_t *targets;                               /* int32 [rows] or NULL                         */

@@ -303,7 +303,8 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (!im.logprobs) return give(NOT_BOUND, {Tensor(), Tensor(), Tensor(), Tensor(), Tensor()});
         c10::cuda::CUDAGuard guard(device);
         // 4 rows bytes each: entropy, lse, and logprob where asked for; then the alternatives
-        const int64_t row = 4 * rows, numbers = g.targets ? 3 : 2, list = row * g.top;
+        // (no room for lists longer than the library makes: it refuses them before it writes)
+        const int64_t row = 4 * rows, numbers = g.targets ? 3 : 2, list = g.top <= KRAKEN_LOGPROBS_MAX_TOP ? row * g.top : 0;
         const Tensor bytes = at::empty({row * numbers + 2 * list}, x.options().dtype(at::kByte));
         const Tensor entropy = part(bytes, 0, at::kFloat, {rows}), lse = part(bytes, row, at::kFloat, {rows});
         Tensor logprob, ids, best;

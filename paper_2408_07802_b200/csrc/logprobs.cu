@@ -28,7 +28,7 @@ namespace kr {
 
 namespace {
 
-constexpr int LP_MAX_TOP = 32;
+constexpr int LP_MAX_TOP = KRAKEN_LOGPROBS_MAX_TOP;
 constexpr int PER_THREAD = 16;                       // logits of a thread in a chunk
 constexpr int GROUP = 4;
 constexpr int MAX_CLUSTER = 8;

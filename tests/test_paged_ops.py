@@ -640,6 +640,19 @@ def test_logprobs_targets_and_rows():
     assert kr.op_token_logprobs(x[:0], top=2).top_ids.shape == (0, 2)
 
 
+@gpu
+def test_logprobs_refusals_take_no_memory():
+    x = torch.zeros(64, 1 << 20, device=DEV)
+    kr.op_token_logprobs(x, top=1)
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    for top, code in ((1 << 20, kr.EUNSUPPORTED), (33, kr.EUNSUPPORTED), (1 << 21, kr.EINVAL)):
+        with pytest.raises(kr.KrakenError) as e:
+            kr.op_token_logprobs(x, top=top)
+        assert e.value.status == code
+    assert torch.cuda.max_memory_allocated() - before < 1 << 16
+
+
 # ---------------------------------------------------------------------------------------------------- calls nobody wrote down
 
 @gpu

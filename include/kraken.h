@@ -489,7 +489,8 @@ int kraken_op_paged_append(const kraken_paged_cache *cache, const kraken_paged_a
  * n_keys, row_seq and the page table must not change while the call runs.  A bounded wait that gave up raises bit 1 of
  * the status word; the outputs then mean nothing.  Rows or heads of out or lse must not lie on one another (EINVAL for a
  * stride of 0), and none of them may overlap another tensor of the call.
- * Errors: EINVAL, EUNSUPPORTED, ECAPACITY (workspace_bytes too small), ECUDA. */
+ * Errors: EINVAL, EUNSUPPORTED (alignment, head_dim; 2^23 rows or more; rows times positions that the page table has room
+ * for of 2^46 or more), ECAPACITY (workspace_bytes too small), ECUDA. */
 typedef struct kraken_paged_attention_args {
     const void *q;  int64_t q_row_stride, q_head_stride;                                    /* [rows][n_head]    */
     void *out;      int64_t out_row_stride, out_head_stride;                                /* [rows][n_head]    */

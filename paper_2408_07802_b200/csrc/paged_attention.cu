@@ -303,6 +303,10 @@ __device__ __forceinline__ void copy16(uint32_t smem, const void *gmem, bool liv
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(gmem), "r"(live ? 16 : 0) : "memory");
 }
 
+// The tiles of a call are added up in the lower bits of a 64-bit number, and the rows that have some above them; a call that might
+// not fit is refused.  (Two numbers would take twice the shuffles before the first key is asked for.)
+constexpr int ROWS_AT = 40;
+
 // A place on the line of tiles
 struct Place {
     int r, unit, tile;
@@ -373,7 +377,6 @@ __global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_kernel(const __grid_
         // where this CTA's share begins: every thread adds up the tiles of a run of rows
         const int per = (p.rows + PA_WARPS * 32 - 1) / (PA_WARPS * 32);
         const int row_lo = min(p.rows, (int)threadIdx.x * per), row_hi = min(p.rows, row_lo + per);
-        constexpr int ROWS_AT = 40;   // a sum of tiles, and above it of rows that have some
         long long mine = 0;
         int most = 0;
         for (int r = row_lo; r < row_hi; ++r) {
@@ -913,6 +916,9 @@ extern "C" int kraken_op_paged_attention(const kraken_paged_cache *cache, const 
     if (!aligned16(a->q) || !aligned16(a->out) ||
         ((a->q_row_stride | a->q_head_stride | a->out_row_stride | a->out_head_stride) & 7))
         return KRAKEN_EUNSUPPORTED;
+    // (the smallest tile has 64 keys)
+    const long long capacity = (long long)cache->max_pages * cache->page_size;
+    if (a->rows >= 1 << (63 - ROWS_AT) || a->rows * (capacity / 64 + 2) >= 1LL << ROWS_AT) return KRAKEN_EUNSUPPORTED;
     if (!a->workspace || a->workspace_bytes < workspace_bytes(a->n_head / cache->n_kv_head, cache->head_dim)) return KRAKEN_ECAPACITY;
     if (!aligned16(a->workspace)) return KRAKEN_EINVAL;
     p.workspace = static_cast<uint8_t *>(a->workspace);

@@ -896,6 +896,19 @@ def test_scales_and_caps_that_leave_the_type_are_refused(dtype):
     assert L.kraken_op_token_logprobs(C.byref(logprob_args(scale=2.4e38)), None, None) == kr.EINVAL
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_attention_more_rows_than_its_counters_hold_are_refused(dtype):
+    """Tiles and rows are added up in one 64-bit number, 40 and 23 bits of it."""
+    L = kr.lib(dtype)
+    wide = dict(max_pages=1 << 15, table_stride=1 << 15, page_size=1 << 15, slot_stride=64, head_stride=1 << 21, page_stride=1 << 22)
+    for cache, rows in ((cache_args(), 1 << 23), (cache_args(), (1 << 31) - 1), (cache_args(**wide), 1 << 16)):
+        a = attention_args(rows=rows)
+        assert L.kraken_op_paged_attention(C.byref(cache), C.byref(a), None, None) == kr.EUNSUPPORTED, rows
+    # one row less is taken, as far as its workspace
+    a = attention_args(rows=(1 << 23) - 1, workspace_bytes=0)
+    assert L.kraken_op_paged_attention(C.byref(cache_args()), C.byref(a), None, None) == kr.ECAPACITY
+
+
 def test_struct_sizes():
     assert C.sizeof(kr.PagedCacheArgs) == 7 * 8 + 6 * 4
     assert C.sizeof(kr.PagedAppendArgs) == 15 * 8 + 4 * 4

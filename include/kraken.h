@@ -477,15 +477,18 @@ int kraken_op_paged_append(const kraken_paged_cache *cache, const kraken_paged_a
  * (scale * log2(e) and 1 / score_cap have to be finite in fp32, EINVAL otherwise);
  * out = sum_j softmax(x)_j v_j, and lse (or NULL) = log sum_j exp(x_j), with which attention over other keys can be
  * joined.  Query head h reads key/value head h / (n_head / n_kv_head).  n_keys[r] = 0 gives out = 0 and lse = -inf; so
- * does a row all of whose scores are -inf.  Several rows may name the same sequence (draft tokens: n_keys grows from
- * row to row).  A row with row_seq[r] < 0 is padding: its out and lse are left as they were.  So are those of a row
- * whose sequence does not exist, or whose n_keys[r] is negative or more than max_pages * page_size; a key whose
- * page does not exist is not visible; all of these raise the status bit.  Table entries of pages wholly in front of
- * the window are of no importance: a server may give these pages back and leave any number there.
+ * does a row all of whose scores are -inf.  A NaN or +inf among a head's scores makes its out and lse NaN; a value that is
+ * not finite makes that element of out NaN or infinite, and no other.
+ * Several rows may name the same sequence (draft tokens: n_keys grows from row to row); each reads its keys for itself.
+ * A row with row_seq[r] < 0 is padding: its out and lse are left as they were.  So are those of a row whose sequence
+ * does not exist, or whose n_keys[r] is negative or more than max_pages * page_size; a key whose page does not exist
+ * is not visible; all of these raise the status bit.  Table entries of pages wholly in front of the window are of no
+ * importance: a server may give these pages back and leave any number there.
  * The keys are shared out evenly over the whole grid, whatever the lengths, and rows that several CTAs worked on are
  * joined by a second kernel through `workspace` (kraken_paged_attention_workspace bytes, 16-byte aligned, contents of
  * no importance; calls that may overlap on the device each need their own).  The result depends on the device's
- * number of SMs and on all the lengths of the call in its last bits only, and is the same from run to run.
+ * number of SMs, on all the lengths of the call and on the positions that the page table has room for (max_pages *
+ * page_size) in its last bits only, and is the same from run to run.
  * n_keys, row_seq and the page table must not change while the call runs.  A bounded wait that gave up raises bit 1 of
  * the status word; the outputs then mean nothing.  Rows or heads of out or lse must not lie on one another (EINVAL for a
  * stride of 0), and none of them may overlap another tensor of the call.

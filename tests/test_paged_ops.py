@@ -215,6 +215,54 @@ def test_attention_rows_and_pages_that_do_not_exist():
     assert (out[0].double() - p @ pages.get(pages.v, 0, 0, 100)[:, 0]).abs().max() < 2.0 ** -8 * 4
 
 
+class Some(Pages):
+    """The same pages without the keys whose position `hidden` names."""
+
+    def __init__(self, pages, hidden):
+        self.k, self.v, self.table, self.page, self.hidden = pages.k, pages.v, pages.table.clone(), pages.page, hidden
+
+    def get(self, cache, s, lo, hi):
+        return super().get(cache, s, lo, hi)[[i for i in range(lo, hi) if not self.hidden(i)]]
+
+
+def near_reference(pages, q, out, lse, n_keys, row_seq, rows):
+    """Those rows of (out, lse) against 64 bits, with the tolerances of check_attention."""
+    ref, ref_lse, tol, tol_l = attention_ref(pages, q, n_keys, row_seq, q.shape[2] ** -0.5)
+    half = torch.finfo(q.dtype).eps / 2
+    assert bool(((out.double() - ref).abs() <= half * ref.abs() * (1 + 1e-3) + tol + 2.0 ** -25)[rows].all())
+    assert bool(((lse.double() - ref_lse).abs() <= tol_l)[rows].all())
+
+
+@gpu
+@pytest.mark.parametrize("page,width", [(16, 7), (16, 600), (7, 15), (7, 1200), (8, 13), (100, 1)])
+@pytest.mark.parametrize("kind", ["too long", "negative length", "no sequence", "page past the end", "page below zero"])
+def test_attention_what_does_not_exist_one_at_a_time(page, width, kind):
+    """Each kind alone raises the bit, in the middle one of three rows: with copies as boxes and by the lanes, with page tables
+    by which the host knows that nothing is split and others."""
+    lens = [100, 100, 100]
+    pages = Pages(37, lens, 2, 64, page, "bf16", width=width)
+    q = normal(38, 3, 8, 64).to(torch.bfloat16)
+    lengths = {"too long": width * page + 1, "negative length": -1}
+    n, seq = [100, lengths.get(kind, 100), 100], [0, 3 if kind == "no sequence" else 1, 2]
+    left_alone = kind in ("too long", "negative length", "no sequence")
+    lost = (100 - 1) // page                                     # number of the page that does not exist
+    seen = Some(pages, lambda i: i // page == lost and not left_alone)
+    if not left_alone:
+        pages.table[1, lost] = pages.n_pages if kind == "page past the end" else -1
+    out, lse = torch.full_like(q, 9.0), torch.full((3, 8), 9.0, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    kr.op_paged_decode_attention(q, pages.k, pages.v, pages.table, torch.tensor(n, dtype=torch.int32, device=DEV),
+                                 row_seq=torch.tensor(seq, dtype=torch.int32, device=DEV), out=out, lse=lse, status=status)
+    assert int(status.item()) == kr.STATUS_BAD_PAGE
+    near_reference(Some(pages, lambda i: False), q, out, lse, [100, 0, 100], [0, -1, 2], [0, 2])
+    if left_alone:
+        assert bool((out[1] == 9).all()) and bool((lse[1] == 9).all())
+    elif lost == 0:                                              # no key is left
+        assert bool((out[1] == 0).all()) and bool((lse[1] == -math.inf).all())
+    else:
+        near_reference(seen, q, out, lse, [0, 100, 0], [-1, 1, -1], [1])
+
+
 @gpu
 def test_attention_many_rows_of_unequal_length_and_a_row_alone():
     """A row's result does not depend on the rows beside it (up to the order of the sums)."""
@@ -250,6 +298,69 @@ def test_attention_extreme_scores():
         pages.k[pages.table[2, i // 16].item(), 0, i % 16, 0] = -math.inf
     out, lse = kr.op_paged_decode_attention(q[2:], pages.k, pages.v, pages.table[2:], torch.tensor([17], dtype=torch.int32, device=DEV))
     assert bool((out == 0).all()) and lse.item() == -math.inf
+
+
+@gpu
+@pytest.mark.parametrize("n,page", [(60, 16), (60, 7), (3000, 16), (3000, 7)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_attention_nan_and_infinity_in_visible_places(n, page, dtype):
+    """They reach the heads (of a value: the elements) that they belong to and nothing else, whoever of the CTAs meets them."""
+    pages = Pages(39, [n, n], 2, 64, page, dtype)
+    q = normal(40, 2, 6, 64).to(T16[dtype])
+    q[:, 0, 0], q[:, 1, 0], q[:, 2, 0] = 1.0, -1.0, 0.0            # heads of key/value head 0
+    lens = torch.tensor([n, n], dtype=torch.int32, device=DEV)
+    at = 29
+    slot = (pages.table[1, at // page].item(), 0, at % page)         # of head 0
+    run = lambda q=q: kr.op_paged_decode_attention(q, pages.k, pages.v, pages.table, lens)
+    clean, clean_lse = run()
+    k, v = pages.k[slot].clone(), pages.v[slot].clone()
+
+    def others_as_before(out, lse, row, heads):
+        keep = torch.ones(2, 6, dtype=torch.bool, device=DEV)
+        keep[row, heads] = False
+        assert torch.equal(out[keep], clean[keep]) and torch.equal(lse[keep], clean_lse[keep])
+
+    # a query: its head
+    bad = q.clone()
+    bad[1, 4, 5] = math.nan
+    out, lse = run(bad)
+    assert bool(out[1, 4].isnan().all()) and bool(lse[1, 4].isnan())
+    others_as_before(out, lse, 1, [4])
+    # a key: the heads that share it.  NaN, and +inf as a score: NaN; -inf as a score: that key does not count
+    pages.k[slot][7] = math.nan
+    out, lse = run()
+    assert bool(out[1, :3].isnan().all()) and bool(lse[1, :3].isnan().all())
+    others_as_before(out, lse, 1, [0, 1, 2])
+    pages.k[slot][7] = k[7]
+    pages.k[slot][0] = math.inf
+    out, lse = run()
+    assert bool(out[1, [0, 2]].isnan().all()) and bool(lse[1, [0, 2]].isnan().all())       # inf, and 0 times inf
+    others_as_before(out, lse, 1, [0, 1, 2])
+    pages.k[slot][0] = k[0]
+    near = Some(pages, lambda i: i == at)
+    ref, ref_lse, tol, tol_l = attention_ref(near, q, [0, n], [-1, 1], 64 ** -0.5)
+    half = torch.finfo(q.dtype).eps / 2
+    assert bool(((out[1, 1].double() - ref[1, 1]).abs() <= half * ref[1, 1].abs() * (1 + 1e-3) + tol[1, 1] + 2.0 ** -25).all())
+    assert bool((lse[1, 1].double() - ref_lse[1, 1]).abs() <= tol_l[1, 1])
+    # a value: its element of the heads that share it, which is not finite; the other elements and lse as before
+    for x in (math.nan, math.inf, -math.inf):
+        pages.v[slot][9] = x
+        out, lse = run()
+        assert not bool(out[1, :3, 9].isfinite().any()) and torch.equal(lse, clean_lse)
+        out[1, :3, 9] = clean[1, :3, 9]
+        assert torch.equal(out, clean)
+        pages.v[slot][9] = v[9]
+
+
+@gpu
+@pytest.mark.parametrize("form", ["cap", "slopes", "all"])
+@pytest.mark.parametrize("lens,H,Hkv,hd,page,dtype", [ATTEND[1], ATTEND[3], ATTEND[5], ATTEND[8]])
+def test_attention_slots_before_heads(lens, H, Hkv, hd, page, dtype, form):
+    """Pages laid out [slot][head], with a score cap and with slopes."""
+    pages = Pages(len(lens) + 2 * H, lens, Hkv, hd, page, dtype, by_slot=True)
+    slopes = (2.0 ** -torch.linspace(1, 8, H)).to(DEV) if form in ("slopes", "all") else None
+    check_attention(pages, normal(41, len(lens), H, hd).to(T16[dtype]), torch.tensor(lens, dtype=torch.int32, device=DEV),
+                    cap=3.0 if form in ("cap", "all") else 0.0, window=50 if form == "all" else 0, slopes=slopes)
 
 
 @gpu

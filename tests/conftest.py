@@ -1,3 +1,4 @@
+import gc
 import os
 import sys
 
@@ -6,6 +7,14 @@ import pytest
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 if ROOT not in sys.path:
     sys.path.insert(0, ROOT)
+
+
+@pytest.fixture(autouse=True, scope="module")
+def nothing_left_to_collect():
+    """A test that keeps an exception keeps its own frame too, and the device tensors in it, until Python's collector comes by.
+    It does so between modules, and not in the middle of a test that counts the memory in use."""
+    yield
+    gc.collect()
 
 
 def pytest_configure(config):

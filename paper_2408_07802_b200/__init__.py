@@ -620,8 +620,8 @@ def op_paged_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_c
     head_dim] (any row and head strides: slices of one qkv product do) go to position positions[r] of sequence row_seq[r]
     (None: sequence r; negative: padding).  k_cache, v_cache: [pages, key/value heads, page size, head_dim], page_table
     int32 [sequences, pages].  inv_freq (float32 [rot_dim / 2]) turns keys and queries by their position; the queries q
-    [rows, heads, head_dim] go to q_out (created when not given, with the padding rows zero; may be q itself), which is
-    returned.  The rows of one call must go to distinct positions."""
+    [rows, heads, head_dim] go to q_out (created when not given, filled with zeros first for the padding rows' sake; may be q
+    itself), which is returned.  The rows of one call must go to distinct positions."""
     m = _native or _load_marshal()
     args = (k, v, k_cache, v_cache, page_table, positions, row_seq, q, q_out, inv_freq, interleaved, status)
     got = m.paged_append(*args)
@@ -648,7 +648,9 @@ def op_paged_decode_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: t
     head_dim], against the first n_keys[r] positions of sequence row_seq[r] (None: sequence r; negative: padding, whose
     rows of out and lse stay as they were).  scale: 1 / sqrt(head_dim) by default; score_cap: scores become
     cap * tanh(score / cap); window: only that many last positions are visible; slopes (float32 [heads]): a bias of
-    slope * (distance back to the key, negative).  Returns (out, lse): out like q, lse float32 [rows, heads]."""
+    slope * (distance back to the key, negative).  Returns (out, lse): out like q, lse float32 [rows, heads].  Where neither
+    is given they are made, as parts of one allocation: keeping either keeps both (clone the one to be kept), and padding
+    rows hold anything."""
     m = _native or _load_marshal()
     args = (q, k_cache, v_cache, page_table, n_keys, row_seq, scale, score_cap, window, slopes, out, lse, workspace, status)
     got = m.paged_attention(*args)
@@ -669,7 +671,8 @@ def op_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = No
                       status: Optional[torch.Tensor] = None) -> TokenLogprobs:
     """Reads rows of logits (kraken_op_token_logprobs): log probability of targets[r] (int32; negative: not asked for),
     entropy of the row's distribution and its `top` largest tokens with their log probabilities, for the distribution
-    softmax(scale * logits).  logits: [rows, vocab] float32, bfloat16 or float16, any row stride."""
+    softmax(scale * logits).  logits: [rows, vocab] float32, bfloat16 or float16, any row stride.  The results are parts of
+    one allocation: keeping one keeps all (clone the one to be kept)."""
     m = _native or _load_marshal()
     args = (logits, targets, top, scale, status, _current_dtype == "f16")
     got = m.token_logprobs(*args)

@@ -3,8 +3,9 @@
 //   x = scale * logit, m = max x, S = sum e^(x - m):  lse = m + log S,  logprob = x_t - lse,
 //   entropy = log S + sum (m - x) e^(x - m) / S       (every term of the sum is positive: nothing cancels)
 //
-// Bound by HBM: 4 (or 2) bytes a logit against about 6 instructions.  Every thread keeps a maximum and the two sums of its
-// own logits, brought to a larger maximum 16 logits at a time; the threads of a row meet at the end.
+// 4 (or 2) bytes a logit against 13 instructions (2048 x 50257, k = 5): 148 SMs can issue those of 2.9e12 logits a second, so fp32
+// is bound by HBM and 16-bit logits by issue.  Every thread keeps a maximum and the two sums of its own logits, brought to a larger
+// maximum 16 logits at a time; the threads of a row meet at the end.
 //
 // The alternatives are found in the same pass.  After chunks 1, 3, 9, 27 ... the largest logits so far of groups of 4 threads are
 // looked at: the k-th largest of them is a bound that k logits reach.  A thread compares the maximum of its 16 logits, which
@@ -13,7 +14,8 @@
 // than k, are ranked by counting, by keys of a logit and its index whose order is that of the list.  Where more places or
 // logits reach the bound than there is room for (a vocabulary in rising order, or of few different values) the row is gone
 // through again by exact_top(), which works with the distinct keys and cuts down what it has put aside.
-// Measured on 2048 x 50257 fp32: 72.5 us with k = 5 (5.7 TB/s), 63.6 without alternatives (6.5 TB/s, the copy bandwidth).  Logits
+// Measured on 2048 x 50257 fp32: 72.3 us with k = 5 (5.7 TB/s), 62.6 without alternatives (6.6 TB/s, the copy bandwidth); bf16 57.0
+// and 43.4 us.  Spills: 4 loads and 18 stores a warp and row, none in the loop over the chunks.  Logits
 // put aside at once (a warp then goes through the 16 of a thread some hundred times a row): 98 us with k = 20 against 80; looks
 // without barriers at 32 groups: 144 with k = 32; a ring of bulk copies filled by a warp of its own: 88 with k = 5.
 //
@@ -541,8 +543,8 @@ __global__ void __launch_bounds__(T, Shape<T>::CTAS) logprobs_kernel(const Logpr
     }
 }
 
-// CTAs of a row: more while they do not fill half the SMs, none with less than a chunk.  (48 x 51200 bf16, k = 20: 9.3 us with 2
-// a row, 10.1 with 4, 11.8 with 8; one row of 50257 fp32: 7.9 with 8, 10.8 with one.)
+// CTAs of a row: more while they do not fill half the SMs, none with less than a chunk.  (48 x 51200 bf16, k = 20: 11.4 us with one
+// a row, 9.8 with 2, 10.0 with 4, 11.7 with 8; one row of 50257 fp32: 12.1 with one, 10.0 with 2, 9.0 with 4, 8.9 with 8.)
 int cluster_of(int rows, int vocab) {
     const int sms = sm_count() > 0 ? sm_count() : 148;
     int c = 1;

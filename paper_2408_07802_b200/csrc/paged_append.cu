@@ -51,9 +51,12 @@ __device__ __forceinline__ void turn_pairs(uint32_t &a, uint32_t &b, uint64_t c,
 // One CTA per row.  A thread has the same piece i of every head that it works on, so the piece's cosines and sines are in its
 // registers and nothing is divided per piece, and the first AHEAD pieces of queries and keys, and again of values, are
 // requested before the row's page is looked up and its angles are formed: what is read does not depend on where it goes.
-//   64 threads, 4 pieces ahead    many rows: more rows side by side (four prompts, 5900 rows of 16 + 2 x 16 heads of 128: 24.2
-//                                 against 25.8 us, a plain copy of as many bytes 25.5)
-//   128 threads, 2 pieces ahead   few rows: a row takes less time (one row of 32 + 2 x 8 heads: 2.7 against 3.2 us)
+//   64 threads, 4 pieces ahead    many rows: more rows side by side (four prompts, 6010 rows of 16 + 2 x 16 heads of 128: 25.8
+//                                 against 26.1 us, an elementwise kernel over as many bytes 23.7)
+//   128 threads, 2 pieces ahead   few rows: a row takes less time (one row of 32 + 2 x 8 heads: 2.2 against 2.7 us; 64 rows of
+//                                 16 + 2 x 16 heads of 64: 1.8 against 2.1)
+// (In a graph, on rotating inputs larger than L2 together; on one input over and over the prompts take 23.1 us.)  The 128-thread
+// kernel for far pairs spills 20 bytes a thread: 3 of a warp's 550 instructions read them back.
 // Tried: 256 threads that work each piece's head and place out (232 instructions a warp and piece: 31 us, bound by issue);
 // CTAs that stay and request a row ahead (31 us: the registers of two rows halve the rows side by side).
 template <AppendForm FORM, int THREADS, int AHEAD>

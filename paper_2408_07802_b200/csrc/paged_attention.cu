@@ -3,9 +3,10 @@
 //
 //   x_j = scale q.k_j  [cap tanh(x/cap)]  [+ slope (j - (n - 1))],  out = sum_j softmax(x)_j v_j,  lse = log sum_j e^x_j
 //
-// Every key and value is used by the n_head / n_kv_head query heads that share it and read once: 4 bytes a key element
-// against 4 FLOP per query head, so up to 16 heads a group this is bound by HBM (16 FLOP a byte: 100 TFLOP/s at the copy
-// bandwidth) and the products run on the warp-level tensor instructions, which take both operands from registers.
+// A row reads every key and value once for up to 16 of the n_head / n_kv_head query heads that share it (for more heads once for
+// each 16 of them): 4 bytes a key element against 4 FLOP per query head, at most 16 FLOP a byte or 100 TFLOP/s at the copy
+// bandwidth.  So this is bound by HBM, and the products run on the warp-level tensor instructions, which take both operands from
+// registers.  Rows of the same sequence read its keys each for itself.
 //
 // The products of 16 keys with the 8 or 16 query heads of a tile (m16n8k16):
 //   S[head, key] = Q K^T        the heads are the rows (rows 8..15 are empty up to 8 heads); a lane reads 16 bytes (8
@@ -19,7 +20,7 @@
 // is only raised when a score exceeds it by more than 8 in the exponent of 2 (numerator and denominator carry the same
 // factor), so most blocks need one vote of the warp where a running maximum would take shuffles and a rescaling.
 //
-// Measured: one sequence of 131072 keys, 32 query heads on 8 of 128: 88 us = 6.1 TB/s; 64 sequences of 8192: 318 us = 6.75 TB/s.
+// Measured, 32 query heads on 8 of 128: one sequence of 131072 keys 86 us = 6.2 TB/s; 64 sequences of 8192 322 us = 6.7 TB/s.
 // On the way there (the one sequence): a CTA per row and head 3955 us; the keys shared out 133; blocks copied ahead by the lanes
 // into shared memory 120, whatever the number of instructions (541, then 350 a block) and of stages: 16-byte copies of 64-byte
 // pieces; by the copy engine 90.  Below that, 5 us pass before the first key is there and 3 in the joining kernel.
@@ -326,6 +327,9 @@ struct Smem {
     uint32_t gave_up;
 };
 
+// Spills: up to 24 bytes a thread, 44 in the instance for 64-wide heads (128 registers), where they are one store and less than one
+// load a step and warp, 0.3 % of its instructions.
+//
 // BOXES: pages of a multiple of 16 (or 8) keys, which the copy engine brings in as boxes of 16 (8) keys, one 64-element half at
 // a time, by tensor maps over (element, slot, head, page); with other page sizes the lanes copy, each the pieces that it will
 // read itself.

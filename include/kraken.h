@@ -484,6 +484,7 @@ int kraken_op_paged_append(const kraken_paged_cache *cache, const kraken_paged_a
  * does not exist, or whose n_keys[r] is negative or more than max_pages * page_size; a key whose page does not exist
  * is not visible; all of these raise the status bit.  Table entries of pages wholly in front of the window are of no
  * importance: a server may give these pages back and leave any number there.
+ * Pages, heads or slots of the cache that is read may lie on one another (a stride of 0: one head's keys for all).
  * The keys are shared out evenly over the whole grid, whatever the lengths, and rows that several CTAs worked on are
  * joined by a second kernel through `workspace` (kraken_paged_attention_workspace bytes, 16-byte aligned, contents of
  * no importance; calls that may overlap on the device each need their own).  The result depends on the device's

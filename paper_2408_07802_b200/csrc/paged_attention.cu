@@ -872,9 +872,13 @@ template <int HD>
 int launch(const PagedAttnParams &p, cudaStream_t st) {
     const bool narrow = p.n_head / p.c.n_kv_head <= 8;
     CUtensorMap tm_k, tm_v;
-    if (p.c.page_size % 8 == 0) {
+    // Places of the cache that lie on one another (one head's keys for all, as an expanded tensor) are not a tensor map's: the lanes
+    // copy.  A dimension of one may have any stride.
+    const long long slot = p.c.page_size > 1 ? p.c.slot_stride : HD, head = p.c.n_kv_head > 1 ? p.c.head_stride : HD,
+                    page = p.c.n_pages > 1 ? p.c.page_stride : HD;
+    if (p.c.page_size % 8 == 0 && slot > 0 && head > 0 && page > 0) {
         const uint64_t dims[4] = {(uint64_t)HD, (uint64_t)p.c.page_size, (uint64_t)p.c.n_kv_head, (uint64_t)p.c.n_pages};
-        const uint64_t strides[3] = {(uint64_t)p.c.slot_stride, (uint64_t)p.c.head_stride, (uint64_t)p.c.page_stride};
+        const uint64_t strides[3] = {(uint64_t)slot, (uint64_t)head, (uint64_t)page};
         const uint32_t box[4] = {64, (uint32_t)p.box, 1, 1};
         // (strides that a tensor map cannot hold: the lanes copy)
         if (encode_tma_4d_bf16(&tm_k, p.c.k, dims, strides, box) == KRAKEN_OK &&

@@ -462,6 +462,24 @@ def test_strides_of_dimensions_of_one():
 
 
 @gpu
+@pytest.mark.parametrize("page", [16, 7])
+def test_attention_cache_whose_heads_or_pages_lie_on_one_another(page):
+    """Expanded caches, which are only read: one head's keys for all heads, one page for all pages."""
+    lens = [200, 1, 90, 3000]
+    pages = Pages(44, lens, 1, 64, page, "bf16")
+    q = normal(45, 4, 12, 64).to(torch.bfloat16)
+    n = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    pages.k, pages.v = pages.k.expand(-1, 3, -1, -1), pages.v.expand(-1, 3, -1, -1)
+    out, lse = check_attention(pages, q, n)
+    again, lse2 = kr.op_paged_decode_attention(q, pages.k.contiguous(), pages.v.contiguous(), pages.table, n)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    one = Pages(46, [page], 2, 64, page, "bf16", spare=0)
+    one.k, one.v = one.k.expand(50, -1, -1, -1), one.v.expand(50, -1, -1, -1)
+    one.table = torch.arange(50, dtype=torch.int32, device=DEV).view(2, 25)
+    check_attention(one, q[:2], torch.tensor([25 * page, 3 * page + 1], dtype=torch.int32, device=DEV))
+
+
+@gpu
 def test_calls_on_two_streams_at_once():
     """Calls that overlap on the device, each with its own workspace, eager and as two graphs replayed side by side."""
     sets = []

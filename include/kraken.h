@@ -470,6 +470,20 @@ typedef struct kraken_paged_append_args {
 int kraken_op_paged_append(const kraken_paged_cache *cache, const kraken_paged_append_args *args, uint32_t *d_status,
                            void *stream);
 
+/* kraken_op_paged_append with norms of queries and keys, head by head, before the rotation:
+ *     x_e -> x_e * w_e / sqrt(sum_e x_e^2 / head_dim + eps)      over all head_dim elements of a head, in fp32,
+ * rounded once, after the rotation.  q_weight, k_weight: 16-bit, element e of head h at h * head_stride + e (a head stride of 0:
+ * the same for all heads), or NULL (ones).  The weights must not overlap what the call writes.  Values are copied as they are.
+ * Everything else as there; besides, EINVAL: norm NULL, eps negative or not finite; EUNSUPPORTED: weights that are not 16-byte
+ * aligned, head strides no multiple of 8. */
+typedef struct kraken_paged_norm_args {
+    const void *q_weight;  int64_t q_head_stride;
+    const void *k_weight;  int64_t k_head_stride;
+    float eps;
+} kraken_paged_norm_args;
+int kraken_op_paged_append_norm(const kraken_paged_cache *cache, const kraken_paged_append_args *args,
+                                const kraken_paged_norm_args *norm, uint32_t *d_status, void *stream);
+
 /* Decode-step attention over the pages: row r holds one query per head of sequence row_seq[r] (NULL: sequence r), which
  * sees the n_keys[r] first positions of the sequence, with window > 0 only the last `window` of these.  For key j
  *     x_j = scale * q . k_j;   score_cap > 0:  x_j = score_cap * tanh(x_j / score_cap);
@@ -510,6 +524,45 @@ int kraken_op_paged_attention(const kraken_paged_cache *cache, const kraken_page
 /* Workspace bytes that kraken_op_paged_attention needs on the current device, whatever the lengths (host arithmetic
  * and a device query). */
 int kraken_paged_attention_workspace(int32_t n_head, int32_t n_kv_head, int32_t head_dim, size_t *bytes);
+
+/* Attention of chunks of new tokens over the pages: the rows q_start[c] .. q_start[c + 1] - 1 of q are consecutive tokens of sequence
+ * chunk_seq[c] (NULL: sequence c), the last of them at position n_keys[c] - 1, all of whose keys and values are in the cache
+ * (kraken_op_paged_append puts them there).  A token at position p sees the keys 0 .. p, with window > 0 only the last `window`
+ * of these.  For key j
+ *     x_j = scale * q . k_j;   score_cap > 0:  x_j = score_cap * tanh(x_j / score_cap);   slopes != NULL:  x_j += slopes[h] * (j - p);
+ * (scale * log2(e) and 1 / score_cap have to be finite in fp32, EINVAL otherwise);
+ * out = sum_j softmax(x)_j v_j, and lse (or NULL) = log sum_j exp(x_j).  Query head h reads key/value head
+ * h / (n_head / n_kv_head).  Chunks of one token, of a draft, pieces of prompts and whole prompts may share a call.
+ * A token at a negative position (more tokens than n_keys) sees nothing: out = 0, lse = -inf; so does one all of whose scores are
+ * -inf.  A NaN or +inf among a row's scores makes its out and lse NaN; a value that is not finite makes that element of out
+ * NaN or infinite, of the rows that see its key and no others.
+ * q_start does not descend.  Chunks without rows are skipped.  The rows of a chunk with chunk_seq[c] < 0 (padding), and rows
+ * before q_start[0] and from q_start[chunks] on, are left as they were.  So are those of a chunk whose rows, sequence or n_keys do
+ * not exist (outside 0 .. rows; more than max_pages * page_size keys); a key whose page does not exist is not visible; all of
+ * these raise the status bit.  Table entries of pages wholly in front of what the chunk's first token sees are of no importance.
+ * The weights are rounded to the 16-bit type for the product with the values; maxima and sums are fp32.
+ * The key tiles are shared out evenly over the whole grid; rows that several CTAs worked on are joined by a second kernel through
+ * `workspace` (kraken_paged_chunk_attention_workspace bytes, 16-byte aligned, contents of no importance; calls that may overlap
+ * on the device each need their own).  The result depends on the device's number of SMs and on all the lengths of the call in
+ * its last bits only, and is the same from run to run.
+ * q_start, chunk_seq, n_keys and the page table must not change while the call runs.  A bounded wait that gave up raises bit 1 of
+ * the status word; the outputs then mean nothing.  Rows or heads of out or lse must not lie on one another (EINVAL for a stride
+ * of 0), and none of them may overlap another tensor of the call.
+ * Errors: EINVAL, EUNSUPPORTED (alignment, head_dim; 2^22 rows or chunks), ECAPACITY (workspace_bytes too small), ECUDA. */
+typedef struct kraken_paged_chunk_args {
+    const void *q;  int64_t q_row_stride, q_head_stride;                                    /* [rows][n_head]    */
+    void *out;      int64_t out_row_stride, out_head_stride;                                /* [rows][n_head]    */
+    float *lse;     int64_t lse_row_stride;                                                 /* [rows][n_head]    */
+    const int32_t *chunk_seq, *q_start, *n_keys;          /* int32 [chunks], [chunks + 1], [chunks]       */
+    const float *slopes;                                  /* fp32 [n_head] or NULL                        */
+    void *workspace;  size_t workspace_bytes;
+    float scale, score_cap;
+    int32_t chunks, rows, n_head, window;
+} kraken_paged_chunk_args;
+int kraken_op_paged_chunk_attention(const kraken_paged_cache *cache, const kraken_paged_chunk_args *args,
+                                    uint32_t *d_status, void *stream);
+/* Workspace bytes that kraken_op_paged_chunk_attention needs on the current device, whatever the lengths. */
+int kraken_paged_chunk_attention_workspace(int32_t head_dim, size_t *bytes);
 
 /* Reads rows of logits: with x = scale * logits[r, :] and p = softmax(x),
  *     lse[r] = log sum_j exp(x_j);       logprob[r] = x_target - lse[r]   (0 for a target < 0: not asked for);

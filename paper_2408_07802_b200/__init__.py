@@ -45,7 +45,8 @@ EXPORTS = (
     "kraken_op_decode_attention_static", "kraken_decode_attention_static_capacity", "kraken_storage_dtype",
     "kraken_tuning_set", "kraken_test_wait_limit", "kraken_test_mma_issue_rate",
     "kraken_op_paged_append", "kraken_op_paged_attention", "kraken_paged_attention_workspace",
-    "kraken_op_token_logprobs",
+    "kraken_op_token_logprobs", "kraken_op_paged_append_norm", "kraken_op_paged_chunk_attention",
+    "kraken_paged_chunk_attention_workspace",
 )
 
 TUNE_LN_ROW_KERNEL, TUNE_ATTN_SCHEDULE, TUNE_LN_FUSION, TUNE_LAST_LAYER = 0, 1, 2, 3
@@ -120,6 +121,25 @@ class PagedAttentionArgs(C.Structure):
         ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
         ("scale", C.c_float), ("score_cap", C.c_float),
         ("rows", C.c_int32), ("n_head", C.c_int32), ("window", C.c_int32),
+    ]
+
+
+class PagedNormArgs(C.Structure):
+    _fields_ = [
+        ("q_weight", C.c_void_p), ("q_head_stride", C.c_int64), ("k_weight", C.c_void_p), ("k_head_stride", C.c_int64),
+        ("eps", C.c_float),
+    ]
+
+
+class PagedChunkArgs(C.Structure):
+    _fields_ = [
+        ("q", C.c_void_p), ("q_row_stride", C.c_int64), ("q_head_stride", C.c_int64),
+        ("out", C.c_void_p), ("out_row_stride", C.c_int64), ("out_head_stride", C.c_int64),
+        ("lse", C.c_void_p), ("lse_row_stride", C.c_int64),
+        ("chunk_seq", C.c_void_p), ("q_start", C.c_void_p), ("n_keys", C.c_void_p), ("slopes", C.c_void_p),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+        ("scale", C.c_float), ("score_cap", C.c_float),
+        ("chunks", C.c_int32), ("rows", C.c_int32), ("n_head", C.c_int32), ("window", C.c_int32),
     ]
 
 
@@ -220,6 +240,9 @@ def lib(dtype: Optional[str] = None) -> C.CDLL:
         L.kraken_op_paged_attention.argtypes = [C.POINTER(PagedCacheArgs), C.POINTER(PagedAttentionArgs), vp, vp]
         L.kraken_paged_attention_workspace.argtypes = [i32, i32, i32, C.POINTER(C.c_size_t)]
         L.kraken_op_token_logprobs.argtypes = [C.POINTER(LogprobsArgs), vp, vp]
+        L.kraken_op_paged_append_norm.argtypes = [C.POINTER(PagedCacheArgs), C.POINTER(PagedAppendArgs), C.POINTER(PagedNormArgs), vp, vp]
+        L.kraken_op_paged_chunk_attention.argtypes = [C.POINTER(PagedCacheArgs), C.POINTER(PagedChunkArgs), vp, vp]
+        L.kraken_paged_chunk_attention_workspace.argtypes = [i32, C.POINTER(C.c_size_t)]
         if L.kraken_storage_dtype() != (1 if dtype == "f16" else 0):
             raise RuntimeError(f"{path} was not built for storage dtype {dtype}")
         _libs[dtype] = L
@@ -591,7 +614,8 @@ def _bind(module, dtype: str):
     """Hands the addresses of an image's functions to the marshalling module."""
     L = _libs[dtype]
     module.bind(int(dtype == "f16"), *(C.cast(f, C.c_void_p).value for f in (
-        L.kraken_op_paged_append, L.kraken_op_paged_attention, L.kraken_paged_attention_workspace, L.kraken_op_token_logprobs)))
+        L.kraken_op_paged_append, L.kraken_op_paged_attention, L.kraken_paged_attention_workspace, L.kraken_op_token_logprobs,
+        L.kraken_op_paged_append_norm, L.kraken_op_paged_chunk_attention, L.kraken_paged_chunk_attention_workspace)))
 
 
 def _failed(code: int, what: str, dtype: str, again):
@@ -630,6 +654,23 @@ def op_paged_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_c
     return got[1]
 
 
+def op_paged_append_norm(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                         page_table: torch.Tensor, positions: torch.Tensor, k_weight: Optional[torch.Tensor] = None,
+                         q_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, row_seq: Optional[torch.Tensor] = None,
+                         q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                         inv_freq: Optional[torch.Tensor] = None, interleaved: bool = False,
+                         status: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """op_paged_append with norms (kraken_op_paged_append_norm): the keys and queries of every head are divided by their root
+    mean square, sqrt(mean of the squares + eps), and multiplied by their weights before they are turned, all in one pass.
+    k_weight, q_weight: [head_dim] for all heads or [heads, head_dim], of the caches' type; None: ones."""
+    m = _native or _load_marshal()
+    args = (k, v, k_cache, v_cache, page_table, positions, row_seq, q, q_out, inv_freq, interleaved, status, k_weight, q_weight, eps)
+    got = m.paged_append_norm(*args)
+    if got[0]:
+        got = _failed(got[0], "kraken_op_paged_append_norm", _image_of(k_cache), lambda: m.paged_append_norm(*args))
+    return got[1]
+
+
 def paged_attention_workspace(n_head: int, n_kv_head: int, head_dim: int) -> int:
     """Workspace bytes of op_paged_decode_attention on the current device."""
     n = C.c_size_t(0)
@@ -656,6 +697,34 @@ def op_paged_decode_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: t
     got = m.paged_attention(*args)
     if got[0]:
         got = _failed(got[0], "kraken_op_paged_attention", _image_of(k_cache), lambda: m.paged_attention(*args))
+    return got[1], got[2]
+
+
+def paged_chunk_attention_workspace(head_dim: int) -> int:
+    """Workspace bytes of op_paged_chunk_attention on the current device."""
+    n = C.c_size_t(0)
+    _check(lib().kraken_paged_chunk_attention_workspace(head_dim, C.byref(n)), "kraken_paged_chunk_attention_workspace")
+    return int(n.value)
+
+
+def op_paged_chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor,
+                             q_start: torch.Tensor, n_keys: torch.Tensor, chunk_seq: Optional[torch.Tensor] = None,
+                             scale: Optional[float] = None, score_cap: float = 0.0, window: int = 0,
+                             slopes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                             lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                             status: Optional[torch.Tensor] = None):
+    """Attention of chunks of new tokens over a cache in pages (kraken_op_paged_chunk_attention): rows q_start[c] ..
+    q_start[c + 1] - 1 of q [rows, heads, head_dim] are consecutive tokens of sequence chunk_seq[c] (None: sequence c; negative:
+    padding), the last of them at position n_keys[c] - 1; each sees the cached keys up to its own (which op_paged_append has
+    put there).  Prompts, pieces of them, drafted tokens and single ones may share a call.  scale, score_cap, window, slopes:
+    as for op_paged_decode_attention, seen from each token.  Returns (out, lse): out like q, lse float32 [rows, heads].  Where
+    neither is given they are made, as parts of one allocation: keeping either keeps both (clone the one to be kept), and rows
+    of no chunk hold anything; rows of no chunk in given ones stay as they were."""
+    m = _native or _load_marshal()
+    args = (q, k_cache, v_cache, page_table, q_start, n_keys, chunk_seq, scale, score_cap, window, slopes, out, lse, workspace, status)
+    got = m.paged_chunk(*args)
+    if got[0]:
+        got = _failed(got[0], "kraken_op_paged_chunk_attention", _image_of(k_cache), lambda: m.paged_chunk(*args))
     return got[1], got[2]
 
 

@@ -53,49 +53,6 @@ struct AttnTcArgs {
     uint32_t *status;
 };
 
-// MN-major operand (V: rows = keys, 64 head-dim columns = 128 bytes per row, 128-byte swizzle):
-// groups of 8 keys are 1024 bytes apart (stride byte offset); the next 64 columns of the head
-// dimension live in a separate tile `lbo_bytes` further (leading byte offset).
-__device__ __forceinline__ uint64_t umma_desc_sw128_mnmajor(uint32_t smem_addr, uint32_t lbo_bytes) {
-    uint64_t d = 0;
-    d |= static_cast<uint64_t>((smem_addr & 0x3FFFFu) >> 4);
-    d |= static_cast<uint64_t>((lbo_bytes >> 4) & 0x3FFFu) << 16;
-    d |= static_cast<uint64_t>(1024 >> 4) << 32;
-    d |= static_cast<uint64_t>(1) << 46;
-    d |= static_cast<uint64_t>(2) << 61;
-    return d;
-}
-
-// 32 lanes x 16 columns store
-__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
-}
-
-__device__ __forceinline__ float max3f(float a, float b, float c) {
-    float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
-
-// (x0, x1) * a + b on the packed fp32 pipe
-__device__ __forceinline__ void fma2(float &x0, float &x1, float a, float b) {
-    asm("{\n"
-        ".reg .b64 rx, ra, rb;\n"
-        "mov.b64 rx, {%0, %1};\n"
-        "mov.b64 ra, {%2, %2};\n"
-        "mov.b64 rb, {%3, %3};\n"
-        "fma.rn.f32x2 rx, rx, ra, rb;\n"
-        "mov.b64 {%0, %1}, rx;\n"
-        "}\n"
-        : "+f"(x0), "+f"(x1)
-        : "f"(a), "f"(b));
-}
-
 template <int HD>
 struct AtcCfg {
     static constexpr int HALVES = HD / 64;                 // 64-column (128-byte) pieces of the head dim

@@ -28,6 +28,9 @@ struct Image {
     decltype(&kraken_op_paged_attention) attention;
     decltype(&kraken_paged_attention_workspace) workspace;
     decltype(&kraken_op_token_logprobs) logprobs;
+    decltype(&kraken_op_paged_append_norm) append_norm;
+    decltype(&kraken_op_paged_chunk_attention) chunk;
+    decltype(&kraken_paged_chunk_attention_workspace) chunk_workspace;
 };
 Image images[2];   // bfloat16, half
 
@@ -164,9 +167,23 @@ PyObject *guarded(Py_ssize_t n, Py_ssize_t want, F f) {
     END_HANDLE_TH_ERRORS
 }
 
-// (k, v, k_cache, v_cache, page_table, positions, row_seq, q, q_out, inv_freq, interleaved, status) -> (code, q_out)
-PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 12, [&] {
+// Weights of a norm: [head_dim] for all heads, [heads, head_dim], or None
+const void *norm_weight(PyObject *o, int64_t heads, const Tensor &like, int64_t *head_stride, const char *name) {
+    *head_stride = 0;
+    if (o == Py_None) return nullptr;
+    const Tensor &t = tensor(o, name);
+    if ((t.dim() != 1 && t.dim() != 2) || t.size(-1) != like.size(3) || (t.dim() == 2 && t.size(0) != heads) || t.stride(-1) != 1 ||
+        t.scalar_type() != like.scalar_type() || t.device() != like.device())
+        throw Refused{std::string(name) + " must be [" + std::to_string(like.size(3)) + "] or [" + std::to_string(heads) + ", " +
+                      std::to_string(like.size(3)) + "] of the caches' type and device, contiguous in the last dimension"};
+    if (t.dim() == 2) *head_stride = stride_of(t, 0);
+    return t.data_ptr();
+}
+
+// (k, v, k_cache, v_cache, page_table, positions, row_seq, q, q_out, inv_freq, interleaved, status) and, with norms,
+// (k_weight, q_weight, eps) -> (code, q_out)
+PyObject *append(PyObject *const *a, Py_ssize_t n, bool with_norm) {
+    return guarded(n, with_norm ? 15 : 12, [&] {
         const Tensor &k = tensor(a[0], "k"), &v = tensor(a[1], "v"), &kc = tensor(a[2], "k_cache"), &vc = tensor(a[3], "v_cache");
         const kraken_paged_cache c = paged_cache(kc, vc, tensor(a[4], "page_table"));
         const at::Device device = kc.device();
@@ -212,9 +229,54 @@ PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
         uint32_t *status = status_word(a[11], device);
         const Image &im = images[kc.scalar_type() == at::kHalf];
         if (!im.append) return give(NOT_BOUND, {Tensor()});
+        kraken_paged_norm_args norm = {};
+        if (with_norm) {
+            norm.k_weight = norm_weight(a[12], c.n_kv_head, kc, &norm.k_head_stride, "k_weight");
+            need(a[13] == Py_None || a[7] != Py_None, "q_weight is for queries, and there is no q");
+            if (a[7] != Py_None) norm.q_weight = norm_weight(a[13], g.n_head, kc, &norm.q_head_stride, "q_weight");
+            norm.eps = float_arg(a[14], "eps");
+        }
         c10::cuda::CUDAGuard guard(device);
-        return give(im.append(&c, &g, status, c10::cuda::getCurrentCUDAStream(device.index()).stream()), {out});
+        const cudaStream_t stream = c10::cuda::getCurrentCUDAStream(device.index()).stream();
+        return give(with_norm ? im.append_norm(&c, &g, &norm, status, stream) : im.append(&c, &g, status, stream), {out});
     });
+}
+
+PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) { return append(a, n, false); }
+PyObject *paged_append_norm(PyObject *, PyObject *const *a, Py_ssize_t n) { return append(a, n, true); }
+
+struct Outputs {
+    Tensor out, lse;
+    Rows rows;
+};
+
+// out and lse of an attention call; where the caller brings neither: parts of one tensor
+Outputs outputs(const Tensor &q, const Tensor &cache, int64_t rows, int64_t heads, PyObject *out, PyObject *lse) {
+    Outputs o;
+    const int64_t out_bytes = rows * heads * q.size(2) * 2;
+    Tensor both;
+    if (out == Py_None && lse == Py_None) both = at::empty({out_bytes + rows * heads * 4}, q.options().dtype(at::kByte));
+    o.out = out != Py_None   ? tensor(out, "out")
+            : both.defined() ? part(both, 0, q.scalar_type(), {rows, heads, q.size(2)})
+                             : at::empty({rows, heads, q.size(2)}, q.options());
+    o.rows = rows_of(o.out, rows, heads, cache, "out");
+    o.lse = lse != Py_None   ? tensor(lse, "lse")
+            : both.defined() ? part(both, out_bytes, at::kFloat, {rows, heads})
+                             : at::empty({rows, heads}, q.options().dtype(at::kFloat));
+    const Tensor &l = o.lse;
+    need(l.device() == cache.device() && l.scalar_type() == at::kFloat && l.dim() == 2 && l.size(0) == rows && l.size(1) == heads &&
+             (l.stride(1) == 1 || heads <= 1), "lse must be float32 [rows, heads] on the caches' device, contiguous in the last dimension");
+    return o;
+}
+
+float scale_of(PyObject *o, int head_dim) {
+    return o == Py_None ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(head_dim))) : float_arg(o, "scale");
+}
+
+float cap_of(PyObject *o) {
+    const float cap = float_arg(o, "score_cap");
+    need(cap != 0.f || PyFloat_AsDouble(o) == 0.0, "score_cap is too small for 32 bits");   // (0 is no cap)
+    return cap;
 }
 
 // (q, k_cache, v_cache, page_table, n_keys, row_seq, scale or None, score_cap, window, slopes, out, lse, workspace, status)
@@ -236,33 +298,20 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
         need(a[4] != Py_None, "n_keys are needed");
         g.n_keys = vector<const int32_t>(a[4], at::kInt, rows, device, "n_keys");
         g.row_seq = vector<const int32_t>(a[5], at::kInt, rows, device, "row_seq");
-        g.scale = a[6] == Py_None ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(c.head_dim))) : float_arg(a[6], "scale");
-        g.score_cap = float_arg(a[7], "score_cap");
-        need(g.score_cap != 0.f || PyFloat_AsDouble(a[7]) == 0.0, "score_cap is too small for 32 bits");   // (0 is no cap)
+        g.scale = scale_of(a[6], c.head_dim);
+        g.score_cap = cap_of(a[7]);
         g.window = int_arg(a[8], "window");
         g.slopes = vector<const float>(a[9], at::kFloat, heads, device, "slopes");
         g.rows = to_int32(rows, "the number of rows");
         g.n_head = to_int32(heads, "the number of heads");
         uint32_t *status = status_word(a[13], device);
         c10::cuda::CUDAGuard guard(device);
-        // out and lse where the caller brings neither: parts of one tensor
-        const int64_t out_bytes = rows * heads * q.size(2) * 2;
-        Tensor both;
-        if (a[10] == Py_None && a[11] == Py_None) both = at::empty({out_bytes + rows * heads * 4}, q.options().dtype(at::kByte));
-        const Tensor out = a[10] != Py_None ? tensor(a[10], "out")
-                           : both.defined() ? part(both, 0, q.scalar_type(), {rows, heads, q.size(2)})
-                                            : at::empty({rows, heads, q.size(2)}, q.options());
-        const Rows outr = rows_of(out, rows, heads, kc, "out");
-        g.out = outr.p;
-        g.out_row_stride = outr.row;
-        g.out_head_stride = outr.head;
-        const Tensor lse = a[11] != Py_None ? tensor(a[11], "lse")
-                           : both.defined() ? part(both, out_bytes, at::kFloat, {rows, heads})
-                                            : at::empty({rows, heads}, q.options().dtype(at::kFloat));
-        need(lse.device() == device && lse.scalar_type() == at::kFloat && lse.dim() == 2 && lse.size(0) == rows && lse.size(1) == heads &&
-                 (lse.stride(1) == 1 || heads <= 1), "lse must be float32 [rows, heads] on the caches' device, contiguous in the last dimension");
-        g.lse = static_cast<float *>(lse.data_ptr());
-        g.lse_row_stride = lse.stride(0);
+        const Outputs o = outputs(q, kc, rows, heads, a[10], a[11]);
+        g.out = o.rows.p;
+        g.out_row_stride = o.rows.row;
+        g.out_head_stride = o.rows.head;
+        g.lse = static_cast<float *>(o.lse.data_ptr());
+        g.lse_row_stride = o.lse.stride(0);
         Tensor workspace;
         if (a[12] == Py_None) {
             size_t bytes = 0;
@@ -275,7 +324,61 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
         }
         g.workspace = workspace.data_ptr();
         g.workspace_bytes = workspace.nbytes();
-        return give(im.attention(&c, &g, status, c10::cuda::getCurrentCUDAStream(device.index()).stream()), {out, lse});
+        return give(im.attention(&c, &g, status, c10::cuda::getCurrentCUDAStream(device.index()).stream()), {o.out, o.lse});
+    });
+}
+
+// (q, k_cache, v_cache, page_table, q_start, n_keys, chunk_seq, scale or None, score_cap, window, slopes, out, lse, workspace,
+// status) -> (code, out, lse)
+PyObject *paged_chunk(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 15, [&] {
+        const Tensor &q = tensor(a[0], "q"), &kc = tensor(a[1], "k_cache"), &vc = tensor(a[2], "v_cache");
+        const kraken_paged_cache c = paged_cache(kc, vc, tensor(a[3], "page_table"));
+        const at::Device device = kc.device();
+        need(q.dim() == 3, "q must be [rows, heads, head_dim]");
+        const int64_t rows = q.size(0), heads = q.size(1);
+        const Rows qr = rows_of(q, rows, heads, kc, "q");
+        const Image &im = images[kc.scalar_type() == at::kHalf];
+        if (!im.chunk) return give(NOT_BOUND, {Tensor(), Tensor()});
+        const Tensor &keys = tensor(a[5], "n_keys");
+        need(keys.dim() == 1, "n_keys must be a vector");
+        const int64_t chunks = keys.size(0);
+        kraken_paged_chunk_args g = {};
+        g.q = qr.p;
+        g.q_row_stride = qr.row;
+        g.q_head_stride = qr.head;
+        need(a[4] != Py_None, "q_start is needed");
+        g.q_start = vector<const int32_t>(a[4], at::kInt, chunks + 1, device, "q_start");
+        g.n_keys = vector<const int32_t>(a[5], at::kInt, chunks, device, "n_keys");
+        g.chunk_seq = vector<const int32_t>(a[6], at::kInt, chunks, device, "chunk_seq");
+        g.scale = scale_of(a[7], c.head_dim);
+        g.score_cap = cap_of(a[8]);
+        g.window = int_arg(a[9], "window");
+        g.slopes = vector<const float>(a[10], at::kFloat, heads, device, "slopes");
+        g.chunks = to_int32(chunks, "the number of chunks");
+        g.rows = to_int32(rows, "the number of rows");
+        g.n_head = to_int32(heads, "the number of heads");
+        uint32_t *status = status_word(a[14], device);
+        c10::cuda::CUDAGuard guard(device);
+        const Outputs o = outputs(q, kc, rows, heads, a[11], a[12]);
+        g.out = o.rows.p;
+        g.out_row_stride = o.rows.row;
+        g.out_head_stride = o.rows.head;
+        g.lse = static_cast<float *>(o.lse.data_ptr());
+        g.lse_row_stride = o.lse.stride(0);
+        Tensor workspace;
+        if (a[13] == Py_None) {
+            size_t bytes = 0;
+            const int code = im.chunk_workspace(c.head_dim, &bytes);
+            if (code) return give(code, {Tensor(), Tensor()});
+            workspace = at::empty({static_cast<int64_t>(bytes)}, q.options().dtype(at::kByte));
+        } else {
+            workspace = tensor(a[13], "workspace");
+            need(workspace.device() == device && workspace.is_contiguous(), "workspace must be contiguous, on the caches' device");
+        }
+        g.workspace = workspace.data_ptr();
+        g.workspace_bytes = workspace.nbytes();
+        return give(im.chunk(&c, &g, status, c10::cuda::getCurrentCUDAStream(device.index()).stream()), {o.out, o.lse});
     });
 }
 
@@ -325,14 +428,17 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 
 // (image, addresses of kraken_op_paged_append, kraken_op_paged_attention, kraken_paged_attention_workspace,
-// kraken_op_token_logprobs)
+// kraken_op_token_logprobs, kraken_op_paged_append_norm, kraken_op_paged_chunk_attention, kraken_paged_chunk_attention_workspace)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 5, [&]() -> PyObject * {
+    return guarded(n, 8, [&]() -> PyObject * {
         Image im;
         im.append = reinterpret_cast<decltype(im.append)>(PyLong_AsVoidPtr(a[1]));
         im.attention = reinterpret_cast<decltype(im.attention)>(PyLong_AsVoidPtr(a[2]));
         im.workspace = reinterpret_cast<decltype(im.workspace)>(PyLong_AsVoidPtr(a[3]));
         im.logprobs = reinterpret_cast<decltype(im.logprobs)>(PyLong_AsVoidPtr(a[4]));
+        im.append_norm = reinterpret_cast<decltype(im.append_norm)>(PyLong_AsVoidPtr(a[5]));
+        im.chunk = reinterpret_cast<decltype(im.chunk)>(PyLong_AsVoidPtr(a[6]));
+        im.chunk_workspace = reinterpret_cast<decltype(im.chunk_workspace)>(PyLong_AsVoidPtr(a[7]));
         if (PyErr_Occurred()) throw python_error();
         images[int_arg(a[0], "image") != 0] = im;
         Py_RETURN_NONE;
@@ -341,7 +447,9 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
 
 PyMethodDef methods[] = {
     {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(paged_append)), METH_FASTCALL, nullptr},
+    {"paged_append_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(paged_append_norm)), METH_FASTCALL, nullptr},
     {"paged_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(paged_attention)), METH_FASTCALL, nullptr},
+    {"paged_chunk", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(paged_chunk)), METH_FASTCALL, nullptr},
     {"token_logprobs", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(token_logprobs)), METH_FASTCALL, nullptr},
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(bind)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},

@@ -1,4 +1,4 @@
-// What the kernels on the paged key/value cache share: the cache's description and the checked page lookup.
+// What the kernels on the paged key/value cache share: the cache's description and small helpers.
 #pragma once
 #include "internal.h"
 #include "ptx.cuh"
@@ -36,6 +36,31 @@ inline int paged_view(const kraken_paged_cache *c, PagedView *v) {
     v->max_pages = c->max_pages;
     return KRAKEN_OK;
 }
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.69314718055994531f;
+
+// n / d for 0 <= n < 2^31 by a product: with 2^(s-1) < d <= 2^s, m = floor(2^(31+s) / d) + 1 is off by less than d 2^-(31+s)
+// of itself, which n < 2^31 cannot carry past the next integer.
+struct Divisor {
+    uint32_t m;
+    int s;
+    explicit Divisor(uint32_t d) : m(0), s(0) {
+        if (d == 1) return;
+        int up = 0;
+        while ((1ull << up) < d) ++up;
+        m = static_cast<uint32_t>((1ull << (31 + up)) / d + 1);
+        s = up - 1;
+    }
+    Divisor() = default;
+    __device__ __forceinline__ int quotient(int n) const { return m ? static_cast<int>(__umulhi(n, m) >> s) : n; }
+};
+
+__device__ __forceinline__ void copy16(uint32_t smem, const void *gmem, bool live) {   // zeros where not live
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(gmem), "r"(live ? 16 : 0) : "memory");
+}
+
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * LN2; }
 
 constexpr uint32_t STATUS_BAD_PAGE = KRAKEN_STATUS_BAD_PAGE;
 

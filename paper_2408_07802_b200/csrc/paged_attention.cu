@@ -44,29 +44,11 @@ constexpr int BEGIN = 1;
 // no longer than joining parts (24 sequences of 500 keys, 16 heads of 64: 11.4 against 16.4 us; one sequence: 8.3 against 8.1;
 // with 8 tiles, one sequence of 1000 keys: 12.4 against 8.3).
 constexpr int WHOLE_TILES = 4;
-constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LN2 = 0.69314718055994531f;
 // A weight is 2^(score - m) with m so chosen that the largest of a block is 2^HEADROOM when m is set, and m is raised when a
 // score would get past 2^(HEADROOM + 8).  HEADROOM = 7 in the half image: half numbers end at 2^16 and 2^-24, and weights that
 // round to nothing against the largest one, 10^5 of them, would be missing from the output and not from the sum.
 constexpr float HEADROOM = KRAKEN_F16 ? 7.f : 0.f;
 constexpr float RAISE = HEADROOM + 8.f;
-
-// n / d for 0 <= n < 2^31 by a product: with 2^(s-1) < d <= 2^s, m = floor(2^(31+s) / d) + 1 is off by less than d 2^-(31+s)
-// of itself, which n < 2^31 cannot carry past the next integer.
-struct Divisor {
-    uint32_t m;
-    int s;
-    explicit Divisor(uint32_t d) : m(0), s(0) {
-        if (d == 1) return;
-        int up = 0;
-        while ((1ull << up) < d) ++up;
-        m = static_cast<uint32_t>((1ull << (31 + up)) / d + 1);
-        s = up - 1;
-    }
-    Divisor() = default;
-    __device__ __forceinline__ int quotient(int n) const { return m ? static_cast<int>(__umulhi(n, m) >> s) : n; }
-};
 
 struct PagedAttnParams {
     PagedView c;
@@ -296,12 +278,6 @@ __device__ __forceinline__ void store_pair(const PagedAttnParams &p, int row, in
     const float i0 = l[0] == 0.f ? 0.f : 1.f / l[0], i1 = l[1] == 0.f ? 0.f : 1.f / l[1];
     if (h < heads) *reinterpret_cast<uint32_t *>(out) = pack_h16x2(o.x * i0, o.z * i0);
     if (h + 1 < heads) *reinterpret_cast<uint32_t *>(out + p.out_head) = pack_h16x2(o.y * i1, o.w * i1);
-}
-
-__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * LN2; }
-
-__device__ __forceinline__ void copy16(uint32_t smem, const void *gmem, bool live) {   // zeros where not live
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(gmem), "r"(live ? 16 : 0) : "memory");
 }
 
 // The tiles of a call are added up in the lower bits of a 64-bit number, and the rows that have some above them; a call that might

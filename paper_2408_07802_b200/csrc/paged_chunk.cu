@@ -1,0 +1,1177 @@
+// Attention of chunks of new tokens over a key/value cache in pages, on the sm_100a tensor cores (tcgen05 + TMEM).
+//
+//   x_ij = scale q_i.k_j  [cap tanh(x/cap)]  [+ slope (j - p_i)]  for  p_i - window < j <= p_i,   p_i = n_keys - tokens + i
+//   out_i = sum_j softmax(x_i)_j v_j,   lse_i = log sum_j e^x_ij
+//
+// A work unit is two tiles of query rows of one (chunk, key/value head) against the keys that any of them sees.  A tile has up to
+// 128 rows: 128 / rep consecutive tokens times the rep = n_head / n_kv_head query heads that share the keys, so a few tokens of
+// grouped heads fill it as well as many tokens of single ones, and keys and values are fetched once for all of them.
+//
+//   warp 0      cuts the work, hands the units out (a ring of two in shared memory), looks pages up and starts the copies:
+//               both Q tiles, then per step a stage of V_j and K_{j+1} (two stages)
+//   warp 1      issues the products, per key tile j and query tile w:  S_w = Q_w K_j^T,  O_w (+)= P_w V_j
+//               (P from tensor memory, where it takes the place of S for head dims above 64)
+//   warps 2-3   see to the values of masked tiles; copy what the copy engine cannot (LANES)
+//   warps 4-11  softmax: one thread per query row, warps 4-7 tile 0, warps 8-11 tile 1
+//
+// The maximum in use is only raised when a row's maximum gets past it by more than 8 in the exponent of 2 (numerator and
+// denominator carry the same factor).  P is rounded to 16 bits for the second product, like the output it is summed to; the sum
+// of the weights is fp32 of the unrounded ones.
+//
+// Hidden keys have weight 0, and 0 times a NaN or an infinity is one: in tiles that some row does not see all of ("masked", at
+// both ends of a unit's keys only), values that no row sees are zeroed in shared memory before the product, and values that are
+// not finite are zeroed and noted; rows that do see them get NaN in these elements at the end.
+//
+// The tiles of a call are one line that is cut into equal parts, one for each CTA (one per SM).  A unit cut apart leaves its parts
+// (maximum, sum, output) in the workspace and a second kernel joins them.
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "paged.cuh"
+
+namespace kr {
+
+namespace {
+
+constexpr int TQ = 128;         // rows of a query tile
+constexpr int TK = 128;         // keys of a tile
+constexpr int THREADS = 384, AUX = 64;
+constexpr int SIDE = 3;         // masked tiles at either end of a unit's keys: its tokens' limits span at most 255 keys
+constexpr int BEGIN = 1;        // what beginning and finishing a unit costs, in tiles
+constexpr int MIN_PART = 3;     // places of a CTA at least
+// A weight is 2^(score - m); the first tile's largest is 2^HEADROOM, and m is raised when one gets past 2^(HEADROOM + RAISE).  Half numbers end at 2^16 and 2^-24: with 7, 10^5 weights of 2^-25 of the largest still count.
+constexpr float HEADROOM = KRAKEN_F16 ? 7.f : 0.f;
+constexpr float RAISE = 8.f;
+
+// m: the score that has the weight 2^HEADROOM; l: the sum of the weights
+__device__ __forceinline__ float lse_of_weights(float m, float l) { return l == 0.f ? -INFINITY : m + (log2f(l) - HEADROOM) * LN2; }
+
+struct ChunkParams {
+    PagedView c;
+    const uint16_t *q;
+    uint16_t *out;
+    float *lse;
+    const int *chunk_seq, *q_start, *n_keys;
+    const float *slopes;
+    long long q_row, q_head, out_row, out_head, lse_row;
+    float scale, cap;
+    int chunks, rows, n_head, rep, window, head_dim;
+    int heads;        // query heads of a tile
+    int head_tiles;   // tiles that the heads of a key/value head make
+    int tokens;       // tokens of a tile
+    uint32_t *status;
+    uint8_t *workspace;
+    Divisor by_page, by_heads;
+    int box;          // keys of a copy
+};
+
+// Scores that are more than the product times a positive factor (the instances of the kernel with GENERAL)
+__host__ __device__ inline bool is_general(const ChunkParams &p) { return p.cap > 0.f || p.slopes || !(p.scale > 0.f); }
+
+// Whether a 16-bit number, or one of a pair, is infinite or NaN
+constexpr uint32_t EXPONENT = KRAKEN_F16 ? 0x7C00u : 0x7F80u;
+__device__ __forceinline__ bool odd_h16(uint32_t pair) {
+    return (pair & EXPONENT) == EXPONENT || (pair & (EXPONENT << 16)) == EXPONENT << 16;
+}
+
+// tanh y: from its series up to 1/4 (the first term left out is below 4e-7 of it), else 1 - 2 / (1 + e^2y), whose rounding is up to
+// 2e-7 of 1, so below 1e-6 of it
+__device__ __forceinline__ float tanh_of(float y) {
+    const float y2 = y * y;
+    const float near = y * fmaf(y2, fmaf(y2, fmaf(y2, -0.053968254f, 0.13333333f), -0.33333333f), 1.f);
+    const float far = fmaf(-2.f, rcp_approx(1.f + ex2_approx(y * (2.f * LOG2E))), 1.f);
+    return fabsf(y) < 0.25f ? near : far;
+}
+
+// What a chunk brings
+struct Chunk {
+    int row0, tokens, seq, pos0;   // first row; tokens (0: nothing to do); position of the first token (negative: it sees nothing)
+};
+
+__device__ __forceinline__ Chunk chunk_of(const ChunkParams &p, int c, bool &bad) {
+    Chunk k;
+    k.row0 = p.q_start[c];
+    const int end = p.q_start[c + 1], n = p.n_keys[c];
+    k.seq = p.chunk_seq ? p.chunk_seq[c] : c;
+    k.tokens = 0;
+    k.pos0 = 0;
+    if (k.seq < 0 || (k.row0 == end && end >= 0 && end <= p.rows)) return k;
+    if (k.row0 < 0 || end < k.row0 || end > p.rows || k.seq >= p.c.n_seqs || n < 0 || n > (long long)p.c.max_pages * p.c.page_size) {
+        bad = true;
+        return k;
+    }
+    k.tokens = end - k.row0;
+    k.pos0 = n - k.tokens;
+    return k;
+}
+
+// First key that a query at position `pos` sees (pos may be negative, and then sees none)
+__device__ __forceinline__ int first_seen(const ChunkParams &p, int pos) {
+    return p.window > 0 && pos >= p.window ? pos - p.window + 1 : 0;
+}
+
+// Keys that tokens [t0, t1) of a chunk see: [lo, hi), key tiles [j0, j1)
+struct Span {
+    int lo, hi, j0, j1;
+};
+
+__device__ __forceinline__ Span span_of(const ChunkParams &p, const Chunk &k, int t0, int t1) {
+    Span s;
+    s.hi = max(0, k.pos0 + t1);
+    s.lo = first_seen(p, k.pos0 + t0);
+    if (s.hi <= s.lo) s.hi = s.lo = 0;
+    s.j0 = s.lo / TK;
+    s.j1 = (s.hi + TK - 1) / TK;
+    return s;
+}
+
+// sum over i < n of floor((a i + b) / 128), a <= 256, n < 2^22: the lattice points under a line, by Euclid's steps
+__device__ __forceinline__ long long floors(unsigned n, unsigned a, unsigned b) {
+    unsigned m = TK;
+    long long sum = 0;
+    while (n > 0) {
+        sum += (long long)(n - 1) * n / 2 * (a / m);
+        a %= m;
+        sum += (long long)n * (b / m);
+        b %= m;
+        const unsigned y = a * n + b;
+        if (y < m) break;
+        n = y / m;
+        b = y % m;
+        const unsigned t = m;
+        m = a;
+        a = t;
+    }
+    return sum;
+}
+
+// Tiles of all pairs of query tiles of a chunk (of one head): ceil(hi / 128) - floor(lo / 128) summed, of which all but the last
+// hi and all lo lie on lines
+__device__ __forceinline__ long long chunk_tiles(const ChunkParams &p, const Chunk &k) {
+    const int S = 2 * p.tokens, n = (k.tokens + S - 1) / S;
+    long long sum = 0;
+    // pairs i < n - 1 end at pos0 + (i + 1) S; from i0 on that is above 0
+    const int i0 = k.pos0 >= 0 ? 0 : min(n - 1, -k.pos0 / S);
+    if (n - 1 > i0) sum += floors(n - 1 - i0, S, k.pos0 + (i0 + 1) * S + TK - 1);
+    sum += (max(0, k.pos0 + k.tokens) + TK - 1) / TK;
+    if (p.window > 0) {
+        // pairs begin at pos0 + i S + 1 - window; from i1 on that is at least 0
+        const long long first = (long long)k.pos0 + 1 - p.window, i1 = first >= 0 ? 0 : (S - 1 - first) / S;
+        if (n > i1) sum -= floors(n - (int)i1, S, (unsigned)(first + i1 * S));
+    }
+    return sum;
+}
+
+struct Item {
+    int row0, tokens, pos0, seq, kvh, h0, heads;
+    int t0;              // first token of the pair of query tiles
+    int lo, hi;          // keys that some row of the unit sees
+    int lo_max, hi_min;  // a tile within [lo_max, hi_min) is seen whole by every row
+    int j0, j1;          // key tiles of this CTA's part
+    int a0[2], a1[2];    // of these, those of query tile w
+    int u0;              // first key tile of the unit
+    int r0;              // first masked tile at the far end
+    int part;            // -1: the whole unit; 1: its beginning; 0: what follows
+    int tile0;           // key tiles of this CTA before
+    int last;            // no more items
+    __device__ __forceinline__ bool masked(int j) const { return j * TK < lo_max || (j + 1) * TK > hi_min; }
+    __device__ __forceinline__ int place(int j) const { return (j + 1) * TK > hi_min ? SIDE + j - r0 : j - u0; }
+};
+
+// A unit in parts: who has them and what it is
+struct Joint {
+    int last_cta;   // -1: nothing to join
+    int row0, tokens, t0, h0, heads;
+    int pad[2];
+};
+
+template <int HD>
+struct Cfg {
+    static constexpr int HALVES = HD / 64;
+    static constexpr int TILE_BYTES = TK * 128;            // 128 rows x 64 elements
+    static constexpr int Q_BYTES = HALVES * TILE_BYTES, KV_BYTES = HALVES * TILE_BYTES;
+    static constexpr bool SEPARATE_P = HD <= 64;           // tensor memory has room for P beside S
+    static constexpr int P_COL0 = SEPARATE_P ? 256 : 0, P_STRIDE = SEPARATE_P ? TK / 2 : TK;
+    static constexpr int O_COL0 = SEPARATE_P ? 384 : 256, O_STRIDE = SEPARATE_P ? HD : TK;
+    static constexpr int TMEM_COLS = 512;
+    static constexpr int WORDS = HD / 32;
+    static constexpr int PART_FLOATS = 2 * TQ * (HD + 2);  // [w][HD / 4][128 rows][4] output, [w][m, l][128 rows]
+};
+
+template <int HD>
+struct Smem {
+    uint8_t q[2][Cfg<HD>::Q_BYTES];
+    struct {
+        uint8_t v[Cfg<HD>::KV_BYTES], k[Cfg<HD>::KV_BYTES];
+    } ring[2];
+    uint32_t odd[2][2 * SIDE][TK][Cfg<HD>::WORDS];   // bits of the elements that are not finite, of the item's masked tiles
+    long long at[4][TK];                             // LANES: where a key's row of its page begins, -1: nowhere
+    Item items[2];
+    uint32_t odd_tiles[2][2];                        // which of them have any: [item slot][aux warp]
+    uint32_t visible[4][4], missing[4][2];           // of a tile's keys, those whose page exists; whether any does not
+    uint64_t q_full, q_empty, b_full[2], b_empty[2], s_full[2], p_ready[2], pv_done[2], s_free[2], p_free[2], v_full[2], v_ready[2], item_full[2],
+        item_empty[2];
+    long long sum[THREADS / 32];
+    Chunk cut_chunk[2];
+    long long cut_at[2];
+    int cut_c[2];
+    uint32_t tmem, gave_up;
+};
+
+// A place between two tiles on the line of all tiles
+struct Cut {
+    int c, u, pair, t;   // chunk, unit head, pair of query tiles, tiles of the unit before it
+};
+
+template <int HD, bool GENERAL, bool LANES>
+__global__ void __launch_bounds__(THREADS, 1)
+paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                   const ChunkParams p) {
+    using C = Cfg<HD>;
+    extern __shared__ uint8_t smem_raw[];
+    Smem<HD> &sm = *reinterpret_cast<Smem<HD> *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    volatile uint32_t *gave_up = &sm.gave_up;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        mbar_init(&sm.q_full, LANES ? AUX : 1);
+        mbar_init(&sm.q_empty, 1);
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&sm.b_full[s], LANES ? AUX : 1);
+            mbar_init(&sm.b_empty[s], 1);
+            mbar_init(&sm.s_full[s], 1);
+            mbar_init(&sm.p_ready[s], 4);
+            mbar_init(&sm.pv_done[s], 1);
+            mbar_init(&sm.s_free[s], 4);
+            mbar_init(&sm.p_free[s], 1);
+            mbar_init(&sm.v_full[s], 1);
+            mbar_init(&sm.v_ready[s], 2);
+            mbar_init(&sm.item_full[s], 1);
+            mbar_init(&sm.item_empty[s], 11);   // the issuer, two aux warps, eight softmax warps
+        }
+        sm.gave_up = 0;
+        sm.cut_c[0] = sm.cut_c[1] = p.chunks;
+        fence_barrier_init();
+        if (!LANES) {
+            prefetch_tensormap(&tm_q);
+            prefetch_tensormap(&tm_k);
+            prefetch_tensormap(&tm_v);
+        }
+    }
+    if (warp == 1) {
+        tmem_alloc(&sm.tmem, C::TMEM_COLS);
+        tmem_relinquish();
+    }
+    pdl_wait();
+    const int units = p.c.n_kv_head * p.head_tiles, S = 2 * p.tokens;
+    Joint *joints = reinterpret_cast<Joint *>(p.workspace);
+    float *slots = reinterpret_cast<float *>(p.workspace + sizeof(Joint) * gridDim.x);
+    if (threadIdx.x == 0) joints[blockIdx.x].last_cta = -1;
+
+    // where this CTA's share begins and ends: every thread adds up the places of a run of chunks
+    bool bad = false;
+    auto places = [&](const Chunk &k) -> long long { return chunk_tiles(p, k) + (long long)BEGIN * ((k.tokens + S - 1) / S); };   // of a unit head
+    long long total = 0, n_cta = 0;
+    {
+        const int per = (p.chunks + THREADS - 1) / THREADS;
+        const int c_lo = min(p.chunks, (int)threadIdx.x * per), c_hi = min(p.chunks, c_lo + per);
+        long long mine = 0;
+        for (int c = c_lo; c < c_hi; ++c) {
+            const Chunk k = chunk_of(p, c, bad);
+            if (k.tokens > 0) mine += places(k) * units;
+        }
+        if (bad && blockIdx.x == 0 && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
+        long long upto = mine;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, off);
+            if (lane >= off) upto += v;
+        }
+        if (lane == 31) sm.sum[warp] = upto;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < THREADS / 32; ++w) {
+            if (w < warp) upto += sm.sum[w];
+            total += sm.sum[w];
+        }
+        n_cta = max(1LL, min((long long)gridDim.x, total / MIN_PART));
+        long long before = upto - mine;
+        for (int e = 0; e < 2; ++e) {
+            const long long x = blockIdx.x + e < n_cta ? total * (blockIdx.x + e) / n_cta : total;
+            if (x < before || x >= upto) continue;
+            long long b = before;
+            for (int c = c_lo; c < c_hi; ++c) {
+                const Chunk k = chunk_of(p, c, bad);
+                const long long here = k.tokens > 0 ? places(k) * units : 0;
+                if (x < b + here) {
+                    sm.cut_c[e] = c;
+                    sm.cut_chunk[e] = k;
+                    sm.cut_at[e] = x - b;
+                    break;
+                }
+                b += here;
+            }
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    pdl_trigger();
+    const uint32_t tmem_base = sm.tmem;
+
+    // registers of a thread, of the 168 that it was launched with: 128 x 120 + 256 x 192 = 384 x 168
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
+        if (warp == 0) {
+            // ------------------------------------------------------------------ units and copies
+            const int share = static_cast<int>(min((long long)1 << 28, total / n_cta));
+            const int snap = 2 + share / 16;   // a cut so near to a unit's end goes there: joining costs more than being late
+            auto snapped = [&](int t, int tiles) { return t < snap ? 0 : (tiles - t < snap ? tiles : t); };
+            int end_last = -1;                 // the last CTA that has a part of the unit at the second cut
+            Cut cut[2];
+#pragma unroll 1
+            for (int e = 0; e < 2; ++e) {
+                cut[e].c = sm.cut_c[e];
+                cut[e].u = cut[e].pair = cut[e].t = 0;
+                if (cut[e].c >= p.chunks) continue;
+                const Chunk k = sm.cut_chunk[e];
+                const long long head = places(k), x = sm.cut_at[e];
+                cut[e].u = static_cast<int>(x / head);
+                long long left = x - cut[e].u * head;
+                const int pairs = (k.tokens + S - 1) / S;
+                for (int i0 = 0; i0 < pairs; i0 += 32) {   // 32 pairs at a time
+                    const int i = i0 + lane;
+                    int tiles = 0;
+                    long long upto = 0;
+                    if (i < pairs) {
+                        const Span s = span_of(p, k, i * S, min(k.tokens, (i + 1) * S));
+                        tiles = s.j1 - s.j0;
+                        upto = tiles + BEGIN;
+                    }
+                    const long long mine = upto;
+#pragma unroll
+                    for (int off = 1; off < 32; off <<= 1) {
+                        const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, off);
+                        if (lane >= off) upto += v;
+                    }
+                    const uint32_t found = __ballot_sync(0xFFFFFFFFu, left < upto);
+                    if (found) {
+                        const int l = __ffs(found) - 1;
+                        const int o = __shfl_sync(0xFFFFFFFFu, static_cast<int>(left - (upto - mine)), l);
+                        tiles = __shfl_sync(0xFFFFFFFFu, tiles, l);
+                        cut[e].pair = i0 + l;
+                        cut[e].t = snapped(max(0, o - BEGIN), tiles);
+                        if (e == 1 && cut[1].t > 0 && cut[1].t < tiles) {
+                            // of the cuts after this one, those that lie in the same unit and stay there
+                            const long long x0 = total * (blockIdx.x + 1) / n_cta - o;
+                            for (int c0 = blockIdx.x + 1; c0 < n_cta; c0 += 32) {
+                                const int cta = c0 + lane;
+                                const long long at = total * cta / n_cta - x0;
+                                const int t = at < tiles + BEGIN ? snapped(max(0, static_cast<int>(at) - BEGIN), tiles) : tiles;
+                                const uint32_t in = __ballot_sync(0xFFFFFFFFu, cta < n_cta && t < tiles);
+                                if (in) end_last = c0 + 31 - __clz(in);
+                                if (in != 0xFFFFFFFFu) break;
+                            }
+                        }
+                        break;
+                    }
+                    left -= __shfl_sync(0xFFFFFFFFu, upto, 31);
+                }
+            }
+            bool ok = true;
+            uint32_t n_items = 0, loads = 0, bundles = 0;
+            int tile0 = 0;
+            bool bad_page = false;
+            auto publish = [&](const Item &it) {
+                const int slot = n_items & 1;
+                ok = mbar_wait(&sm.item_empty[slot], ((n_items >> 1) & 1u) ^ 1u, gave_up);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) return;
+                if (lane == 0) {
+                    sm.items[slot] = it;
+                    sm.odd_tiles[slot][0] = sm.odd_tiles[slot][1] = 0;
+                    mbar_arrive(&sm.item_full[slot]);
+                }
+                ++n_items;
+            };
+            Item it;
+            memset(&it, 0, sizeof(it));
+            int c = cut[0].c, u = cut[0].u, pair = cut[0].pair, t = cut[0].t;
+            Chunk k;
+            if (blockIdx.x >= n_cta) c = p.chunks;
+            if (c < p.chunks) k = sm.cut_chunk[0];
+            const int nbox = TK / p.box;
+            while (ok && c < p.chunks) {
+                const bool at_end = c == cut[1].c && u == cut[1].u && pair == cut[1].pair;
+                if (at_end && cut[1].t == 0) break;
+                const int t0 = pair * S, t1 = min(k.tokens, t0 + S);
+                const Span all = span_of(p, k, t0, t1);
+                const int tiles = all.j1 - all.j0, te = at_end ? cut[1].t : tiles;
+                if (te > t || tiles == 0) {
+                    it.row0 = k.row0;
+                    it.tokens = k.tokens;
+                    it.pos0 = k.pos0;
+                    it.seq = k.seq;
+                    it.kvh = u / p.head_tiles;
+                    const int first = u % p.head_tiles * p.heads;
+                    it.h0 = it.kvh * p.rep + first;
+                    it.heads = min(p.heads, p.rep - first);
+                    it.t0 = t0;
+                    it.lo = all.lo;
+                    it.hi = all.hi;
+                    it.lo_max = first_seen(p, k.pos0 + t1 - 1);
+                    it.hi_min = max(0, k.pos0 + t0 + 1);
+                    it.u0 = all.j0;
+                    it.r0 = it.hi_min / TK;
+                    it.j0 = all.j0 + t;
+                    it.j1 = all.j0 + te;
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        const int b = min(t1, t0 + w * p.tokens), e = min(t1, b + p.tokens);
+                        it.a0[w] = it.a1[w] = it.j0;
+                        if (e > b) {
+                            const Span s = span_of(p, k, b, e);
+                            it.a0[w] = max(it.j0, s.j0);
+                            it.a1[w] = max(it.a0[w], min(it.j1, s.j1));
+                        }
+                    }
+                    it.part = te - t == tiles ? -1 : (t == 0 ? 1 : 0);
+                    it.tile0 = tile0;
+                    if (it.part == 1 && lane == 0) {
+                        Joint j;
+                        j.last_cta = end_last;
+                        j.row0 = k.row0;
+                        j.tokens = k.tokens;
+                        j.t0 = t0;
+                        j.h0 = it.h0;
+                        j.heads = it.heads;
+                        j.pad[0] = j.pad[1] = 0;
+                        joints[blockIdx.x] = j;
+                    }
+                    publish(it);
+                    if (!LANES && ok && it.j0 < it.j1) {
+                        // lane i looks up box i of a tile, one step before its copies
+                        const int *table = p.c.table + it.seq * p.c.table_stride;
+                        int page = 0, slot = 0;
+                        auto look_up = [&](int j) {
+                            const int key = j * TK + lane * p.box, n = p.by_page.quotient(key);
+                            slot = key - n * p.c.page_size;
+                            page = p.c.n_pages;   // (nothing there: zeros)
+                            if (lane < nbox && j < it.j1 && key < it.hi && key + p.box > it.lo) page = table[n];
+                        };
+                        auto check = [&](int j) {   // pages that do not exist: their keys are not visible
+                            const bool missing = page < 0 || page > p.c.n_pages || (page == p.c.n_pages && lane < nbox && j < it.j1 &&
+                                                                                   j * TK + lane * p.box < it.hi && j * TK + (lane + 1) * p.box > it.lo);
+                            if (missing) page = p.c.n_pages;
+                            const uint32_t boxes = __ballot_sync(0xFFFFFFFFu, missing);
+                            const int at = (tile0 + j - it.j0) & 3;
+                            if (boxes) {
+                                bad_page = true;
+                                if (lane < 4) {
+                                    uint32_t bits = 0;
+                                    for (int i = 0; i < 32; ++i)
+                                        if (!(boxes >> ((lane * 32 + i) / p.box) & 1)) bits |= 1u << i;
+                                    sm.visible[at][lane] = bits;
+                                }
+                            }
+                            if (lane == 0) {
+                                sm.missing[at][0] = boxes != 0;
+                                sm.missing[at][1] = 0;
+                            }
+                            __syncwarp();
+                        };
+                        look_up(it.j0);
+                        ok = mbar_wait(&sm.q_empty, (loads & 1u) ^ 1u, gave_up);
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        if (!ok) break;
+                        ++loads;
+                        if (lane == 0) {
+                            const bool use[2] = {it.a0[0] < it.a1[0], it.a0[1] < it.a1[1]};
+                            mbar_expect_tx(&sm.q_full, (use[0] + use[1]) * C::HALVES * 128 * p.heads * p.tokens);
+#pragma unroll
+                            for (int w = 0; w < 2; ++w)
+                                if (use[w])
+#pragma unroll
+                                    for (int hf = 0; hf < C::HALVES; ++hf)
+                                        tma_load_4d(sm.q[w] + hf * C::TILE_BYTES, &tm_q, &sm.q_full, hf * 64, it.h0,
+                                                    k.row0 + t0 + w * p.tokens, 0);
+                        }
+                        int v_page = p.c.n_pages, v_slot = 0;
+                        for (int j = it.j0 - 1; j < it.j1; ++j, ++bundles) {
+                            const bool has_v = j >= it.j0, has_k = j + 1 < it.j1;
+                            if (has_k) check(j + 1);
+                            const int k_page = page, k_slot = slot;
+                            look_up(j + 2);
+                            const int st = bundles & 1;
+                            ok = mbar_wait(&sm.b_empty[st], ((bundles >> 1) & 1u) ^ 1u, gave_up);
+                            ok = __all_sync(0xFFFFFFFFu, ok);
+                            if (!ok) break;
+                            // (values of a masked tile go by way of the aux warps)
+                            const bool mend_v = has_v && it.masked(j);
+                            uint64_t *v_bar = mend_v ? &sm.v_full[st] : &sm.b_full[st];
+                            if (lane == 0) {
+                                mbar_expect_tx(&sm.b_full[st], ((has_v && !mend_v) + has_k) * C::KV_BYTES);
+                                if (mend_v) mbar_expect_tx(&sm.v_full[st], C::KV_BYTES);
+                            }
+                            __syncwarp();
+                            if (lane < nbox) {
+#pragma unroll
+                                for (int hf = 0; hf < C::HALVES; ++hf) {
+                                    const int to = hf * C::TILE_BYTES + lane * p.box * 128;
+                                    if (has_k) tma_load_4d(sm.ring[st].k + to, &tm_k, &sm.b_full[st], hf * 64, k_slot, it.kvh, k_page);
+                                    if (has_v) tma_load_4d(sm.ring[st].v + to, &tm_v, v_bar, hf * 64, v_slot, it.kvh, v_page);
+                                }
+                            }
+                            __syncwarp();
+                            v_page = k_page;
+                            v_slot = k_slot;
+                        }
+                    }
+                    tile0 += it.j1 - it.j0;
+                }
+                if (at_end) break;
+                t = 0;
+                if (++pair * S >= k.tokens) {
+                    pair = 0;
+                    if (++u == units) {
+                        u = 0;
+                        k.tokens = 0;
+                        for (int c0 = c + 1; c0 < p.chunks && k.tokens == 0; c0 += 32) {   // the next chunk with tokens
+                            Chunk mine;
+                            mine.row0 = mine.tokens = mine.seq = mine.pos0 = 0;
+                            if (c0 + lane < p.chunks) mine = chunk_of(p, c0 + lane, bad);
+                            const uint32_t any = __ballot_sync(0xFFFFFFFFu, mine.tokens > 0);
+                            const int l = any ? __ffs(any) - 1 : 0;
+                            if (any) c = c0 + l;
+                            k.row0 = __shfl_sync(0xFFFFFFFFu, mine.row0, l);
+                            k.tokens = __shfl_sync(0xFFFFFFFFu, mine.tokens, l);
+                            k.seq = __shfl_sync(0xFFFFFFFFu, mine.seq, l);
+                            k.pos0 = __shfl_sync(0xFFFFFFFFu, mine.pos0, l);
+                        }
+                        if (k.tokens == 0) break;
+                    }
+                }
+            }
+            if (ok) {
+                it.last = 1;
+                publish(it);
+            }
+            if (bad_page && lane == 0 && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
+        } else if (warp == 1) {
+            // ------------------------------------------------------------------ products
+            if (lane == 0) {
+                // head dims below HD: K is zero beyond head_dim
+                const int qk_steps = (p.head_dim + 15) / 16;
+                constexpr uint32_t idesc_qk = umma_idesc_h16(TQ, TK);
+                const uint32_t idesc_pv = umma_idesc_h16(TQ, qk_steps * 16) | (1u << 16);   // V is MN-major
+                auto issue_qk = [&](int w, int st) {
+                    const uint32_t q_addr = smem_u32(sm.q[w]), k_addr = smem_u32(sm.ring[st].k), d_tmem = tmem_base + w * TK;
+#pragma unroll
+                    for (int ks = 0; ks < HD / 16; ++ks) {
+                        if (ks >= qk_steps) break;
+                        const uint32_t off = (ks >> 2) * C::TILE_BYTES + (ks & 3) * 32;
+                        umma_bf16_ss(d_tmem, umma_desc_sw128_kmajor(q_addr + off), umma_desc_sw128_kmajor(k_addr + off), idesc_qk, ks != 0 ? 1u : 0u);
+                    }
+                    umma_commit(&sm.s_full[w]);
+                };
+                auto issue_pv = [&](int w, int st, bool first, bool last) {
+                    const uint32_t v_addr = smem_u32(sm.ring[st].v);
+                    const uint32_t p_tmem = tmem_base + C::P_COL0 + w * C::P_STRIDE, o_tmem = tmem_base + C::O_COL0 + w * C::O_STRIDE;
+#pragma unroll
+                    for (int ks = 0; ks < TK / 16; ++ks)
+                        umma_bf16_ts(o_tmem, p_tmem + ks * 8, umma_desc_sw128_mnmajor(v_addr + ks * 2048, C::TILE_BYTES), idesc_pv,
+                                     (first && ks == 0) ? 0u : 1u);
+                    if (last) umma_commit(&sm.pv_done[w]);
+                    else if (C::SEPARATE_P) umma_commit(&sm.p_free[w]);
+                };
+                bool ok = true;
+                uint32_t n_items = 0, loads = 0, bundles = 0, tile_cnt[2] = {0, 0}, fixes[2] = {0, 0};
+                while (ok) {
+                    const int slot = n_items & 1;
+                    if (!(ok = mbar_wait(&sm.item_full[slot], (n_items >> 1) & 1u, gave_up))) break;
+                    ++n_items;
+                    const Item it = sm.items[slot];
+                    mbar_arrive(&sm.item_empty[slot]);
+                    if (it.last) break;
+                    if (it.j0 >= it.j1) continue;
+                    if (!(ok = mbar_wait(&sm.q_full, loads & 1u, gave_up))) break;
+                    ++loads;
+                    for (int j = it.j0 - 1; ok && j < it.j1; ++j, ++bundles) {
+                        const int st = bundles & 1;
+                        if (!(ok = mbar_wait(&sm.b_full[st], (bundles >> 1) & 1u, gave_up))) break;
+                        if (!LANES && j >= it.j0 && it.masked(j)) {
+                            if (!(ok = mbar_wait(&sm.v_ready[st], fixes[st] & 1u, gave_up))) break;
+                            ++fixes[st];
+                        }
+                        tc_fence_after_sync();
+                        if (C::SEPARATE_P) {
+#pragma unroll
+                            for (int w = 0; w < 2; ++w) {
+                                if (j + 1 >= it.a0[w] && j + 1 < it.a1[w]) {
+                                    // the scores before are in the softmax warps' registers
+                                    if (j >= it.a0[w] && !(ok = mbar_wait(&sm.s_free[w], tile_cnt[w] & 1u, gave_up))) break;
+                                    tc_fence_after_sync();
+                                    issue_qk(w, st);
+                                }
+                            }
+                            if (!ok) break;
+                        }
+#pragma unroll
+                        for (int w = 0; w < 2; ++w) {
+                            if (j >= it.a0[w] && j < it.a1[w]) {
+                                if (!(ok = mbar_wait(&sm.p_ready[w], tile_cnt[w] & 1u, gave_up))) break;
+                                ++tile_cnt[w];
+                                tc_fence_after_sync();
+                                issue_pv(w, st, j == it.a0[w], j + 1 == it.a1[w]);
+                            }
+                            if (!C::SEPARATE_P && j + 1 >= it.a0[w] && j + 1 < it.a1[w]) issue_qk(w, st);
+                        }
+                        if (!ok) break;
+                        umma_commit(&sm.b_empty[st]);
+                        if (j + 2 == it.j1) umma_commit(&sm.q_empty);   // the item's last scores are issued
+                    }
+                }
+            }
+            __syncwarp();
+        } else if (warp < 4) {
+            // ------------------------------------------------------------------ values of masked tiles; copies by lanes
+            const int aux = warp - 2, tid = aux * 32 + lane;
+            bool ok = true, bad_page = false;
+            uint32_t n_items = 0, loads = 0, bundles = 0, fixes[2] = {0, 0};
+            while (ok) {
+                const int slot = n_items & 1;
+                ok = mbar_wait(&sm.item_full[slot], (n_items >> 1) & 1u, gave_up);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                ++n_items;
+                const Item it = sm.items[slot];
+                if (it.last) break;
+                // V_j: rows that nobody sees are zeroed, elements that are not finite zeroed and noted.  Warp `aux` has keys 64 aux ..
+                // + 63; eight lanes have a row's pieces.
+                auto mend = [&](int j, uint8_t *v) {
+                    const int key0 = j * TK + aux * 64, sub = lane >> 3, piece = lane & 7;
+                    bool any = false;
+#pragma unroll 4
+                    for (int i = 0; i < 16 * C::HALVES; ++i) {
+                        const int hf = i >> 4, row = aux * 64 + (i & 15) * 4 + sub, key = key0 + (i & 15) * 4 + sub;
+                        uint4 *at = reinterpret_cast<uint4 *>(v + hf * C::TILE_BYTES + row * 128 + ((piece ^ (row & 7)) * 16));
+                        if (key < it.lo || key >= it.hi) {
+                            *at = make_uint4(0u, 0u, 0u, 0u);
+                        } else {
+                            const uint4 x = *at;
+                            any |= odd_h16(x.x) | odd_h16(x.y) | odd_h16(x.z) | odd_h16(x.w);
+                        }
+                    }
+                    if (__any_sync(0xFFFFFFFFu, any)) {
+                        const int place = it.place(j);
+                        for (int i = lane; i < 64 * C::WORDS; i += 32) {   // a word: 32 elements of a key, four pieces
+                            const int row = aux * 64 + i / C::WORDS, word = i % C::WORDS;
+                            uint32_t bits = 0;
+                            for (int q = 0; q < 4; ++q) {
+                                const int piece = (word & 1) * 4 + q;
+                                uint16_t *at = reinterpret_cast<uint16_t *>(v + (word >> 1) * C::TILE_BYTES + row * 128 + ((piece ^ (row & 7)) * 16));
+                                for (int e = 0; e < 8; ++e)
+                                    if ((at[e] & EXPONENT) == EXPONENT) {
+                                        bits |= 1u << (q * 8 + e);
+                                        at[e] = 0;
+                                    }
+                            }
+                            sm.odd[slot][place][row][word] = bits;
+                        }
+                        if (lane == 0) sm.odd_tiles[slot][aux] |= 1u << place;
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                };
+                if (!LANES) {
+                    for (int j = it.j0; ok && j < it.j1; ++j) {
+                        if (!it.masked(j)) continue;
+                        const int st = (bundles + 1 + j - it.j0) & 1;
+                        ok = mbar_wait(&sm.v_full[st], fixes[st] & 1u, gave_up);
+                        ++fixes[st];
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        if (!ok) break;
+                        mend(j, sm.ring[st].v);
+                        if (lane == 0) mbar_arrive(&sm.v_ready[st]);
+                    }
+                    if (it.j0 < it.j1) bundles += it.j1 - it.j0 + 1;
+                } else if (it.j0 < it.j1) {
+                    ok = mbar_wait(&sm.q_empty, (loads & 1u) ^ 1u, gave_up);
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    if (!ok) break;
+                    ++loads;
+                    const int pieces = p.head_dim / 8;
+                    for (int i = tid; i < 2 * TQ * C::HALVES * 8; i += AUX) {
+                        const int piece = i % (C::HALVES * 8), row = i / (C::HALVES * 8) % TQ, w = i / (C::HALVES * 8 * TQ);
+                        const int token = p.by_heads.quotient(row), g = row - token * p.heads, tk = it.t0 + w * p.tokens + token;
+                        const bool live = token < p.tokens && tk < it.tokens && g < it.heads && piece < pieces;
+                        const uint16_t *src = p.q + (live ? (long long)(it.row0 + tk) * p.q_row + (it.h0 + g) * p.q_head + piece * 8 : 0);
+                        copy16(smem_u32(sm.q[w] + (piece >> 3) * C::TILE_BYTES + row * 128 + (((piece & 7) ^ (row & 7)) * 16)), src, live);
+                    }
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                    fence_proxy_async_smem();
+                    mbar_arrive(&sm.q_full);
+                    const int *table = p.c.table + it.seq * p.c.table_stride;
+                    for (int j = it.j0 - 1; j < it.j1; ++j, ++bundles) {
+                        const bool has_v = j >= it.j0, has_k = j + 1 < it.j1;
+                        const int mark = (it.tile0 + j + 1 - it.j0) & 3;   // of K's tile; V's is the one before
+                        if (has_k) {
+                            // thread t has keys t and t + 64; a warp of 32 keys makes a word
+                            uint32_t words[2];
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const int local = tid + i * 64, key = (j + 1) * TK + local, n = p.by_page.quotient(key);
+                                long long at = -1;
+                                bool missing = false;
+                                if (key >= it.lo && key < it.hi) {
+                                    const int page = table[n];
+                                    missing = page < 0 || page >= p.c.n_pages;
+                                    if (!missing) at = page * p.c.page_stride + (key - n * p.c.page_size) * p.c.slot_stride + it.kvh * p.c.head_stride;
+                                }
+                                sm.at[mark][local] = at;
+                                words[i] = __ballot_sync(0xFFFFFFFFu, missing);
+                            }
+                            if (lane == 0) {
+                                sm.visible[mark][aux] = ~words[0];
+                                sm.visible[mark][2 + aux] = ~words[1];
+                                sm.missing[mark][aux] = (words[0] | words[1]) != 0;
+                            }
+                            bad_page |= (words[0] | words[1]) != 0;
+                        }
+                        asm volatile("bar.sync 1, 64;" ::: "memory");
+                        const int st = bundles & 1;
+                        ok = mbar_wait(&sm.b_empty[st], ((bundles >> 1) & 1u) ^ 1u, gave_up);
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        if (!ok) break;
+                        // a warp has its half of the rows, so that it mends what it copied itself
+#pragma unroll 1
+                        for (int kv = 0; kv < 2; ++kv) {
+                            if (kv ? !has_v : !has_k) continue;
+                            const uint16_t *base = kv ? p.c.v : p.c.k;
+                            uint8_t *to = kv ? sm.ring[st].v : sm.ring[st].k;
+                            const long long *at = sm.at[kv ? (mark + 3) & 3 : mark];
+#pragma unroll 8
+                            for (int i = lane; i < 64 * C::HALVES * 8; i += 32) {
+                                const int piece = i % (C::HALVES * 8), row = aux * 64 + i / (C::HALVES * 8);
+                                const long long a = at[row];
+                                const bool live = a >= 0 && piece < pieces;
+                                copy16(smem_u32(to + (piece >> 3) * C::TILE_BYTES + row * 128 + (((piece & 7) ^ (row & 7)) * 16)),
+                                       base + (live ? a + piece * 8 : 0), live);
+                            }
+                        }
+                        asm volatile("cp.async.wait_all;" ::: "memory");
+                        __syncwarp();
+                        if (has_v && it.masked(j)) mend(j, sm.ring[st].v);
+                        fence_proxy_async_smem();
+                        mbar_arrive(&sm.b_full[st]);
+                    }
+                }
+                if (!ok) break;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.item_empty[slot]);
+            }
+            if (bad_page && lane == 0 && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        // ------------------------------------------------------------------ softmax
+        const int w = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+        const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
+        const uint32_t s_addr = lane_addr + w * TK, p_addr = lane_addr + C::P_COL0 + w * C::P_STRIDE, o_addr = lane_addr + C::O_COL0 + w * C::O_STRIDE;
+        const int token = p.by_heads.quotient(row), g = row - token * p.heads;
+        const float to_log2 = GENERAL ? LOG2E : p.scale * LOG2E, to_score = GENERAL ? 1.f : p.scale;   // of what s holds below
+        bool ok = true;
+        uint32_t n_items = 0, tile_cnt = 0, done_cnt = 0, pf_cnt = 0;
+        while (ok) {
+            const int slot = n_items & 1;
+            ok = mbar_wait(&sm.item_full[slot], (n_items >> 1) & 1u, gave_up);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+            if (!ok) break;
+            ++n_items;
+            const Item &it = sm.items[slot];
+            if (it.last) break;
+            const int tk = it.t0 + w * p.tokens + token, pos = it.pos0 + tk;
+            const bool live = token < p.tokens && tk < it.tokens && g < it.heads;
+            const int hi = live ? max(0, pos + 1) : 0, lo = first_seen(p, pos);
+            const float slope = GENERAL && p.slopes && live ? p.slopes[it.h0 + g] : 0.f;
+            const int a0 = it.a0[w], a1 = it.a1[w];
+            float m = -INFINITY, l = 0.f;
+            for (int j = a0; j < a1; ++j, ++tile_cnt) {
+                ok = mbar_wait(&sm.s_full[w], tile_cnt & 1u, gave_up);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                tc_fence_after_sync();
+                float s[TK];
+#pragma unroll
+                for (int c = 0; c < TK / 32; ++c) tmem_ld_32x32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
+                tmem_ld_wait();
+                if (C::SEPARATE_P) {
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sm.s_free[w]);
+                }
+                if (GENERAL) {
+                    const float back = static_cast<float>(j * TK - pos), inv_cap = 1.f / p.cap;
+#pragma unroll
+                    for (int i = 0; i < TK; ++i) {
+                        float x = s[i] * p.scale;
+                        if (p.cap > 0.f) x = p.cap * tanh_of(x * inv_cap);
+                        s[i] = fmaf(slope, back + i, x);
+                    }
+                }
+                if (it.masked(j)) {
+                    const int from = lo - j * TK, to = hi - j * TK;
+#pragma unroll
+                    for (int i = 0; i < TK; ++i)
+                        if (i < from || i >= to) s[i] = -INFINITY;
+                }
+                const int mark = (it.tile0 + j - it.j0) & 3;
+                if (sm.missing[mark][0] | sm.missing[mark][1]) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t bits = sm.visible[mark][c];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!(bits >> i & 1)) s[c * 32 + i] = -INFINITY;
+                    }
+                }
+                float mc[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    mc[q] = max3f(s[q * 32], s[q * 32 + 1], s[q * 32 + 2]);
+#pragma unroll
+                    for (int i = 3; i + 1 < 32; i += 2) mc[q] = max3f(mc[q], s[q * 32 + i], s[q * 32 + i + 1]);
+                    mc[q] = fmaxf(mc[q], s[q * 32 + 31]);
+                }
+                const float mx = fmaxf(fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3]));
+                bool raise = false;
+                float f = 1.f;
+                if (j == a0) {
+                    m = mx;
+                } else if ((mx - m) * to_log2 > RAISE) {   // (also from -inf; not from -inf to -inf)
+                    raise = true;
+                    f = ex2_approx((m - mx) * to_log2);
+                    m = mx;
+                }
+                float neg = m == -INFINITY ? 0.f : HEADROOM - m * to_log2;
+                if (__any_sync(0xFFFFFFFFu, fabsf(neg) > 65536.f)) {
+                    // scores whose product with log2(e) may be infinite, or further from the rounded one than weights last
+#pragma unroll
+                    for (int i = 0; i < TK; ++i) s[i] -= m == -INFINITY ? 0.f : m;
+                    neg = HEADROOM;
+                }
+                if (C::SEPARATE_P && j > a0) {
+                    ok = mbar_wait(&sm.p_free[w], pf_cnt & 1u, gave_up);
+                    ++pf_cnt;
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                }
+                float sum0 = 0.f, sum1 = 0.f, sum2 = 0.f, sum3 = 0.f;
+#pragma unroll
+                for (int c = 0; c < TK / 32; ++c) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                        float x0 = s[c * 32 + 2 * i], x1 = s[c * 32 + 2 * i + 1], x2 = s[c * 32 + 2 * i + 2], x3 = s[c * 32 + 2 * i + 3];
+                        fma2(x0, x1, to_log2, neg);
+                        fma2(x2, x3, to_log2, neg);
+                        x0 = ex2_approx(x0);
+                        x1 = ex2_approx(x1);
+                        x2 = ex2_approx(x2);
+                        x3 = ex2_approx(x3);
+                        sum0 += x0;
+                        sum1 += x1;
+                        sum2 += x2;
+                        sum3 += x3;
+                        pk[i] = pack_h16x2(x0, x1);
+                        pk[i + 1] = pack_h16x2(x2, x3);
+                    }
+                    tmem_st_32x16(p_addr + c * 16, pk);
+                }
+                l = l * f + ((sum0 + sum1) + (sum2 + sum3));
+                if (__any_sync(0xFFFFFFFFu, raise)) {
+                    // (rare) O_w holds every product issued so far: these scores were committed after the last one, and the next
+                    // one waits for this warp
+#pragma unroll 1
+                    for (int c = 0; c < HD / 32; ++c) {
+                        uint32_t r[32];
+                        tmem_ld_32x32(o_addr + c * 32, r);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
+                        tmem_st_32x32(o_addr + c * 32, r);
+                    }
+                }
+                tmem_st_wait();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.p_ready[w]);
+            }
+            if (!ok) break;
+            if (a0 < a1) {
+                ok = mbar_wait(&sm.pv_done[w], done_cnt & 1u, gave_up);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                ++done_cnt;
+                tc_fence_after_sync();
+            }
+            uint32_t odd[C::WORDS];
+#pragma unroll
+            for (int i = 0; i < C::WORDS; ++i) odd[i] = 0;
+            const uint32_t odd0 = sm.odd_tiles[slot][0], odd1 = sm.odd_tiles[slot][1];
+            if (odd0 | odd1) {   // (rare)
+#pragma unroll 1
+                for (int j = a0; j < a1; ++j) {
+                    if (!it.masked(j)) continue;
+                    const int place = it.place(j);
+#pragma unroll 1
+                    for (int i = 0; i < TK; ++i) {
+                        if (!((i < 64 ? odd0 : odd1) >> place & 1) || j * TK + i < lo || j * TK + i >= hi) continue;
+#pragma unroll
+                        for (int q = 0; q < C::WORDS; ++q) odd[q] |= sm.odd[slot][place][i][q];
+                    }
+                }
+            }
+            const float inv = 1.f / l;
+            const bool empty = l == 0.f;   // (then O may hold anything)
+            uint16_t *dst = p.out + (long long)(it.row0 + tk) * p.out_row + (it.h0 + g) * p.out_head;
+            float *slot_o = slots + ((long long)blockIdx.x * 2 + (it.part & 1)) * C::PART_FLOATS + w * TQ * HD;
+            const bool whole = it.part < 0;
+#pragma unroll
+            for (int c = 0; c < HD / 32; ++c) {
+                uint32_t r[32];
+                if (a0 < a1) {
+                    tmem_ld_32x32(o_addr + c * 32, r);
+                    tmem_ld_wait();
+                }
+                if (odd[c]) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (odd[c] >> i & 1) r[i] = 0x7FFFFFFFu;
+                }
+                if (whole) {
+                    if (live) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (c * 32 + 8 * i >= p.head_dim) break;
+                            uint4 u = make_uint4(0u, 0u, 0u, 0u);
+                            if (!empty) {
+                                u.x = pack_h16x2(__uint_as_float(r[8 * i + 0]) * inv, __uint_as_float(r[8 * i + 1]) * inv);
+                                u.y = pack_h16x2(__uint_as_float(r[8 * i + 2]) * inv, __uint_as_float(r[8 * i + 3]) * inv);
+                                u.z = pack_h16x2(__uint_as_float(r[8 * i + 4]) * inv, __uint_as_float(r[8 * i + 5]) * inv);
+                                u.w = pack_h16x2(__uint_as_float(r[8 * i + 6]) * inv, __uint_as_float(r[8 * i + 7]) * inv);
+                            }
+                            reinterpret_cast<uint4 *>(dst + c * 32)[i] = u;
+                        }
+                    }
+                } else if (live && !empty) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        reinterpret_cast<uint4 *>(slot_o)[(c * 8 + i) * TQ + row] = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+                }
+            }
+            if (live) {
+                if (!whole) {
+                    float *ml = slots + ((long long)blockIdx.x * 2 + (it.part & 1)) * C::PART_FLOATS + 2 * TQ * HD + w * 2 * TQ;
+                    ml[row] = m;
+                    ml[TQ + row] = l;
+                } else if (p.lse) {
+                    p.lse[(long long)(it.row0 + tk) * p.lse_row + it.h0 + g] = lse_of_weights(m * to_score, l);
+                }
+            }
+            // O_w may be overwritten once this warp group has released its next P, which comes later in program order
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.item_empty[slot]);
+        }
+    }
+
+    __syncwarp();
+    if (*gave_up) {
+        for (int i = 0; i < 64; ++i) __nanosleep(10000);
+        if (threadIdx.x == 0 && p.status) atomicOr(p.status, STATUS_WAIT_LIMIT);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 1) tmem_dealloc(tmem_base, C::TMEM_COLS);
+}
+
+// Joins the parts of the units that were cut: out = sum_i o_i 2^(m_i - m) / sum_i l_i 2^(m_i - m).  CTA (i, y) has columns
+// y HD / JOIN_Y .. of the unit that begins in CTA i of the kernel above, if one does; a thread has a row.
+constexpr int JOIN_Y = 8;
+
+template <int HD>
+__global__ void __launch_bounds__(2 * TQ) paged_chunk_join_kernel(const ChunkParams p, int n_cta) {
+    using C = Cfg<HD>;
+    constexpr int Q4 = HD / JOIN_Y / 4;   // groups of four columns
+    pdl_wait();
+    const int begin = blockIdx.x;
+    const Joint u = reinterpret_cast<const Joint *>(p.workspace)[begin];
+    if (u.last_cta < 0) return;
+    const float *slots = reinterpret_cast<const float *>(p.workspace + sizeof(Joint) * n_cta);
+    const int w = threadIdx.x / TQ, row = threadIdx.x % TQ;
+    const int token = p.by_heads.quotient(row), g = row - token * p.heads, tk = u.t0 + w * p.tokens + token;
+    const int e0 = blockIdx.y * (HD / JOIN_Y);
+    if (token >= p.tokens || tk >= u.tokens || g >= u.heads || e0 >= p.head_dim) return;
+    const bool general = is_general(p);
+    const float to_log2 = general ? LOG2E : p.scale * LOG2E, to_score = general ? 1.f : p.scale;
+    auto slot = [&](int i) { return slots + ((long long)i * 2 + (i == begin ? 1 : 0)) * C::PART_FLOATS; };
+    float m = -INFINITY;
+    for (int i = begin; i <= u.last_cta; ++i) {
+        const float *ml = slot(i) + 2 * TQ * HD + w * 2 * TQ;
+        if (ml[TQ + row] != 0.f) m = fmaxf(m, ml[row]);
+    }
+    float l = 0.f, o[Q4 * 4];
+#pragma unroll
+    for (int e = 0; e < Q4 * 4; ++e) o[e] = 0.f;
+#pragma unroll 2
+    for (int i = begin; i <= u.last_cta; ++i) {
+        const float *s = slot(i), *ml = s + 2 * TQ * HD + w * 2 * TQ;
+        const float li = ml[TQ + row];
+        if (li == 0.f) continue;   // (nothing seen: its output was not written)
+        const float f = ex2_approx((ml[row] - m) * to_log2);
+        l += li * f;
+#pragma unroll
+        for (int q = 0; q < Q4; ++q) {
+            const float4 x = reinterpret_cast<const float4 *>(s + w * TQ * HD)[(e0 / 4 + q) * TQ + row];
+            o[4 * q] += x.x * f;
+            o[4 * q + 1] += x.y * f;
+            o[4 * q + 2] += x.z * f;
+            o[4 * q + 3] += x.w * f;
+        }
+    }
+    const long long r = u.row0 + tk;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint16_t *dst = p.out + r * p.out_row + (u.h0 + g) * p.out_head + e0;
+#pragma unroll
+    for (int q = 0; q < Q4; q += 2) {
+        if (e0 + 4 * q >= p.head_dim) break;
+        *reinterpret_cast<uint4 *>(dst + 4 * q) =
+            make_uint4(pack_h16x2(o[4 * q] * inv, o[4 * q + 1] * inv), pack_h16x2(o[4 * q + 2] * inv, o[4 * q + 3] * inv),
+                       pack_h16x2(o[4 * q + 4] * inv, o[4 * q + 5] * inv), pack_h16x2(o[4 * q + 6] * inv, o[4 * q + 7] * inv));
+    }
+    if (p.lse && blockIdx.y == 0) p.lse[r * p.lse_row + u.h0 + g] = lse_of_weights(m * to_score, l);
+}
+
+template <int HD>
+size_t workspace_bytes() {
+    const int sms = sm_count() > 0 ? sm_count() : 148;
+    return (size_t)sms * (sizeof(Joint) + 2 * Cfg<HD>::PART_FLOATS * sizeof(float));
+}
+
+template <int HD, bool GENERAL, bool LANES>
+int launch_form(const ChunkParams &p, const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v, cudaStream_t st) {
+    static DeviceOnce configured;
+    constexpr int SMEM = sizeof(Smem<HD>) + 1024;
+    static_assert(SMEM <= 227 * 1024, "shared memory of a CTA");
+    if (!configured.done()) {
+        int rc = cuda_check(cudaFuncSetAttribute(paged_chunk_kernel<HD, GENERAL, LANES>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM),
+                            "paged chunk attention: shared memory opt-in");
+        if (rc) return rc;
+        configured.set();
+    }
+    const int sms = sm_count();
+    if (sms <= 0) return KRAKEN_ECUDA;
+    // at most so many places: every pair of query tiles against all the keys that the page table has room for
+    const long long pairs = (p.rows + 2 * p.tokens - 1) / (2 * p.tokens) + p.chunks;
+    const long long tiles = ((long long)p.c.max_pages * p.c.page_size + TK - 1) / TK + BEGIN;
+    const int grid = static_cast<int>(std::max(1LL, std::min<long long>(sms, pairs * p.c.n_kv_head * p.head_tiles * tiles / MIN_PART)));
+    int rc = cuda_check(launch_pdl(paged_chunk_kernel<HD, GENERAL, LANES>, dim3(grid), dim3(THREADS), SMEM, st, tm_q, tm_k, tm_v, p),
+                        "paged chunk attention: launch");
+    if (rc || grid == 1) return rc;
+    return cuda_check(launch_pdl(paged_chunk_join_kernel<HD>, dim3(grid, JOIN_Y), dim3(2 * TQ), 0, st, p, grid), "paged chunk attention join: launch");
+}
+
+template <int HD>
+int launch(const ChunkParams &p, cudaStream_t st) {
+    const bool general = is_general(p);
+    CUtensorMap tm_q, tm_k, tm_v;
+    // Strides of 0 and what else a tensor map cannot hold: the lanes copy.  A dimension of one may have any stride.
+    const long long hd = p.head_dim;
+    const long long slot = p.c.page_size > 1 ? p.c.slot_stride : hd, head = p.c.n_kv_head > 1 ? p.c.head_stride : hd,
+                    page = p.c.n_pages > 1 ? p.c.page_stride : hd, q_row = p.rows > 1 ? p.q_row : hd, q_head = p.n_head > 1 ? p.q_head : hd;
+    if (p.c.page_size % 8 == 0 && slot > 0 && head > 0 && page > 0 && q_row > 0 && q_head > 0) {
+        const uint64_t dims[4] = {(uint64_t)hd, (uint64_t)p.c.page_size, (uint64_t)p.c.n_kv_head, (uint64_t)p.c.n_pages};
+        const uint64_t strides[3] = {(uint64_t)slot, (uint64_t)head, (uint64_t)page};
+        const uint32_t box[4] = {64, (uint32_t)p.box, 1, 1};
+        const uint64_t q_dims[4] = {(uint64_t)hd, (uint64_t)p.n_head, (uint64_t)p.rows, 1};
+        const uint64_t q_strides[3] = {(uint64_t)q_head, (uint64_t)q_row, (uint64_t)hd};
+        const uint32_t q_box[4] = {64, (uint32_t)p.heads, (uint32_t)p.tokens, 1};
+        if (encode_tma_4d_bf16(&tm_k, p.c.k, dims, strides, box) == KRAKEN_OK && encode_tma_4d_bf16(&tm_v, p.c.v, dims, strides, box) == KRAKEN_OK &&
+            encode_tma_4d_bf16(&tm_q, p.q, q_dims, q_strides, q_box) == KRAKEN_OK)
+            return general ? launch_form<HD, true, false>(p, tm_q, tm_k, tm_v, st) : launch_form<HD, false, false>(p, tm_q, tm_k, tm_v, st);
+    }
+    memset(&tm_q, 0, sizeof(tm_q));
+    return general ? launch_form<HD, true, true>(p, tm_q, tm_q, tm_q, st) : launch_form<HD, false, true>(p, tm_q, tm_q, tm_q, st);
+}
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+}  // namespace
+
+}  // namespace kr
+
+extern "C" int kraken_paged_chunk_attention_workspace(int32_t head_dim, size_t *bytes) {
+    using namespace kr;
+    if (!bytes) return KRAKEN_EINVAL;
+    if (!decode_head_dim_ok(head_dim)) return KRAKEN_EUNSUPPORTED;
+    *bytes = head_dim <= 64 ? workspace_bytes<64>() : workspace_bytes<128>();
+    return KRAKEN_OK;
+}
+
+extern "C" int kraken_op_paged_chunk_attention(const kraken_paged_cache *cache, const kraken_paged_chunk_args *a, uint32_t *d_status,
+                                               void *stream) {
+    using namespace kr;
+    ChunkParams p;
+    if (!a) return KRAKEN_EINVAL;
+    int rc = paged_view(cache, &p.c);
+    if (rc) return rc;
+    if (a->rows == 0 || a->chunks == 0) return KRAKEN_OK;
+    if (a->rows < 0 || a->chunks < 0 || !a->q || !a->out || !a->q_start || !a->n_keys || a->n_head < 1 || a->n_head % cache->n_kv_head != 0 ||
+        a->window < 0 || !isfinite(a->score_cap) || a->score_cap < 0.f)
+        return KRAKEN_EINVAL;
+    // (factors in the kernel: a score of 0 times an infinite one would be a NaN)
+    if (!isfinite(a->scale * LOG2E) || (a->score_cap > 0.f && !isfinite(1.f / a->score_cap)))
+        return KRAKEN_EINVAL;
+    if (!a->chunk_seq && a->chunks > cache->n_seqs) return KRAKEN_EINVAL;
+    if ((a->rows > 1 && a->out_row_stride == 0) || (a->n_head > 1 && a->out_head_stride == 0) || (a->lse && a->rows > 1 && a->lse_row_stride == 0))
+        return KRAKEN_EINVAL;
+    if (!aligned16(a->q) || !aligned16(a->out) || ((a->q_row_stride | a->q_head_stride | a->out_row_stride | a->out_head_stride) & 7))
+        return KRAKEN_EUNSUPPORTED;
+    if (a->rows >= 1 << 22 || a->chunks >= 1 << 22) return KRAKEN_EUNSUPPORTED;
+    if (!a->workspace || a->workspace_bytes < (cache->head_dim <= 64 ? workspace_bytes<64>() : workspace_bytes<128>())) return KRAKEN_ECAPACITY;
+    if (!aligned16(a->workspace)) return KRAKEN_EINVAL;
+    p.workspace = static_cast<uint8_t *>(a->workspace);
+    p.q = static_cast<const uint16_t *>(a->q);
+    p.out = static_cast<uint16_t *>(a->out);
+    p.lse = a->lse;
+    p.chunk_seq = a->chunk_seq;
+    p.q_start = a->q_start;
+    p.n_keys = a->n_keys;
+    p.slopes = a->slopes;
+    p.q_row = a->q_row_stride;
+    p.q_head = a->q_head_stride;
+    p.out_row = a->out_row_stride;
+    p.out_head = a->out_head_stride;
+    p.lse_row = a->lse_row_stride;
+    p.scale = a->scale;
+    p.cap = a->score_cap;
+    p.chunks = a->chunks;
+    p.rows = a->rows;
+    p.n_head = a->n_head;
+    p.rep = a->n_head / cache->n_kv_head;
+    p.window = a->window;
+    p.head_dim = cache->head_dim;
+    p.head_tiles = (p.rep + TQ - 1) / TQ;
+    p.heads = (p.rep + p.head_tiles - 1) / p.head_tiles;
+    p.tokens = TQ / p.heads;
+    p.status = d_status;
+    p.by_page = Divisor(cache->page_size);
+    p.by_heads = Divisor(p.heads);
+    p.box = 8;
+    while (p.box < TK && cache->page_size % (2 * p.box) == 0) p.box *= 2;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return cache->head_dim <= 64 ? launch<64>(p, st) : launch<128>(p, st);
+}

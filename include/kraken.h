@@ -587,6 +587,37 @@ typedef struct kraken_logprobs_args {
 } kraken_logprobs_args;
 int kraken_op_token_logprobs(const kraken_logprobs_args *args, uint32_t *d_status, void *stream);
 
+/* Draws one token of every row of logits with a given random number.  The logits x of a row in descending order (equal ones by
+ * ascending index), with T the row's temperature and w_i = exp((x_i - x_0) / T):
+ *     top_k > 0:   the first top_k tokens are left;
+ *     min_p > 0:   of these the ones with w_i >= min_p;
+ *     top_p < 1:   of these, with Z the sum of their weights, the ones before which less than top_p * Z lies;
+ * the first token is always left.  With M the sum of the weights left, ids[r] is the first token up to which (it included) more than
+ * uniforms[r] * M lies, and logprob[r] = log(w / M), the logarithm of the probability with which it was drawn.  So a uniform
+ * of 0 gives the likeliest token; a temperature of 0 too, of several the first, with logprob 0.
+ * Weights and sums are formed in 64 bits: the token is the one that the definition gives, but where u * M, top_p * Z or min_p is
+ * within about 1e-13 of a border.
+ * logits: [rows, vocab], row stride in elements, any alignment of the element type; dtype 0 = fp32, 1 = the library's 16-bit type.
+ * temperature, top_k, top_p, min_p: device arrays [rows], or NULL: the value ..._all for every row.  top_k <= 0 or >= vocab, top_p >= 1
+ * and min_p <= 0 are no limit; min_p above 1 counts as 1.  uniforms: fp32 [rows], in [0, 1).
+ * -inf logits (forbidden tokens) are never drawn.  A row that holds a NaN or +inf, or nothing but -inf, whose uniform is not in
+ * [0, 1), whose temperature is negative or not finite, or whose top_p or min_p is NaN, gets the id -1 and a NaN.
+ * ids: int32 [rows]; logprob: fp32 [rows] or NULL; neither overlaps another tensor of the call.
+ * Errors: EINVAL, EUNSUPPORTED (vocab above KRAKEN_SAMPLE_MAX_VOCAB, 2^27 rows), ECUDA. */
+#define KRAKEN_SAMPLE_MAX_VOCAB (1 << 24)
+
+typedef struct kraken_sample_args {
+    const void *logits;  int64_t row_stride;
+    const float *uniforms;                                /* fp32 [rows]                                  */
+    const float *temperature, *top_p, *min_p;             /* fp32 [rows] or NULL                          */
+    const int32_t *top_k;                                 /* int32 [rows] or NULL                         */
+    float temperature_all, top_p_all, min_p_all;
+    int32_t top_k_all;
+    int32_t *ids;  float *logprob;
+    int32_t rows, vocab, dtype;
+} kraken_sample_args;
+int kraken_op_sample_tokens(const kraken_sample_args *args, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -46,7 +46,7 @@ EXPORTS = (
     "kraken_tuning_set", "kraken_test_wait_limit", "kraken_test_mma_issue_rate",
     "kraken_op_paged_append", "kraken_op_paged_attention", "kraken_paged_attention_workspace",
     "kraken_op_token_logprobs", "kraken_op_paged_append_norm", "kraken_op_paged_chunk_attention",
-    "kraken_paged_chunk_attention_workspace",
+    "kraken_paged_chunk_attention_workspace", "kraken_op_sample_tokens",
 )
 
 TUNE_LN_ROW_KERNEL, TUNE_ATTN_SCHEDULE, TUNE_LN_FUSION, TUNE_LAST_LAYER = 0, 1, 2, 3
@@ -152,6 +152,16 @@ class LogprobsArgs(C.Structure):
     ]
 
 
+class SampleArgs(C.Structure):
+    _fields_ = [
+        ("logits", C.c_void_p), ("row_stride", C.c_int64), ("uniforms", C.c_void_p),
+        ("temperature", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p), ("top_k", C.c_void_p),
+        ("temperature_all", C.c_float), ("top_p_all", C.c_float), ("min_p_all", C.c_float), ("top_k_all", C.c_int32),
+        ("ids", C.c_void_p), ("logprob", C.c_void_p),
+        ("rows", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32),
+    ]
+
+
 class KrakenError(RuntimeError):
     def __init__(self, status: int, what: str):
         self.status = status
@@ -243,6 +253,7 @@ def lib(dtype: Optional[str] = None) -> C.CDLL:
         L.kraken_op_paged_append_norm.argtypes = [C.POINTER(PagedCacheArgs), C.POINTER(PagedAppendArgs), C.POINTER(PagedNormArgs), vp, vp]
         L.kraken_op_paged_chunk_attention.argtypes = [C.POINTER(PagedCacheArgs), C.POINTER(PagedChunkArgs), vp, vp]
         L.kraken_paged_chunk_attention_workspace.argtypes = [i32, C.POINTER(C.c_size_t)]
+        L.kraken_op_sample_tokens.argtypes = [C.POINTER(SampleArgs), vp]
         if L.kraken_storage_dtype() != (1 if dtype == "f16" else 0):
             raise RuntimeError(f"{path} was not built for storage dtype {dtype}")
         _libs[dtype] = L
@@ -354,6 +365,23 @@ class KrakenModel:
         following = torch.full_like(tokens, -1)
         following[:, :-1] = tokens[:, 1:]
         return op_token_logprobs(logits, following.view(-1), top=top, scale=scale)
+
+    def generate(self, tokens: torch.Tensor, uniforms: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0) -> "SampledTokens":
+        """Prefill of tokens [batch, seqlen] and one new token of every sequence for each row of uniforms [steps, batch], each
+        drawn by op_sample_tokens (which see for the parameters) and fed to the next decode step.  Nothing waits for the host.
+        ids int32 and logprob float32 [steps, batch]."""
+        steps, b = uniforms.shape
+        assert uniforms.dtype == torch.float32 and uniforms.device == self.device and b == tokens.shape[0]
+        ids = torch.empty(steps, b, dtype=torch.int32, device=self.device)
+        logprob = torch.empty(steps, b, dtype=torch.float32, device=self.device)
+        logits = self.prefill(tokens)
+        for i, u in enumerate(uniforms.contiguous()):
+            if i:
+                self.decode_step(ids[i - 1], logits)
+            got = op_sample_tokens(logits, u, temperature, top_k, top_p, min_p)
+            ids[i].copy_(got.ids)
+            logprob[i].copy_(got.logprob)
+        return SampledTokens(ids, logprob)
 
     def prefill_packed(self, tokens: torch.Tensor, seq_lens, logits: Optional[torch.Tensor] = None) -> torch.Tensor:
         """tokens: device int32 [sum(seq_lens)], the sequences back to back -> fp32 [batch, V] logits of every
@@ -615,7 +643,8 @@ def _bind(module, dtype: str):
     L = _libs[dtype]
     module.bind(int(dtype == "f16"), *(C.cast(f, C.c_void_p).value for f in (
         L.kraken_op_paged_append, L.kraken_op_paged_attention, L.kraken_paged_attention_workspace, L.kraken_op_token_logprobs,
-        L.kraken_op_paged_append_norm, L.kraken_op_paged_chunk_attention, L.kraken_paged_chunk_attention_workspace)))
+        L.kraken_op_paged_append_norm, L.kraken_op_paged_chunk_attention, L.kraken_paged_chunk_attention_workspace,
+        L.kraken_op_sample_tokens)))
 
 
 def _failed(code: int, what: str, dtype: str, again):
@@ -748,6 +777,26 @@ def op_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = No
     if got[0]:
         got = _failed(got[0], "kraken_op_token_logprobs", _image_of(logits), lambda: m.token_logprobs(*args))
     return TokenLogprobs._make(got[1:])
+
+
+class SampledTokens(NamedTuple):
+    ids: torch.Tensor        # int32 [rows]
+    logprob: torch.Tensor    # float32 [rows], log of the probability with which each was drawn
+
+
+def op_sample_tokens(logits: torch.Tensor, uniforms: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0) -> SampledTokens:
+    """Draws one token of every row of logits [rows, vocab] (float32, bfloat16 or float16, any row stride) with the random
+    numbers uniforms (float32 [rows], in [0, 1)) (kraken_op_sample_tokens): after the temperature (0: the likeliest token) the top_k
+    likeliest tokens are left (0: all), of these the ones with at least min_p of the first one's probability, of these the
+    likeliest ones that make top_p of the mass; a uniform of 0 gives the likeliest, one near 1 the least likely token left.
+    temperature, top_p, min_p: a number for all rows or float32 [rows]; top_k: likewise, int32 [rows].  A row without a
+    distribution or with parameters out of range gets the id -1.  The results are parts of one allocation."""
+    m = _native or _load_marshal()
+    args = (logits, uniforms, temperature, top_k, top_p, min_p, _current_dtype == "f16")
+    got = m.sample_tokens(*args)
+    if got[0]:
+        got = _failed(got[0], "kraken_op_sample_tokens", _image_of(logits), lambda: m.sample_tokens(*args))
+    return SampledTokens._make(got[1:])
 
 
 def set_tuning(key: int, value: int) -> None:

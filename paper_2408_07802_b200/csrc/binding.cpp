@@ -31,6 +31,7 @@ struct Image {
     decltype(&kraken_op_paged_append_norm) append_norm;
     decltype(&kraken_op_paged_chunk_attention) chunk;
     decltype(&kraken_paged_chunk_attention_workspace) chunk_workspace;
+    decltype(&kraken_op_sample_tokens) sample;
 };
 Image images[2];   // bfloat16, half
 
@@ -427,10 +428,48 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// (logits, uniforms, temperature, top_k, top_p, min_p: numbers or a tensor each, image for float32) -> (code, ids, logprob)
+PyObject *sample_tokens(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 7, [&] {
+        const Tensor &x = tensor(a[0], "logits");
+        need(x.is_cuda() && x.dim() == 2 && (x.scalar_type() == at::kFloat || is_16bit(x)),
+             "logits must be a CUDA tensor [rows, vocab] of float32 or a 16-bit type");
+        need(x.stride(1) == 1 || x.size(1) <= 1, "logits must be contiguous in the last dimension");
+        const at::Device device = x.device();
+        const int64_t rows = x.size(0);
+        kraken_sample_args g = {};
+        g.logits = x.data_ptr();
+        g.row_stride = x.stride(0);
+        need(a[1] != Py_None, "uniforms are needed");
+        g.uniforms = vector<const float>(a[1], at::kFloat, rows, device, "uniforms");
+        auto either = [&](PyObject *o, const char *name, const float *&each, float &all) {
+            if (THPVariable_Check(o)) each = vector<const float>(o, at::kFloat, rows, device, name);
+            else all = float_arg(o, name);
+        };
+        either(a[2], "temperature", g.temperature, g.temperature_all);
+        if (THPVariable_Check(a[3])) g.top_k = vector<const int32_t>(a[3], at::kInt, rows, device, "top_k");
+        else g.top_k_all = int_arg(a[3], "top_k");
+        either(a[4], "top_p", g.top_p, g.top_p_all);
+        either(a[5], "min_p", g.min_p, g.min_p_all);
+        g.rows = to_int32(rows, "the number of rows");
+        g.vocab = to_int32(x.size(1), "the vocabulary");
+        g.dtype = x.scalar_type() != at::kFloat;
+        const Image &im = images[g.dtype ? x.scalar_type() == at::kHalf : int_arg(a[6], "image") != 0];
+        if (!im.sample) return give(NOT_BOUND, {Tensor(), Tensor()});
+        c10::cuda::CUDAGuard guard(device);
+        const Tensor bytes = at::empty({8 * rows}, x.options().dtype(at::kByte));
+        const Tensor ids = part(bytes, 0, at::kInt, {rows}), logprob = part(bytes, 4 * rows, at::kFloat, {rows});
+        g.ids = static_cast<int32_t *>(ids.data_ptr());
+        g.logprob = static_cast<float *>(logprob.data_ptr());
+        return give(im.sample(&g, c10::cuda::getCurrentCUDAStream(device.index()).stream()), {ids, logprob});
+    });
+}
+
 // (image, addresses of kraken_op_paged_append, kraken_op_paged_attention, kraken_paged_attention_workspace,
-// kraken_op_token_logprobs, kraken_op_paged_append_norm, kraken_op_paged_chunk_attention, kraken_paged_chunk_attention_workspace)
+// kraken_op_token_logprobs, kraken_op_paged_append_norm, kraken_op_paged_chunk_attention, kraken_paged_chunk_attention_workspace,
+// kraken_op_sample_tokens)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 8, [&]() -> PyObject * {
+    return guarded(n, 9, [&]() -> PyObject * {
         Image im;
         im.append = reinterpret_cast<decltype(im.append)>(PyLong_AsVoidPtr(a[1]));
         im.attention = reinterpret_cast<decltype(im.attention)>(PyLong_AsVoidPtr(a[2]));
@@ -439,6 +478,7 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
         im.append_norm = reinterpret_cast<decltype(im.append_norm)>(PyLong_AsVoidPtr(a[5]));
         im.chunk = reinterpret_cast<decltype(im.chunk)>(PyLong_AsVoidPtr(a[6]));
         im.chunk_workspace = reinterpret_cast<decltype(im.chunk_workspace)>(PyLong_AsVoidPtr(a[7]));
+        im.sample = reinterpret_cast<decltype(im.sample)>(PyLong_AsVoidPtr(a[8]));
         if (PyErr_Occurred()) throw python_error();
         images[int_arg(a[0], "image") != 0] = im;
         Py_RETURN_NONE;
@@ -451,6 +491,7 @@ PyMethodDef methods[] = {
     {"paged_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(paged_attention)), METH_FASTCALL, nullptr},
     {"paged_chunk", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(paged_chunk)), METH_FASTCALL, nullptr},
     {"token_logprobs", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(token_logprobs)), METH_FASTCALL, nullptr},
+    {"sample_tokens", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(sample_tokens)), METH_FASTCALL, nullptr},
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(bind)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -548,7 +548,8 @@ int kraken_paged_attention_workspace(int32_t n_head, int32_t n_kv_head, int32_t 
  * q_start, chunk_seq, n_keys and the page table must not change while the call runs.  A bounded wait that gave up raises bit 1 of
  * the status word; the outputs then mean nothing.  Rows or heads of out or lse must not lie on one another (EINVAL for a stride
  * of 0), and none of them may overlap another tensor of the call.
- * Errors: EINVAL, EUNSUPPORTED (alignment, head_dim; 2^22 rows or chunks), ECAPACITY (workspace_bytes too small), ECUDA. */
+ * Errors: EINVAL, EUNSUPPORTED (alignment, head_dim; 2^22 rows or chunks; so many rows, chunks and
+ * positions that the page table has room for that their tiles, two for up to 256 query rows and 128 keys, might be 2^31), ECAPACITY (workspace_bytes too small), ECUDA. */
 typedef struct kraken_paged_chunk_args {
     const void *q;  int64_t q_row_stride, q_head_stride;                                    /* [rows][n_head]    */
     void *out;      int64_t out_row_stride, out_head_stride;                                /* [rows][n_head]    */

@@ -100,12 +100,6 @@ struct Sums {
     }
 };
 
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-
 template <int T>
 struct Smem {
     Key aside[Shape<T>::ASIDE];

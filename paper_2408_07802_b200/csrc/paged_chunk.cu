@@ -70,20 +70,29 @@ struct ChunkParams {
 // Scores that are more than the product times a positive factor (the instances of the kernel with GENERAL)
 __host__ __device__ inline bool is_general(const ChunkParams &p) { return p.cap > 0.f || p.slopes || !(p.scale > 0.f); }
 
+// The n lowest bits (none for n <= 0, all for n >= 32)
+__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u); }
+
 // Whether a 16-bit number, or one of a pair, is infinite or NaN
 constexpr uint32_t EXPONENT = KRAKEN_F16 ? 0x7C00u : 0x7F80u;
 __device__ __forceinline__ bool odd_h16(uint32_t pair) {
     return (pair & EXPONENT) == EXPONENT || (pair & (EXPONENT << 16)) == EXPONENT << 16;
 }
 
-// tanh y: from its series up to 1/4 (the first term left out is below 4e-7 of it), else 1 - 2 / (1 + e^2y), whose rounding is up to
-// 2e-7 of 1, so below 1e-6 of it
-__device__ __forceinline__ float tanh_of(float y) {
-    const float y2 = y * y;
-    const float near = y * fmaf(y2, fmaf(y2, fmaf(y2, -0.053968254f, 0.13333333f), -0.33333333f), 1.f);
-    const float far = fmaf(-2.f, rcp_approx(1.f + ex2_approx(y * (2.f * LOG2E))), 1.f);
-    return fabsf(y) < 0.25f ? near : far;
+// x -> cap tanh(x scale / cap), to_cap = scale / cap, for |x to_cap| <= 1/2: an odd polynomial of degree 9 fitted to tanh there
+// (to 1.4e-8 of it, 1.2e-7 with the roundings)
+__device__ __forceinline__ void tanh_near(float (&s)[TK], float to_cap, float scale) {
+    const float q = to_cap * to_cap;
+    const uint64_t c4 = splat2(0.017135004f * scale * q * q * q * q), c3 = splat2(-0.052986074f * scale * q * q * q),
+                   c2 = splat2(0.13324779f * scale * q * q), c1 = splat2(-0.33333069f * scale * q), c0 = splat2(scale);
+#pragma unroll
+    for (int i = 0; i < TK; i += 2) {
+        const uint64_t x = pk2(s[i], s[i + 1]), y = mul2(x, x);
+        upk2(mul2(x, fma2(y, fma2(y, fma2(y, fma2(y, c4, c3), c2), c1), c0)), s[i], s[i + 1]);
+    }
 }
+// cap tanh(y / 2 log2(e)) = cap - 2 cap / (1 + 2^y), off by up to 2e-7 cap
+__device__ __forceinline__ float tanh_far(float y, float cap) { return fmaf(-2.f * cap, rcp_approx(1.f + ex2_approx(y)), cap); }
 
 // What a chunk brings
 struct Chunk {
@@ -147,21 +156,37 @@ __device__ __forceinline__ long long floors(unsigned n, unsigned a, unsigned b) 
     return sum;
 }
 
-// Tiles of all pairs of query tiles of a chunk (of one head): ceil(hi / 128) - floor(lo / 128) summed, of which all but the last
-// hi and all lo lie on lines
-__device__ __forceinline__ long long chunk_tiles(const ChunkParams &p, const Chunk &k) {
+// Places of all pairs of query tiles of a chunk (of one head): ceil(hi / 128) - floor(lo / 128) + BEGIN summed, of which all but the
+// last hi and all lo lie on lines
+__device__ __forceinline__ int chunk_places(const ChunkParams &p, const Chunk &k) {
     const int S = 2 * p.tokens, n = (k.tokens + S - 1) / S;
-    long long sum = 0;
+    if (n <= 2) {
+        int sum = 0;
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            const Span s = span_of(p, k, i * S, min(k.tokens, (i + 1) * S));
+            sum += s.j1 - s.j0 + BEGIN;
+        }
+        return sum;
+    }
+    long long sum = (long long)n * BEGIN;
     // pairs i < n - 1 end at pos0 + (i + 1) S; from i0 on that is above 0
     const int i0 = k.pos0 >= 0 ? 0 : min(n - 1, -k.pos0 / S);
-    if (n - 1 > i0) sum += floors(n - 1 - i0, S, k.pos0 + (i0 + 1) * S + TK - 1);
-    sum += (max(0, k.pos0 + k.tokens) + TK - 1) / TK;
+    int from[2] = {i0, n};
+    unsigned at[2] = {(unsigned)(k.pos0 + (i0 + 1) * S + TK - 1), 0u};
     if (p.window > 0) {
         // pairs begin at pos0 + i S + 1 - window; from i1 on that is at least 0
         const long long first = (long long)k.pos0 + 1 - p.window, i1 = first >= 0 ? 0 : (S - 1 - first) / S;
-        if (n > i1) sum -= floors(n - (int)i1, S, (unsigned)(first + i1 * S));
+        from[1] = (int)min((long long)n, i1);
+        at[1] = (unsigned)(first + i1 * S);
     }
-    return sum;
+#pragma unroll 1
+    for (int e = 0; e < 2; ++e) {
+        const int many = (e ? n : n - 1) - (e ? from[1] : from[0]);
+        const long long part = many > 0 ? floors(many, S, e ? at[1] : at[0]) : 0;
+        sum += e ? -part : part;
+    }
+    return static_cast<int>(sum + (max(0, k.pos0 + k.tokens) + TK - 1) / TK);   // (all chunks' together are below 2^31)
 }
 
 struct Item {
@@ -185,6 +210,11 @@ struct Joint {
     int last_cta;   // -1: nothing to join
     int row0, tokens, t0, h0, heads;
     int pad[2];
+};
+
+// A place between two tiles on the line of all tiles
+struct Cut {
+    int u, c, pair, t;   // unit head (all: the end), chunk, pair of query tiles, tiles of the unit before it
 };
 
 template <int HD>
@@ -213,16 +243,11 @@ struct Smem {
     uint32_t visible[4][4], missing[4][2];           // of a tile's keys, those whose page exists; whether any does not
     uint64_t q_full, q_empty, b_full[2], b_empty[2], s_full[2], p_ready[2], pv_done[2], s_free[2], p_free[2], v_full[2], v_ready[2], item_full[2],
         item_empty[2];
-    long long sum[THREADS / 32];
+    uint32_t upto[THREADS], sum[THREADS / 32];
     Chunk cut_chunk[2];
-    long long cut_at[2];
-    int cut_c[2];
+    Cut cut[2];
+    int end_last;
     uint32_t tmem, gave_up;
-};
-
-// A place between two tiles on the line of all tiles
-struct Cut {
-    int c, u, pair, t;   // chunk, unit head, pair of query tiles, tiles of the unit before it
 };
 
 template <int HD, bool GENERAL, bool LANES>
@@ -251,7 +276,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             mbar_init(&sm.item_empty[s], 11);   // the issuer, two aux warps, eight softmax warps
         }
         sm.gave_up = 0;
-        sm.cut_c[0] = sm.cut_c[1] = p.chunks;
         fence_barrier_init();
         if (!LANES) {
             prefetch_tensormap(&tm_q);
@@ -269,49 +293,110 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     float *slots = reinterpret_cast<float *>(p.workspace + sizeof(Joint) * gridDim.x);
     if (threadIdx.x == 0) joints[blockIdx.x].last_cta = -1;
 
-    // where this CTA's share begins and ends: every thread adds up the places of a run of chunks
+    // The line: head by head, of each the chunks in order, of each its pairs of query tiles, of each BEGIN places and then one for every
+    // key tile.  CTA i of n has the places from x_i = floor(total / n) i + min(i, total mod n) on.
     bool bad = false;
-    auto places = [&](const Chunk &k) -> long long { return chunk_tiles(p, k) + (long long)BEGIN * ((k.tokens + S - 1) / S); };   // of a unit head
-    long long total = 0, n_cta = 0;
+    uint32_t per_head;
+    const int run = (p.chunks + THREADS - 1) / THREADS;   // chunks that a thread adds up
     {
-        const int per = (p.chunks + THREADS - 1) / THREADS;
-        const int c_lo = min(p.chunks, (int)threadIdx.x * per), c_hi = min(p.chunks, c_lo + per);
-        long long mine = 0;
+        const int c_lo = min(p.chunks, (int)threadIdx.x * run), c_hi = min(p.chunks, c_lo + run);
+        uint32_t upto = 0;
+#pragma unroll 1
         for (int c = c_lo; c < c_hi; ++c) {
             const Chunk k = chunk_of(p, c, bad);
-            if (k.tokens > 0) mine += places(k) * units;
+            if (k.tokens > 0) upto += chunk_places(p, k);
         }
         if (bad && blockIdx.x == 0 && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
-        long long upto = mine;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
-            const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, off);
+            const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, upto, off);
             if (lane >= off) upto += v;
         }
         if (lane == 31) sm.sum[warp] = upto;
+        sm.upto[threadIdx.x] = upto;   // of the warp
         __syncthreads();
+    }
+    if (warp < 2) {   // where this CTA's share begins (warp 0) and ends (warp 1)
+        uint32_t warps = lane < THREADS / 32 ? sm.sum[lane] : 0u;
 #pragma unroll
-        for (int w = 0; w < THREADS / 32; ++w) {
-            if (w < warp) upto += sm.sum[w];
-            total += sm.sum[w];
+        for (int off = 1; off < 16; off <<= 1) {
+            const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, warps, off);
+            if (lane >= off) warps += v;
         }
-        n_cta = max(1LL, min((long long)gridDim.x, total / MIN_PART));
-        long long before = upto - mine;
-        for (int e = 0; e < 2; ++e) {
-            const long long x = blockIdx.x + e < n_cta ? total * (blockIdx.x + e) / n_cta : total;
-            if (x < before || x >= upto) continue;
-            long long b = before;
-            for (int c = c_lo; c < c_hi; ++c) {
-                const Chunk k = chunk_of(p, c, bad);
-                const long long here = k.tokens > 0 ? places(k) * units : 0;
-                if (x < b + here) {
-                    sm.cut_c[e] = c;
-                    sm.cut_chunk[e] = k;
-                    sm.cut_at[e] = x - b;
+        per_head = __shfl_sync(0xFFFFFFFFu, warps, THREADS / 32 - 1);
+        const unsigned long long total = (unsigned long long)per_head * units;
+        const int n_cta = static_cast<int>(max(1ull, min((unsigned long long)gridDim.x, total / MIN_PART)));
+        const unsigned long long share = total >> 32 ? total / n_cta : (uint32_t)total / (uint32_t)n_cta, rest = total - share * n_cta;
+        auto place = [&](int cta) { return share * cta + min((unsigned long long)cta, rest); };
+        // a cut so near to a unit's end goes there: joining costs more than being late
+        const int snap = 2 + static_cast<int>(min(share, 1ull << 20)) / 16;
+        auto snapped = [&](int t, int tiles) { return t < snap ? 0 : (tiles - t < snap ? tiles : t); };
+        Cut cut = {units, 0, 0, 0};
+        int end_last = -1;   // the last CTA that has a part of the unit at the second cut
+        const int cta = blockIdx.x + warp;
+        if (cta < n_cta && per_head > 0) {
+            const unsigned long long x = place(cta);
+            cut.u = x >> 32 ? static_cast<int>(x / per_head) : static_cast<int>((uint32_t)x / per_head);
+            uint32_t left = static_cast<uint32_t>(x - (unsigned long long)cut.u * per_head);
+            // the warp, the thread and the chunk
+            const int w = __ffs(__ballot_sync(0xFFFFFFFFu, warps > left)) - 1;
+            left -= w ? __shfl_sync(0xFFFFFFFFu, warps, w - 1) : 0u;
+            const uint32_t upto = sm.upto[w * 32 + lane];
+            const int t = __ffs(__ballot_sync(0xFFFFFFFFu, upto > left)) - 1;
+            left -= t ? __shfl_sync(0xFFFFFFFFu, upto, t - 1) : 0u;
+            Chunk k;
+#pragma unroll 1
+            for (cut.c = (w * 32 + t) * run;; ++cut.c) {
+                k = chunk_of(p, cut.c, bad);
+                if (run == 1) break;
+                const uint32_t here = k.tokens > 0 ? chunk_places(p, k) : 0;
+                if (left < here) break;
+                left -= here;
+            }
+#pragma unroll 1
+            for (int i0 = 0;; i0 += 32) {   // 32 pairs at a time
+                const int i = i0 + lane;
+                int tiles = 0;
+                uint32_t up = 0;
+                if (i * S < k.tokens) {
+                    const Span s = span_of(p, k, i * S, min(k.tokens, (i + 1) * S));
+                    tiles = s.j1 - s.j0;
+                    up = tiles + BEGIN;
+                }
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, up, off);
+                    if (lane >= off) up += v;
+                }
+                const uint32_t found = __ballot_sync(0xFFFFFFFFu, left < up);
+                if (found) {
+                    const int l = __ffs(found) - 1;
+                    tiles = __shfl_sync(0xFFFFFFFFu, tiles, l);
+                    const int o = left - (__shfl_sync(0xFFFFFFFFu, up, l) - tiles - BEGIN);
+                    cut.pair = i0 + l;
+                    cut.t = snapped(max(0, o - BEGIN), tiles);
+                    if (warp == 1 && cut.t > 0 && cut.t < tiles) {
+                        // of the cuts after this one, those that lie in the same unit and stay there
+                        const unsigned long long x0 = x - o;
+#pragma unroll 1
+                        for (int c0 = cta; c0 < n_cta; c0 += 32) {
+                            const unsigned long long at = place(c0 + lane) - x0;
+                            const int t = at < tiles + BEGIN ? snapped(max(0, static_cast<int>(at) - BEGIN), tiles) : tiles;
+                            const uint32_t in = __ballot_sync(0xFFFFFFFFu, c0 + lane < n_cta && t < tiles);
+                            if (in) end_last = c0 + 31 - __clz(in);
+                            if (in != 0xFFFFFFFFu) break;
+                        }
+                    }
                     break;
                 }
-                b += here;
+                left -= __shfl_sync(0xFFFFFFFFu, up, 31);
+                if ((i0 + 32) * S >= k.tokens) break;   // (the lengths changed under the kernel)
             }
+            if (lane == 0) sm.cut_chunk[warp] = k;
+        }
+        if (lane == 0) {
+            sm.cut[warp] = cut;
+            if (warp == 1) sm.end_last = end_last;
         }
     }
     tc_fence_before_sync();
@@ -325,60 +410,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
         if (warp == 0) {
             // ------------------------------------------------------------------ units and copies
-            const int share = static_cast<int>(min((long long)1 << 28, total / n_cta));
-            const int snap = 2 + share / 16;   // a cut so near to a unit's end goes there: joining costs more than being late
-            auto snapped = [&](int t, int tiles) { return t < snap ? 0 : (tiles - t < snap ? tiles : t); };
-            int end_last = -1;                 // the last CTA that has a part of the unit at the second cut
-            Cut cut[2];
-#pragma unroll 1
-            for (int e = 0; e < 2; ++e) {
-                cut[e].c = sm.cut_c[e];
-                cut[e].u = cut[e].pair = cut[e].t = 0;
-                if (cut[e].c >= p.chunks) continue;
-                const Chunk k = sm.cut_chunk[e];
-                const long long head = places(k), x = sm.cut_at[e];
-                cut[e].u = static_cast<int>(x / head);
-                long long left = x - cut[e].u * head;
-                const int pairs = (k.tokens + S - 1) / S;
-                for (int i0 = 0; i0 < pairs; i0 += 32) {   // 32 pairs at a time
-                    const int i = i0 + lane;
-                    int tiles = 0;
-                    long long upto = 0;
-                    if (i < pairs) {
-                        const Span s = span_of(p, k, i * S, min(k.tokens, (i + 1) * S));
-                        tiles = s.j1 - s.j0;
-                        upto = tiles + BEGIN;
-                    }
-                    const long long mine = upto;
-#pragma unroll
-                    for (int off = 1; off < 32; off <<= 1) {
-                        const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, off);
-                        if (lane >= off) upto += v;
-                    }
-                    const uint32_t found = __ballot_sync(0xFFFFFFFFu, left < upto);
-                    if (found) {
-                        const int l = __ffs(found) - 1;
-                        const int o = __shfl_sync(0xFFFFFFFFu, static_cast<int>(left - (upto - mine)), l);
-                        tiles = __shfl_sync(0xFFFFFFFFu, tiles, l);
-                        cut[e].pair = i0 + l;
-                        cut[e].t = snapped(max(0, o - BEGIN), tiles);
-                        if (e == 1 && cut[1].t > 0 && cut[1].t < tiles) {
-                            // of the cuts after this one, those that lie in the same unit and stay there
-                            const long long x0 = total * (blockIdx.x + 1) / n_cta - o;
-                            for (int c0 = blockIdx.x + 1; c0 < n_cta; c0 += 32) {
-                                const int cta = c0 + lane;
-                                const long long at = total * cta / n_cta - x0;
-                                const int t = at < tiles + BEGIN ? snapped(max(0, static_cast<int>(at) - BEGIN), tiles) : tiles;
-                                const uint32_t in = __ballot_sync(0xFFFFFFFFu, cta < n_cta && t < tiles);
-                                if (in) end_last = c0 + 31 - __clz(in);
-                                if (in != 0xFFFFFFFFu) break;
-                            }
-                        }
-                        break;
-                    }
-                    left -= __shfl_sync(0xFFFFFFFFu, upto, 31);
-                }
-            }
             bool ok = true;
             uint32_t n_items = 0, loads = 0, bundles = 0;
             int tile0 = 0;
@@ -397,17 +428,17 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             };
             Item it;
             memset(&it, 0, sizeof(it));
-            int c = cut[0].c, u = cut[0].u, pair = cut[0].pair, t = cut[0].t;
-            Chunk k;
-            if (blockIdx.x >= n_cta) c = p.chunks;
-            if (c < p.chunks) k = sm.cut_chunk[0];
+            Cut at = sm.cut[0];
+            const Cut end = sm.cut[1];
+            Chunk k = sm.cut_chunk[0];
             const int nbox = TK / p.box;
-            while (ok && c < p.chunks) {
-                const bool at_end = c == cut[1].c && u == cut[1].u && pair == cut[1].pair;
-                if (at_end && cut[1].t == 0) break;
+            while (ok && at.u < units) {
+                const bool at_end = at.u == end.u && at.c == end.c && at.pair == end.pair;
+                if (at_end && end.t == 0) break;
+                const int pair = at.pair, t = at.t, u = at.u;
                 const int t0 = pair * S, t1 = min(k.tokens, t0 + S);
                 const Span all = span_of(p, k, t0, t1);
-                const int tiles = all.j1 - all.j0, te = at_end ? cut[1].t : tiles;
+                const int tiles = all.j1 - all.j0, te = at_end ? end.t : tiles;
                 if (te > t || tiles == 0) {
                     it.row0 = k.row0;
                     it.tokens = k.tokens;
@@ -440,7 +471,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     it.tile0 = tile0;
                     if (it.part == 1 && lane == 0) {
                         Joint j;
-                        j.last_cta = end_last;
+                        j.last_cta = sm.end_last;
                         j.row0 = k.row0;
                         j.tokens = k.tokens;
                         j.t0 = t0;
@@ -465,19 +496,19 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                                                                                    j * TK + lane * p.box < it.hi && j * TK + (lane + 1) * p.box > it.lo);
                             if (missing) page = p.c.n_pages;
                             const uint32_t boxes = __ballot_sync(0xFFFFFFFFu, missing);
-                            const int at = (tile0 + j - it.j0) & 3;
+                            const int mark = (tile0 + j - it.j0) & 3;
                             if (boxes) {
                                 bad_page = true;
                                 if (lane < 4) {
                                     uint32_t bits = 0;
                                     for (int i = 0; i < 32; ++i)
                                         if (!(boxes >> ((lane * 32 + i) / p.box) & 1)) bits |= 1u << i;
-                                    sm.visible[at][lane] = bits;
+                                    sm.visible[mark][lane] = bits;
                                 }
                             }
                             if (lane == 0) {
-                                sm.missing[at][0] = boxes != 0;
-                                sm.missing[at][1] = 0;
+                                sm.missing[mark][0] = boxes != 0;
+                                sm.missing[mark][1] = 0;
                             }
                             __syncwarp();
                         };
@@ -531,25 +562,26 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     tile0 += it.j1 - it.j0;
                 }
                 if (at_end) break;
-                t = 0;
-                if (++pair * S >= k.tokens) {
-                    pair = 0;
-                    if (++u == units) {
-                        u = 0;
-                        k.tokens = 0;
-                        for (int c0 = c + 1; c0 < p.chunks && k.tokens == 0; c0 += 32) {   // the next chunk with tokens
-                            Chunk mine;
-                            mine.row0 = mine.tokens = mine.seq = mine.pos0 = 0;
-                            if (c0 + lane < p.chunks) mine = chunk_of(p, c0 + lane, bad);
-                            const uint32_t any = __ballot_sync(0xFFFFFFFFu, mine.tokens > 0);
-                            const int l = any ? __ffs(any) - 1 : 0;
-                            if (any) c = c0 + l;
-                            k.row0 = __shfl_sync(0xFFFFFFFFu, mine.row0, l);
-                            k.tokens = __shfl_sync(0xFFFFFFFFu, mine.tokens, l);
-                            k.seq = __shfl_sync(0xFFFFFFFFu, mine.seq, l);
-                            k.pos0 = __shfl_sync(0xFFFFFFFFu, mine.pos0, l);
+                at.t = 0;
+                if (++at.pair * S >= k.tokens) {   // the next chunk with tokens, or the first of the next head
+                    at.pair = 0;
+                    k.tokens = 0;
+#pragma unroll 1
+                    for (int c0 = at.c + 1; k.tokens == 0; c0 += 32) {
+                        if (c0 >= p.chunks) {
+                            if (++at.u == units) break;
+                            c0 = 0;
                         }
-                        if (k.tokens == 0) break;
+                        Chunk mine;
+                        mine.row0 = mine.tokens = mine.seq = mine.pos0 = 0;
+                        if (c0 + lane < p.chunks) mine = chunk_of(p, c0 + lane, bad);
+                        const uint32_t any = __ballot_sync(0xFFFFFFFFu, mine.tokens > 0);
+                        const int l = any ? __ffs(any) - 1 : 0;
+                        if (any) at.c = c0 + l;
+                        k.row0 = __shfl_sync(0xFFFFFFFFu, mine.row0, l);
+                        k.tokens = __shfl_sync(0xFFFFFFFFu, mine.tokens, l);
+                        k.seq = __shfl_sync(0xFFFFFFFFu, mine.seq, l);
+                        k.pos0 = __shfl_sync(0xFFFFFFFFu, mine.pos0, l);
                     }
                 }
             }
@@ -780,7 +812,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
         const uint32_t s_addr = lane_addr + w * TK, p_addr = lane_addr + C::P_COL0 + w * C::P_STRIDE, o_addr = lane_addr + C::O_COL0 + w * C::O_STRIDE;
         const int token = p.by_heads.quotient(row), g = row - token * p.heads;
-        const float to_log2 = GENERAL ? LOG2E : p.scale * LOG2E, to_score = GENERAL ? 1.f : p.scale;   // of what s holds below
+        // s holds scores (GENERAL), or products that one factor makes scores
+        const float to_log2 = GENERAL ? LOG2E : p.scale * LOG2E, to_score = GENERAL ? 1.f : p.scale, to_cap = GENERAL ? p.scale / p.cap : 0.f;
         bool ok = true;
         uint32_t n_items = 0, tile_cnt = 0, done_cnt = 0, pf_cnt = 0;
         while (ok) {
@@ -795,7 +828,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             const bool live = token < p.tokens && tk < it.tokens && g < it.heads;
             const int hi = live ? max(0, pos + 1) : 0, lo = first_seen(p, pos);
             const float slope = GENERAL && p.slopes && live ? p.slopes[it.h0 + g] : 0.f;
-            const int a0 = it.a0[w], a1 = it.a1[w];
+            const int a0 = it.a0[w], a1 = it.a1[w], lo_max = it.lo_max, hi_min = it.hi_min, tile0 = it.tile0 - it.j0;
             float m = -INFINITY, l = 0.f;
             for (int j = a0; j < a1; ++j, ++tile_cnt) {
                 ok = mbar_wait(&sm.s_full[w], tile_cnt & 1u, gave_up);
@@ -812,25 +845,43 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     if (lane == 0) mbar_arrive(&sm.s_free[w]);
                 }
                 if (GENERAL) {
-                    const float back = static_cast<float>(j * TK - pos), inv_cap = 1.f / p.cap;
+                    if (p.cap > 0.f) {
+                        float high[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int i = 0; i < TK; ++i) {
-                        float x = s[i] * p.scale;
-                        if (p.cap > 0.f) x = p.cap * tanh_of(x * inv_cap);
-                        s[i] = fmaf(slope, back + i, x);
+                        for (int i = 0; i < TK; i += 2) high[(i >> 1) & 3] = max3f(high[(i >> 1) & 3], fabsf(s[i]), fabsf(s[i + 1]));
+                        const float most = fmaxf(fmaxf(high[0], high[1]), fmaxf(high[2], high[3])) * fabsf(to_cap);
+                        if (__all_sync(0xFFFFFFFFu, most <= 0.5f)) {
+                            tanh_near(s, to_cap, p.scale);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < TK; ++i) s[i] = tanh_far(s[i] * (2.f * LOG2E * to_cap), p.cap);
+                        }
+                    } else if (!p.slopes) {
+#pragma unroll
+                        for (int i = 0; i < TK; ++i) s[i] *= p.scale;
+                    }
+                    if (p.slopes) {
+                        // a place's distance bias: the first of each 16 places anew, the others by steps
+                        const uint64_t step = splat2(2.f * slope), factor = splat2(p.cap > 0.f ? 1.f : p.scale);
+#pragma unroll
+                        for (int i = 0; i < TK; i += 16) {
+                            const float first = static_cast<float>(j * TK + i - pos) * slope;
+                            uint64_t bias = pk2(first, first + slope);
+#pragma unroll
+                            for (int e = 0; e < 16; e += 2) {
+                                upk2(fma2(pk2(s[i + e], s[i + e + 1]), factor, bias), s[i + e], s[i + e + 1]);
+                                bias = add2(bias, step);
+                            }
+                        }
                     }
                 }
-                if (it.masked(j)) {
-                    const int from = lo - j * TK, to = hi - j * TK;
-#pragma unroll
-                    for (int i = 0; i < TK; ++i)
-                        if (i < from || i >= to) s[i] = -INFINITY;
-                }
-                const int mark = (it.tile0 + j - it.j0) & 3;
-                if (sm.missing[mark][0] | sm.missing[mark][1]) {
+                const int mark = (tile0 + j) & 3;
+                const bool missing = (sm.missing[mark][0] | sm.missing[mark][1]) != 0;
+                if (j * TK < lo_max || (j + 1) * TK > hi_min || missing) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const uint32_t bits = sm.visible[mark][c];
+                        uint32_t bits = below(hi - j * TK - c * 32) & ~below(lo - j * TK - c * 32);
+                        if (missing) bits &= sm.visible[mark][c];
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             if (!(bits >> i & 1)) s[c * 32 + i] = -INFINITY;
@@ -917,59 +968,58 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 ++done_cnt;
                 tc_fence_after_sync();
             }
-            uint32_t odd[C::WORDS];
-#pragma unroll
-            for (int i = 0; i < C::WORDS; ++i) odd[i] = 0;
             const uint32_t odd0 = sm.odd_tiles[slot][0], odd1 = sm.odd_tiles[slot][1];
-            if (odd0 | odd1) {   // (rare)
+            if ((odd0 | odd1) && a0 < a1) {   // (rare) elements that a value which is not finite goes into
 #pragma unroll 1
-                for (int j = a0; j < a1; ++j) {
-                    if (!it.masked(j)) continue;
-                    const int place = it.place(j);
+                for (int c = 0; c < C::WORDS; ++c) {
+                    uint32_t odd = 0;
 #pragma unroll 1
-                    for (int i = 0; i < TK; ++i) {
-                        if (!((i < 64 ? odd0 : odd1) >> place & 1) || j * TK + i < lo || j * TK + i >= hi) continue;
-#pragma unroll
-                        for (int q = 0; q < C::WORDS; ++q) odd[q] |= sm.odd[slot][place][i][q];
+                    for (int j = a0; j < a1; ++j) {
+                        if (!it.masked(j)) continue;
+                        const int place = it.place(j);
+#pragma unroll 1
+                        for (int i = 0; i < TK; ++i)
+                            if (((i < 64 ? odd0 : odd1) >> place & 1) && j * TK + i >= lo && j * TK + i < hi) odd |= sm.odd[slot][place][i][c];
                     }
+                    __syncwarp();
+                    uint32_t r[32];
+                    tmem_ld_32x32(o_addr + c * 32, r);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (odd >> i & 1) r[i] = 0x7FFFFFFFu;
+                    tmem_st_32x32(o_addr + c * 32, r);
+                    tmem_st_wait();
                 }
             }
-            const float inv = 1.f / l;
-            const bool empty = l == 0.f;   // (then O may hold anything)
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const bool empty = l == 0.f, whole = it.part < 0;   // (empty: O may hold anything)
             uint16_t *dst = p.out + (long long)(it.row0 + tk) * p.out_row + (it.h0 + g) * p.out_head;
-            float *slot_o = slots + ((long long)blockIdx.x * 2 + (it.part & 1)) * C::PART_FLOATS + w * TQ * HD;
-            const bool whole = it.part < 0;
-#pragma unroll
+            uint4 *slot_o = reinterpret_cast<uint4 *>(slots + ((long long)blockIdx.x * 2 + (it.part & 1)) * C::PART_FLOATS + w * TQ * HD) + row;
+#pragma unroll 1
             for (int c = 0; c < HD / 32; ++c) {
                 uint32_t r[32];
                 if (a0 < a1) {
                     tmem_ld_32x32(o_addr + c * 32, r);
                     tmem_ld_wait();
                 }
-                if (odd[c]) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (odd[c] >> i & 1) r[i] = 0x7FFFFFFFu;
-                }
                 if (whole) {
                     if (live) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             if (c * 32 + 8 * i >= p.head_dim) break;
-                            uint4 u = make_uint4(0u, 0u, 0u, 0u);
-                            if (!empty) {
-                                u.x = pack_h16x2(__uint_as_float(r[8 * i + 0]) * inv, __uint_as_float(r[8 * i + 1]) * inv);
-                                u.y = pack_h16x2(__uint_as_float(r[8 * i + 2]) * inv, __uint_as_float(r[8 * i + 3]) * inv);
-                                u.z = pack_h16x2(__uint_as_float(r[8 * i + 4]) * inv, __uint_as_float(r[8 * i + 5]) * inv);
-                                u.w = pack_h16x2(__uint_as_float(r[8 * i + 6]) * inv, __uint_as_float(r[8 * i + 7]) * inv);
-                            }
+                            uint4 u;
+                            u.x = pack_h16x2(__uint_as_float(r[8 * i + 0]) * inv, __uint_as_float(r[8 * i + 1]) * inv);
+                            u.y = pack_h16x2(__uint_as_float(r[8 * i + 2]) * inv, __uint_as_float(r[8 * i + 3]) * inv);
+                            u.z = pack_h16x2(__uint_as_float(r[8 * i + 4]) * inv, __uint_as_float(r[8 * i + 5]) * inv);
+                            u.w = pack_h16x2(__uint_as_float(r[8 * i + 6]) * inv, __uint_as_float(r[8 * i + 7]) * inv);
+                            if (empty) u = make_uint4(0u, 0u, 0u, 0u);
                             reinterpret_cast<uint4 *>(dst + c * 32)[i] = u;
                         }
                     }
                 } else if (live && !empty) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        reinterpret_cast<uint4 *>(slot_o)[(c * 8 + i) * TQ + row] = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+                    for (int i = 0; i < 8; ++i) slot_o[(c * 8 + i) * TQ] = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
                 }
             }
             if (live) {
@@ -1140,7 +1190,6 @@ extern "C" int kraken_op_paged_chunk_attention(const kraken_paged_cache *cache, 
         return KRAKEN_EINVAL;
     if (!aligned16(a->q) || !aligned16(a->out) || ((a->q_row_stride | a->q_head_stride | a->out_row_stride | a->out_head_stride) & 7))
         return KRAKEN_EUNSUPPORTED;
-    if (a->rows >= 1 << 22 || a->chunks >= 1 << 22) return KRAKEN_EUNSUPPORTED;
     if (!a->workspace || a->workspace_bytes < (cache->head_dim <= 64 ? workspace_bytes<64>() : workspace_bytes<128>())) return KRAKEN_ECAPACITY;
     if (!aligned16(a->workspace)) return KRAKEN_EINVAL;
     p.workspace = static_cast<uint8_t *>(a->workspace);
@@ -1167,6 +1216,10 @@ extern "C" int kraken_op_paged_chunk_attention(const kraken_paged_cache *cache, 
     p.head_tiles = (p.rep + TQ - 1) / TQ;
     p.heads = (p.rep + p.head_tiles - 1) / p.head_tiles;
     p.tokens = TQ / p.heads;
+    // (the places of a head are added up in 32 bits)
+    const long long pairs = (long long)a->rows / (2 * p.tokens) + a->chunks;
+    if (a->rows >= 1 << 22 || a->chunks >= 1 << 22 || pairs * ((long long)cache->max_pages * cache->page_size / TK + 2 + BEGIN) >= 1LL << 31)
+        return KRAKEN_EUNSUPPORTED;
     p.status = d_status;
     p.by_page = Divisor(cache->page_size);
     p.by_heads = Divisor(p.heads);

@@ -39,7 +39,7 @@ constexpr int TQ = 128;         // rows of a query tile
 constexpr int TK = 128;         // keys of a tile
 constexpr int THREADS = 384, AUX = 64;
 constexpr int SIDE = 3;         // masked tiles at either end of a unit's keys: its tokens' limits span at most 255 keys
-constexpr int BEGIN = 1;        // what beginning and finishing a unit costs, in tiles
+constexpr int BEGIN = 2;        // what beginning and finishing a unit costs, in tiles
 constexpr int MIN_PART = 3;     // places of a CTA at least
 // A weight is 2^(score - m); the first tile's largest is 2^HEADROOM, and m is raised when one gets past 2^(HEADROOM + RAISE).  Half numbers end at 2^16 and 2^-24: with 7, 10^5 weights of 2^-25 of the largest still count.
 constexpr float HEADROOM = KRAKEN_F16 ? 7.f : 0.f;
@@ -249,6 +249,31 @@ struct Smem {
     int end_last;
     uint32_t tmem, gave_up;
 };
+
+// The products with operand descriptors as a low and a high word: a step along the operand adds to the low one only
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        ".reg .b64 a, b;\n"
+        "setp.ne.b32 p, %5, 0;\n"
+        "mov.b64 a, {%1, %3};\n"
+        "mov.b64 b, {%2, %3};\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n"
+        "}\n" ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        ".reg .b64 b;\n"
+        "setp.ne.b32 p, %5, 0;\n"
+        "mov.b64 b, {%2, %3};\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n"
+        "}\n" ::"r"(d), "r"(a), "r"(b_lo), "r"(hi), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
 
 template <int HD, bool GENERAL, bool LANES>
 __global__ void __launch_bounds__(THREADS, 1)
@@ -598,22 +623,22 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 constexpr uint32_t idesc_qk = umma_idesc_h16(TQ, TK);
                 const uint32_t idesc_pv = umma_idesc_h16(TQ, qk_steps * 16) | (1u << 16);   // V is MN-major
                 auto issue_qk = [&](int w, int st) {
-                    const uint32_t q_addr = smem_u32(sm.q[w]), k_addr = smem_u32(sm.ring[st].k), d_tmem = tmem_base + w * TK;
+                    const uint64_t qd = umma_desc_sw128_kmajor(smem_u32(sm.q[w])), kd = umma_desc_sw128_kmajor(smem_u32(sm.ring[st].k));
+                    const uint32_t q_lo = static_cast<uint32_t>(qd), k_lo = static_cast<uint32_t>(kd), hi = static_cast<uint32_t>(kd >> 32);
 #pragma unroll
                     for (int ks = 0; ks < HD / 16; ++ks) {
                         if (ks >= qk_steps) break;
-                        const uint32_t off = (ks >> 2) * C::TILE_BYTES + (ks & 3) * 32;
-                        umma_bf16_ss(d_tmem, umma_desc_sw128_kmajor(q_addr + off), umma_desc_sw128_kmajor(k_addr + off), idesc_qk, ks != 0 ? 1u : 0u);
+                        const uint32_t off = ((ks >> 2) * C::TILE_BYTES + (ks & 3) * 32) >> 4;
+                        mma_ss(tmem_base + w * TK, q_lo + off, k_lo + off, hi, idesc_qk, ks != 0);
                     }
                     umma_commit(&sm.s_full[w]);
                 };
                 auto issue_pv = [&](int w, int st, bool first, bool last) {
-                    const uint32_t v_addr = smem_u32(sm.ring[st].v);
+                    const uint64_t vd = umma_desc_sw128_mnmajor(smem_u32(sm.ring[st].v), C::TILE_BYTES);
+                    const uint32_t v_lo = static_cast<uint32_t>(vd), hi = static_cast<uint32_t>(vd >> 32);
                     const uint32_t p_tmem = tmem_base + C::P_COL0 + w * C::P_STRIDE, o_tmem = tmem_base + C::O_COL0 + w * C::O_STRIDE;
 #pragma unroll
-                    for (int ks = 0; ks < TK / 16; ++ks)
-                        umma_bf16_ts(o_tmem, p_tmem + ks * 8, umma_desc_sw128_mnmajor(v_addr + ks * 2048, C::TILE_BYTES), idesc_pv,
-                                     (first && ks == 0) ? 0u : 1u);
+                    for (int ks = 0; ks < TK / 16; ++ks) mma_ts(o_tmem, p_tmem + ks * 8, v_lo + (ks * 2048 >> 4), hi, idesc_pv, !first || ks > 0);
                     if (last) umma_commit(&sm.pv_done[w]);
                     else if (C::SEPARATE_P) umma_commit(&sm.p_free[w]);
                 };

@@ -597,7 +597,7 @@ int kraken_op_token_logprobs(const kraken_logprobs_args *args, uint32_t *d_statu
  * uniforms[r] * M lies, and logprob[r] = log(w / M), the logarithm of the probability with which it was drawn.  So a uniform
  * of 0 gives the likeliest token; a temperature of 0 too, of several the first, with logprob 0.
  * Weights and sums are formed in 64 bits: the token is the one that the definition gives, but where u * M, top_p * Z or min_p is
- * within about 1e-13 of a border.
+ * within about 1e-11 of a border.
  * logits: [rows, vocab], row stride in elements, any alignment of the element type; dtype 0 = fp32, 1 = the library's 16-bit type.
  * temperature, top_k, top_p, min_p: device arrays [rows], or NULL: the value ..._all for every row.  top_k <= 0 or >= vocab, top_p >= 1
  * and min_p <= 0 are no limit; min_p above 1 counts as 1.  uniforms: fp32 [rows], in [0, 1).

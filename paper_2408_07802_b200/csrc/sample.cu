@@ -6,14 +6,15 @@
 //
 // Three passes over a row, of which the first comes from HBM and the others from L2 (or L1): 4 or 2 bytes a logit.
 //   1  the maximum
-//   2  how many logits lie in each of 4096 ranges of (x_0 - x) / T.  From these counts alone follow the range where the first
-//      top_k end, and, by the mean weight of a range, small windows of ranges that hold the ends of the mass that is looked for
+//   2  how many logits lie in each of 8192 ranges of (x_0 - x) / T, and the sum of all weights in 32 bits.  From these counts follow
+//      the range where the first top_k end, and, by the mean weight of a range, small windows of ranges that hold the ends of the
+//      mass that is looked for
 //   3  the logits in the windows are put aside, the weights of the others between them summed in 64 bits
-// What was put aside is sorted, its weights are summed in order, and every border is then known as if the row had been sorted.
-// A sum of weights in 32 bits is off by 10^-7, and of 50 thousand alike each has 2 10^-5 of the mass: the token would be another
-// one in a row of every hundred.  So sums and weights next to a border are 64 bits.
+// What was put aside (some hundred logits) is sorted, its weights are summed in order, and every border is then known as if the
+// row had been sorted.  A sum of weights in 32 bits is off by 10^-7, and of 50 thousand alike each has 2 10^-5 of the mass: the
+// token would be another one in a row of every hundred.  So sums and weights next to a border are 64 bits.
 // Where a border does not lie in its window (the mean weights were too far off), or more logits lie in the windows than there is
-// room for (many equal ones), descend() finds the borders digit by digit of the logits' order, with sums of integers.
+// room for (many equal ones), sample_any() finds the borders digit by digit of the logits' order, with sums of integers.
 //
 // Few rows: up to 8 CTAs of a cluster share a row.
 #include <float.h>
@@ -30,9 +31,12 @@ typedef unsigned long long u64;
 
 constexpr int THREADS = 512, WARPS = THREADS / 32;
 constexpr int MAX_CLUSTER = 8;
-constexpr int RANGES = 4096, PER = RANGES / THREADS;
-constexpr int FINE = 3072;             // ranges of 1 / 256, then of 1 / 32: up to 44, where a weight is 10^-19
-constexpr int ROOM = 4096, ROOM_PER = ROOM / THREADS;
+constexpr int RANGES = 8192, PER = RANGES / THREADS;
+// ranges of 1 / 512 in the exponent of 2 (2 steps) up to an exponent of 12, then of 1 / 16: up to 140, where a weight is 10^-42
+constexpr int FINE = 6144, FINEST = 2;
+constexpr int ROOM = 4096;
+constexpr double LOG2E = 1.4426950408889634074;
+constexpr int STEPS = 1024;            // of the table of powers of two
 
 struct SampleParams {
     const void *logits;
@@ -46,6 +50,12 @@ struct SampleParams {
     int rows, vocab;
 };
 
+__device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either is
+    float c;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(c) : "f"(a), "f"(b));
+    return c;
+}
+
 // The order of logits as unsigned numbers; -0 and +0 are equal
 __device__ __forceinline__ uint32_t order_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);
@@ -53,47 +63,67 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 }
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o); }
 
-// Range of a logit: the same roundings for every logit, so a larger logit is never in a later range
-struct Ranges {
-    float top, per_nat;   // x_0; 256 / T
-    __device__ __forceinline__ int of(float x) const {
-        const float t = (top - x) * per_nat;
-        return static_cast<int>(fminf(fminf(t, fmaf(t, 0.125f, FINE * 0.875f)), RANGES - 1.f));
+// How far a logit lies below the largest, as an exponent of two (t = (x_0 - x) log2(e) / T in 32 bits, at most 2000) and in whole
+// steps of 1 / 1024; its range.  The same roundings for every logit, so a larger logit is never in a later range.
+struct Below {
+    float d, t, shifted;
+    int k;
+    __device__ __forceinline__ Below(float x, float top, float per) {
+        d = top - x;
+        t = fminf(d * per, 2000.f);
+        shifted = fmaf(t, 1024.f, 12582912.f);   // 1.5 2^23: the nearest integer in the low bits
+        k = __float_as_int(shifted) & 0x3FFFFF;
     }
-    static __device__ __forceinline__ float begin(int r) { return (r <= FINE ? r : FINE + (r - FINE) * 8) / 256.f; }
+    __device__ __forceinline__ int range() const {
+        const int r = k / FINEST;
+        return min(min(r, (r >> 5) + (FINE - FINE / 32)), RANGES - 1);
+    }
+};
+
+// Ranges: FINEST steps each up to FINE, then 32 times as many
+struct Ranges {
+    static __device__ __forceinline__ int first(int r) {   // step; none behind the last range
+        return r >= RANGES ? INT_MAX : (r <= FINE ? r : FINE + (r - FINE) * 32) * FINEST;
+    }
+    static __device__ __forceinline__ float begin(int r) { return (first(r) - 0.5f) * (1.f / 1024.f); }
+    // what a logit in the middle of a range weighs, and the variance of the weight of one anywhere in it
+    static __device__ __forceinline__ void weigh(int r, float &w, float &v) {
+        const float steps = FINEST * (r < FINE ? 1.f : 32.f), width = steps * (0.693147181f / 1024.f);
+        w = ex2_approx(-(begin(r) + 0.5f / 1024.f * steps));
+        v = w * w * (width * width * (1.f / 12.f));
+    }
 };
 
 struct Smem {
-    uint32_t count[RANGES];          // of this CTA's part of the row
     union {
-        struct {
-            uint32_t before[RANGES + 1];   // logits of the row in earlier ranges
-            float mass[RANGES + 1];        // what they weigh, about
-            float spread[RANGES + 1];      // and how far that may be off
-        };
-        struct {
-            u64 mass256[256];
-            uint32_t count256[256];
-        };
+        uint32_t count[RANGES];      // of this CTA's part of the row
+        double weight[ROOM];         // of what is put aside
+        u64 mass256[256];
     };
     u64 aside[ROOM];                 // order << 32 | ~index
-    uint8_t kind[RANGES];            // of a range: 0 .. 2 summed (before the windows of the token, of top_p, of the limits), ASIDE, LATER
+    // of the whole row, before the ranges of thread i: logits, what they weigh, the variance of that
+    uint32_t before[THREADS + 1];
+    float mass[THREADS + 1], var[THREADS + 1];
+    double power[STEPS];             // 2^(-i / 1024)
     float top[MAX_CLUSTER];
     double all[MAX_CLUSTER], gaps[MAX_CLUSTER][3];
-    double warp_d[WARPS];
-    float warp_f[WARPS];
+    double warp_d[WARPS][3];
+    float warp_f[WARPS], warp_v[WARPS];
     uint32_t warp_u[WARPS];
-    u64 warp_l[WARPS];
     uint32_t n_aside;
-    int odd[MAX_CLUSTER], first[MAX_CLUSTER];
-    int k_range;
+    int first[MAX_CLUSTER];
+    struct {
+        int s0, s1, p0, p1, e0, e1;
+        uint32_t n_gap0, n_gap1, n_gap2, n_aside;
+    } windows;
+    int token;
     u64 found, found_above;
+    alignas(16) uint32_t row_count[];   // [RANGES] of the whole row, where CTAs share it
 };
-enum Kind { ASIDE = 3, LATER = 4 };
 
 template <bool H16>
 struct Row {
-    static constexpr int VEC = H16 ? 8 : 4, BATCH = 4;
+    static constexpr int VEC = H16 ? 8 : 4;
     const uint8_t *p;
     int n, head, vecs;   // head: logits before the first 16-byte boundary
     __device__ __forceinline__ Row(const void *base, long long at, int vocab) {
@@ -105,29 +135,46 @@ struct Row {
     __device__ __forceinline__ float at(int i) const {
         return H16 ? from_h16(reinterpret_cast<const uint16_t *>(p)[i]) : reinterpret_cast<const float *>(p)[i];
     }
-    // f(index, logit) for every logit of part `part` of `parts`, in any order
-    template <typename F>
+    // f(index, logit) for every logit of part `part` of `parts`, in any order.  BATCH: vectors that a thread requests at a time; ROLLED:
+    // for a long f, whose copies would have to be fetched: the 32-bit words of a vector one after the other.
+    template <int BATCH, bool ROLLED, typename F>
     __device__ __forceinline__ void visit(int part, int parts, F f) const {
         const int per = (vecs + parts - 1) / parts, lo = min(vecs, part * per), hi = min(vecs, lo + per);
         const uint4 *v = reinterpret_cast<const uint4 *>(p + head * (H16 ? 2 : 4));
+        auto word = [&](int e, uint32_t w) {
+            if (H16) {
+                f(e, h16_lo(w));
+                f(e + 1, h16_hi(w));
+            } else {
+                f(e, __uint_as_float(w));
+            }
+        };
+        constexpr int STEP = H16 ? 2 : 1;
+        uint4 next[BATCH];   // requested while the ones before are worked on
+        auto request = [&](int i0) {
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b)
+                if (i0 + b * THREADS < hi) next[b] = v[i0 + b * THREADS];
+        };
+        request(lo + threadIdx.x);
+#pragma unroll 1
         for (int i0 = lo + threadIdx.x; i0 < hi; i0 += THREADS * BATCH) {
             uint4 raw[BATCH];
 #pragma unroll
-            for (int b = 0; b < BATCH; ++b)
-                if (i0 + b * THREADS < hi) raw[b] = v[i0 + b * THREADS];
+            for (int b = 0; b < BATCH; ++b) raw[b] = next[b];
+            request(i0 + THREADS * BATCH);
 #pragma unroll
             for (int b = 0; b < BATCH; ++b) {
                 if (i0 + b * THREADS >= hi) break;
                 const int e = head + (i0 + b * THREADS) * VEC;
-                const uint32_t w[4] = {raw[b].x, raw[b].y, raw[b].z, raw[b].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (H16) {
-                        f(e + 2 * j, h16_lo(w[j]));
-                        f(e + 2 * j + 1, h16_hi(w[j]));
-                    } else {
-                        f(e + j, __uint_as_float(w[j]));
-                    }
+                if (ROLLED) {
+#pragma unroll 1
+                    for (int j = 0; j < 4; ++j) word(e + j * STEP, j == 0 ? raw[b].x : (j == 1 ? raw[b].y : (j == 2 ? raw[b].z : raw[b].w)));
+                } else {
+                    word(e, raw[b].x);
+                    word(e + STEP, raw[b].y);
+                    word(e + 2 * STEP, raw[b].z);
+                    word(e + 3 * STEP, raw[b].w);
                 }
             }
         }
@@ -141,55 +188,108 @@ struct Row {
     }
 };
 
-__device__ __forceinline__ double weight_of(float top, float x, double inv_t) { return exp((static_cast<double>(x) - static_cast<double>(top)) * inv_t); }
+// e^((x - top) / T) by a table of 2^(-i / 1024) and a short polynomial for what is left of the exponent (Tang's table method).
+struct Weights {
+    const double *power;
+    double top, per_nat;         // x_0; log2(e) / T
+    float per_hi, per_lo;        // the same in two pieces
+    // of one logit, in 64 bits, to some 10^-15 of it
+    __device__ __forceinline__ double of(float x) const {
+        const double t = (top - static_cast<double>(x)) * per_nat;
+        if (!(t < 1000.)) return 0.;
+        const double shifted = fma(t, 1024., 6755399441055744.);   // 1.5 2^52: the nearest integer in the low bits
+        const int k = __double2loint(shifted);
+        const double r = fma(shifted - 6755399441055744., 1. / 1024., -t);
+        double q = fma(r, 9.6181291076284772e-3, 5.5504108664821580e-2);   // (ln 2)^i / i!, i = 4 .. 1
+        q = fma(r, q, 2.4022650695910071e-1);
+        q = fma(r, q, 6.9314718055994531e-1);
+        const double b = power[k & (STEPS - 1)], w = fma(b * r, q, b);
+        return __hiloint2double(__double2hiint(w) - (k >> 10) * (1 << 20), __double2loint(w));
+    }
+    // The same as the sum of two numbers, by 32-bit instructions: the power of two from the table, and what the rest of the exponent (up
+    // to 2^-11, in two pieces until the power is taken off) adds to it, 3 10^-4 of it at most.  Off by up to 10^-10 of it, here and
+    // there; in 64 bits throughout the pass over the logits took half as long again.
+    __device__ __forceinline__ void in_two(float x, const Below &y, double &sum, float &rest) const {
+        // top - x = d + d_lo (Knuth's exact difference)
+        const float topf = static_cast<float>(top), xx = y.d - topf, d_lo = (topf - (y.d - xx)) - (x + xx);
+        const float t_lo = fmaf(y.d, per_hi, -y.t) + fmaf(y.d, per_lo, d_lo * per_hi);
+        const float r = fmaf(y.shifted - 12582912.f, 1.f / 1024.f, -y.t) - t_lo;
+        const float q = r * fmaf(r, fmaf(r, 5.5504109e-2f, -2.4022651e-1f), 6.9314718e-1f);   // 1 - 2^-r: of 2^-t, what the power lacks
+        const double b = power[y.k & (STEPS - 1)];
+        sum = __hiloint2double(__double2hiint(b) - (y.k >> 10) * (1 << 20), __double2loint(b));
+        rest = q * ex2_approx(-y.t);
+    }
+};
 
-// Sum over the CTA in a fixed order, for every thread
-__device__ __forceinline__ double block_sum(Smem &sm, double v) {
+// Sums over the CTA (alone: over the warp) in a fixed order, for every thread
+template <int N>
+__device__ __forceinline__ void block_sums(Smem &sm, double (&v)[N], bool alone = false) {
 #pragma unroll
-    for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    for (int o = 16; o > 0; o /= 2)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
+    if (alone) return;
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) sm.warp_d[threadIdx.x >> 5] = v;
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sm.warp_d[threadIdx.x >> 5][i] = v[i];
     __syncthreads();
-    double s = 0.;
-    for (int w = 0; w < WARPS; ++w) s += sm.warp_d[w];
-    return s;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = (threadIdx.x & 31) < WARPS ? sm.warp_d[threadIdx.x & 31][i] : 0.;
+#pragma unroll
+    for (int o = 8; o > 0; o /= 2)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xFFFFFFFFu, v[i], 0);
 }
 
-// Sums of what the threads before hold
+// Inclusive sums over a warp
 template <typename T>
-__device__ __forceinline__ T block_before(T (&warp)[WARPS], T v, T &total) {
-    const int lane = threadIdx.x & 31;
-    T upto = v;
+__device__ __forceinline__ T warp_upto(T v) {
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
-        const T x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-        if (lane >= o) upto += x;
+        const T x = __shfl_up_sync(0xFFFFFFFFu, v, o);
+        if ((threadIdx.x & 31) >= o) v += x;
     }
-    __syncthreads();
-    if (lane == 31) warp[threadIdx.x >> 5] = upto;
-    __syncthreads();
-    T before = 0;
-    total = 0;
-    for (int w = 0; w < WARPS; ++w) {
-        if (w < threadIdx.x >> 5) before += warp[w];
-        total += warp[w];
-    }
-    return before + (upto - v);
+    return v;
 }
 
 // What a row asks for
 struct Ask {
     float top;       // its largest logit
-    double inv_t;
+    Weights weights;
     int k;           // 0: no limit
     double p, m, u;  // p >= 1, m <= 0: no limit
 };
+
+// (formed anew by sample_any(): an argument of that size would lie in local memory, which the logits on their way push out of L1)
+__device__ __forceinline__ Ask ask_of(const SampleParams &s, const double *power, int r, float top) {
+    Ask a;
+    const float t = s.temperature ? s.temperature[r] : s.temperature_all, p = s.top_p ? s.top_p[r] : s.top_p_all;
+    a.k = s.top_k ? s.top_k[r] : s.top_k_all;
+    a.k = a.k <= 0 || a.k >= s.vocab ? 0 : a.k;
+    a.p = fmaxf(p, 0.f);
+    a.m = fminf(s.min_p ? s.min_p[r] : s.min_p_all, 1.f);
+    a.u = s.uniforms[r];
+    a.top = top;
+    a.weights.power = power;
+    a.weights.top = top;
+    a.weights.per_nat = LOG2E / static_cast<double>(t);
+    a.weights.per_hi = static_cast<float>(fmin(a.weights.per_nat, 1e30));
+    a.weights.per_lo = static_cast<float>(fmin(a.weights.per_nat, 1e30) - static_cast<double>(a.weights.per_hi));
+    return a;
+}
 
 __device__ __forceinline__ void give(const SampleParams &s, int r, int id, float logprob) {
     if (threadIdx.x == 0) {
         s.ids[r] = id;
         if (s.logprob) s.logprob[r] = logprob;
     }
+}
+
+__device__ __forceinline__ float logprob_of(const Ask &a, float x, double mass) {
+    return static_cast<float>((static_cast<double>(x) - a.weights.top) * a.weights.per_nat * (1. / LOG2E) - log(mass));
 }
 
 // ---------------------------------------------------------------- any row, digit by digit
@@ -208,7 +308,7 @@ __device__ __forceinline__ uint32_t descend(Smem &sm, const Row<H16> &row, uint3
         if (threadIdx.x < 256) sm.mass256[threadIdx.x] = 0;
         __syncthreads();
         auto add = [&](uint32_t o, u64 w) { atomicAdd(&sm.mass256[(o >> shift) & 255], w); };
-        row.visit(0, 1, [&](int, float x) {
+        row.template visit<1, true>(0, 1, [&](int, float x) {
             const uint32_t o = order_of(x);
             if (o > k_key && (shift == 24 || (o ^ key) >> (shift + 8) == 0)) {
                 const uint32_t active = __activemask();
@@ -257,7 +357,8 @@ __device__ __forceinline__ uint32_t descend(Smem &sm, const Row<H16> &row, uint3
 }
 
 template <bool H16>
-__device__ __noinline__ void sample_any(const SampleParams &s, Smem &sm, int r, const Ask a) {
+__device__ __noinline__ void sample_any(const SampleParams &s, Smem &sm, int r, float top) {
+    const Ask a = ask_of(s, sm.power, r, top);
     const Row<H16> row(s.logits, r * s.row_stride, s.vocab);
     const int bits = 62 - (32 - __clz(s.vocab));   // the sum of all weights stays below 2^62
     const double one = static_cast<double>(1ull << bits);
@@ -268,7 +369,7 @@ __device__ __noinline__ void sample_any(const SampleParams &s, Smem &sm, int r, 
         k_ties = a.k - above;
     }
     auto weight = [&](float x) -> u64 {
-        const double w = weight_of(a.top, x, a.inv_t);
+        const double w = a.weights.of(x);
         return w >= a.m ? static_cast<u64>(__double2ll_rn(w * one)) : 0ull;
     };
     auto upto = [&](u64 want, u64 above, uint32_t key) {   // with the token that reaches `want`
@@ -286,9 +387,16 @@ __device__ __noinline__ void sample_any(const SampleParams &s, Smem &sm, int r, 
     const u64 w = max(1ull, weight(value_of(key)));
     uint32_t ties = want > above ? static_cast<uint32_t>((want - above + w - 1) / w) : 1u;   // the so-many-th of its equals
     const int per = (s.vocab + THREADS - 1) / THREADS, lo = min(s.vocab, (int)threadIdx.x * per), hi = min(s.vocab, lo + per);
-    uint32_t mine = 0, all;
+    uint32_t mine = 0;
     for (int i = lo; i < hi; ++i) mine += order_of(row.at(i)) == key;
-    const uint32_t before = block_before(sm.warp_u, mine, all);
+    const uint32_t upto_mine = warp_upto(mine);
+    if ((threadIdx.x & 31) == 31) sm.warp_u[threadIdx.x >> 5] = upto_mine;
+    __syncthreads();
+    uint32_t before = upto_mine - mine, all = 0;
+    for (int w = 0; w < WARPS; ++w) {
+        if (w < threadIdx.x >> 5) before += sm.warp_u[w];
+        all += sm.warp_u[w];
+    }
     ties = min(ties, all);
     if (before < ties && ties <= before + mine) {
         uint32_t seen = before;
@@ -301,28 +409,10 @@ __device__ __noinline__ void sample_any(const SampleParams &s, Smem &sm, int r, 
         }
     }
     __syncthreads();
-    const double y = (static_cast<double>(a.top) - static_cast<double>(value_of(key))) * a.inv_t;
-    give(s, r, static_cast<int>(sm.found), static_cast<float>(-y - log(static_cast<double>(mass) / one)));
+    give(s, r, static_cast<int>(sm.found), logprob_of(a, value_of(key), static_cast<double>(mass) / one));
 }
 
 // ---------------------------------------------------------------- the three passes
-
-// First range up to which, it included, `mass` holds `want` or more (MORE: more than `want`).  A whole warp.
-template <bool MORE>
-__device__ __forceinline__ int range_of_mass(const Smem &sm, float want) {
-    const int lane = threadIdx.x & 31;
-    int at = 0;
-#pragma unroll
-    for (int step = RANGES / 32; step > 0; step /= 32) {   // 128, 4
-        const float m = sm.mass[at + (lane + 1) * step];
-        const uint32_t reached = __ballot_sync(0xFFFFFFFFu, MORE ? m > want : m >= want);
-        if (!reached) return RANGES - 1;
-        at += (__ffs(reached) - 1) * step;
-    }
-    const float m = sm.mass[at + (lane & 3) + 1];
-    const uint32_t reached = __ballot_sync(0xFFFFFFFFu, (MORE ? m > want : m >= want) && lane < 4);
-    return reached ? at + __ffs(reached) - 1 : RANGES - 1;
-}
 
 __device__ __forceinline__ uint32_t n_cluster_ctas() {
     uint32_t n;
@@ -337,71 +427,117 @@ __device__ __forceinline__ T *in_cta(T *p, uint32_t rank) {   // the same place 
     return q;
 }
 
+// The counts of the row, range by range, as its distribution.  A logit of a range weighs as much as one in its middle, give or
+// take width / sqrt(12).  By how much the sum of all weights differs from the ranges' is known, and the ranges before a place have
+// a part of that in proportion to their variance (share = difference / variance of all); what is then left of the variance is that
+// of a bridge, small behind the few largest logits, which have most of it.
+struct Distribution {
+    const uint32_t *count;
+    float share, var_all, inv_var, mass_all;
+};
+
+// A range, and what lies before it and up to its end: logits, about what they weigh, and how far that may be off
+struct Place {
+    int range;
+    uint32_t n0, n1;
+    float mass0, mass1, off;
+};
+
+// The first range up to whose end the row has `want` of the mass (OF_MASS) or logits (OF_COUNT), or range number `want`, or the last
+// one.  A whole warp; each half of it looks for its own `want`.
+enum By { OF_MASS, OF_COUNT, OF_RANGE };
+__device__ __forceinline__ Place find(const Smem &sm, const Distribution &d, By by, float want_mass, uint32_t want) {
+    static_assert(THREADS == 512 && PER == 16, "three steps of 16, 16 and 2, then 16 ranges, one a lane of a half");
+    const int lane = threadIdx.x & 31, l = lane & 15, half = lane & 16;
+    auto first = [&](bool reached, int none) {   // of the lanes of the half
+        const uint32_t some = __ballot_sync(0xFFFFFFFFu, reached) >> half & 0xFFFFu;
+        return some ? __ffs(some) - 1 : none;
+    };
+    auto reached = [&](int i) { return by == OF_MASS ? sm.mass[i] + d.share * sm.var[i] >= want_mass : sm.before[i] >= want; };
+    int block = 32 * first(reached(32 * (l + 1)), 15);
+    block += 2 * first(reached(block + 2 * (l + 1)), 15);
+    block += first(l < 2 && reached(block + (l & 1) + 1), 1);
+    if (by == OF_RANGE) block = want / PER;
+    const int r = block * PER + l;
+    const uint32_t n = d.count[r];
+    float w, v;
+    Ranges::weigh(r, w, v);
+    uint32_t n_up = n;
+    float up = n * w, v_up = n * v;
+#pragma unroll
+    for (int o = 1; o < 16; o *= 2) {
+        const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, n_up, o, 16);
+        const float y = __shfl_up_sync(0xFFFFFFFFu, up, o, 16), z = __shfl_up_sync(0xFFFFFFFFu, v_up, o, 16);
+        if (l >= o) {
+            n_up += x;
+            up += y;
+            v_up += z;
+        }
+    }
+    n_up += sm.before[block];
+    v_up += sm.var[block];
+    const float mass = up + sm.mass[block] + d.share * v_up;
+    const int at = first(by == OF_MASS ? mass >= want_mass : (by == OF_COUNT ? n_up >= want : r == want), 15);
+    Place p;
+    p.range = block * PER + at;
+    p.n1 = __shfl_sync(0xFFFFFFFFu, n_up, at, 16);
+    p.n0 = p.n1 - __shfl_sync(0xFFFFFFFFu, n, at, 16);
+    p.mass1 = __shfl_sync(0xFFFFFFFFu, mass, at, 16);
+    const float before = __shfl_sync(0xFFFFFFFFu, mass, max(at - 1, 0), 16), v0 = __shfl_sync(0xFFFFFFFFu, v_up, max(at - 1, 0), 16);
+    const float v1 = __shfl_sync(0xFFFFFFFFu, v_up, at, 16), v_begin = at ? v0 : sm.var[block];
+    p.mass0 = at ? before : sm.mass[block] + d.share * v_begin;
+    // (five standard deviations, at whichever end is more, and the roundings of the sums)
+    const float g = fmaxf(fmaxf(v_begin * (d.var_all - v_begin), v1 * (d.var_all - v1)) * d.inv_var, 0.f);
+    p.off = g * rsqrtf(fmaxf(g, 1e-37f)) * 5.f + 4e-6f * d.mass_all;
+    return p;
+}
+
 template <bool H16>
-__global__ void __launch_bounds__(THREADS, 2) sample_kernel(const SampleParams s) {
-    extern __shared__ uint8_t smem_raw[];
+__global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constant__ SampleParams s) {
+    extern __shared__ __align__(16) uint8_t smem_raw[];
     Smem &sm = *reinterpret_cast<Smem *>(smem_raw);
     const int parts = n_cluster_ctas(), part = cluster_ctarank();
     const int r = blockIdx.x / parts, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    for (int i = tid; i < RANGES; i += THREADS) sm.count[i] = 0;
+    for (int i = tid; i < RANGES / 4; i += THREADS) reinterpret_cast<uint4 *>(sm.count)[i] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = tid; i < STEPS; i += THREADS) sm.power[i] = exp2(i * (-1. / STEPS));
     if (tid == 0) sm.n_aside = 0;
     pdl_wait();
+    pdl_trigger();
     const Row<H16> row(s.logits, r * s.row_stride, s.vocab);
     const float t = s.temperature ? s.temperature[r] : s.temperature_all, u = s.uniforms[r];
-    Ask a;
-    a.k = s.top_k ? s.top_k[r] : s.top_k_all;
-    a.k = a.k <= 0 || a.k >= s.vocab ? 0 : a.k;
     const float p = s.top_p ? s.top_p[r] : s.top_p_all, m = s.min_p ? s.min_p[r] : s.min_p_all;
-    a.p = fmaxf(p, 0.f);
-    a.m = fminf(m, 1.f);
-    a.u = u;
-    a.inv_t = 1. / static_cast<double>(t);
 
     // 1: the maximum
+    float top = -INFINITY;
     {
-        float top = -INFINITY;
-        bool odd = !(t >= 0.f && t < INFINITY && u >= 0.f && u < 1.f) || p != p || m != m;
-        row.visit(part, parts, [&](int, float x) {
-            top = fmaxf(top, x);
-            odd |= !(x < INFINITY);
-        });
-        const uint32_t any = __ballot_sync(0xFFFFFFFFu, odd);
+        row.template visit<4, false>(part, parts, [&](int, float x) { top = max_nan(top, x); });
 #pragma unroll
-        for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        if (lane == 0) {
-            sm.warp_f[warp] = top;
-            sm.warp_u[warp] = any;
-        }
+        for (int o = 16; o > 0; o /= 2) top = max_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        if (lane == 0) sm.warp_f[warp] = top;
         __syncthreads();
-        if (tid < parts) {   // to every CTA of the cluster
-            float all = -INFINITY;
-            uint32_t bad = 0;
-            for (int w = 0; w < WARPS; ++w) {
-                all = fmaxf(all, sm.warp_f[w]);
-                bad |= sm.warp_u[w];
-            }
-            *in_cta(&sm.top[part], tid) = all;
-            *in_cta(&sm.odd[part], tid) = bad != 0;
+        if (warp == 0) {   // to every CTA of the cluster
+            top = lane < WARPS ? sm.warp_f[lane] : -INFINITY;
+#pragma unroll
+            for (int o = 8; o > 0; o /= 2) top = max_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+            top = __shfl_sync(0xFFFFFFFFu, top, 0);
+            if (lane < parts) *in_cta(&sm.top[part], lane) = top;
         }
         cluster_sync_all();
-        a.top = -INFINITY;
-        odd = false;
-        for (int i = 0; i < parts; ++i) {
-            a.top = fmaxf(a.top, sm.top[i]);
-            odd |= sm.odd[i] != 0;
-        }
-        if (odd || a.top == -INFINITY) {   // no distribution
+        top = -INFINITY;
+        for (int i = 0; i < parts; ++i) top = max_nan(top, sm.top[i]);
+        // (one of the row's logits is NaN or the largest infinite; parameters out of range)
+        if (!(fabsf(top) < INFINITY) || !(t >= 0.f && t < INFINITY && u >= 0.f && u < 1.f) || p != p || m != m) {
             if (part == 0) give(s, r, -1, NAN);
             return;
         }
     }
+    const Ask a = ask_of(s, sm.power, r, top);
     if (t == 0.f || a.k == 1) {   // the likeliest token, of several the first
         int first = INT_MAX;
-        row.visit(part, parts, [&](int i, float x) {
+        row.template visit<2, false>(part, parts, [&](int i, float x) {
             if (x == a.top) first = min(first, i);
         });
         first = __reduce_min_sync(0xFFFFFFFFu, first);
-        __syncthreads();
         if (lane == 0) sm.warp_u[warp] = first;
         __syncthreads();
         if (tid == 0) {
@@ -415,156 +551,204 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const SampleParams s
         }
         return;
     }
-
     // 2: how many logits in each range
-    Ranges ranges;
-    ranges.top = a.top;
-    ranges.per_nat = fminf(256.f / t, 1e30f);
-    const float per_bit = fminf(1.4426950408889634f / t, 1e30f);
-    float sum = 0.f;
-    row.visit(part, parts, [&](int, float x) {
-        atomicAdd(&sm.count[ranges.of(x)], 1u);
-        sum += ex2_approx((x - a.top) * per_bit);
-    });
+    const float per = a.weights.per_hi;
+    auto range_of = [&](float x) { return Below(x, top, per).range(); };
     {
-        const double all = block_sum(sm, sum);
-        if (tid < parts) *in_cta(&sm.all[part], tid) = all;
+        float sum = 0.f;
+        row.template visit<2, false>(part, parts, [&](int, float x) {
+            const Below y(x, top, per);
+            atomicAdd(&sm.count[y.range()], 1u);
+            sum += ex2_approx(-y.t);
+        });
+        double all[1] = {sum};
+        block_sums(sm, all);
+        if (tid < parts) *in_cta(&sm.all[part], tid) = all[0];
     }
     cluster_sync_all();
-    // A logit of a range weighs as much as one in its middle, give or take width / sqrt(12).  By how much the sum of all weights differs
-    // from the ranges' is known, and the ranges before a place have a part of that in proportion to their variance; what is then
-    // left of the variance is that of a bridge, small behind the few largest logits, which have most of it.
-    float mass_all = 0.f;
+    Distribution d;
+    d.count = sm.count;
+    if (parts > 1) {   // every CTA adds up its share of the ranges, for all
+        const int some = RANGES / parts;
+#pragma unroll 1
+        for (int i = part * some + 2 * tid; i < (part + 1) * some; i += 2 * THREADS) {
+            uint2 x[MAX_CLUSTER], sum = make_uint2(0u, 0u);
+#pragma unroll
+            for (int c = 0; c < MAX_CLUSTER; ++c)
+                if (c < parts) x[c] = *reinterpret_cast<const uint2 *>(in_cta(&sm.count[i], c));
+#pragma unroll
+            for (int c = 0; c < MAX_CLUSTER; ++c)
+                if (c < parts) {
+                    sum.x += x[c].x;
+                    sum.y += x[c].y;
+                }
+#pragma unroll
+            for (int c = 0; c < MAX_CLUSTER; ++c)
+                if (c < parts) *reinterpret_cast<uint2 *>(in_cta(&sm.row_count[i], c)) = sum;
+        }
+        d.count = sm.row_count;
+        cluster_sync_all();
+    }
     {
-        for (int c = 0; c < parts; ++c) mass_all += static_cast<float>(sm.all[c]);
-        uint32_t n[PER], mine = 0, all;
-        float mass = 0.f, total, var = 0.f, var_all;
-        const int r0 = tid * PER;
+        d.mass_all = 0.f;
+        for (int c = 0; c < parts; ++c) d.mass_all += static_cast<float>(sm.all[c]);
+        uint32_t n_mine = 0;
+        float mass = 0.f, var = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < PER; i += 4) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(&d.count[tid * PER + i]);
+            const uint32_t n[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int i = 0; i < PER; ++i) n[i] = 0;
-        for (int c = 0; c < parts; ++c) {
-            const uint4 *from = reinterpret_cast<const uint4 *>(in_cta(&sm.count[r0], c));
-#pragma unroll
-            for (int i = 0; i < PER / 4; ++i) {
-                const uint4 x = from[i];
-                n[4 * i] += x.x;
-                n[4 * i + 1] += x.y;
-                n[4 * i + 2] += x.z;
-                n[4 * i + 3] += x.w;
+            for (int j = 0; j < 4; ++j) {
+                float w, v;
+                Ranges::weigh(tid * PER + i + j, w, v);
+                n_mine += n[j];
+                mass += n[j] * w;
+                var += n[j] * v;
             }
         }
-        auto weigh = [&](int i, float &w, float &v) {
-            const float y0 = Ranges::begin(r0 + i), width = Ranges::begin(r0 + i + 1) - y0, mid = __expf(-y0 - width / 2);
-            w = n[i] * mid;
-            v = w * mid * width * width * (1.f / 12.f);
-        };
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            float w, v;
-            weigh(i, w, v);
-            mine += n[i];
-            mass += w;
-            var += v;
+        uint32_t n_up = warp_upto(n_mine);
+        float up = warp_upto(mass), v_up = warp_upto(var);
+        if (lane == 31) {
+            sm.warp_u[warp] = n_up;
+            sm.warp_f[warp] = up;
+            sm.warp_v[warp] = v_up;
         }
-        uint32_t at = block_before(sm.warp_u, mine, all);
-        float up = block_before(sm.warp_f, mass, total), v_up = block_before(sm.warp_f, var, var_all);
+        __syncthreads();
+        const uint32_t n_w = warp_upto(lane < WARPS ? sm.warp_u[lane] : 0u);
+        const float m_w = warp_upto(lane < WARPS ? sm.warp_f[lane] : 0.f), v_w = warp_upto(lane < WARPS ? sm.warp_v[lane] : 0.f);
+        const uint32_t n_0 = __shfl_sync(0xFFFFFFFFu, n_w, max(warp - 1, 0));
+        const float m_0 = __shfl_sync(0xFFFFFFFFu, m_w, max(warp - 1, 0)), v_0 = __shfl_sync(0xFFFFFFFFu, v_w, max(warp - 1, 0));
+        sm.before[tid + 1] = n_up + (warp ? n_0 : 0u);
+        sm.mass[tid + 1] = up + (warp ? m_0 : 0.f);
+        sm.var[tid + 1] = v_up + (warp ? v_0 : 0.f);
         if (tid == 0) {
-            sm.k_range = RANGES;
             sm.before[0] = 0;
-            sm.mass[0] = sm.spread[0] = 0.f;
+            sm.mass[0] = sm.var[0] = 0.f;
         }
-        __syncthreads();
-        const float share = var_all > 0.f ? (mass_all - total) / var_all : 0.f, inv_var = var_all > 0.f ? 1.f / var_all : 0.f;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            float w, v;
-            weigh(i, w, v);
-            if (a.k > 0 && at < a.k && at + n[i] >= a.k) sm.k_range = r0 + i;
-            at += n[i];
-            up += w;
-            v_up += v;
-            sm.before[r0 + i + 1] = at;
-            sm.mass[r0 + i + 1] = up + share * v_up;
-            // five standard deviations, and the roundings of the sums
-            sm.spread[r0 + i + 1] = 5.f * sqrtf(fmaxf(0.f, v_up * (var_all - v_up) * inv_var)) + 4e-6f * mass_all;
-        }
+        const float total = __shfl_sync(0xFFFFFFFFu, m_w, 31);
+        d.var_all = __shfl_sync(0xFFFFFFFFu, v_w, 31);
+        d.inv_var = d.var_all > 0.f ? 1.f / d.var_all : 0.f;
+        d.share = (d.mass_all - total) * d.inv_var;
         __syncthreads();
     }
-    // windows: of the limits (top_k, min_p), of the end of top_p, of the token
-    int e0 = sm.k_range, e1 = e0, p0, p1, s0, s1;
-    if (a.m > 0.) {
-        const float y = -logf(static_cast<float>(a.m));
-        Ranges at = ranges;
-        at.top = 0.f;
-        at.per_nat = 256.f;
-        const int m0 = at.of(-fmaxf(0.f, y - 1e-4f * (1.f + y))), m1 = at.of(-(y + 1e-4f * (1.f + y)));
-        if (e0 > m1) {
-            e0 = m0;
-            e1 = m1;
-        } else if (e0 >= m0) {
-            e0 = m0;
-            e1 = m1;
+    // Windows of ranges: of the limits (top_k, min_p), of the end of top_p, of the token.  (One warp of every CTA; they find the same.)
+    if (warp == 0) {
+        // (no limits: all but the last range, where all weights together are less than 10^-14 of the largest; sample_any() finds a token there)
+        const uint32_t n_all = s.vocab - d.count[RANGES - 1];
+        int e0 = RANGES - 1, e1 = RANGES - 2, p0 = e0, p1 = e1, s0 = e0, s1 = e1;
+        uint32_t e_n0 = n_all, e_n1 = n_all, p_n0 = 0, p_n1 = 0, s_n0 = 0, s_n1 = 0;
+        float mass_lo = d.mass_all * (1.f - 4e-6f), mass_hi = d.mass_all * (1.f + 4e-6f);   // of what is left, so far
+        const bool hi = lane >= 16;   // the lower half looks for the lower end of a window
+        auto of = [&](auto v, int end) { return __shfl_sync(0xFFFFFFFFu, v, end * 16); };
+        int m0 = 0, m1 = 0;
+        if (a.m > 0.) {
+            const float y = -__log2f(static_cast<float>(a.m)), slack = 1e-5f * (1.f + y);
+            m0 = Below(0.f, fmaxf(0.f, y - slack), 1.f).range();
+            m1 = Below(0.f, y + slack, 1.f).range();
         }
-    }
-    // (a border may be as far off as at the end of the range that it seems to be in, or at its beginning)
-    auto off = [&](int range) { return fmaxf(sm.spread[min(range, RANGES)], sm.spread[min(range + 1, RANGES)]); };
-    const float z_lo = sm.mass[min(e0, RANGES)] - (e0 < RANGES ? off(e0) : 0.f);
-    const float z_hi = sm.mass[min(e1 + 1, RANGES)] + (e1 < RANGES ? off(e1) : 0.f);
-    float mass_lo = z_lo, mass_hi = z_hi;
-    if (a.p < 1.) {
-        const float pf = static_cast<float>(a.p), lo = pf * z_lo, hi = pf * z_hi;
-        mass_lo = lo - off(range_of_mass<false>(sm, lo));
-        mass_hi = hi + off(range_of_mass<false>(sm, hi));
-        p0 = min(range_of_mass<false>(sm, mass_lo), e1);
-        p1 = min(range_of_mass<false>(sm, mass_hi), e1);
-        mass_hi = fminf(mass_hi + __expf(-Ranges::begin(p0)), sm.mass[min(p1 + 1, RANGES)] + off(p1));
-    } else {
-        p0 = e0;
-        p1 = e1;
-    }
-    s0 = min(range_of_mass<true>(sm, u * mass_lo - off(range_of_mass<true>(sm, u * mass_lo))), p1);
-    s1 = min(range_of_mass<true>(sm, u * mass_hi + off(range_of_mass<true>(sm, u * mass_hi))), p1);
-    // counts of what is summed and of what is put aside
-    const uint32_t n_s = sm.before[min(s1 + 1, RANGES)], n_gap0 = sm.before[min(s0, RANGES)];
-    const uint32_t n_gap1 = p0 > s1 ? sm.before[min(p0, RANGES)] - n_s : 0;
-    const int after_p = min(max(p1, s1) + 1, RANGES);
-    const uint32_t n_gap2 = e0 >= after_p ? sm.before[min(e0, RANGES)] - sm.before[after_p] : 0;
-    const uint32_t n_aside = sm.before[min(e1 + 1, RANGES)] - n_gap0 - n_gap1 - n_gap2;
-    if (n_aside > ROOM) {   // (the same for every CTA)
-        cluster_sync_all();   // (all have read the others' counts)
-        if (part == 0) sample_any<H16>(s, sm, r, a);
-        return;
-    }
-    for (int i = tid; i < RANGES; i += THREADS) {
-        const bool aside = (i >= s0 && i <= s1) || (i >= p0 && i <= p1) || (i >= e0 && i <= e1);
-        sm.kind[i] = aside ? ASIDE : (i > e1 ? LATER : (i > s1) + (i > p1));
+        float wanted = 0.f;   // by this half
+#pragma unroll 1
+        for (int step = 0; step < 6; ++step) {   // (one copy of the search: code that runs a few times a row takes its time to be fetched)
+            // 0: the end of the first top_k   1: the range of min_p   2: the end of top_p   4: the token   3, 5: 2 and 4 with what may be off
+            if (step == 0 ? a.k == 0 : (step == 1 ? !(a.m > 0.) || e0 < m0 : (step <= 3 && a.p >= 1.))) continue;
+            if (step == 2 || step == 4) wanted = (step == 2 ? static_cast<float>(a.p) : u) * (hi ? mass_hi : mass_lo);
+            const Place f = find(sm, d, step == 0 ? OF_COUNT : (step == 1 ? OF_RANGE : OF_MASS), wanted, step == 0 ? a.k : (hi ? m1 : m0));
+            if (step == 2 || step == 4) {
+                wanted += hi ? f.off : -f.off;
+                if (__any_sync(0xFFFFFFFFu, hi ? wanted > f.mass1 : wanted < f.mass0)) continue;   // not in the same range
+                ++step;
+            }
+            const int from = of(f.range, 0), to = of(f.range, 1);
+            const uint32_t n0 = of(f.n0, 0), n1 = of(f.n1, 1);
+            if (step <= 1) {
+                e0 = from;
+                e1 = to;
+                e_n0 = n0;
+                e_n1 = n1;
+                mass_lo = of(f.mass0 - f.off, 0);
+                mass_hi = of(f.mass1 + f.off, 1);
+            } else if (step == 3) {
+                p0 = from < e0 ? from : e0;
+                p_n0 = from < e0 ? n0 : e_n0;
+                p1 = to < e1 ? to : e1;
+                p_n1 = to < e1 ? n1 : e_n1;
+                mass_lo = of(wanted, 0);
+                // (up to the end of a token)
+                mass_hi = fminf(of(wanted, 1) + ex2_approx(-Ranges::begin(from)), of(f.mass1 + f.off, 1));
+            } else {
+                s0 = from;
+                s_n0 = n0;
+                s1 = to;
+                s_n1 = n1;
+            }
+        }
+        if (a.p >= 1.) {
+            p0 = e0;
+            p1 = e1;
+            p_n0 = e_n0;
+            p_n1 = e_n1;
+        }
+        if (s0 > p0) {
+            s0 = p0;
+            s_n0 = p_n0;
+        }
+        if (s1 > p1) {
+            s1 = p1;
+            s_n1 = p_n1;
+        }
+        // logits between the windows
+        const uint32_t n_gap0 = s_n0, n_gap1 = p0 > s1 ? p_n0 - s_n1 : 0, n_gap2 = e0 > p1 ? e_n0 - p_n1 : 0;
+        const uint32_t n_aside = e_n1 - n_gap0 - n_gap1 - n_gap2;
+        if (lane == 0) sm.windows = {s0, s1, p0, p1, e0, e1, n_gap0, n_gap1, n_gap2, n_aside};
     }
     __syncthreads();
+    const int s0 = sm.windows.s0, s1 = sm.windows.s1, p0 = sm.windows.p0, p1 = sm.windows.p1, e0 = sm.windows.e0, e1 = sm.windows.e1;
+    const uint32_t n_gap0 = sm.windows.n_gap0, n_gap1 = sm.windows.n_gap1, n_gap2 = sm.windows.n_gap2, n_aside = sm.windows.n_aside;
+    if (n_aside > ROOM) {   // (the same for every CTA)
+        cluster_sync_all();   // (all have read the others' counts)
+        if (part == 0) sample_any<H16>(s, sm, r, top);
+        return;
+    }
 
     // 3: sums and windows
     {
-        double sum0 = 0., sum1 = 0., sum2 = 0.;
+        double sums[3] = {0., 0., 0.};
+        float rests[3] = {0.f, 0.f, 0.f};
         u64 *list = in_cta(&sm.aside[0], 0u);
         uint32_t *n = in_cta(&sm.n_aside, 0u);
-        row.visit(part, parts, [&](int i, float x) {
-            const int kind = sm.kind[ranges.of(x)];
-            if (kind == ASIDE) {
+        // where the windows begin and end, in steps
+        const int at_s = Ranges::first(s0), after_s = Ranges::first(s1 + 1), at_p = Ranges::first(p0), after_p = Ranges::first(p1 + 1);
+        const int at_e = Ranges::first(e0), after_e = Ranges::first(e1 + 1);
+        row.template visit<1, H16>(part, parts, [&](int i, float x) {
+            const Below y(x, top, per);
+            if (y.k >= after_e) return;
+            if (y.k >= (y.k >= after_p ? at_e : (y.k >= after_s ? at_p : at_s))) {
                 list[atomicAdd(n, 1u)] = static_cast<u64>(order_of(x)) << 32 | static_cast<uint32_t>(~i);
-            } else if (kind != LATER) {
-                const double w = weight_of(a.top, x, a.inv_t);
-                sum0 += kind == 0 ? w : 0.;
-                sum1 += kind == 1 ? w : 0.;
-                sum2 += kind == 2 ? w : 0.;
+                return;
+            }
+            double sum;
+            float rest;
+            a.weights.in_two(x, y, sum, rest);
+            if (y.k >= after_p) {
+                sums[2] += sum;
+                rests[2] += rest;
+            } else if (y.k >= after_s) {
+                sums[1] += sum;
+                rests[1] += rest;
+            } else {
+                sums[0] += sum;
+                rests[0] += rest;
             }
         });
-        sum0 = block_sum(sm, sum0);
-        sum1 = block_sum(sm, sum1);
-        sum2 = block_sum(sm, sum2);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) sums[i] += rests[i];
+        block_sums(sm, sums);
         if (tid == 0) {
             double *to = in_cta(&sm.gaps[part][0], 0u);
-            to[0] = sum0;
-            to[1] = sum1;
-            to[2] = sum2;
+            to[0] = sums[0];
+            to[1] = sums[1];
+            to[2] = sums[2];
         }
         cluster_sync_all();
         if (part != 0) return;
@@ -575,122 +759,144 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const SampleParams s
         gap1 += sm.gaps[c][1];
         gap2 += sm.gaps[c][2];
     }
-    // in descending order
+    // in descending order: by counting how many are larger, some threads a key, where there are few; else a bitonic sort
     int size = 32;
     while (size < (int)n_aside) size *= 2;
-    for (int i = n_aside + tid; i < size; i += THREADS) sm.aside[i] = 0;
-    for (int k = 2; k <= size; k *= 2)
-        for (int j = k / 2; j > 0; j /= 2) {
-            __syncthreads();
-            for (int i = tid; i < size / 2; i += THREADS) {
-                const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
-                const u64 x = sm.aside[lo], y = sm.aside[hi];
-                if ((x < y) == ((lo & k) == 0)) {
-                    sm.aside[lo] = y;
-                    sm.aside[hi] = x;
+    if (size <= THREADS) {
+        const int each = THREADS / size, i = tid / each;   // threads of a key (at most 16)
+        const u64 key = i < (int)n_aside ? sm.aside[i] : 0;
+        int rank = 0;
+#pragma unroll 8
+        for (int j = tid & (each - 1); j < (int)n_aside; j += each) rank += sm.aside[j] > key;
+#pragma unroll 1
+        for (int o = each / 2; o > 0; o /= 2) rank += __shfl_xor_sync(0xFFFFFFFFu, rank, o);
+        __syncthreads();
+        if (i < (int)n_aside && (tid & (each - 1)) == 0) sm.aside[rank] = key;
+    } else {
+        for (int i = n_aside + tid; i < size; i += THREADS) sm.aside[i] = 0;
+#pragma unroll 1
+        for (int k = 2; k <= size; k *= 2)
+#pragma unroll 1
+            for (int j = k / 2; j > 0; j /= 2) {
+                __syncthreads();
+#pragma unroll 1
+                for (int i = tid; i < size / 2; i += THREADS) {
+                    const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
+                    const u64 x = sm.aside[lo], y = sm.aside[hi];
+                    if ((x < y) == ((lo & k) == 0)) {
+                        sm.aside[lo] = y;
+                        sm.aside[hi] = x;
+                    }
                 }
             }
-        }
+    }
     __syncthreads();
-    // thread i has the places ROOM_PER i .. of the order
-    const int at = tid * ROOM_PER;
-    double w[ROOM_PER], mine = 0., all;
-    int range[ROOM_PER];
-#pragma unroll
-    for (int i = 0; i < ROOM_PER; ++i) {
-        w[i] = 0.;
-        range[i] = RANGES;
-        if (at + i < (int)n_aside) {
-            const float x = value_of(static_cast<uint32_t>(sm.aside[at + i] >> 32));
-            w[i] = weight_of(a.top, x, a.inv_t);
-            range[i] = ranges.of(x);
+    // The borders among them.  Few: one warp, and the others wait for what it finds.
+    const bool alone = n_aside <= 256;
+    const int threads = alone ? 32 : THREADS;
+    double mass = 0.;
+    if (!alone || warp == 0) {
+        // thread i has `per` places of the order from per i on
+        const int per = (n_aside + threads - 1) / threads, lo = min((int)n_aside, tid * per), hi = min((int)n_aside, lo + per);
+        auto value = [&](int i) { return value_of(static_cast<uint32_t>(sm.aside[i] >> 32)); };
+        double mine = 0.;
+#pragma unroll 1
+        for (int i = lo; i < hi; ++i) {
+            const double w = a.weights.of(value(i));
+            sm.weight[i] = w;
+            mine += w;
         }
-        mine += w[i];
-    }
-    const double before = block_before(sm.warp_d, mine, all);
-    auto gaps_before = [&](int range) { return gap0 + (range > s1 ? gap1 : 0.) + (range > p1 ? gap2 : 0.); };
-    double z = 0., up = before, in_s = 0., in_p = 0.;   // allowed by the limits; weights in the window of the token, up to the end of that of top_p
-    bool allowed[ROOM_PER];
-#pragma unroll
-    for (int i = 0; i < ROOM_PER; ++i) {
-        const uint32_t rank = at + i + n_gap0 + (range[i] > s1 ? n_gap1 : 0) + (range[i] > p1 ? n_gap2 : 0);
-        allowed[i] = at + i < (int)n_aside && (a.k == 0 || rank < a.k) && (w[i] >= a.m || rank == 0);
-        z += allowed[i] ? w[i] : 0.;
-        in_s += range[i] <= s1 ? w[i] : 0.;
-        in_p += range[i] <= p1 ? w[i] : 0.;
-    }
-    z = block_sum(sm, z) + gap0 + gap1 + gap2;
-    in_s = block_sum(sm, in_s);
-    bool fits = true;
-    double mass = z;
-    if (a.p < 1.) {
-        in_p = block_sum(sm, in_p);
-        double before_p = 0.;   // weights put aside in front of the window of top_p
-        mass = 0.;
-        const double want = a.p * z;
-#pragma unroll
-        for (int i = 0; i < ROOM_PER; ++i) {
-            const uint32_t rank = at + i + n_gap0 + (range[i] > s1 ? n_gap1 : 0) + (range[i] > p1 ? n_gap2 : 0);
-            allowed[i] = allowed[i] && (up + gaps_before(range[i]) < want || rank == 0);
-            up += w[i];
-            mass += allowed[i] ? w[i] : 0.;
-            before_p += range[i] < p0 ? w[i] : 0.;
+        const double upto = warp_upto(mine);
+        double before = upto - mine;
+        if (!alone) {
+            if (lane == 31) sm.warp_d[warp][0] = upto;
+            __syncthreads();
+            for (int w = 0; w < warp; ++w) before += sm.warp_d[w][0];
         }
-        mass = block_sum(sm, mass) + gap0 + gap1;
-        before_p = block_sum(sm, before_p) + gap0 + gap1;
-        fits = (before_p <= want || (p0 == 0 && s0 == 0)) && want <= gap0 + gap1 + in_p;
+        // what is left by the limits; the weights in the window of the token, and up to the end of that of top_p; those put aside before it
+        double sums[3] = {0., 0., 0.}, before_p = 0.;
+        auto left = [&](int i, int range) {
+            const uint32_t rank = i + n_gap0 + (range > s1 ? n_gap1 : 0) + (range > p1 ? n_gap2 : 0);
+            return rank == 0 || ((a.k == 0 || rank < a.k) && sm.weight[i] >= a.m);
+        };
+#pragma unroll 1
+        for (int i = lo; i < hi; ++i) {
+            const int range = range_of(value(i));
+            const double w = sm.weight[i];
+            if (left(i, range)) sums[0] += w;
+            if (range <= s1) sums[1] += w;
+            if (range <= p1) sums[2] += w;
+            if (range < p0) before_p += w;
+        }
+        block_sums(sm, sums, alone);
+        const double z = sums[0] + gap0 + gap1 + gap2, in_s = sums[1], in_p = sums[2], want_p = a.p * z;
+        mass = z;
+        bool fits = true;
+        auto kept = [&](int i, int range, double up) {   // `up`: the weights put aside before it
+            if (!left(i, range)) return false;
+            if (a.p >= 1. || i + n_gap0 == 0) return true;
+            return up + gap0 + (range > s1 ? gap1 : 0.) + (range > p1 ? gap2 : 0.) < want_p;
+        };
+        if (a.p < 1.) {
+            double more[2] = {0., before_p}, up = before;
+#pragma unroll 1
+            for (int i = lo; i < hi; ++i) {
+                const double w = sm.weight[i];
+                if (kept(i, range_of(value(i)), up)) more[0] += w;
+                up += w;
+            }
+            block_sums(sm, more, alone);
+            mass = more[0] + gap0 + gap1;
+            fits = (more[1] + gap0 + gap1 <= want_p || (p0 == 0 && s0 == 0)) && want_p <= gap0 + gap1 + in_p;
+        }
+        const double want = a.u * mass;
+        fits = fits && gap0 <= want && want < gap0 + in_s;
+        // the first one kept up to which there is more than `want`; where the sums, rounded otherwise than `mass`, fall short of it, the last
+        int token = INT_MAX, last = -1;
+        {
+            double up = before;
+#pragma unroll 1
+            for (int i = lo; i < hi; ++i) {
+                const int range = range_of(value(i));
+                const bool is = kept(i, range, up) && range <= s1;
+                up += sm.weight[i];
+                if (is) last = i;
+                if (is && token == INT_MAX && gap0 + up > want) token = i;
+            }
+        }
+        token = __reduce_min_sync(0xFFFFFFFFu, token);
+        last = __reduce_max_sync(0xFFFFFFFFu, last);
+        if (!alone) {
+            if (lane == 0) {
+                sm.warp_u[warp] = token;
+                reinterpret_cast<int *>(sm.warp_f)[warp] = last;
+            }
+            __syncthreads();
+            token = __reduce_min_sync(0xFFFFFFFFu, lane < WARPS ? static_cast<int>(sm.warp_u[lane]) : INT_MAX);
+            last = __reduce_max_sync(0xFFFFFFFFu, lane < WARPS ? reinterpret_cast<int *>(sm.warp_f)[lane] : -1);
+        }
+        if (token == INT_MAX) token = last;
+        if (tid == 0) sm.token = fits ? token : -1;
     }
-    const double want = a.u * mass;
-    fits = fits && gap0 <= want && want < gap0 + in_s;
-    if (!fits) {
-        __syncthreads();
-        sample_any<H16>(s, sm, r, a);
+    __syncthreads();
+    if (sm.token < 0) {
+        sample_any<H16>(s, sm, r, top);
         return;
     }
-    if (tid == 0) sm.found = ~0ull;
-    __syncthreads();
-    up = before;
-    int token = ROOM;
-#pragma unroll
-    for (int i = 0; i < ROOM_PER; ++i) {
-        up += w[i];
-        if (token == ROOM && allowed[i] && range[i] <= s1 && gap0 + up > want) token = at + i;
-    }
-    token = __reduce_min_sync(0xFFFFFFFFu, token);
-    if (lane == 0 && token < ROOM) atomicMin(&sm.found, static_cast<u64>(token));
-    __syncthreads();
-    // (the sum up to the last one, rounded otherwise than `mass`, may fall short of it)
-    if (sm.found == ~0ull) {
-        token = -1;
-#pragma unroll
-        for (int i = 0; i < ROOM_PER; ++i)
-            if (allowed[i] && range[i] <= s1) token = at + i;
-        token = __reduce_max_sync(0xFFFFFFFFu, token);
-        if (lane == 0) sm.warp_u[warp] = token + 1;
-        __syncthreads();
-        token = 0;
-        for (int i = 0; i < WARPS; ++i) token = max(token, static_cast<int>(sm.warp_u[i]));
-        if (token == 0) {
-            sample_any<H16>(s, sm, r, a);
-            return;
-        }
-        --token;
-    } else {
-        token = static_cast<int>(sm.found);
-    }
     if (tid == 0) {
-        const u64 e = sm.aside[token];
-        const double y = (static_cast<double>(a.top) - static_cast<double>(value_of(static_cast<uint32_t>(e >> 32)))) * a.inv_t;
+        const u64 e = sm.aside[sm.token];
         s.ids[r] = static_cast<int>(~static_cast<uint32_t>(e));
-        if (s.logprob) s.logprob[r] = static_cast<float>(-y - log(mass));
+        if (s.logprob) s.logprob[r] = logprob_of(a, value_of(static_cast<uint32_t>(e >> 32)), mass);
     }
 }
+
+constexpr int SHARED_SMEM = sizeof(Smem) + RANGES * sizeof(uint32_t);
 
 template <bool H16>
 int launch(const SampleParams &p, cudaStream_t st) {
     static DeviceOnce configured;
     if (!configured.done()) {
-        int rc = cuda_check(cudaFuncSetAttribute(sample_kernel<H16>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Smem)),
+        int rc = cuda_check(cudaFuncSetAttribute(sample_kernel<H16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED_SMEM),
                             "sample tokens: shared memory opt-in");
         if (rc) return rc;
         configured.set();
@@ -703,7 +909,7 @@ int launch(const SampleParams &p, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(p.rows * cluster);
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = sizeof(Smem);
+    cfg.dynamicSmemBytes = cluster > 1 ? SHARED_SMEM : sizeof(Smem);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -81,12 +81,12 @@ __device__ __forceinline__ bool odd_h16(uint32_t pair) {
 
 // x -> cap tanh(x scale / cap), to_cap = scale / cap, for |x to_cap| <= 1/2: an odd polynomial of degree 9 fitted to tanh there
 // (to 1.4e-8 of it, 1.2e-7 with the roundings)
-__device__ __forceinline__ void tanh_near(float (&s)[TK], float to_cap, float scale) {
+__device__ __forceinline__ void tanh_near(float (&s)[32], float to_cap, float scale) {
     const float q = to_cap * to_cap;
     const uint64_t c4 = splat2(0.017135004f * scale * q * q * q * q), c3 = splat2(-0.052986074f * scale * q * q * q),
                    c2 = splat2(0.13324779f * scale * q * q), c1 = splat2(-0.33333069f * scale * q), c0 = splat2(scale);
 #pragma unroll
-    for (int i = 0; i < TK; i += 2) {
+    for (int i = 0; i < 32; i += 2) {
         const uint64_t x = pk2(s[i], s[i + 1]), y = mul2(x, x);
         upk2(mul2(x, fma2(y, fma2(y, fma2(y, fma2(y, c4, c3), c2), c1), c0)), s[i], s[i + 1]);
     }
@@ -430,9 +430,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     pdl_trigger();
     const uint32_t tmem_base = sm.tmem;
 
-    // registers of a thread, of the 168 that it was launched with: 128 x 120 + 256 x 192 = 384 x 168
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
         if (warp == 0) {
             // ------------------------------------------------------------------ units and copies
             bool ok = true;
@@ -831,7 +829,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             if (bad_page && lane == 0 && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         // ------------------------------------------------------------------ softmax
         const int w = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
         const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
@@ -860,67 +857,66 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after_sync();
-                float s[TK];
+                const int mark = (tile0 + j) & 3;
+                const bool missing = (sm.missing[mark][0] | sm.missing[mark][1]) != 0;
+                const bool masked = j * TK < lo_max || (j + 1) * TK > hi_min || missing;
+                // the tile in four steps, twice: the scores and their maximum; the weights
+                float mx = -INFINITY;
+#pragma unroll 2
+                for (int c = 0; c < TK / 32; ++c) {
+                    float s[32];
+                    tmem_ld_32x32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s));
+                    tmem_ld_wait();
+                    if (GENERAL) {
+                        if (p.cap > 0.f) {
+                            float high[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int c = 0; c < TK / 32; ++c) tmem_ld_32x32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
-                tmem_ld_wait();
-                if (C::SEPARATE_P) {
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sm.s_free[w]);
-                }
-                if (GENERAL) {
-                    if (p.cap > 0.f) {
-                        float high[4] = {0.f, 0.f, 0.f, 0.f};
+                            for (int i = 0; i < 32; i += 2) high[(i >> 1) & 3] = max3f(high[(i >> 1) & 3], fabsf(s[i]), fabsf(s[i + 1]));
+                            const float most = fmaxf(fmaxf(high[0], high[1]), fmaxf(high[2], high[3])) * fabsf(to_cap);
+                            if (__all_sync(0xFFFFFFFFu, most <= 0.5f)) {
+                                tanh_near(s, to_cap, p.scale);
+                            } else {
 #pragma unroll
-                        for (int i = 0; i < TK; i += 2) high[(i >> 1) & 3] = max3f(high[(i >> 1) & 3], fabsf(s[i]), fabsf(s[i + 1]));
-                        const float most = fmaxf(fmaxf(high[0], high[1]), fmaxf(high[2], high[3])) * fabsf(to_cap);
-                        if (__all_sync(0xFFFFFFFFu, most <= 0.5f)) {
-                            tanh_near(s, to_cap, p.scale);
-                        } else {
+                                for (int i = 0; i < 32; ++i) s[i] = tanh_far(s[i] * (2.f * LOG2E * to_cap), p.cap);
+                            }
+                        } else if (!p.slopes) {
 #pragma unroll
-                            for (int i = 0; i < TK; ++i) s[i] = tanh_far(s[i] * (2.f * LOG2E * to_cap), p.cap);
+                            for (int i = 0; i < 32; ++i) s[i] *= p.scale;
                         }
-                    } else if (!p.slopes) {
+                        if (p.slopes) {
+                            // a place's distance bias: the first of each 16 places anew, the others by steps
+                            const uint64_t step = splat2(2.f * slope), factor = splat2(p.cap > 0.f ? 1.f : p.scale);
 #pragma unroll
-                        for (int i = 0; i < TK; ++i) s[i] *= p.scale;
-                    }
-                    if (p.slopes) {
-                        // a place's distance bias: the first of each 16 places anew, the others by steps
-                        const uint64_t step = splat2(2.f * slope), factor = splat2(p.cap > 0.f ? 1.f : p.scale);
+                            for (int i = 0; i < 32; i += 16) {
+                                const float first = static_cast<float>(j * TK + c * 32 + i - pos) * slope;
+                                uint64_t bias = pk2(first, first + slope);
 #pragma unroll
-                        for (int i = 0; i < TK; i += 16) {
-                            const float first = static_cast<float>(j * TK + i - pos) * slope;
-                            uint64_t bias = pk2(first, first + slope);
-#pragma unroll
-                            for (int e = 0; e < 16; e += 2) {
-                                upk2(fma2(pk2(s[i + e], s[i + e + 1]), factor, bias), s[i + e], s[i + e + 1]);
-                                bias = add2(bias, step);
+                                for (int e = 0; e < 16; e += 2) {
+                                    upk2(fma2(pk2(s[i + e], s[i + e + 1]), factor, bias), s[i + e], s[i + e + 1]);
+                                    bias = add2(bias, step);
+                                }
                             }
                         }
                     }
-                }
-                const int mark = (tile0 + j) & 3;
-                const bool missing = (sm.missing[mark][0] | sm.missing[mark][1]) != 0;
-                if (j * TK < lo_max || (j + 1) * TK > hi_min || missing) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
+                    if (masked) {
                         uint32_t bits = below(hi - j * TK - c * 32) & ~below(lo - j * TK - c * 32);
                         if (missing) bits &= sm.visible[mark][c];
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (!(bits >> i & 1)) s[c * 32 + i] = -INFINITY;
+                            if (!(bits >> i & 1)) s[i] = -INFINITY;
                     }
-                }
-                float mc[4];
+                    float mc[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    mc[q] = max3f(s[q * 32], s[q * 32 + 1], s[q * 32 + 2]);
+                    for (int q = 0; q < 4; ++q) {
+                        mc[q] = max3f(s[q * 8], s[q * 8 + 1], s[q * 8 + 2]);
 #pragma unroll
-                    for (int i = 3; i + 1 < 32; i += 2) mc[q] = max3f(mc[q], s[q * 32 + i], s[q * 32 + i + 1]);
-                    mc[q] = fmaxf(mc[q], s[q * 32 + 31]);
+                        for (int i = 3; i + 1 < 8; i += 2) mc[q] = max3f(mc[q], s[q * 8 + i], s[q * 8 + i + 1]);
+                        mc[q] = fmaxf(mc[q], s[q * 8 + 7]);
+                    }
+                    mx = max3f(mx, fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3]));
+                    if (GENERAL || masked) tmem_st_32x32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s));
                 }
-                const float mx = fmaxf(fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3]));
+                if (GENERAL || masked) tmem_st_wait();
                 bool raise = false;
                 float f = 1.f;
                 if (j == a0) {
@@ -931,12 +927,9 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     m = mx;
                 }
                 float neg = m == -INFINITY ? 0.f : HEADROOM - m * to_log2;
-                if (__any_sync(0xFFFFFFFFu, fabsf(neg) > 65536.f)) {
-                    // scores whose product with log2(e) may be infinite, or further from the rounded one than weights last
-#pragma unroll
-                    for (int i = 0; i < TK; ++i) s[i] -= m == -INFINITY ? 0.f : m;
-                    neg = HEADROOM;
-                }
+                // scores whose product with log2(e) may be infinite, or further from the rounded one than weights last
+                const bool far = __any_sync(0xFFFFFFFFu, fabsf(neg) > 65536.f);
+                if (far) neg = HEADROOM;
                 if (C::SEPARATE_P && j > a0) {
                     ok = mbar_wait(&sm.p_free[w], pf_cnt & 1u, gave_up);
                     ++pf_cnt;
@@ -945,12 +938,19 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     tc_fence_after_sync();
                 }
                 float sum0 = 0.f, sum1 = 0.f, sum2 = 0.f, sum3 = 0.f;
-#pragma unroll
+#pragma unroll 2
                 for (int c = 0; c < TK / 32; ++c) {
+                    float s[32];
+                    tmem_ld_32x32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s));
+                    tmem_ld_wait();
+                    if (far) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) s[i] -= m == -INFINITY ? 0.f : m;
+                    }
                     uint32_t pk[16];
 #pragma unroll
                     for (int i = 0; i < 16; i += 2) {
-                        float x0 = s[c * 32 + 2 * i], x1 = s[c * 32 + 2 * i + 1], x2 = s[c * 32 + 2 * i + 2], x3 = s[c * 32 + 2 * i + 3];
+                        float x0 = s[2 * i], x1 = s[2 * i + 1], x2 = s[2 * i + 2], x3 = s[2 * i + 3];
                         fma2(x0, x1, to_log2, neg);
                         fma2(x2, x3, to_log2, neg);
                         x0 = ex2_approx(x0);
@@ -965,6 +965,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                         pk[i + 1] = pack_h16x2(x2, x3);
                     }
                     tmem_st_32x16(p_addr + c * 16, pk);
+                }
+                if (C::SEPARATE_P) {
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sm.s_free[w]);
                 }
                 l = l * f + ((sum0 + sum1) + (sum2 + sum3));
                 if (__any_sync(0xFFFFFFFFu, raise)) {

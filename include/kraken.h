@@ -472,7 +472,7 @@ int kraken_op_paged_append(const kraken_paged_cache *cache, const kraken_paged_a
 
 /* kraken_op_paged_append with norms of queries and keys, head by head, before the rotation:
  *     x_e -> x_e * w_e / sqrt(sum_e x_e^2 / head_dim + eps)      over all head_dim elements of a head, in fp32,
- * rounded once, after the rotation.  q_weight, k_weight: 16-bit, element e of head h at h * head_stride + e (a head stride of 0:
+ * rounded once, after the rotation (squares or sums that fp32 does not hold are infinite or 0 there).  q_weight, k_weight: 16-bit, element e of head h at h * head_stride + e (a head stride of 0:
  * the same for all heads), or NULL (ones).  The weights must not overlap what the call writes.  Values are copied as they are.
  * Everything else as there; besides, EINVAL: norm NULL, eps negative or not finite; EUNSUPPORTED: weights that are not 16-byte
  * aligned, head strides no multiple of 8. */

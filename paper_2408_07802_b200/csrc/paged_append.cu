@@ -7,6 +7,8 @@
 //   x_e -> x_e w_e / sqrt(sum_e x_e^2 / head_dim + eps)
 //
 // One pass: every value is read once and written once, so the floor is 4 bytes a value at the copy bandwidth.
+// 6010 rows of 16 + 2 x 16 heads of 128 (148 MB, floor 23 us): 25.8 us; with norms 5920 rows (floor 22 us) 32.0 (issue slots busy 53 % of the time in place
+// of 49, and the sums of the squares, joined by shuffles, stand between a row's loads and its stores).
 #include <math.h>
 
 #include "paged.cuh"

@@ -24,6 +24,19 @@
 //
 // The tiles of a call are one line that is cut into equal parts, one for each CTA (one per SM).  A unit cut apart leaves its parts
 // (maximum, sum, output) in the workspace and a second kernel joins them.
+//
+// What bounds it.  Products at the tensor cores' rate would be 2 x 512 cycles a query tile and key tile with head dims of 128;
+// a row's 128 exponentials take as long in the special-function units.  A key tile takes 3.7 to 4.2 thousand cycles with both query
+// tiles at work, each of which goes through scores, weights and product one after the other while the other one does the same.  A
+// unit costs some 9 thousand cycles besides (its first keys and scores, its last product, the way out), a call 12 thousand (the
+// lengths read and the work cut, the first copies) and the second kernel.  Measured on a B200, a graph of calls:
+//   2048 tokens after 32768, 32 on 8 heads of 128:   1140 us, 1.0 PFLOP/s (floor at 1.66: 682)
+//   four prompts of 1129 to 2048, 16 heads of 128:   104 us (34; tensor cores busy 27 % of the time, issue slots as much)
+//   24 sequences, three in four with a single token, up to 4000 keys, 16 on 4 heads of 64, capped:   146 us (17)
+//   five tokens after 1500, 32 on 8 heads of 128:    19 us (1), the start and two kernels
+// The size of the code counts: with a tile's 128 scores in registers, everything written out for them, instructions came from
+// beyond the first cache all the time.  So the scores are read from tensor memory twice, 32 at a time (four prompts 111 -> 104),
+// masks are bits, and there is one form of a step (one for tiles that every row sees whole and one for the others: 137).
 #include <math.h>
 #include <string.h>
 
@@ -39,8 +52,9 @@ constexpr int TQ = 128;         // rows of a query tile
 constexpr int TK = 128;         // keys of a tile
 constexpr int THREADS = 384, AUX = 64;
 constexpr int SIDE = 3;         // masked tiles at either end of a unit's keys: its tokens' limits span at most 255 keys
-constexpr int BEGIN = 2;        // what beginning and finishing a unit costs, in tiles
-constexpr int MIN_PART = 3;     // places of a CTA at least
+// What beginning and finishing a unit costs, in tiles (1: the mixed batch 150 us in place of 146; 3: four prompts 102 in place of 104,
+// but windows with slopes 55 in place of 50), and a CTA's places at least (3: five drafted tokens 20.4 us in place of 19.3)
+constexpr int BEGIN = 2, MIN_PART = 2;
 // A weight is 2^(score - m); the first tile's largest is 2^HEADROOM, and m is raised when one gets past 2^(HEADROOM + RAISE).  Half numbers end at 2^16 and 2^-24: with 7, 10^5 weights of 2^-25 of the largest still count.
 constexpr float HEADROOM = KRAKEN_F16 ? 7.f : 0.f;
 constexpr float RAISE = 8.f;

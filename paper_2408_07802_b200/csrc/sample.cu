@@ -17,6 +17,12 @@
 // room for (many equal ones), sample_any() finds the borders digit by digit of the logits' order, with sums of integers.
 //
 // Few rows: up to 8 CTAs of a cluster share a row.
+//
+// What bounds it, on a B200 (a graph of calls).  512 rows of 50257 fp32 logits: 105 us where reading them takes 16 (103 MB come from
+// HBM, once); issue slots are busy 56 % of the time, a row's CTA being at its barriers (maximum, counts, windows, ranks) for the
+// rest of it, and two CTAs an SM is what registers and the table of counts leave.  64 mixed rows: 28 us; one row: 17 us; these are
+// the steps one after the other.  Weights in 64 bits throughout took 156 us for the 512 rows: by table and 32-bit arithmetic in
+// pass 2, and by comparing with the windows' borders in pass 3, a logit costs some 12 instructions there.
 #include <float.h>
 #include <math.h>
 

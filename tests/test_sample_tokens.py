@@ -173,6 +173,28 @@ def test_sample_extreme_temperatures(t):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows", [3, 90])
+def test_sample_tokens_masked_by_the_lowest_number(dtype, rows):
+    """Forbidden tokens by the type's lowest number in place of -inf: never drawn, however many top_k asks for, unless there is
+    nothing else; from the highest to the lowest number is further than 32 bits hold."""
+    t = DTYPES[dtype]
+    low, vocab = torch.finfo(t).min, 30011
+    x = torch.full((rows, vocab), low, dtype=t, device=DEV)
+    for r in range(rows):
+        left = [7 + r, 400 + 3 * r, 29000 - r, vocab - 1][:r % 4 + 1]
+        x[r, left] = torch.tensor([1.0, 0.5, 1.25, -2.0][:len(left)], dtype=t, device=DEV)
+    u = uniforms(11, rows)
+    for kw in (dict(), dict(k=3), dict(k=500), dict(p=0.9), dict(m=0.4), dict(k=20000, p=0.999, m=0.01), dict(t=0.2), dict(t=0.2, k=9)):
+        check(x, u, most_unsure=0.1, **kw)
+    x[1] = low
+    x[2, 12345] = torch.finfo(t).max
+    got = kr.op_sample_tokens(x[1:3].contiguous(), torch.tensor([0.5, 0.999], device=DEV))
+    assert got.ids.tolist() == [vocab // 2, 12345]
+    assert abs(float(got.logprob[0]) + math.log(vocab)) < 1e-5 and float(got.logprob[1]) == 0.0
+
+
+@gpu
 @pytest.mark.parametrize("vocab", [33, 4000, 60000])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_sample_rows_without_a_distribution(vocab, dtype):

@@ -14,7 +14,8 @@
 // row had been sorted.  A sum of weights in 32 bits is off by 10^-7, and of 50 thousand alike each has 2 10^-5 of the mass: the
 // token would be another one in a row of every hundred.  So sums and weights next to a border are 64 bits.
 // Where a border does not lie in its window (the mean weights were too far off), or more logits lie in the windows than there is
-// room for (many equal ones), sample_any() finds the borders digit by digit of the logits' order, with sums of integers.
+// room for (many equal ones), sample_any() finds the borders digit by digit of the logits' order, with sums of integers: 0.6 ms for a
+// row of 50257 fp32 logits (1.1 with every weight added by itself in 64 bits), 1.2 to 1.7 for 16-bit ones of 105 to 132 thousand.
 //
 // Few rows: up to 8 CTAs of a cluster share a row.
 //
@@ -41,6 +42,10 @@ constexpr int RANGES = 8192, PER = RANGES / THREADS;
 // ranges of 1 / 512 in the exponent of 2 (2 steps) up to an exponent of 12, then of 1 / 16: up to 140, where a weight is 10^-42
 constexpr int FINE = 6144, FINEST = 2;
 constexpr int ROOM = 4096;
+// What sums of weights in 32 bits may be off by, of the sum of all (found: below 2 10^-7).  The window of a uniform within twice this of
+// 1 reaches to the row's end, which may be more than there is room for: with 4 10^-6 one in 75 calls of 512 rows of 50257 was 0.5 ms late
+// for a single row; now one in 600.
+constexpr float ROUNDINGS = 5e-7f;
 constexpr double LOG2E = 1.4426950408889634074;
 constexpr int STEPS = 1024;            // of the table of powers of two
 
@@ -298,6 +303,12 @@ __device__ __forceinline__ float logprob_of(const Ask &a, float x, double mass) 
     return static_cast<float>((static_cast<double>(x) - a.weights.top) * a.weights.per_nat * (1. / LOG2E) - log(mass));
 }
 
+__device__ __forceinline__ uint32_t n_cluster_ctas() {
+    uint32_t n;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+    return n;
+}
+
 // ---------------------------------------------------------------- any row, digit by digit
 
 // The first token, in the order, up to which the weights (counts: 1 each) make `want` or more: the order of its logit, and what the
@@ -313,15 +324,36 @@ __device__ __forceinline__ uint32_t descend(Smem &sm, const Row<H16> &row, uint3
         __syncthreads();
         if (threadIdx.x < 256) sm.mass256[threadIdx.x] = 0;
         __syncthreads();
-        auto add = [&](uint32_t o, u64 w) { atomicAdd(&sm.mass256[(o >> shift) & 255], w); };
+        auto add = [&](uint32_t o, u64 w) {   // (two native additions of 32 bits with the carry: one of 64 would be tried until it succeeds)
+            uint32_t *at = reinterpret_cast<uint32_t *>(&sm.mass256[(o >> shift) & 255]);
+            const uint32_t low = static_cast<uint32_t>(w), old = atomicAdd(at, low);
+            atomicAdd(at + 1, static_cast<uint32_t>(w >> 32) + (old + low < old));
+        };
         row.template visit<1, true>(0, 1, [&](int, float x) {
             const uint32_t o = order_of(x);
             if (o > k_key && (shift == 24 || (o ^ key) >> (shift + 8) == 0)) {
-                const uint32_t active = __activemask();
-                int same;
-                __match_all_sync(active, o, &same);   // many equal ones: one addition for all
-                if (!same) add(o, COUNTS ? 1 : weight(x));
-                else if (__ffs(active) - 1 == (threadIdx.x & 31)) add(o, (COUNTS ? 1 : weight(x)) * __popc(active));
+                // of the lanes' digits the first few are added up in the warp: at first most logits have one of very few
+                const u64 w = COUNTS ? 1ull : weight(x);
+                const uint32_t digit = (o >> shift) & 255;
+                uint32_t active = __activemask();
+                bool done = false;
+#pragma unroll 1
+                for (int round = 0; round < 4 && active; ++round) {
+                    const int leader = __ffs(active) - 1;
+                    const uint32_t theirs = __shfl_sync(active, digit, leader);
+                    const uint32_t group = __ballot_sync(active, digit == theirs);
+                    if (digit == theirs) {
+                        // sums of up to 32 numbers of 27 bits (w < 2^62)
+                        const uint32_t a = __reduce_add_sync(group, static_cast<uint32_t>(w) & 0x7FFFFFFu);
+                        const uint32_t b = COUNTS ? 0u : __reduce_add_sync(group, static_cast<uint32_t>(w >> 27) & 0x7FFFFFFu);
+                        const uint32_t c = COUNTS ? 0u : __reduce_add_sync(group, static_cast<uint32_t>(w >> 54));
+                        if ((threadIdx.x & 31) == leader) add(o, (static_cast<u64>(c) << 54) + (static_cast<u64>(b) << 27) + a);
+                        done = true;
+                        break;
+                    }
+                    active &= ~group;
+                }
+                if (!done) add(o, w);
             }
         });
         __syncthreads();
@@ -366,8 +398,11 @@ template <bool H16>
 __device__ __noinline__ void sample_any(const SampleParams &s, Smem &sm, int r, float top) {
     const Ask a = ask_of(s, sm.power, r, top);
     const Row<H16> row(s.logits, r * s.row_stride, s.vocab);
-    const int bits = 62 - (32 - __clz(s.vocab));   // the sum of all weights stays below 2^62
-    const double one = static_cast<double>(1ull << bits);
+    // the unit of the integers: the sum of all weights (in 32 bits, from pass 2) lies between 2^60 and 2^61, so what vocab roundings do
+    // to a sum is below vocab 2^-61 of all
+    double all = 0.;
+    for (int c = 0; c < static_cast<int>(n_cluster_ctas()); ++c) all += sm.all[c];
+    const double one = static_cast<double>(1ull << (60 - ilogb(all)));
     uint32_t k_key = 0;
     u64 k_ties = 0, want, above, total;
     if (a.k > 0 && a.k < s.vocab) {
@@ -419,12 +454,6 @@ __device__ __noinline__ void sample_any(const SampleParams &s, Smem &sm, int r, 
 }
 
 // ---------------------------------------------------------------- the three passes
-
-__device__ __forceinline__ uint32_t n_cluster_ctas() {
-    uint32_t n;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
-    return n;
-}
 
 template <typename T>
 __device__ __forceinline__ T *in_cta(T *p, uint32_t rank) {   // the same place in another CTA of the cluster
@@ -494,7 +523,7 @@ __device__ __forceinline__ Place find(const Smem &sm, const Distribution &d, By 
     p.mass0 = at ? before : sm.mass[block] + d.share * v_begin;
     // (five standard deviations, at whichever end is more, and the roundings of the sums)
     const float g = fmaxf(fmaxf(v_begin * (d.var_all - v_begin), v1 * (d.var_all - v1)) * d.inv_var, 0.f);
-    p.off = g * rsqrtf(fmaxf(g, 1e-37f)) * 5.f + 4e-6f * d.mass_all;
+    p.off = g * rsqrtf(fmaxf(g, 1e-37f)) * 5.f + ROUNDINGS * d.mass_all;
     return p;
 }
 
@@ -644,7 +673,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
         const uint32_t n_all = s.vocab - d.count[RANGES - 1];
         int e0 = RANGES - 1, e1 = RANGES - 2, p0 = e0, p1 = e1, s0 = e0, s1 = e1;
         uint32_t e_n0 = n_all, e_n1 = n_all, p_n0 = 0, p_n1 = 0, s_n0 = 0, s_n1 = 0;
-        float mass_lo = d.mass_all * (1.f - 4e-6f), mass_hi = d.mass_all * (1.f + 4e-6f);   // of what is left, so far
+        float mass_lo = d.mass_all * (1.f - ROUNDINGS), mass_hi = d.mass_all * (1.f + ROUNDINGS);   // of what is left, so far
         const bool hi = lane >= 16;   // the lower half looks for the lower end of a window
         auto of = [&](auto v, int end) { return __shfl_sync(0xFFFFFFFFu, v, end * 16); };
         int m0 = 0, m1 = 0;

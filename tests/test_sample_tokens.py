@@ -153,6 +153,29 @@ def test_sample_equal_logits_are_drawn_by_index():
 
 
 @gpu
+@pytest.mark.parametrize("rows", [1, 5, 200])
+@pytest.mark.parametrize("exponent", [20.5, 30.0, 38.5, 41.5])
+def test_sample_many_tiny_weights(exponent, rows):
+    """One token of weight 1 and a million of 2^-exponent each, which together are drawn by uniforms close to 1: the sums are right
+    to 1e-11 of the mass, however small the single weights are."""
+    vocab = 1 << 20
+    x = torch.full((vocab,), -exponent * math.log(2.0), device=DEV)
+    x[4321] = 0.0
+    w = math.exp(float(x[0]))
+    mass = 1.0 + (vocab - 1) * w
+    u = torch.full((rows,), 1 - 2.0 ** -24)
+    u[rows // 2] = 1 / mass + 0.3 * (1 - 1 / mass)
+    got = kr.op_sample_tokens(x.expand(rows, -1), u.to(DEV)).ids.tolist()
+    for r in range(rows):
+        want = (float(u[r]) * mass - 1.0) / w
+        if want < -1e-11 * mass / w:
+            assert got[r] == 4321
+        else:   # (ties go by index, from which the likeliest one is left out; 1e-15: the reference's own sum)
+            place = got[r] - (got[r] > 4321)
+            assert got[r] == 4321 or abs(place - want) <= (1e-11 + 1e-15) * mass / w + 1, (r, place, want)
+
+
+@gpu
 def test_sample_zero_temperature_and_one_token_left():
     x = logits_of(5, 30, 5000, "bf16")
     first = torch.tensor([int((x[r] == x[r].max()).nonzero()[0]) for r in range(30)])

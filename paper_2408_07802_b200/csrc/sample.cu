@@ -400,9 +400,9 @@ __device__ __noinline__ void sample_any(const SampleParams &s, Smem &sm, int r, 
     const Row<H16> row(s.logits, r * s.row_stride, s.vocab);
     // the unit of the integers: the sum of all weights (in 32 bits, from pass 2) lies between 2^60 and 2^61, so what vocab roundings do
     // to a sum is below vocab 2^-61 of all
-    double all = 0.;
-    for (int c = 0; c < static_cast<int>(n_cluster_ctas()); ++c) all += sm.all[c];
-    const double one = static_cast<double>(1ull << (60 - ilogb(all)));
+    double about = 0.;
+    for (int c = 0; c < static_cast<int>(n_cluster_ctas()); ++c) about += sm.all[c];
+    const double one = static_cast<double>(1ull << (60 - ilogb(about)));
     uint32_t k_key = 0;
     u64 k_ties = 0, want, above, total;
     if (a.k > 0 && a.k < s.vocab) {

@@ -533,6 +533,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     Smem &sm = *reinterpret_cast<Smem *>(smem_raw);
     const int parts = n_cluster_ctas(), part = cluster_ctarank();
     const int r = blockIdx.x / parts, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    cluster_arrive();   // (waited for before the first store into another CTA's shared memory: by then all of them run)
     for (int i = tid; i < RANGES / 4; i += THREADS) reinterpret_cast<uint4 *>(sm.count)[i] = make_uint4(0u, 0u, 0u, 0u);
     for (int i = tid; i < STEPS; i += THREADS) sm.power[i] = exp2(i * (-1. / STEPS));
     if (tid == 0) sm.n_aside = 0;
@@ -550,6 +551,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
         for (int o = 16; o > 0; o /= 2) top = max_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
         if (lane == 0) sm.warp_f[warp] = top;
         __syncthreads();
+        cluster_wait();
         if (warp == 0) {   // to every CTA of the cluster
             top = lane < WARPS ? sm.warp_f[lane] : -INFINITY;
 #pragma unroll

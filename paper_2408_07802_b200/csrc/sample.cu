@@ -671,7 +671,8 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     }
     // Windows of ranges: of the limits (top_k, min_p), of the end of top_p, of the token.  (One warp of every CTA; they find the same.)
     if (warp == 0) {
-        // (no limits: all but the last range, where all weights together are less than 10^-14 of the largest; sample_any() finds a token there)
+        // (no limits, or none that is reached before the last range: all but that range, where the weights of 2^24 tokens together are less
+        // than 10^-34 of the largest.  With the range in the window, 20 allowed tokens of 50257 and a top_k of 50 took 310 us a row in place of 14.)
         const uint32_t n_all = s.vocab - d.count[RANGES - 1];
         int e0 = RANGES - 1, e1 = RANGES - 2, p0 = e0, p1 = e1, s0 = e0, s1 = e1;
         uint32_t e_n0 = n_all, e_n1 = n_all, p_n0 = 0, p_n1 = 0, s_n0 = 0, s_n1 = 0;
@@ -699,6 +700,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
             const int from = of(f.range, 0), to = of(f.range, 1);
             const uint32_t n0 = of(f.n0, 0), n1 = of(f.n1, 1);
             if (step <= 1) {
+                if (from == RANGES - 1) continue;   // (no limit either: what it cuts off or leaves is in the last range)
                 e0 = from;
                 e1 = to;
                 e_n0 = n0;

@@ -42,3 +42,46 @@ def test_rows_shared_by_ctas_call_after_call(dtype, vec, ctas):
         for n, g in enumerate(got):
             assert g.ids.tolist() == at[n % 16].tolist(), (rows, n)
             assert bool((g.logprob.abs() < 1e-6).all())
+
+
+# ------------------------------------------------------------------ limits that nothing reaches
+
+def device_us(call, n=20):
+    """Least device time of a call, from a graph of them"""
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(n):
+            call()
+    best = math.inf
+    for _ in range(5):
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        a.record()
+        graph.replay()
+        b.record()
+        b.synchronize()
+        best = min(best, a.elapsed_time(b) * 1e3 / n)
+    del graph
+    return best
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows", [1, 160])
+@pytest.mark.parametrize("kind", ["few allowed", "cold", "lowest number"])
+def test_top_k_beyond_what_is_left(kind, rows, dtype):
+    """Fewer tokens of any weight than top_k asks for: the same tokens as without the limit, by the same way and not digit by digit
+    (ten times as long and more)."""
+    vocab, k, t = 50257, 50, 1.0
+    g = torch.Generator().manual_seed(rows)
+    if kind == "cold":   # few of the logits lie within 140 ln(2) T = 0.5 of the largest
+        x, t = 2 * torch.randn(rows, vocab, generator=g), 0.005
+    else:
+        x = torch.full((rows, vocab), -math.inf if kind == "few allowed" else torch.finfo(dtype).min)
+        x[:, torch.randperm(vocab, generator=g)[:20]] = torch.randn(rows, 20, generator=g)
+    x, u = x.to(dtype).to(DEV), torch.rand(rows, generator=g).to(DEV)
+    limited, free = kr.op_sample_tokens(x, u, temperature=t, top_k=k), kr.op_sample_tokens(x, u, temperature=t)
+    assert limited.ids.tolist() == free.ids.tolist() and bool((limited.logprob == free.logprob).all())
+    a, b = (device_us(lambda: kr.op_sample_tokens(x, u, temperature=t, top_k=limit)) for limit in (k, 0))
+    assert a < 4 * b, (a, b)

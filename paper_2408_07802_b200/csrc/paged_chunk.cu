@@ -256,7 +256,7 @@ struct Smem {
     uint32_t odd_tiles[2][2];                        // which of them have any: [item slot][aux warp]
     uint32_t visible[4][4], missing[4][2];           // of a tile's keys, those whose page exists; whether any does not
     uint64_t q_full, q_empty, b_full[2], b_empty[2], s_full[2], p_ready[2], pv_done[2], s_free[2], p_free[2], v_full[2], v_ready[2], item_full[2],
-        item_empty[2];
+        item_empty[2], at_ready;
     uint32_t upto[THREADS], sum[THREADS / 32];
     Chunk cut_chunk[2];
     Cut cut[2];
@@ -301,6 +301,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     if (threadIdx.x == 0) {
         mbar_init(&sm.q_full, LANES ? AUX : 1);
         mbar_init(&sm.q_empty, 1);
+        mbar_init(&sm.at_ready, 2);
         for (int s = 0; s < 2; ++s) {
             mbar_init(&sm.b_full[s], LANES ? AUX : 1);
             mbar_init(&sm.b_empty[s], 1);
@@ -707,7 +708,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             // ------------------------------------------------------------------ values of masked tiles; copies by lanes
             const int aux = warp - 2, tid = aux * 32 + lane;
             bool ok = true, bad_page = false;
-            uint32_t n_items = 0, loads = 0, bundles = 0, fixes[2] = {0, 0};
+            uint32_t n_items = 0, loads = 0, bundles = 0, look_ups = 0, fixes[2] = {0, 0};
             while (ok) {
                 const int slot = n_items & 1;
                 ok = mbar_wait(&sm.item_full[slot], (n_items >> 1) & 1u, gave_up);
@@ -808,7 +809,12 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                             }
                             bad_page |= (words[0] | words[1]) != 0;
                         }
-                        asm volatile("bar.sync 1, 64;" ::: "memory");
+                        // the other warp's places too (a wait with a limit, like all here: the other warp may have given up)
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sm.at_ready);
+                        ok = mbar_wait(&sm.at_ready, look_ups++ & 1u, gave_up);
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        if (!ok) break;
                         const int st = bundles & 1;
                         ok = mbar_wait(&sm.b_empty[st], ((bundles >> 1) & 1u) ^ 1u, gave_up);
                         ok = __all_sync(0xFFFFFFFFu, ok);

@@ -538,7 +538,8 @@ int kraken_paged_attention_workspace(int32_t n_head, int32_t n_kv_head, int32_t 
  * NaN or infinite, of the rows that see its key and no others.
  * q_start does not descend.  Chunks without rows are skipped.  The rows of a chunk with chunk_seq[c] < 0 (padding), and rows
  * before q_start[0] and from q_start[chunks] on, are left as they were.  So are those of a chunk whose rows, sequence or n_keys do
- * not exist (outside 0 .. rows; more than max_pages * page_size keys); a key whose page does not exist is not visible; all of
+ * not exist (outside 0 .. rows; more than max_pages * page_size keys), and all rows of a call whose q_start goes back so often that the
+ * chunks, lying on one another, have 2^31 tiles (as counted below); a key whose page does not exist is not visible; all of
  * these raise the status bit.  Table entries of pages wholly in front of what the chunk's first token sees are of no importance.
  * The weights are rounded to the 16-bit type for the product with the values; maxima and sums are fp32.
  * The key tiles are shared out evenly over the whole grid; rows that several CTAs worked on are joined by a second kernel through

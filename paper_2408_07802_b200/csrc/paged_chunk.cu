@@ -55,6 +55,10 @@ constexpr int SIDE = 3;         // masked tiles at either end of a unit's keys: 
 // What beginning and finishing a unit costs, in tiles (1: the mixed batch 150 us in place of 146; 3: four prompts 102 in place of 104,
 // but windows with slopes 55 in place of 50), and a CTA's places at least (3: five drafted tokens 20.4 us in place of 19.3)
 constexpr int BEGIN = 2, MIN_PART = 2;
+// Where the sums of a head's places end: more than the places of chunks that lie behind one another can be (the host sees to that), and
+// two of them still fit 32 bits.  Chunks may lie on one another as often as q_start goes back, and a sum that wrapped round would send
+// the search for a CTA's share out of the list of chunks.
+constexpr uint32_t MOST_PLACES = 0x7FFFFFFFu;
 // A weight is 2^(score - m); the first tile's largest is 2^HEADROOM, and m is raised when one gets past 2^(HEADROOM + RAISE).  Half numbers end at 2^16 and 2^-24: with 7, 10^5 weights of 2^-25 of the largest still count.
 constexpr float HEADROOM = KRAKEN_F16 ? 7.f : 0.f;
 constexpr float RAISE = 8.f;
@@ -344,13 +348,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll 1
         for (int c = c_lo; c < c_hi; ++c) {
             const Chunk k = chunk_of(p, c, bad);
-            if (k.tokens > 0) upto += chunk_places(p, k);
+            if (k.tokens > 0) upto = min(upto + chunk_places(p, k), MOST_PLACES);
         }
         if (bad && blockIdx.x == 0 && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
             const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, upto, off);
-            if (lane >= off) upto += v;
+            if (lane >= off) upto = min(upto + v, MOST_PLACES);
         }
         if (lane == 31) sm.sum[warp] = upto;
         sm.upto[threadIdx.x] = upto;   // of the warp
@@ -361,9 +365,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll
         for (int off = 1; off < 16; off <<= 1) {
             const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, warps, off);
-            if (lane >= off) warps += v;
+            if (lane >= off) warps = min(warps + v, MOST_PLACES);
         }
         per_head = __shfl_sync(0xFFFFFFFFu, warps, THREADS / 32 - 1);
+        if (per_head == MOST_PLACES) {   // (only where chunks lie on one another: nothing is done)
+            per_head = 0;
+            if (blockIdx.x == 0 && threadIdx.x == 0 && p.status) atomicOr(p.status, STATUS_BAD_PAGE);
+        }
         const unsigned long long total = (unsigned long long)per_head * units;
         const int n_cta = static_cast<int>(max(1ull, min((unsigned long long)gridDim.x, total / MIN_PART)));
         const unsigned long long share = total >> 32 ? total / n_cta : (uint32_t)total / (uint32_t)n_cta, rest = total - share * n_cta;

@@ -38,3 +38,28 @@ def test_copies_by_lanes_give_the_same_bits(H, Hkv, hd, dtype, window):
             assert int(status) == 0
     for out, lse in got[1:]:
         assert bool((out == got[0][0]).all()) and bool((lse == got[0][1]).all())
+
+
+@gpu
+def test_chunks_on_one_another_beyond_all_counting():
+    """q_start that goes back and forth over all rows: every second chunk is one that exists, and all of them together have more than
+    2^32 tiles.  Nothing is done, and the status word says so."""
+    rows, keys, page, chunks = 1 << 17, 1 << 18, 256, 1 << 14
+    q = torch.zeros(rows, 1, 64, dtype=torch.bfloat16, device=DEV)
+    k = torch.zeros(1, 1, page, 64, dtype=torch.bfloat16, device=DEV)
+    table = torch.zeros(1, keys // page, dtype=torch.int32, device=DEV)
+    pairs, tiles = rows // 256, (keys - rows // 2) // 128
+    assert chunks // 2 * pairs * tiles > 2 ** 32
+    starts = torch.zeros(chunks + 1, dtype=torch.int32, device=DEV)
+    starts[1::2] = rows
+    out, lse = torch.full_like(q, 7.0), torch.full((rows, 1), 7.0, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    zeros = torch.zeros(chunks, dtype=torch.int32, device=DEV)
+    kr.op_paged_chunk_attention(q, k, k, table, starts, torch.full_like(zeros, keys), chunk_seq=zeros, out=out, lse=lse, status=status)
+    assert int(status) == kr.STATUS_BAD_PAGE
+    assert bool((out == 7).all()) and bool((lse == 7).all())
+    # one that goes back once: the chunk with the rows from 20 to 10 does not exist, the others do
+    status.zero_()
+    kr.op_paged_chunk_attention(q[:30], k, k, table, int32([0, 20, 10, 30]), int32([40, 40, 40]), chunk_seq=int32([0, 0, 0]), out=out[:30],
+                                lse=lse[:30], status=status)
+    assert int(status) == kr.STATUS_BAD_PAGE and bool((out[:30] == 0).all()) and bool((out[30:] == 7).all())

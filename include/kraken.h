@@ -530,7 +530,7 @@ int kraken_paged_attention_workspace(int32_t n_head, int32_t n_kv_head, int32_t 
  * (kraken_op_paged_append puts them there).  A token at position p sees the keys 0 .. p, with window > 0 only the last `window`
  * of these.  For key j
  *     x_j = scale * q . k_j;   score_cap > 0:  x_j = score_cap * tanh(x_j / score_cap);   slopes != NULL:  x_j += slopes[h] * (j - p);
- * (scale * log2(e) and 1 / score_cap have to be finite in fp32, EINVAL otherwise);
+ * (scale * log2(e), 1 / score_cap and 2 log2(e) scale / score_cap have to be finite in fp32, EINVAL otherwise);
  * out = sum_j softmax(x)_j v_j, and lse (or NULL) = log sum_j exp(x_j).  Query head h reads key/value head
  * h / (n_head / n_kv_head).  Chunks of one token, of a draft, pieces of prompts and whole prompts may share a call.
  * A token at a negative position (more tokens than n_keys) sees nothing: out = 0, lse = -inf; so does one all of whose scores are

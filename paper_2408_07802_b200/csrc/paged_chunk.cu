@@ -37,6 +37,7 @@
 // The size of the code counts: with a tile's 128 scores in registers, everything written out for them, instructions came from
 // beyond the first cache all the time.  So the scores are read from tensor memory twice, 32 at a time (four prompts 111 -> 104),
 // masks are bits, and there is one form of a step (one for tiles that every row sees whole and one for the others: 137).
+#include <float.h>
 #include <math.h>
 #include <string.h>
 
@@ -66,6 +67,25 @@ constexpr float RAISE = 8.f;
 // m: the score that has the weight 2^HEADROOM; l: the sum of the weights
 __device__ __forceinline__ float lse_of_weights(float m, float l) { return l == 0.f ? -INFINITY : m + (log2f(l) - HEADROOM) * LN2; }
 
+// s -> cap tanh(scale s / cap) by way of u = 2 log2(e) scale s / cap, which is of the size of the result's exponent whatever the two
+// factors are.  Up to `border` an odd polynomial in u, fitted to tanh up to 1/2 (to 1.4e-8 of it, 1.2e-7 with the roundings); beyond,
+// cap (1 - 2 / (1 + 2^u)), off by up to 2e-7 cap.  (With coefficients for s itself, powers of scale / cap had to fit 32 bits.)
+struct Cap {
+    float by, border, cap, c[5];
+    Cap() = default;
+    Cap(double scale, double cap_) : cap(static_cast<float>(cap_)) {
+        constexpr double FIT[5] = {1., -0.33333069, 0.13324779, -0.052986074, 0.017135004}, TO_T = 0.5 * 0.693147180559945309417;
+        const double ideal = scale / cap_ / TO_T;
+        // A factor so small that 32 bits hold it with less than 22 of their own: another one, that leaves u below the ideal's border for
+        // every s there is
+        const bool tiny = fabs(ideal) < 0.25 * FLT_MIN;
+        by = static_cast<float>(tiny ? copysign(FLT_MIN, ideal) : ideal);
+        border = tiny ? FLT_MAX : LOG2E;
+        const double t = tiny ? fabs(ideal) / FLT_MIN * TO_T : TO_T;   // of 1 in u
+        for (int i = 0; i < 5; ++i) c[i] = static_cast<float>(FIT[i] * (tiny ? fabs(scale) / FLT_MIN : cap_ * TO_T) * pow(t, 2 * i));
+    }
+};
+
 struct ChunkParams {
     PagedView c;
     const uint16_t *q;
@@ -75,6 +95,7 @@ struct ChunkParams {
     const float *slopes;
     long long q_row, q_head, out_row, out_head, lse_row;
     float scale, cap;
+    Cap capped;   // where there is a cap
     int chunks, rows, n_head, rep, window, head_dim;
     int heads;        // query heads of a tile
     int head_tiles;   // tiles that the heads of a key/value head make
@@ -97,20 +118,15 @@ __device__ __forceinline__ bool odd_h16(uint32_t pair) {
     return (pair & EXPONENT) == EXPONENT || (pair & (EXPONENT << 16)) == EXPONENT << 16;
 }
 
-// x -> cap tanh(x scale / cap), to_cap = scale / cap, for |x to_cap| <= 1/2: an odd polynomial of degree 9 fitted to tanh there
-// (to 1.4e-8 of it, 1.2e-7 with the roundings)
-__device__ __forceinline__ void tanh_near(float (&s)[32], float to_cap, float scale) {
-    const float q = to_cap * to_cap;
-    const uint64_t c4 = splat2(0.017135004f * scale * q * q * q * q), c3 = splat2(-0.052986074f * scale * q * q * q),
-                   c2 = splat2(0.13324779f * scale * q * q), c1 = splat2(-0.33333069f * scale * q), c0 = splat2(scale);
+__device__ __forceinline__ void tanh_near(float (&s)[32], const Cap &k) {
+    const uint64_t by = splat2(k.by), c4 = splat2(k.c[4]), c3 = splat2(k.c[3]), c2 = splat2(k.c[2]), c1 = splat2(k.c[1]), c0 = splat2(k.c[0]);
 #pragma unroll
     for (int i = 0; i < 32; i += 2) {
-        const uint64_t x = pk2(s[i], s[i + 1]), y = mul2(x, x);
-        upk2(mul2(x, fma2(y, fma2(y, fma2(y, fma2(y, c4, c3), c2), c1), c0)), s[i], s[i + 1]);
+        const uint64_t u = mul2(pk2(s[i], s[i + 1]), by), y = mul2(u, u);
+        upk2(mul2(u, fma2(y, fma2(y, fma2(y, fma2(y, c4, c3), c2), c1), c0)), s[i], s[i + 1]);
     }
 }
-// cap tanh(y / 2 log2(e)) = cap - 2 cap / (1 + 2^y), off by up to 2e-7 cap
-__device__ __forceinline__ float tanh_far(float y, float cap) { return fmaf(-2.f * cap, rcp_approx(1.f + ex2_approx(y)), cap); }
+__device__ __forceinline__ float tanh_far(float u, const Cap &k) { return fmaf(-2.f, rcp_approx(1.f + ex2_approx(u)) * k.cap, k.cap); }
 
 // What a chunk brings
 struct Chunk {
@@ -863,7 +879,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const uint32_t s_addr = lane_addr + w * TK, p_addr = lane_addr + C::P_COL0 + w * C::P_STRIDE, o_addr = lane_addr + C::O_COL0 + w * C::O_STRIDE;
         const int token = p.by_heads.quotient(row), g = row - token * p.heads;
         // s holds scores (GENERAL), or products that one factor makes scores
-        const float to_log2 = GENERAL ? LOG2E : p.scale * LOG2E, to_score = GENERAL ? 1.f : p.scale, to_cap = GENERAL ? p.scale / p.cap : 0.f;
+        const float to_log2 = GENERAL ? LOG2E : p.scale * LOG2E, to_score = GENERAL ? 1.f : p.scale;
         bool ok = true;
         uint32_t n_items = 0, tile_cnt = 0, done_cnt = 0, pf_cnt = 0;
         while (ok) {
@@ -900,12 +916,12 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                             float high[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                             for (int i = 0; i < 32; i += 2) high[(i >> 1) & 3] = max3f(high[(i >> 1) & 3], fabsf(s[i]), fabsf(s[i + 1]));
-                            const float most = fmaxf(fmaxf(high[0], high[1]), fmaxf(high[2], high[3])) * fabsf(to_cap);
-                            if (__all_sync(0xFFFFFFFFu, most <= 0.5f)) {
-                                tanh_near(s, to_cap, p.scale);
+                            const float most = fmaxf(fmaxf(high[0], high[1]), fmaxf(high[2], high[3])) * fabsf(p.capped.by);
+                            if (__all_sync(0xFFFFFFFFu, most <= p.capped.border)) {
+                                tanh_near(s, p.capped);
                             } else {
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) s[i] = tanh_far(s[i] * (2.f * LOG2E * to_cap), p.cap);
+                                for (int i = 0; i < 32; ++i) s[i] = tanh_far(s[i] * p.capped.by, p.capped);
                             }
                         } else if (!p.slopes) {
 #pragma unroll
@@ -1232,7 +1248,7 @@ extern "C" int kraken_paged_chunk_attention_workspace(int32_t head_dim, size_t *
 extern "C" int kraken_op_paged_chunk_attention(const kraken_paged_cache *cache, const kraken_paged_chunk_args *a, uint32_t *d_status,
                                                void *stream) {
     using namespace kr;
-    ChunkParams p;
+    ChunkParams p = {};
     if (!a) return KRAKEN_EINVAL;
     int rc = paged_view(cache, &p.c);
     if (rc) return rc;
@@ -1241,7 +1257,8 @@ extern "C" int kraken_op_paged_chunk_attention(const kraken_paged_cache *cache, 
         a->window < 0 || !isfinite(a->score_cap) || a->score_cap < 0.f)
         return KRAKEN_EINVAL;
     // (factors in the kernel: a score of 0 times an infinite one would be a NaN)
-    if (!isfinite(a->scale * LOG2E) || (a->score_cap > 0.f && !isfinite(1.f / a->score_cap)))
+    if (a->score_cap > 0.f) p.capped = Cap(a->scale, a->score_cap);
+    if (!isfinite(a->scale * LOG2E) || (a->score_cap > 0.f && (!isfinite(1.f / a->score_cap) || !isfinite(p.capped.by))))
         return KRAKEN_EINVAL;
     if (!a->chunk_seq && a->chunks > cache->n_seqs) return KRAKEN_EINVAL;
     if ((a->rows > 1 && a->out_row_stride == 0) || (a->n_head > 1 && a->out_head_stride == 0) || (a->lse && a->rows > 1 && a->lse_row_stride == 0))

@@ -118,15 +118,27 @@ __device__ __forceinline__ bool odd_h16(uint32_t pair) {
     return (pair & EXPONENT) == EXPONENT || (pair & (EXPONENT << 16)) == EXPONENT << 16;
 }
 
+__device__ __forceinline__ uint64_t tanh_poly(uint64_t u, const Cap &k) {
+    const uint64_t y = mul2(u, u);
+    return mul2(u, fma2(y, fma2(y, fma2(y, fma2(y, splat2(k.c[4]), splat2(k.c[3])), splat2(k.c[2])), splat2(k.c[1])), splat2(k.c[0])));
+}
 __device__ __forceinline__ void tanh_near(float (&s)[32], const Cap &k) {
-    const uint64_t by = splat2(k.by), c4 = splat2(k.c[4]), c3 = splat2(k.c[3]), c2 = splat2(k.c[2]), c1 = splat2(k.c[1]), c0 = splat2(k.c[0]);
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) upk2(tanh_poly(mul2(pk2(s[i], s[i + 1]), splat2(k.by)), k), s[i], s[i + 1]);
+}
+// The same where some may be beyond the border (to the last bit as above for one that is not)
+__device__ __forceinline__ void tanh_any(float (&s)[32], const Cap &k) {
 #pragma unroll
     for (int i = 0; i < 32; i += 2) {
-        const uint64_t u = mul2(pk2(s[i], s[i + 1]), by), y = mul2(u, u);
-        upk2(mul2(u, fma2(y, fma2(y, fma2(y, fma2(y, c4, c3), c2), c1), c0)), s[i], s[i + 1]);
+        const uint64_t u = mul2(pk2(s[i], s[i + 1]), splat2(k.by));
+        float u0, u1;
+        upk2(u, u0, u1);
+        upk2(tanh_poly(u, k), s[i], s[i + 1]);
+        const float far0 = fmaf(-2.f, rcp_approx(1.f + ex2_approx(u0)) * k.cap, k.cap), far1 = fmaf(-2.f, rcp_approx(1.f + ex2_approx(u1)) * k.cap, k.cap);
+        s[i] = fabsf(u0) <= k.border ? s[i] : far0;
+        s[i + 1] = fabsf(u1) <= k.border ? s[i + 1] : far1;
     }
 }
-__device__ __forceinline__ float tanh_far(float u, const Cap &k) { return fmaf(-2.f, rcp_approx(1.f + ex2_approx(u)) * k.cap, k.cap); }
 
 // What a chunk brings
 struct Chunk {
@@ -904,9 +916,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 const int mark = (tile0 + j) & 3;
                 const bool missing = (sm.missing[mark][0] | sm.missing[mark][1]) != 0;
                 const bool masked = j * TK < lo_max || (j + 1) * TK > hi_min || missing;
-                // the tile in four steps, twice: the scores and their maximum; the weights
+                // the tile in four steps, twice: the scores and their maximum; the weights.  (GENERAL: one copy of a step with both ways to
+                // tanh; two of them take 160 us in place of 148 for the mixed batch, 215 in place of 205 with five times its scores.)
                 float mx = -INFINITY;
-#pragma unroll 2
+#pragma unroll(GENERAL ? 1 : 2)
                 for (int c = 0; c < TK / 32; ++c) {
                     float s[32];
                     tmem_ld_32x32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s));
@@ -917,11 +930,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll
                             for (int i = 0; i < 32; i += 2) high[(i >> 1) & 3] = max3f(high[(i >> 1) & 3], fabsf(s[i]), fabsf(s[i + 1]));
                             const float most = fmaxf(fmaxf(high[0], high[1]), fmaxf(high[2], high[3])) * fabsf(p.capped.by);
-                            if (__all_sync(0xFFFFFFFFu, most <= p.capped.border)) {
+                            // (each score goes its own way, whatever others a warp holds: where all of them are near, that is known beforehand)
+                            if (__all_sync(0xFFFFFFFFu, !live || most <= p.capped.border)) {
                                 tanh_near(s, p.capped);
                             } else {
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) s[i] = tanh_far(s[i] * p.capped.by, p.capped);
+                                tanh_any(s, p.capped);
                             }
                         } else if (!p.slopes) {
 #pragma unroll
@@ -971,9 +984,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     m = mx;
                 }
                 float neg = m == -INFINITY ? 0.f : HEADROOM - m * to_log2;
-                // scores whose product with log2(e) may be infinite, or further from the rounded one than weights last
-                const bool far = __any_sync(0xFFFFFFFFu, fabsf(neg) > 65536.f);
-                if (far) neg = HEADROOM;
+                // scores whose product with log2(e) may be infinite, or further from the rounded one than weights last: m is taken off first
+                float off = 0.f;
+                if (fabsf(neg) > 65536.f) {
+                    neg = HEADROOM;
+                    off = m;
+                }
+                const bool far = __any_sync(0xFFFFFFFFu, live && off != 0.f);   // (a row that takes off 0 stays as it is)
                 if (C::SEPARATE_P && j > a0) {
                     ok = mbar_wait(&sm.p_free[w], pf_cnt & 1u, gave_up);
                     ++pf_cnt;
@@ -989,7 +1006,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     tmem_ld_wait();
                     if (far) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) s[i] -= m == -INFINITY ? 0.f : m;
+                        for (int i = 0; i < 32; ++i) s[i] -= off;
                     }
                     uint32_t pk[16];
 #pragma unroll

@@ -72,6 +72,51 @@ def call(pages, q, starts, lens, **kw):
     return out, lse
 
 
+# ------------------------------------------------------------------ a row and what is none of its business
+
+def leave_in_shared_memory(value, dtype):
+    """A call with 4 query heads a key/value head fills all rows of its query tiles, on every SM."""
+    pages = Pages(41, [128], 1, 128, 16, dtype, fill=False)
+    pages.k[:], pages.v[:] = 1.0, 1.0
+    q = torch.full((148 * 64, 4, 128), value, dtype=T16[dtype], device=DEV)
+    call(pages, q, [64 * i for i in range(149)], [128] * 148, chunk_seq=int32([0] * 148))
+
+
+@gpu
+@pytest.mark.parametrize("cap,scale", [(0.0, None), (30.0, 0.125), (4.0, 0.125)])
+@pytest.mark.parametrize("H,Hkv,hd,page,dtype", [(3, 1, 64, 16, "bf16"), (10, 2, 128, 16, "f16"), (65, 1, 64, 16, "bf16"), (4, 1, 128, 16, "bf16"),
+                                                 (6, 2, 72, 100, "bf16"), (7, 1, 128, 100, "f16")])
+def test_a_row_follows_from_what_it_sees_alone(H, Hkv, hd, page, dtype, cap, scale):
+    """The same to the last bit whatever the other chunks' queries, padding rows, slots behind the sequences, keys and values behind
+    a token and what an earlier call left in shared memory: also where these would choose another way to the same number."""
+    spans, big = [(200, 50), (90, 40)], 1e30 if dtype == "bf16" else 6e4
+    lens, starts = [p + n for p, n in spans], starts_of(spans, 3)
+    kw = dict(score_cap=cap, scale=scale)
+    pages = Pages(42, lens, Hkv, hd, page, dtype)
+    q = normal(6, starts[-1] + 20, H, hd).to(T16[dtype])
+    leave_in_shared_memory(0.0, dtype)
+    out, lse = call(pages, q, starts, lens, **kw)
+    mine = slice(starts[0], starts[1])
+    same = lambda got, rows: bool((got[0][rows] == out[rows]).all()) and bool((got[1][rows] == lse[rows]).all())  # noqa: E731
+    for value in (1.0, big, math.inf, math.nan):
+        leave_in_shared_memory(value, dtype)
+        assert same(call(pages, q, starts, lens, **kw), slice(None)), value
+    for factor in (0.0, 300.0, big):
+        other = q.clone()
+        other[starts[1]:] = (other[starts[1]:].float() * factor).to(q.dtype)
+        other[:starts[0]] = other[starts[2]:] = big
+        assert same(call(pages, other, starts, lens, **kw), mine), factor
+    for value in (0.0, 500.0, big):
+        for cache in (pages.k, pages.v):
+            cache.nan_to_num_(nan=value)
+        assert same(call(pages, q, starts, lens, **kw), slice(None)), value
+    # the last token's key, which no other row sees
+    pages = Pages(42, lens, Hkv, hd, page, dtype)
+    for value in (500.0, big, math.nan):
+        pages.k[pages.table[0, (lens[0] - 1) // page].item(), :, (lens[0] - 1) % page] = value
+        assert same(call(pages, q, starts, lens, **kw), slice(starts[0], starts[1] - 1)), value
+
+
 # ------------------------------------------------------------------ scores that come near their cap
 
 @gpu

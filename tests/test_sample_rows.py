@@ -85,3 +85,27 @@ def test_top_k_beyond_what_is_left(kind, rows, dtype):
     assert limited.ids.tolist() == free.ids.tolist() and bool((limited.logprob == free.logprob).all())
     a, b = (device_us(lambda: kr.op_sample_tokens(x, u, temperature=t, top_k=limit)) for limit in (k, 0))
     assert a < 4 * b, (a, b)
+
+
+# ------------------------------------------------------------------ weights between the windows
+
+@gpu
+@pytest.mark.parametrize("before,at,after", [(172, 160, 148), (169, 158, 147), (66, 50, 35), (218, 180, 148)])
+def test_many_alike_on_both_sides_of_the_window(before, at, after):
+    """Half a million equal weights before the window of the token and as many behind it, 4000 in it of about a millionth of the mass each;
+    the uniforms are such that u M lies 5 10^-11 to 10^-9 of the mass from a border.  That is more than 1e-11: the definition's token.
+    (Weights of so many 256ths: their sums in 32 bits tell where the windows have to be.)"""
+    n, middle = 1 << 19, 4000
+    x = torch.cat([torch.full((k,), math.log(w / 256)) for k, w in ((n, before), (middle, at), (n, after))])
+    x[77] = 0.0
+    w = [math.exp(float(x[i])) for i in (0, n, n + middle)]
+    lower = 1 + (n - 1) * w[0]
+    mass = lower + middle * w[1] + n * w[2]
+    u = torch.arange(math.ceil(lower / mass * 2 ** 24) + 20, math.floor((lower + middle * w[1]) / mass * 2 ** 24) - 20).double() * 2.0 ** -24
+    place = (u * mass - lower) / w[1]          # (the sums here are off by 2^-53 of the mass, 10^-10 of a place)
+    share = w[1] / mass
+    near = (place - place.round()).abs() * share
+    some = ((near > 5e-11) & (near < 1e-9)).nonzero()[:, 0][:600]
+    assert some.numel() > 40
+    got = kr.op_sample_tokens(x.to(DEV).expand(some.numel(), -1), u[some].float().to(DEV)).ids.cpu() - n
+    assert got.tolist() == place[some].floor().long().tolist()

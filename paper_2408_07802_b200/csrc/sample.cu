@@ -13,8 +13,8 @@
 // What was put aside (some hundred logits) is sorted, its weights are summed in order, and every border is then known as if the
 // row had been sorted.  A sum of weights in 32 bits is off by 10^-7, and of 50 thousand alike each has 2 10^-5 of the mass: the
 // token would be another one in a row of every hundred.  So sums and weights next to a border are 64 bits.
-// Where a border does not lie in its window (the mean weights were too far off), or more logits lie in the windows than there is
-// room for (many equal ones), sample_any() finds the borders digit by digit of the logits' order, with sums of integers: 0.6 ms for a
+// Where a border does not lie in its window (the mean weights were too far off), more logits lie in the windows than there is
+// room for (many equal ones), or the temperature is beyond 10^-29 .. 10^29, sample_any() finds the borders digit by digit of the logits' order, with sums of integers: 0.6 ms for a
 // row of 50257 fp32 logits (1.1 with every weight added by itself in 64 bits), 1.2 to 1.7 for 16-bit ones of 105 to 132 thousand.
 //
 // Few rows: up to 8 CTAs of a cluster share a row.
@@ -396,13 +396,20 @@ __device__ __forceinline__ uint32_t descend(Smem &sm, const Row<H16> &row, uint3
 }
 
 template <bool H16>
-__device__ __noinline__ void sample_any(const SampleParams &s, Smem &sm, int r, float top) {
+__device__ __noinline__ void sample_any(const SampleParams &s, Smem &sm, int r, float top, bool summed) {
     const Ask a = ask_of(s, sm.power, r, top);
     const Row<H16> row(s.logits, r * s.row_stride, s.vocab);
-    // the unit of the integers: the sum of all weights (in 32 bits, from pass 2) lies between 2^60 and 2^61, so what vocab roundings do
-    // to a sum is below vocab 2^-61 of all
+    // the unit of the integers: the sum of all weights (in 32 bits, from pass 2, where that was) lies between 2^60 and 2^61, so what vocab
+    // roundings do to a sum is below vocab 2^-61 of all
     double about = 0.;
-    for (int c = 0; c < static_cast<int>(n_cluster_ctas()); ++c) about += sm.all[c];
+    if (summed) {
+        for (int c = 0; c < static_cast<int>(n_cluster_ctas()); ++c) about += sm.all[c];
+    } else {
+        double all[1] = {0.};
+        row.template visit<1, true>(0, 1, [&](int, float x) { all[0] += a.weights.of(x); });
+        block_sums(sm, all);
+        about = all[0];
+    }
     const double one = static_cast<double>(1ull << (60 - ilogb(about)));
     uint32_t k_key = 0;
     u64 k_ties = 0, want, above, total;
@@ -589,6 +596,12 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
         }
         return;
     }
+    // The passes below take log2(e) / T in two pieces of 32 bits, and differences of logits in 32: beyond these temperatures a piece is no
+    // normal number, and logits that count may be further apart than fp32 holds.
+    if (!(t > 1e-29f && t < 1e29f)) {
+        if (part == 0) sample_any<H16>(s, sm, r, top, false);
+        return;
+    }
     // 2: how many logits in each range
     const float per = a.weights.per_hi;
     auto range_of = [&](float x) { return Below(x, top, per).range(); };
@@ -747,7 +760,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     const uint32_t n_gap0 = sm.windows.n_gap0, n_gap1 = sm.windows.n_gap1, n_gap2 = sm.windows.n_gap2, n_aside = sm.windows.n_aside;
     if (n_aside > ROOM) {   // (the same for every CTA)
         cluster_sync_all();   // (all have read the others' counts)
-        if (part == 0) sample_any<H16>(s, sm, r, top);
+        if (part == 0) sample_any<H16>(s, sm, r, top, true);
         return;
     }
 
@@ -908,7 +921,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     }
     __syncthreads();
     if (sm.token < 0) {
-        sample_any<H16>(s, sm, r, top);
+        sample_any<H16>(s, sm, r, top, true);
         return;
     }
     if (tid == 0) {

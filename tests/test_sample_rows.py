@@ -109,3 +109,27 @@ def test_many_alike_on_both_sides_of_the_window(before, at, after):
     assert some.numel() > 40
     got = kr.op_sample_tokens(x.to(DEV).expand(some.numel(), -1), u[some].float().to(DEV)).ids.cpu() - n
     assert got.tolist() == place[some].floor().long().tolist()
+
+
+# ------------------------------------------------------------------ temperatures at the ends
+
+@gpu
+@pytest.mark.parametrize("rows", [1, 160])
+@pytest.mark.parametrize("vocab", [40, 40000])
+def test_temperatures_at_the_ends(vocab, rows):
+    """Logits further apart than fp32 holds at a temperature as large, and logits below the normal numbers at one as small: weights
+    e^0, e^-1, e^-2 all the same."""
+    for t, step in ((3e38, 3e38), (1e37, 1e37), (2e-42, 2e-42), (1e-38, 1e-38)):
+        tt, st = (float(torch.tensor(v, dtype=torch.float32)) for v in (t, step))
+        x = torch.full((vocab,), -math.inf)
+        x[5], x[9], x[11] = st, 0.0, -st
+        w = [math.exp((float(x[i]) - float(x[5])) / tt) for i in (5, 9, 11)]
+        m = sum(w)
+        u = (torch.arange(rows) + 0.5) / rows
+        u[rows // 2] = 0.999
+        want = [5 if float(v) * m < w[0] else (9 if float(v) * m < w[0] + w[1] else 11) for v in u]
+        got = kr.op_sample_tokens(x.to(DEV).expand(rows, -1), u.to(DEV), temperature=t)
+        assert got.ids.tolist() == want, t
+        p = {5: w[0], 9: w[1], 11: w[2]}
+        for i, l in zip(want, got.logprob.tolist()):   # (rounded to 32 bits)
+            assert abs(l - math.log(p[i] / m)) <= 2.0 ** -23 * abs(l) + 2.0 ** -24

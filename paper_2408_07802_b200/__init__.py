@@ -369,9 +369,12 @@ class KrakenModel:
     def generate(self, tokens: torch.Tensor, uniforms: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0) -> "SampledTokens":
         """Prefill of tokens [batch, seqlen] and one new token of every sequence for each row of uniforms [steps, batch], each
         drawn by op_sample_tokens (which see for the parameters) and fed to the next decode step.  Nothing waits for the host.
+        The prompt and all tokens but the last have to find room in max_pos positions (ECAPACITY, before anything is run).
         ids int32 and logprob float32 [steps, batch]."""
         steps, b = uniforms.shape
         assert uniforms.dtype == torch.float32 and uniforms.device == self.device and b == tokens.shape[0]
+        if tokens.shape[1] + steps - 1 > self.cfg.max_pos:   # (the last token drawn is not fed)
+            raise KrakenError(ECAPACITY, "generate")
         ids = torch.empty(steps, b, dtype=torch.int32, device=self.device)
         logprob = torch.empty(steps, b, dtype=torch.float32, device=self.device)
         logits = self.prefill(tokens)

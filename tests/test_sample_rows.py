@@ -8,6 +8,7 @@ import math
 import pytest
 import torch
 
+import kraken_inputs as ki
 import paper_2408_07802_b200 as kr
 from paper_2408_07802_b200 import build as kbuild
 
@@ -133,3 +134,22 @@ def test_temperatures_at_the_ends(vocab, rows):
         p = {5: w[0], 9: w[1], 11: w[2]}
         for i, l in zip(want, got.logprob.tolist()):   # (rounded to 32 bits)
             assert abs(l - math.log(p[i] / m)) <= 2.0 ** -23 * abs(l) + 2.0 ** -24
+
+
+# ------------------------------------------------------------------ generate
+
+@gpu
+def test_generate_says_beforehand_that_there_is_no_room():
+    """Prompt and steps that do not fit are refused before a token is drawn, and the handle stays as it was; the last step that fits runs."""
+    s = ki.CONFIGS["C0"]
+    model = kr.KrakenModel(kr.make_config(s, max_batch=2, max_pos=24), ki.make_weights(s, seed=0, device=DEV), DEV)
+    prompt = ki.uniform_tokens(1, s.vocab, 2, 20, DEV)
+    model.prefill(prompt[:, :7].contiguous())
+    u = torch.rand(6, 2, generator=torch.Generator().manual_seed(1)).to(DEV)
+    with pytest.raises(kr.KrakenError) as e:
+        model.generate(prompt, u)
+    assert e.value.status == kr.ECAPACITY and model.cur_len == 7
+    got = model.generate(prompt, u[:5])
+    assert model.cur_len == 24 and bool(((got.ids >= 0) & (got.ids < s.vocab)).all())
+    assert model.generate(prompt, u[:0]).ids.shape == (0, 2)
+    model.close()

@@ -472,8 +472,8 @@ int kraken_op_paged_append(const kraken_paged_cache *cache, const kraken_paged_a
 
 /* kraken_op_paged_append with norms of queries and keys, head by head, before the rotation:
  *     x_e -> x_e * w_e / sqrt(sum_e x_e^2 / head_dim + eps)      over all head_dim elements of a head, in fp32,
- * rounded once, after the rotation (squares or sums that fp32 does not hold are infinite or 0 there).  q_weight, k_weight: 16-bit, element e of head h at h * head_stride + e (a head stride of 0:
- * the same for all heads), or NULL (ones).  The weights must not overlap what the call writes.  Values are copied as they are.
+ * rounded once, after the rotation (squares or sums that fp32 does not hold are infinite or 0 there).  q_weight, k_weight: 16-bit,
+ * element e of head h at h * head_stride + e (a head stride of 0: the same for all heads), or NULL (ones).  The weights must not overlap what the call writes.  Values are copied as they are.
  * Everything else as there; besides, EINVAL: norm NULL, eps negative or not finite; EUNSUPPORTED: weights that are not 16-byte
  * aligned, head strides no multiple of 8. */
 typedef struct kraken_paged_norm_args {
@@ -541,11 +541,12 @@ int kraken_paged_attention_workspace(int32_t n_head, int32_t n_kv_head, int32_t 
  * not exist (outside 0 .. rows; more than max_pages * page_size keys), and all rows of a call whose q_start goes back so often that the
  * chunks, lying on one another, have 2^31 tiles (as counted below); a key whose page does not exist is not visible; all of
  * these raise the status bit.  Table entries of pages wholly in front of what the chunk's first token sees are of no importance.
- * The weights are rounded to the 16-bit type for the product with the values; maxima and sums are fp32.
+ * The weights are rounded to the 16-bit type for the product with the values; maxima and sums are fp32.  Up to some 8 new tokens of a
+ * sequence, kraken_op_paged_attention with a row for each is faster and keeps more of the weights' bits.
  * The key tiles are shared out evenly over the whole grid; rows that several CTAs worked on are joined by a second kernel through
  * `workspace` (kraken_paged_chunk_attention_workspace bytes, 16-byte aligned, contents of no importance; calls that may overlap
  * on the device each need their own).  The result depends on the device's number of SMs and on all the lengths of the call in
- * its last bits only, and is the same from run to run.
+ * its last bits only, not on what other rows, hidden keys or padding hold, and is the same from run to run.
  * q_start, chunk_seq, n_keys and the page table must not change while the call runs.  A bounded wait that gave up raises bit 1 of
  * the status word; the outputs then mean nothing.  Rows or heads of out or lse must not lie on one another (EINVAL for a stride
  * of 0), and none of them may overlap another tensor of the call.
@@ -597,8 +598,8 @@ int kraken_op_token_logprobs(const kraken_logprobs_args *args, uint32_t *d_statu
  * the first token is always left.  With M the sum of the weights left, ids[r] is the first token up to which (it included) more than
  * uniforms[r] * M lies, and logprob[r] = log(w / M), the logarithm of the probability with which it was drawn.  So a uniform
  * of 0 gives the likeliest token; a temperature of 0 too, of several the first, with logprob 0.
- * Weights and sums are formed in 64 bits: the token is the one that the definition gives, but where u * M, top_p * Z or min_p is
- * within about 1e-11 of a border.
+ * Sums are formed in 64 bits, of weights that are right to 1.5e-11 (next to a border: to 1e-15) of themselves: the token is the one
+ * that the definition gives, but where u * M, top_p * Z or min_p is within about 1e-11 of a border.
  * logits: [rows, vocab], row stride in elements, any alignment of the element type; dtype 0 = fp32, 1 = the library's 16-bit type.
  * temperature, top_k, top_p, min_p: device arrays [rows], or NULL: the value ..._all for every row.  top_k <= 0 or >= vocab, top_p >= 1
  * and min_p <= 0 are no limit; min_p above 1 counts as 1.  uniforms: fp32 [rows], in [0, 1).

@@ -748,7 +748,8 @@ def op_paged_chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: to
     """Attention of chunks of new tokens over a cache in pages (kraken_op_paged_chunk_attention): rows q_start[c] ..
     q_start[c + 1] - 1 of q [rows, heads, head_dim] are consecutive tokens of sequence chunk_seq[c] (None: sequence c; negative:
     padding), the last of them at position n_keys[c] - 1; each sees the cached keys up to its own (which op_paged_append has
-    put there).  Prompts, pieces of them, drafted tokens and single ones may share a call.  scale, score_cap, window, slopes:
+    put there).  Prompts, pieces of them, drafted tokens and single ones may share a call (up to some 8 new tokens of a sequence alone
+    take less time by op_paged_decode_attention with a row for each).  scale, score_cap, window, slopes:
     as for op_paged_decode_attention, seen from each token.  Returns (out, lse): out like q, lse float32 [rows, heads].  Where
     neither is given they are made, as parts of one allocation: keeping either keeps both (clone the one to be kept), and rows
     of no chunk hold anything; rows of no chunk in given ones stay as they were."""

@@ -27,13 +27,16 @@
 //
 // What bounds it.  Products at the tensor cores' rate would be 2 x 512 cycles a query tile and key tile with head dims of 128;
 // a row's 128 exponentials take as long in the special-function units.  A key tile takes 3.7 to 4.2 thousand cycles with both query
-// tiles at work, each of which goes through scores, weights and product one after the other while the other one does the same.  A
+// tiles at work, each of which goes through scores, weights and product one after the other while the other one does the same; with
+// a cap or slopes (GENERAL) 7 to 8 thousand, as every score goes back to tensor memory on the way.  A
 // unit costs some 9 thousand cycles besides (its first keys and scores, its last product, the way out), a call 12 thousand (the
 // lengths read and the work cut, the first copies) and the second kernel.  Measured on a B200, a graph of calls:
-//   2048 tokens after 32768, 32 on 8 heads of 128:   1140 us, 1.0 PFLOP/s (floor at 1.66: 682)
+//   2048 tokens after 32768, 32 on 8 heads of 128:   1140 us, 1.0 PFLOP/s (floor at 1.66: 682); 1320 us, 0.86 PFLOP/s, on a hot card
 //   four prompts of 1129 to 2048, 16 heads of 128:   104 us (34; tensor cores busy 27 % of the time, issue slots as much)
-//   24 sequences, three in four with a single token, up to 4000 keys, 16 on 4 heads of 64, capped:   146 us (17)
-//   five tokens after 1500, 32 on 8 heads of 128:    19 us (1), the start and two kernels
+//   24 sequences, three in four with a single token, up to 4000 keys, 16 on 4 heads of 64, capped:   148 us (17); 205 with scores five
+//   times as large, where one in 400 is beyond half of the cap and nearly every warp has one
+//   five tokens after 1500, 32 on 8 heads of 128:    19 us (1), the start and two kernels; the decode step with a row for each: 15
+// With copies by lanes (pages of 100 slots) the same take 2010, 161, 181 and 26 us: 64 threads copy what a few requests do otherwise.
 // The size of the code counts: with a tile's 128 scores in registers, everything written out for them, instructions came from
 // beyond the first cache all the time.  So the scores are read from tensor memory twice, 32 at a time (four prompts 111 -> 104),
 // masks are bits, and there is one form of a step (one for tiles that every row sees whole and one for the others: 137).

@@ -14,16 +14,17 @@
 // row had been sorted.  A sum of weights in 32 bits is off by 10^-7, and of 50 thousand alike each has 2 10^-5 of the mass: the
 // token would be another one in a row of every hundred.  So sums and weights next to a border are 64 bits.
 // Where a border does not lie in its window (the mean weights were too far off), more logits lie in the windows than there is
-// room for (many equal ones), or the temperature is beyond 10^-29 .. 10^29, sample_any() finds the borders digit by digit of the logits' order, with sums of integers: 0.6 ms for a
-// row of 50257 fp32 logits (1.1 with every weight added by itself in 64 bits), 1.2 to 1.7 for 16-bit ones of 105 to 132 thousand.
+// room for (many equal ones), or the temperature is beyond 10^-29 .. 10^29, sample_any() finds the borders digit by digit of the logits'
+// order, with sums of integers: 0.3 to 0.6 ms for a row of 50257 fp32 logits (1.1 with every weight added by itself in 64 bits), 1.0 to
+// 1.7 for 16-bit ones of 105 to 132 thousand.
 //
 // Few rows: up to 8 CTAs of a cluster share a row.
 //
-// What bounds it, on a B200 (a graph of calls).  512 rows of 50257 fp32 logits: 105 us where reading them takes 16 (103 MB come from
-// HBM, once); issue slots are busy 56 % of the time, a row's CTA being at its barriers (maximum, counts, windows, ranks) for the
-// rest of it, and two CTAs an SM is what registers and the table of counts leave.  64 mixed rows: 28 us; one row: 17 us; these are
-// the steps one after the other.  Weights in 64 bits throughout took 156 us for the 512 rows: by table and 32-bit arithmetic in
-// pass 2, and by comparing with the windows' borders in pass 3, a logit costs some 12 instructions there.
+// What bounds it, on a B200 (a graph of calls).  512 rows of 50257 fp32 logits: 109 us where reading them takes 16 (103 MB come from
+// HBM, once); issue slots are busy 55 % of the time, a row's CTA being at its barriers (maximum, counts, windows, ranks) for the
+// rest of it, and two CTAs an SM is what registers and the table of counts leave.  64 mixed rows: 28.6 us; one row: 17 us; these are
+// the steps one after the other.  Weights in 64 bits throughout took 156 us for the 512 rows: in pass 2 they are 32 bits, in pass 3 logits
+// are compared with the windows' borders in steps of the exponent and weights are the table's times a 32-bit rest.
 #include <float.h>
 #include <math.h>
 
